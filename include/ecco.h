@@ -238,6 +238,82 @@ int ecco_attn_values(const void* d_meta, const uint8_t* d_vblocks, int32_t batch
  * unspecified blocks, never a fault); values above 448 * 2^e saturate. */
 int ecco_kv_compress(const void* d_meta, const void* d_x_fp16, uint64_t n_groups, uint8_t* d_blocks, void* stream);
 
+/* ---------------------------------------------------------------- paged KV cache (device)
+ * A cache of requests of different lengths.  K and V lie in two pools of n_pages pages; a page holds page_size tokens of
+ * one request, for all KV heads: the block of (page, head, place) is at byte 64 * ((page * n_kv_heads + head) * page_size + place).
+ * Token t of a request is in page table[t / page_size] of the request's row of the block table, at place t % page_size;
+ * its slot is page * page_size + place.  A group is one token's 128-wide head vector, as elsewhere.
+ *
+ * A step of a server is ecco_paged_plan once, then per layer ecco_paged_append of the new tokens' K and V and ecco_paged_attn
+ * of their queries.  All lengths are device arrays, and the sizes that the host passes are upper bounds, so a step
+ * may be captured into a graph and replayed with other lengths.
+ *
+ * Pools are 32-byte aligned, arrays of int32 4-byte aligned; page_size is a power of two up to 4096, and
+ * n_pages * page_size is below 2^31.  Whatever the device arrays hold, no call reads or writes outside the buffers that
+ * it was given. */
+typedef struct ecco_paged_cache {
+    const void* d_k_meta;      /* device: metadata images of the K and of the V cache */
+    const void* d_v_meta;
+    uint8_t* d_k_blocks;       /* device: 64 * n_pages * n_kv_heads * page_size bytes each */
+    uint8_t* d_v_blocks;
+    int32_t n_pages, n_kv_heads, page_size;
+} ecco_paged_cache;
+
+/* Block tables and slots from request lengths.  Request r holds d_ctx_lens[r] tokens, in the first ceil(ctx / page_size) entries of
+ * its row of d_block_tables [n_req][table_stride], and gets d_new_lens[r] more.  The pages that it lacks are taken from d_free_pages
+ * [n_free] in order, request after request, and appended to its row; other entries stay as they are.  Written:
+ *   d_cu_new [n_req + 1]    prefix sums of the new lengths: request r's new tokens are rows cu_new[r] .. cu_new[r + 1] - 1
+ *   d_slots [n_slots]       the slot of every new token, -1 in the rows behind the last one (and where a page id is not one of the pool)
+ *   d_kv_lens [n_req]       ctx + new
+ *   d_kv_tiles [n_req + 1]  prefix sums of ceil(kv_len / 32), which ecco_paged_attn takes
+ *   d_result [4]            error code, pages taken, new tokens, d_kv_tiles[n_req]
+ * All requests are served or none: a negative length, a request that does not fit table_stride, or more than 2^31 - 1 tokens or tiles in
+ * all give d_result[0] = ECCO_ERR_INVALID_ARG, too few free pages or rows of d_slots ECCO_ERR_WORKSPACE.  Then the tables stay
+ * as they are, every slot is -1 and the other outputs are zero: calls that use them do nothing.  Outputs overlap neither each
+ * other nor the inputs.  n_req in 0..65535. */
+int ecco_paged_plan(int32_t page_size, int32_t n_pages, int32_t n_req, const int32_t* d_ctx_lens, const int32_t* d_new_lens,
+                    const int32_t* d_free_pages, int32_t n_free, int32_t* d_block_tables, int32_t table_stride, int32_t* d_slots,
+                    int32_t n_slots, int32_t* d_cu_new, int32_t* d_kv_lens, int32_t* d_kv_tiles, int32_t* d_result, void* stream);
+
+/* Online compression of new tokens into their slots: K and V of token i, fp16 [n_kv_heads][128] at d_k_fp16 and d_v_fp16 +
+ * i * token_stride values (parts of the rows of one projection, say), become the blocks of slot d_slots[i].  The blocks are those of
+ * ecco_kv_compress.  Tokens whose slot is negative or beyond the pool are left out (the padding of a batch of fixed size).
+ * The slots of a call are distinct; a slot given twice holds a mixture.  token_stride is a multiple of 8, at least
+ * 128 * n_kv_heads; d_k_fp16 and d_v_fp16 16-byte aligned. */
+int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k_fp16, const void* d_v_fp16, int64_t token_stride,
+                      const int32_t* d_slots, int32_t n_tokens, void* stream);
+
+/* Attention of the new tokens of a batch of requests over the requests' pages (Eq. 3).  Row i of request r (cu_new[r] + i of d_q_fp16) sees
+ * the first kv_len tokens of the request, with ECCO_ATTN_CAUSAL the first kv_len - new + i + 1: the new tokens are the last of
+ * the cache.  (Without: an encoder's states, whose number has nothing to do with the number of new tokens.)
+ *   out[row][hq] = sum_t p_t V~[t][hq / q_per_kv],  p = softmax_t(scale * q[row][hq] . K~[t][hq / q_per_kv]),  lse = log of the sum of exp
+ * q is fp16, row i at d_q_fp16 + i * q_stride values, [n_kv_heads * q_per_kv][128] each; out is fp16 [n_tokens][n_kv_heads * q_per_kv][128], and
+ * d_lse, which may be NULL, fp32 [n_tokens][n_kv_heads * q_per_kv].  A row that sees no token gets zeros and -infinity.  Rows behind
+ * cu_new[n_req] are left as they are.  q_per_kv in 1..16; q_stride a multiple of 8.
+ * Scores, maxima, sums of weights and the sums over tokens are held in fp32; weights enter the tensor cores as fp16 (relative
+ * rounding 2^-11 of each weight).  A decoded value beyond fp16's range enters as +-65504.  A q that is not finite
+ * spoils the rows of its own token only, scale is finite.  The result does not depend on scheduling.
+ * Upper bounds that the host knows: max_new and max_kv of one request's new tokens and of its length, max_tiles of
+ * d_kv_tiles[n_req].  What exceeds them, and tokens whose page is not one of the pool, give unspecified values for the request and make
+ * ecco_device_status() report ECCO_ERR_INVALID_ARG.
+ * The blocks are decoded once per call, into 512 bytes of the workspace per token and KV head.  A workspace that is smaller than
+ * ecco_paged_attn_workspace_bytes (for the same arguments), down to what that gives for n_kv_heads = 1, makes the call
+ * take some heads at a time.  16-byte aligned; contents irrelevant before and undefined after; calls sharing a workspace must
+ * not overlap. */
+#define ECCO_ATTN_CAUSAL 1u
+typedef struct ecco_paged_batch {
+    const int32_t* d_block_tables;     /* [n_req][table_stride] */
+    const int32_t* d_cu_new;           /* [n_req + 1] */
+    const int32_t* d_kv_lens;          /* [n_req] */
+    const int32_t* d_kv_tiles;         /* [n_req + 1]: see ecco_paged_plan */
+    int32_t table_stride, n_req, n_tokens;
+    int32_t max_new, max_kv, max_tiles;
+} ecco_paged_batch;
+size_t ecco_paged_attn_workspace_bytes(const ecco_paged_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv);
+int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q_fp16,
+                    int64_t q_stride, float scale, uint32_t flags, void* d_out_fp16, float* d_lse_or_null, void* d_workspace,
+                    size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------- variable-length container */
 
 /* The same per-group fields as the 64-byte block (scale byte, ID_HF, ID_KP codeword, 128 codewords;

@@ -19,6 +19,7 @@ MAX_PATTERNS = 64
 SELECT_MSE = 0
 SELECT_MINMAX = 1
 KEEP_EXPONENT = 2
+ATTN_CAUSAL = 1
 
 ECCO_OK = 0
 ERR_INVALID_ARG = -1
@@ -35,6 +36,7 @@ EXPORTS = [
     "ecco_meta_device_bytes", "ecco_meta_serialize_device", "ecco_decompress", "ecco_decompress_batch", "ecco_gemv_workspace_bytes",
     "ecco_gemv", "ecco_gemv_batch_workspace_bytes", "ecco_gemv_batch", "ecco_gemv_static_ws", "ecco_attn_scores", "ecco_act_compress", "ecco_act_decompress",
     "ecco_attn_values_workspace_bytes", "ecco_attn_values", "ecco_kv_compress",
+    "ecco_paged_plan", "ecco_paged_append", "ecco_paged_attn_workspace_bytes", "ecco_paged_attn",
     "ecco_var_stream_bytes_bound", "ecco_var_index_bytes", "ecco_var_encode_host", "ecco_var_decompress", "ecco_error_string", "ecco_last_cuda_error", "ecco_device_status",
     "ecco_kernel_launch_count", "ecco_test_wait_timeout", "ecco_test_gemv_give_up", "ecco_test_attn_values_give_up",
 ]
@@ -49,6 +51,19 @@ class GemvItem(C.Structure):
     """ecco_gemv_item of include/ecco.h."""
     _fields_ = [("d_meta", C.c_void_p), ("d_blocks", C.c_void_p), ("n_out", C.c_int32), ("k", C.c_int32),
                 ("d_x_fp16", C.c_void_p), ("d_y", C.c_void_p)]
+
+
+class PagedCache(C.Structure):
+    """ecco_paged_cache of include/ecco.h."""
+    _fields_ = [("d_k_meta", C.c_void_p), ("d_v_meta", C.c_void_p), ("d_k_blocks", C.c_void_p), ("d_v_blocks", C.c_void_p),
+                ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("page_size", C.c_int32)]
+
+
+class PagedBatch(C.Structure):
+    """ecco_paged_batch of include/ecco.h."""
+    _fields_ = [("d_block_tables", C.c_void_p), ("d_cu_new", C.c_void_p), ("d_kv_lens", C.c_void_p), ("d_kv_tiles", C.c_void_p),
+                ("table_stride", C.c_int32), ("n_req", C.c_int32), ("n_tokens", C.c_int32),
+                ("max_new", C.c_int32), ("max_kv", C.c_int32), ("max_tiles", C.c_int32)]
 
 
 class EccoError(RuntimeError):
@@ -110,6 +125,11 @@ def lib():
         L.ecco_attn_values_workspace_bytes.restype = sz
         L.ecco_attn_values.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
         L.ecco_kv_compress.argtypes = [vp, vp, u64, vp, vp]
+        L.ecco_paged_plan.argtypes = [i32, i32, i32, vp, vp, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp]
+        L.ecco_paged_append.argtypes = [C.POINTER(PagedCache), vp, vp, C.c_int64, vp, i32, vp]
+        L.ecco_paged_attn_workspace_bytes.argtypes = [C.POINTER(PagedCache), C.POINTER(PagedBatch), i32]
+        L.ecco_paged_attn_workspace_bytes.restype = sz
+        L.ecco_paged_attn.argtypes = [C.POINTER(PagedCache), C.POINTER(PagedBatch), i32, vp, C.c_int64, C.c_float, C.c_uint32, vp, vp, vp, sz, vp]
         L.ecco_var_stream_bytes_bound.argtypes = [u64]
         L.ecco_var_stream_bytes_bound.restype = sz
         L.ecco_var_index_bytes.argtypes = [u64]
@@ -373,6 +393,44 @@ def ecco_attn_values(d_meta, d_vblocks, batch: int, n_kv_heads: int, seq: int, q
 def ecco_kv_compress(d_meta, d_x_fp16, n_groups: int, d_blocks, stream=None) -> None:
     """Online 4x compressor (min/max pattern selection, calibrated exponent): fp16 device tensor -> 64-byte blocks."""
     _check(lib().ecco_kv_compress(_ptr(d_meta), _ptr(d_x_fp16), n_groups, _ptr(d_blocks), _stream(stream)), "ecco_kv_compress")
+
+
+def paged_cache(d_k_meta, d_v_meta, d_k_blocks, d_v_blocks, n_pages: int, n_kv_heads: int, page_size: int) -> PagedCache:
+    """The pools of a paged cache as ecco_paged_append and ecco_paged_attn take them; built once and kept, like the tensors."""
+    return PagedCache(_ptr(d_k_meta), _ptr(d_v_meta), _ptr(d_k_blocks), _ptr(d_v_blocks), n_pages, n_kv_heads, page_size)
+
+
+def paged_batch(d_block_tables, table_stride: int, d_cu_new, d_kv_lens, d_kv_tiles, n_req: int, n_tokens: int, max_new: int,
+                max_kv: int, max_tiles: int) -> PagedBatch:
+    """A batch of requests as ecco_paged_attn takes it: the arrays that ecco_paged_plan writes, and upper bounds of what they hold."""
+    return PagedBatch(_ptr(d_block_tables), _ptr(d_cu_new), _ptr(d_kv_lens), _ptr(d_kv_tiles), table_stride, n_req, n_tokens, max_new, max_kv,
+                      max_tiles)
+
+
+def ecco_paged_plan(page_size: int, n_pages: int, n_req: int, d_ctx_lens, d_new_lens, d_free_pages, n_free: int, d_block_tables,
+                    table_stride: int, d_slots, n_slots: int, d_cu_new, d_kv_lens, d_kv_tiles, d_result, stream=None) -> None:
+    """Pages, slots and prefix sums of a step's new tokens (see include/ecco.h)."""
+    _check(lib().ecco_paged_plan(page_size, n_pages, n_req, _ptr(d_ctx_lens), _ptr(d_new_lens), _ptr(d_free_pages), n_free, _ptr(d_block_tables),
+                                 table_stride, _ptr(d_slots), n_slots, _ptr(d_cu_new), _ptr(d_kv_lens), _ptr(d_kv_tiles), _ptr(d_result),
+                                 _stream(stream)), "ecco_paged_plan")
+
+
+def ecco_paged_append(cache: PagedCache, d_k_fp16, d_v_fp16, token_stride: int, d_slots, n_tokens: int, stream=None) -> None:
+    """Online 4x compressor into the slots of a paged cache."""
+    _check(lib().ecco_paged_append(C.byref(cache), _ptr(d_k_fp16), _ptr(d_v_fp16), token_stride, _ptr(d_slots), n_tokens, _stream(stream)),
+           "ecco_paged_append")
+
+
+def ecco_paged_attn_workspace_bytes(cache: PagedCache, batch: PagedBatch, q_per_kv: int) -> int:
+    return int(lib().ecco_paged_attn_workspace_bytes(C.byref(cache), C.byref(batch), q_per_kv))
+
+
+def ecco_paged_attn(cache: PagedCache, batch: PagedBatch, q_per_kv: int, d_q_fp16, q_stride: int, scale: float, flags: int, d_out_fp16,
+                    d_lse, d_workspace, workspace_bytes: int, stream=None) -> None:
+    """Attention of the batch's new tokens over the pages of their requests -> fp16 [n_tokens][n_kv_heads*q_per_kv][128]; d_lse may be None."""
+    _check(lib().ecco_paged_attn(C.byref(cache), C.byref(batch), q_per_kv, _ptr(d_q_fp16), q_stride, C.c_float(scale), flags, _ptr(d_out_fp16),
+                                 _ptr(d_lse) if d_lse is not None else None, _ptr(d_workspace) if d_workspace is not None else None,
+                                 workspace_bytes, _stream(stream)), "ecco_paged_attn")
 
 
 def ecco_var_decompress(d_meta, d_stream, d_index, n_groups: int, d_out_fp16, stream=None) -> None:

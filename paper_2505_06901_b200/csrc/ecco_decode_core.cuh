@@ -139,6 +139,8 @@ struct LaneGroup {
 // (hdr, first bit in bit 0), then value = fp16_rn(centroid * scale).  The product of two fp16 numbers rounded once to fp16 is
 // the same number whether it is formed by one fp16 multiplication or in fp32 (where it is exact), so the packed fp16
 // product is used whenever the scale is an fp16 number: 448 * 2^e finite and 2^-9 * 2^e not below fp16's last place.
+// kFinite: values beyond fp16's range become +-65504 instead of infinities.
+template <bool kFinite = false>
 __device__ __forceinline__ LaneGroup open_lane_group(uint32_t hdr, uint32_t first_bit, const DecodeTables& tb, float T)
 {
     LaneGroup g;
@@ -172,6 +174,14 @@ __device__ __forceinline__ LaneGroup open_lane_group(uint32_t hdr, uint32_t firs
             c[j] = *reinterpret_cast<const uint32_t*>(&v);
         }
     }
+    if (kFinite) {
+        const __half2 most = __float2half2_rn(65504.0f), least = __hneg2(most);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const __half2 v = __hmax2(__hmin2(*reinterpret_cast<const __half2*>(&c[j]), most), least);
+            c[j] = *reinterpret_cast<const uint32_t*>(&v);
+        }
+    }
     const uint32_t sign = (hdr & 0x80u) << ((top & 3u) * 8);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -181,11 +191,12 @@ __device__ __forceinline__ LaneGroup open_lane_group(uint32_t hdr, uint32_t firs
     return g;
 }
 // 64-byte block: its words go to the lane's column of the transposed bit-stream array (bits = address of its row 0)
+template <bool kFinite = false>
 __device__ __forceinline__ LaneGroup open_block(const Block& blk, uint32_t bits, const DecodeTables& tb, float T)
 {
 #pragma unroll
     for (int i = 0; i < 16; ++i) sts_u32(bits + i * 128, blk.w[i]);
-    return open_lane_group(blk.w[0], 0u, tb, T);
+    return open_lane_group<kFinite>(blk.w[0], 0u, tb, T);
 }
 
 // Eight ranks (nibbles, first symbol lowest) -> eight fp16 values, two to a word.  A byte permute selects among eight

@@ -27,6 +27,7 @@
 //   ecco_attn_values_kernels.cuh    softmax(scores) . V over a compressed V cache
 //   ecco_act2x_kernels.cuh          2x activation codec
 //   ecco_kv_compress_kernel.cuh     online 4x compressor
+//   ecco_paged_kernels.cuh          paged KV cache: slots and block tables, pages into tiles, attention of few rows
 //   ecco_launch.cuh                 device query, overlapped launches, work plans
 //   this file                       the C ABI: argument checks and launches
 #include "ecco_device_core.cuh"
@@ -39,6 +40,7 @@
 #include "ecco_launch.cuh"
 #include "ecco_act2x_kernels.cuh"
 #include "ecco_kv_compress_kernel.cuh"
+#include "ecco_paged_kernels.cuh"
 
 
 // ---------------------------------------------------------------------------------------------
@@ -655,6 +657,26 @@ extern "C" int ecco_act_compress(const void* d_x_fp16, uint64_t n_groups, uint8_
 // calls of at least this many groups: eight lanes per group and tables in shared memory (see the kernel)
 constexpr uint64_t kKvManyGroups = 16384;
 
+// kinds: tensors of n_groups groups each that share the CTAs
+template <class Groups>
+static int launch_kv_compress(const DeviceInfo& di, const Groups& groups, uint64_t n_groups, int kinds, cudaStream_t s)
+{
+    if (n_groups * kinds >= kKvManyGroups) {
+        static thread_local bool configured[64] = {};
+        if (!configured[di.device]) {
+            const int rc = set_smem(ecco_kv_compress_many_kernel<Groups>, sizeof(KvManySmem));
+            if (rc) return rc;
+            configured[di.device] = true;
+        }
+        return launch_overlapped(ecco_kv_compress_many_kernel<Groups>, static_cast<unsigned>(kinds * spread_ctas(static_cast<int64_t>((n_groups + 3) / 4), di.sms / kinds)),
+                                 static_cast<unsigned>(kKvManyWarps * 32), sizeof(KvManySmem), s, groups, n_groups);
+    }
+    const uint64_t ctas = (n_groups + kKvWarps - 1) / kKvWarps;
+    const uint64_t cap = static_cast<uint64_t>(di.sms) * 8 / kinds;
+    return launch_overlapped(ecco_kv_compress_kernel<Groups>, static_cast<unsigned>(kinds * (ctas < cap ? ctas : cap)), static_cast<unsigned>(kKvWarps * 32), 0, s, groups,
+                             n_groups);
+}
+
 extern "C" int ecco_kv_compress(const void* d_meta, const void* d_x_fp16, uint64_t n_groups, uint8_t* d_blocks, void* stream)
 {
     if (n_groups == 0) return ECCO_OK;
@@ -664,20 +686,181 @@ extern "C" int ecco_kv_compress(const void* d_meta, const void* d_x_fp16, uint64
     DeviceInfo di;
     int rc = device_info(&di);
     if (rc) return rc;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (n_groups >= kKvManyGroups) {
-        static thread_local bool configured[64] = {};
-        if (!configured[di.device]) {
-            rc = set_smem(ecco_kv_compress_many_kernel, sizeof(KvManySmem));
-            if (rc) return rc;
-            configured[di.device] = true;
-        }
-        return launch_overlapped(ecco_kv_compress_many_kernel, static_cast<unsigned>(spread_ctas(static_cast<int64_t>((n_groups + 3) / 4), di.sms)),
-                                 static_cast<unsigned>(kKvManyWarps * 32), sizeof(KvManySmem), s, static_cast<const uint8_t*>(d_meta),
-                                 static_cast<const __half*>(d_x_fp16), n_groups, d_blocks);
+    const DenseGroups groups = {static_cast<const uint8_t*>(d_meta), static_cast<const __half*>(d_x_fp16), d_blocks};
+    return launch_kv_compress(di, groups, n_groups, 1, static_cast<cudaStream_t>(stream));
+}
+
+// ---------------------------------------------------------------------------------------------
+// Paged KV cache
+// ---------------------------------------------------------------------------------------------
+static bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+// log2 of the page size, or -1
+static int page_shift_of(int32_t page_size)
+{
+    for (int sh = 0; sh <= 12; ++sh)
+        if (page_size == 1 << sh) return sh;
+    return -1;
+}
+static int check_paged_cache(const ecco_paged_cache* c)
+{
+    if (!c || !c->d_k_meta || !c->d_v_meta || !c->d_k_blocks || !c->d_v_blocks) return ECCO_ERR_INVALID_ARG;
+    if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 65535 || page_shift_of(c->page_size) < 0) return ECCO_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(c->n_pages) * c->page_size > INT32_MAX) return ECCO_ERR_INVALID_ARG;
+    if (!aligned16(c->d_k_meta) || !aligned16(c->d_v_meta) || !aligned_to(c->d_k_blocks, 32) || !aligned_to(c->d_v_blocks, 32)) return ECCO_ERR_ALIGNMENT;
+    return ECCO_OK;
+}
+
+extern "C" int ecco_paged_plan(int32_t page_size, int32_t n_pages, int32_t n_req, const int32_t* d_ctx_lens, const int32_t* d_new_lens,
+                               const int32_t* d_free_pages, int32_t n_free, int32_t* d_block_tables, int32_t table_stride, int32_t* d_slots,
+                               int32_t n_slots, int32_t* d_cu_new, int32_t* d_kv_lens, int32_t* d_kv_tiles, int32_t* d_result, void* stream)
+{
+    const int shift = page_shift_of(page_size);
+    if (shift < 0 || n_pages < 1 || static_cast<int64_t>(n_pages) * page_size > INT32_MAX) return ECCO_ERR_INVALID_ARG;
+    if (n_req < 0 || n_req > 65535 || n_free < 0 || table_stride < 0 || n_slots < 0) return ECCO_ERR_INVALID_ARG;
+    if (!d_cu_new || !d_kv_tiles || !d_result || (n_slots && !d_slots) || (n_free && !d_free_pages)) return ECCO_ERR_INVALID_ARG;
+    if (n_req && (!d_ctx_lens || !d_new_lens || !d_kv_lens || (table_stride && !d_block_tables))) return ECCO_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(d_ctx_lens), static_cast<const void*>(d_new_lens), static_cast<const void*>(d_free_pages),
+                          static_cast<const void*>(d_block_tables), static_cast<const void*>(d_slots), static_cast<const void*>(d_cu_new),
+                          static_cast<const void*>(d_kv_lens), static_cast<const void*>(d_kv_tiles), static_cast<const void*>(d_result)})
+        if (!aligned_to(p, 4)) return ECCO_ERR_ALIGNMENT;
+    DeviceInfo di;
+    const int rc = device_info(&di);
+    if (rc) return rc;
+    PagedPlan p = {};
+    p.ctx = d_ctx_lens; p.added = d_new_lens; p.free_pages = d_free_pages;
+    p.tables = d_block_tables; p.slots = d_slots; p.cu_new = d_cu_new; p.kv_lens = d_kv_lens; p.kv_tiles = d_kv_tiles; p.result = d_result;
+    p.page_shift = shift; p.n_pages = n_pages; p.n_req = n_req; p.n_free = n_free; p.stride = table_stride; p.n_slots = n_slots;
+    const int ctas = spread_ctas((static_cast<int64_t>(n_slots) + kPlanThreads - 1) / kPlanThreads, di.sms);
+    return launch_overlapped(ecco_paged_plan_kernel, static_cast<unsigned>(ctas > 0 ? ctas : 1), static_cast<unsigned>(kPlanThreads), 0,
+                             static_cast<cudaStream_t>(stream), p);
+}
+
+extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k, const void* d_v, int64_t token_stride, const int32_t* d_slots,
+                                 int32_t n_tokens, void* stream)
+{
+    int rc = check_paged_cache(cache);
+    if (rc) return rc;
+    if (n_tokens < 0) return ECCO_ERR_INVALID_ARG;
+    if (n_tokens == 0) return ECCO_OK;
+    if (!d_k || !d_v || !d_slots || token_stride < static_cast<int64_t>(cache->n_kv_heads) * kGroup) return ECCO_ERR_INVALID_ARG;
+    if (!aligned16(d_k) || !aligned16(d_v) || token_stride % 8 || !aligned_to(d_slots, 4)) return ECCO_ERR_ALIGNMENT;
+    DeviceInfo di;
+    rc = device_info(&di);
+    if (rc) return rc;
+    PagedGroups g = {};
+    g.k_image = static_cast<const uint8_t*>(cache->d_k_meta); g.v_image = static_cast<const uint8_t*>(cache->d_v_meta);
+    g.k = static_cast<const __half*>(d_k); g.v = static_cast<const __half*>(d_v);
+    g.k_blocks = cache->d_k_blocks; g.v_blocks = cache->d_v_blocks;
+    g.slots = d_slots; g.token_stride = token_stride;
+    g.heads = cache->n_kv_heads; g.page_shift = page_shift_of(cache->page_size); g.n_slots = cache->n_pages * cache->page_size;
+    return launch_kv_compress(di, g, static_cast<uint64_t>(n_tokens) * cache->n_kv_heads, 2, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+struct PagedAttnPlan {
+    int few_ctas, m;                   // CTAs of the kernel for few rows, its tiles of sixteen rows
+    size_t staged_bytes, part_bytes, ml_bytes;
+    size_t bytes() const { return staged_bytes + part_bytes + ml_bytes; }
+};
+// of a launch over `heads` KV heads
+PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, int ctas_max)
+{
+    PagedAttnPlan p;
+    const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
+    p.m = rows <= 16 ? 1 : 2;
+    p.few_ctas = std::max(1, spread_ctas(static_cast<int64_t>(b.max_tiles) * heads, ctas_max));
+    auto up = [](size_t v) { return (v + 255) & ~static_cast<size_t>(255); };
+    const size_t slots = static_cast<size_t>(p.few_ctas) * (p.m == 1 ? kFewWarps<1> : kFewWarps<2>) * 2 * 16 * p.m;
+    p.staged_bytes = static_cast<size_t>(b.max_tiles) * heads * 2 * kKvTileBytes;
+    p.part_bytes = up(slots * kGroup * sizeof(float));
+    p.ml_bytes = up(slots * sizeof(float2));
+    return p;
+}
+bool paged_batch_fine(const ecco_paged_cache& c, const ecco_paged_batch& b, int q_per_kv)
+{
+    return b.n_req >= 0 && b.n_req <= 65535 && b.n_tokens >= 0 && b.table_stride >= 0 && b.max_new >= 0 && b.max_kv >= 0 && b.max_tiles >= 0 && q_per_kv >= 1 &&
+           q_per_kv <= 16 && static_cast<int64_t>(b.max_new) * q_per_kv <= INT32_MAX - 64 && static_cast<int64_t>(b.max_tiles) * c.n_kv_heads <= INT32_MAX / 2 && static_cast<int64_t>(c.n_kv_heads) * q_per_kv <= 65535 &&
+           static_cast<int64_t>(b.n_tokens) * c.n_kv_heads * q_per_kv <= INT32_MAX;
+}
+
+template <int kM>
+int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedAttnPlan& p, cudaStream_t s)
+{
+    static thread_local bool configured[64] = {};
+    if (!configured[di.device]) {
+        const int rc = set_smem(ecco_paged_few_kernel<kM>, kFewSmemBytes<kM>);
+        if (rc) return rc;
+        configured[di.device] = true;
     }
-    const uint64_t ctas = (n_groups + kKvWarps - 1) / kKvWarps;
-    const uint64_t cap = static_cast<uint64_t>(di.sms) * 8;
-    return launch_overlapped(ecco_kv_compress_kernel, static_cast<unsigned>(ctas < cap ? ctas : cap), static_cast<unsigned>(kKvWarps * 32), 0,
-                             s, static_cast<const uint8_t*>(d_meta), static_cast<const __half*>(d_x_fp16), n_groups, d_blocks);
+    int rc = launch_overlapped(ecco_paged_few_kernel<kM>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps<kM> * 32), kFewSmemBytes<kM>, s, kv, o);
+    if (rc) return rc;
+    const int64_t rows = static_cast<int64_t>(kv.n_tokens) * kv.heads * o.q_per_kv;
+    // warps to a row: by how many pieces a request of average length is cut into
+    const int64_t pieces = static_cast<int64_t>(p.few_ctas) * kFewWarps<kM> / (static_cast<int64_t>(kv.n_req) * kv.heads);
+    const int team = pieces > 16 ? 8 : 1;
+    return launch_overlapped(ecco_paged_combine_kernel<kM>, static_cast<unsigned>((rows * team + 7) / 8), 256u, 0, s, kv, o, p.few_ctas, team);
+}
+}  // namespace
+
+extern "C" size_t ecco_paged_attn_workspace_bytes(const ecco_paged_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv)
+{
+    if (!cache || !batch || cache->n_kv_heads < 1 || cache->n_kv_heads > 65535 || !paged_batch_fine(*cache, *batch, q_per_kv)) return 0;
+    return paged_attn_plan(*batch, cache->n_kv_heads, q_per_kv, 256).bytes();
+}
+
+extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q, int64_t q_stride,
+                               float scale, uint32_t flags, void* d_out, float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = check_paged_cache(cache);
+    if (rc) return rc;
+    if (!batch || !paged_batch_fine(*cache, *batch, q_per_kv) || (flags & ~ECCO_ATTN_CAUSAL) || !(scale - scale == 0.0f)) return ECCO_ERR_INVALID_ARG;
+    const ecco_paged_batch& b = *batch;
+    if (b.n_req == 0 || b.n_tokens == 0) return ECCO_OK;
+    const int q_heads = cache->n_kv_heads * q_per_kv;
+    if (!b.d_cu_new || !b.d_kv_lens || !b.d_kv_tiles || (b.table_stride && !b.d_block_tables) || !d_q || !d_out) return ECCO_ERR_INVALID_ARG;
+    if (q_stride < static_cast<int64_t>(q_heads) * kGroup) return ECCO_ERR_INVALID_ARG;
+    if (!aligned16(d_q) || q_stride % 8 || !aligned16(d_out) || !aligned_to(d_lse, 4)) return ECCO_ERR_ALIGNMENT;
+    for (const int32_t* p : {b.d_block_tables, b.d_cu_new, b.d_kv_lens, b.d_kv_tiles})
+        if (!aligned_to(p, 4)) return ECCO_ERR_ALIGNMENT;
+    DeviceInfo di;
+    rc = device_info(&di);
+    if (rc) return rc;
+    if (!d_workspace || !aligned16(d_workspace)) return d_workspace ? ECCO_ERR_ALIGNMENT : ECCO_ERR_WORKSPACE;
+    const int ctas = di.sms < 256 ? di.sms : 256;
+    // as many heads at a time as the workspace holds
+    int heads = cache->n_kv_heads;
+    while (heads > 0 && paged_attn_plan(b, heads, q_per_kv, ctas).bytes() > workspace_bytes) --heads;
+    if (heads == 0) return ECCO_ERR_WORKSPACE;
+    PagedKv kv = {};
+    kv.k_meta = static_cast<const uint8_t*>(cache->d_k_meta); kv.v_meta = static_cast<const uint8_t*>(cache->d_v_meta);
+    kv.k_blocks = cache->d_k_blocks; kv.v_blocks = cache->d_v_blocks;
+    kv.tables = b.d_block_tables; kv.cu_new = b.d_cu_new; kv.kv_lens = b.d_kv_lens; kv.kv_tiles = b.d_kv_tiles;
+    kv.n_pages = cache->n_pages; kv.page_shift = page_shift_of(cache->page_size); kv.all_heads = cache->n_kv_heads;
+    kv.stride = b.table_stride; kv.n_req = b.n_req; kv.n_tokens = b.n_tokens; kv.max_tiles = b.max_tiles;
+    kv.staged = static_cast<uint8_t*>(d_workspace);
+    PagedOut o = {};
+    o.q = static_cast<const __half*>(d_q); o.q_stride = q_stride;
+    o.scale_log2 = scale * 1.4426950408889634f;
+    o.q_per_kv = q_per_kv; o.q_heads = q_heads; o.causal = flags & ECCO_ATTN_CAUSAL;
+    o.out = static_cast<__half*>(d_out); o.lse = d_lse;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    static thread_local bool configured[64] = {};
+    rc = want_all_smem(ecco_paged_stage_kernel<32>, &configured[di.device]);
+    if (rc) return rc;
+    for (kv.head0 = 0; kv.head0 < cache->n_kv_heads; kv.head0 += kv.heads) {
+        kv.heads = std::min(heads, cache->n_kv_heads - kv.head0);
+        const PagedAttnPlan p = paged_attn_plan(b, kv.heads, q_per_kv, ctas);
+        o.part = reinterpret_cast<float*>(kv.staged + p.staged_bytes);
+        o.part_ml = reinterpret_cast<float2*>(kv.staged + p.staged_bytes + p.part_bytes);
+        // an even number of CTAs: half of them for K, half for V
+        const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
+        const int pairs = std::max(1, spread_ctas(units, ctas / 2));
+        rc = launch_overlapped(ecco_paged_stage_kernel<32>, static_cast<unsigned>(2 * pairs), spread_threads(units, pairs, 32), kSmemCtaBytes, s, kv);
+        if (rc) return rc;
+        for (o.row_from = 0; o.row_from < static_cast<int64_t>(b.max_new) * q_per_kv; o.row_from += 16 * p.m) {
+            rc = p.m == 1 ? launch_paged_few<1>(di, kv, o, p, s) : launch_paged_few<2>(di, kv, o, p, s);
+            if (rc) return rc;
+        }
+    }
+    return ECCO_OK;
 }

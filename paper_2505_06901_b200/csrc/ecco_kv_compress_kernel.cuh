@@ -19,12 +19,51 @@
 // ---------------------------------------------------------------------------------------------
 namespace {
 
+// Where the groups of a call lie and where their blocks go.  cta of ctas: this CTA among those that share its groups.
+struct DenseGroups {                                       // one after the other
+    const uint8_t* image;
+    const __half* x;
+    uint8_t* blocks;
+    __device__ __forceinline__ const uint8_t* meta() const { return image; }
+    __device__ __forceinline__ uint32_t cta() const { return blockIdx.x; }
+    __device__ __forceinline__ uint32_t ctas() const { return gridDim.x; }
+    __device__ __forceinline__ const __half* source(uint64_t g) const { return x + g * kGroup; }
+    __device__ __forceinline__ uint8_t* block(uint64_t g) const { return blocks + g * kBlockBytes; }
+};
+// New tokens of a paged cache: group g is head g % heads of token g / heads.  Even CTAs encode K, odd ones V.
+struct PagedGroups {
+    const uint8_t *k_image, *v_image;
+    const __half *k, *v;
+    uint8_t *k_blocks, *v_blocks;
+    const int32_t* slots;
+    int64_t token_stride;
+    int32_t heads, page_shift, n_slots;
+    __device__ __forceinline__ bool is_v() const { return blockIdx.x & 1u; }
+    __device__ __forceinline__ const uint8_t* meta() const { return is_v() ? v_image : k_image; }
+    __device__ __forceinline__ uint32_t cta() const { return blockIdx.x >> 1; }
+    __device__ __forceinline__ uint32_t ctas() const { return gridDim.x >> 1; }
+    __device__ __forceinline__ const __half* source(uint64_t g) const
+    {
+        const uint32_t token = static_cast<uint32_t>(divide(g, static_cast<uint64_t>(heads))), head = static_cast<uint32_t>(g - static_cast<uint64_t>(token) * heads);
+        return (is_v() ? v : k) + token * token_stride + head * kGroup;
+    }
+    // NULL: the token is left out
+    __device__ __forceinline__ uint8_t* block(uint64_t g) const
+    {
+        const uint32_t token = static_cast<uint32_t>(divide(g, static_cast<uint64_t>(heads))), head = static_cast<uint32_t>(g - static_cast<uint64_t>(token) * heads);
+        const int32_t slot = __ldcg(slots + token), page = slot >> page_shift;
+        if (slot < 0 || slot >= n_slots) return nullptr;
+        return (is_v() ? v_blocks : k_blocks) + (((static_cast<int64_t>(page) * heads + head) << page_shift) + (slot - (page << page_shift))) * kBlockBytes;
+    }
+};
+
 constexpr int kKvWarps = 8;
 
+template <class Groups>
 __global__ void __launch_bounds__(kKvWarps * 32)
-ecco_kv_compress_kernel(const uint8_t* __restrict__ d_meta, const __half* __restrict__ d_x, uint64_t n_groups,
-                        uint8_t* __restrict__ d_blocks)
+ecco_kv_compress_kernel(const __grid_constant__ Groups groups, uint64_t n_groups)
 {
+    const uint8_t* const __restrict__ d_meta = groups.meta();
     __shared__ __align__(16) uint16_t pat_s[kMaxPatterns * 16];
     __shared__ __align__(16) uint16_t enc_s[kMaxPatterns * kCodebooks * kSymbols];
     __shared__ __align__(16) uint16_t kp_s[kMaxPatterns];
@@ -48,8 +87,10 @@ ecco_kv_compress_kernel(const uint8_t* __restrict__ d_meta, const __half* __rest
     uint32_t* blk = blk_s[warp];
     auto fp8 = [&](float v) { return static_cast<uint32_t>(__nv_cvt_float_to_fp8(v * invT, __NV_SATFINITE, __NV_E4M3)); };
 
-    for (uint64_t g = static_cast<uint64_t>(blockIdx.x) * kKvWarps + warp; g < n_groups; g += static_cast<uint64_t>(gridDim.x) * kKvWarps) {
-        const uint2 raw = __ldcg(reinterpret_cast<const uint2*>(d_x + g * kGroup) + lane);
+    for (uint64_t g = static_cast<uint64_t>(groups.cta()) * kKvWarps + warp; g < n_groups; g += static_cast<uint64_t>(groups.ctas()) * kKvWarps) {
+        uint8_t* const block = groups.block(g);
+        if (!block) continue;
+        const uint2 raw = __ldcg(reinterpret_cast<const uint2*>(groups.source(g)) + lane);
         const uint32_t h16[4] = {raw.x & 0xffffu, raw.x >> 16, raw.y & 0xffffu, raw.y >> 16};
         float x[4];
         uint32_t key[4];                                   // |x| then low index first
@@ -214,7 +255,7 @@ ecco_kv_compress_kernel(const uint8_t* __restrict__ d_meta, const __half* __rest
             }
         }
         __syncwarp();
-        if (lane < 16) reinterpret_cast<uint32_t*>(d_blocks + g * kBlockBytes)[lane] = blk[lane];
+        if (lane < 16) reinterpret_cast<uint32_t*>(block)[lane] = blk[lane];
         __syncwarp();
     }
 }
@@ -256,9 +297,11 @@ struct KvManySmem {
 
 __device__ __forceinline__ uint32_t kv_key(uint32_t half, int pos) { return ((half & 0x7fffu) << 7) | static_cast<uint32_t>(127 - pos); }
 
+template <class Groups>
 __global__ void __launch_bounds__(kKvManyWarps * 32, 1)
-ecco_kv_compress_many_kernel(const uint8_t* __restrict__ d_meta, const __half* __restrict__ d_x, uint64_t n_groups, uint8_t* __restrict__ d_blocks)
+ecco_kv_compress_many_kernel(const __grid_constant__ Groups groups, uint64_t n_groups)
 {
+    const uint8_t* const __restrict__ d_meta = groups.meta();
     extern __shared__ __align__(1024) uint8_t smem[];
     KvManySmem& sm = *reinterpret_cast<KvManySmem*>(smem);
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5, sub = lane & 7, grp = lane >> 3;
@@ -322,11 +365,11 @@ ecco_kv_compress_many_kernel(const uint8_t* __restrict__ d_meta, const __half* _
     uint16_t* const xs = reinterpret_cast<uint16_t*>(sm.x[warp]) + grp * kGroup;          // this group's values
     uint32_t* const blk = sm.blk[warp] + grp * 16;
     const uint64_t n_units = (n_groups + 3) / 4;
-    for (uint64_t unit = static_cast<uint64_t>(warp) * gridDim.x + blockIdx.x; unit < n_units; unit += static_cast<uint64_t>(gridDim.x) * kKvManyWarps) {
+    for (uint64_t unit = static_cast<uint64_t>(warp) * groups.ctas() + groups.cta(); unit < n_units; unit += static_cast<uint64_t>(groups.ctas()) * kKvManyWarps) {
         const uint64_t g = min(unit * 4 + grp, n_groups - 1);            // past the end: the last group again, not stored
         uint32_t h[8];                                     // x is 16-byte aligned: two loads
         {
-            const uint4* const src = reinterpret_cast<const uint4*>(d_x + g * kGroup + sub * 16);
+            const uint4* const src = reinterpret_cast<const uint4*>(groups.source(g) + sub * 16);
             const uint4 a = __ldcg(src), b = __ldcg(src + 1);
             h[0] = a.x; h[1] = a.y; h[2] = a.z; h[3] = a.w; h[4] = b.x; h[5] = b.y; h[6] = b.z; h[7] = b.w;
         }
@@ -533,7 +576,8 @@ ecco_kv_compress_many_kernel(const uint8_t* __restrict__ d_meta, const __half* _
             }
         }
         __syncwarp();
-        if (unit * 4 + grp < n_groups) reinterpret_cast<uint2*>(d_blocks + g * kBlockBytes)[sub] = make_uint2(blk[sub * 2], blk[sub * 2 + 1]);
+        uint8_t* const block = unit * 4 + grp < n_groups ? groups.block(g) : nullptr;
+        if (block) reinterpret_cast<uint2*>(block)[sub] = make_uint2(blk[sub * 2], blk[sub * 2 + 1]);
         __syncwarp();
     }
 }

@@ -1,0 +1,645 @@
+// ecco_paged_kernels.cuh -- K6: the paged KV cache: slots and block tables, pages into tiles, attention of few rows
+// Part of the one translation unit ecco_kernels.cu; included from there only.
+#pragma once
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// K6p: block tables and slots from request lengths.  One launch; every CTA forms the prefix sums of all requests itself (8 bytes a
+// request, which stay in L2) and writes the rows of d_slots that are its share: no CTA waits for another.
+// Requests pass in rounds of kPlanThreads; a round's prefix sums lie in shared memory, and a row finds its request there by bisection.
+// A page is appended to its table by the row that holds the page's first token, which is always a new one.
+// ---------------------------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024;
+
+struct PagedPlan {
+    const int32_t *ctx, *added, *free_pages;
+    int32_t *tables, *slots, *cu_new, *kv_lens, *kv_tiles, *result;
+    int32_t page_shift, n_pages, n_req, n_free, stride, n_slots;
+};
+
+// inclusive prefix sums over the CTA of three numbers per thread; total: over all threads
+struct Sum3 { int32_t a, b, c; };
+__device__ __forceinline__ Sum3 scan3(Sum3 v, Sum3& total, Sum3 (&warp_sums)[32])
+{
+    constexpr unsigned full = 0xffffffffu;
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
+    auto scan_warp = [&](Sum3& x) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t a = __shfl_up_sync(full, x.a, o), b = __shfl_up_sync(full, x.b, o), c = __shfl_up_sync(full, x.c, o);
+            if (lane >= o) { x.a += a; x.b += b; x.c += c; }
+        }
+    };
+    scan_warp(v);
+    __syncthreads();                                       // the sums of the previous call have been read
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    Sum3 w = warp_sums[lane];
+    scan_warp(w);
+    total = {__shfl_sync(full, w.a, 31), __shfl_sync(full, w.b, 31), __shfl_sync(full, w.c, 31)};
+    const int from = warp > 0 ? warp - 1 : 0;
+    const int32_t a = __shfl_sync(full, w.a, from), b = __shfl_sync(full, w.b, from), c = __shfl_sync(full, w.c, from);
+    if (warp > 0) { v.a += a; v.b += b; v.c += c; }
+    return v;
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 1)
+ecco_paged_plan_kernel(const PagedPlan p)
+{
+    __shared__ Sum3 warp_sums[32];
+    __shared__ long long totals[3];                        // new tokens, pages, tiles of all requests
+    __shared__ int32_t first_row[kPlanThreads + 1], ctx_s[kPlanThreads], page_from[kPlanThreads];
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & 31;
+    const int32_t page_size = 1 << p.page_shift;
+    release_dependents();
+    if (tid < 3) totals[tid] = 0;
+    __syncthreads();
+    dependency_wait();
+    // lengths of request r; those behind the last are zero
+    auto lengths = [&](int r, int32_t& ctx, int32_t& added) {
+        ctx = r < p.n_req ? __ldcg(p.ctx + r) : 0;
+        added = r < p.n_req ? __ldcg(p.added + r) : 0;
+    };
+    // first the totals: all requests are served or none
+    bool fine = true;
+    long long sum[3] = {0, 0, 0};
+    int32_t ctx0 = 0, added0 = 0;                          // of the first round, which usually is the only one
+    for (int r = tid; r < p.n_req; r += kPlanThreads) {
+        int32_t ctx, added;
+        lengths(r, ctx, added);
+        if (r == tid) { ctx0 = ctx; added0 = added; }
+        const long long kv = static_cast<long long>(ctx) + added;
+        fine = fine && ctx >= 0 && added >= 0 && kv <= static_cast<long long>(p.stride) << p.page_shift;
+        sum[0] += added;
+        sum[1] += ((kv + page_size - 1) >> p.page_shift) - ((static_cast<long long>(ctx) + page_size - 1) >> p.page_shift);
+        sum[2] += (kv + 31) >> 5;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+        if (lane == 0 && sum[i]) atomicAdd(reinterpret_cast<unsigned long long*>(&totals[i]), static_cast<unsigned long long>(sum[i]));
+    }
+    fine = __syncthreads_and(fine) && totals[0] <= INT32_MAX && totals[2] <= INT32_MAX;
+    const int32_t status = !fine ? ECCO_ERR_INVALID_ARG : totals[0] > p.n_slots || totals[1] > p.n_free ? ECCO_ERR_WORKSPACE : 0;
+    const int32_t n_new = status ? 0 : static_cast<int32_t>(totals[0]);
+    if (blockIdx.x == 0 && tid < 4) p.result[tid] = tid == 0 ? status : status ? 0 : static_cast<int32_t>(totals[tid == 1 ? 1 : tid == 2 ? 0 : 2]);
+
+    // this CTA's rows
+    const int32_t per = static_cast<int32_t>((static_cast<long long>(p.n_slots) + gridDim.x - 1) / gridDim.x);
+    const int32_t row0 = static_cast<int32_t>(min(static_cast<long long>(p.n_slots), static_cast<long long>(per) * blockIdx.x));
+    const int32_t row1 = static_cast<int32_t>(min(static_cast<long long>(p.n_slots), static_cast<long long>(row0) + per));
+    for (long long i = max(row0, n_new) + static_cast<long long>(tid); i < row1; i += kPlanThreads) p.slots[i] = -1;
+    Sum3 before = {0, 0, 0};
+    const int rounds = (p.n_req + kPlanThreads - 1) / kPlanThreads;
+    for (int round = 0; round < rounds; ++round) {
+        const int r = round * kPlanThreads + tid;
+        int32_t ctx = ctx0, added = added0;
+        if (round > 0) lengths(r, ctx, added);
+        if (status) ctx = added = 0;
+        const long long kv = static_cast<long long>(ctx) + added;
+        const int32_t held = static_cast<int32_t>((static_cast<long long>(ctx) + page_size - 1) >> p.page_shift);
+        const Sum3 mine = {added, static_cast<int32_t>((kv + page_size - 1) >> p.page_shift) - held, static_cast<int32_t>((kv + 31) >> 5)};
+        Sum3 total;
+        const Sum3 upto = scan3(mine, total, warp_sums);   // its barriers: the previous round's rows are done, see below
+        first_row[tid] = before.a + upto.a - mine.a;
+        ctx_s[tid] = ctx;
+        page_from[tid] = before.b + upto.b - mine.b - held;      // free page of table entry e: page_from + e
+        if (tid == 0) first_row[kPlanThreads] = before.a + total.a;
+        if (static_cast<int>(blockIdx.x) == round % static_cast<int>(gridDim.x) && r < p.n_req) {
+            p.kv_lens[r] = static_cast<int32_t>(kv);
+            p.cu_new[r + 1] = before.a + upto.a;
+            p.kv_tiles[r + 1] = before.c + upto.c;
+        }
+        __syncthreads();
+        const int32_t from = max(row0, before.a), to = min(row1, before.a + total.a);
+        for (long long row = from + static_cast<long long>(tid); row < to; row += kPlanThreads) {
+            int lo = 0, hi = kPlanThreads;                 // the last request that begins at or before the row has it: empty ones begin before it
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (first_row[mid] <= row) lo = mid; else hi = mid;
+            }
+            const int32_t t = ctx_s[lo] + static_cast<int32_t>(row) - first_row[lo], e = t >> p.page_shift;
+            int32_t* const entry = p.tables + static_cast<int64_t>(round * kPlanThreads + lo) * p.stride + e;
+            const bool taken = e < (static_cast<int32_t>((static_cast<long long>(ctx_s[lo]) + page_size - 1) >> p.page_shift));
+            const int32_t page = taken ? __ldcg(entry) : __ldcg(p.free_pages + page_from[lo] + e);
+            if (!taken && (t & (page_size - 1)) == 0) *entry = page;
+            p.slots[row] = page >= 0 && page < p.n_pages ? (page << p.page_shift) + (t & (page_size - 1)) : -1;
+        }
+        __syncthreads();
+        before.a += total.a;
+        before.b += total.b;
+        before.c += total.c;
+    }
+    if (blockIdx.x == 0 && tid == 0) { p.cu_new[0] = 0; p.kv_tiles[0] = 0; }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention over the pages.  The blocks are decoded once per call, by the decoder of ecco_decompress at its full rate, into
+// tiles of 32 tokens in the workspace; the attention kernels read these.  A tile is 8 KB:
+//   eight [32 tokens][16 dims] fp16 pieces of 1 KB, the 16-byte halves of a 32-byte row swapped in every second block of four rows
+// which is what the decoder's staging pieces look like in shared memory, what ldmatrix reads without conflicts, and, for tcgen05, the
+// canonical layout of both a K operand (contraction over dims, K-major) and a V operand (contraction over tokens, MN-major)
+// with 32-byte swizzle.  One layout for all, moved by plain bulk copies.
+// Decoding inside of the attention kernel instead leaves the decoder 17 warps (9.6 KB of tiles per warp and two sets of tables) instead
+// of 31 and one symbol per lookup instead of two, and decodes again for every row tile.
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t kPieceBytes = 1024;                     // 32 tokens x 16 dims
+constexpr uint32_t kKvTileBytes = 8 * kPieceBytes;
+
+struct PagedKv {
+    const uint8_t *k_meta, *v_meta, *k_blocks, *v_blocks;
+    const int32_t *tables, *cu_new, *kv_lens, *kv_tiles;
+    int32_t n_pages, page_shift, all_heads, stride, n_req, n_tokens, max_tiles;
+    int32_t head0, heads;      // KV heads of this launch
+    uint8_t* staged;           // [K, V][heads][max_tiles] tiles
+};
+__device__ __forceinline__ uint8_t* staged_tile(const PagedKv& kv, int which, int head, int tile)
+{
+    return kv.staged + ((static_cast<uint64_t>(which) * kv.heads + head) * kv.max_tiles + tile) * kKvTileBytes;
+}
+// tiles of all requests, cut to what the workspace was made for
+__device__ __forceinline__ int32_t paged_tiles(const PagedKv& kv) { return min(max(__ldcg(kv.kv_tiles + kv.n_req), 0), kv.max_tiles); }
+
+// Where a request's tiles and rows are, whatever the arrays hold: inside of the workspace and of q.
+struct PagedReq { int32_t first, tiles, kv, row0, rows; };
+__device__ __forceinline__ PagedReq paged_req(const PagedKv& kv, int r, int32_t T)
+{
+    PagedReq q;
+    const int32_t t0 = __ldcg(kv.kv_tiles + r), t1 = __ldcg(kv.kv_tiles + r + 1), c0 = __ldcg(kv.cu_new + r), c1 = __ldcg(kv.cu_new + r + 1), len = __ldcg(kv.kv_lens + r);
+    q.first = min(max(t0, 0), T);
+    q.tiles = min(max(t1, q.first), T) - q.first;
+    q.kv = static_cast<int32_t>(min(static_cast<int64_t>(max(len, 0)), static_cast<int64_t>(q.tiles) * 32));
+    q.row0 = min(max(c0, 0), kv.n_tokens);
+    q.rows = min(max(c1, q.row0), kv.n_tokens) - q.row0;
+    return q;
+}
+// The last r in 0 .. n - 1 with begin[r] <= x (0 if there is none), by the whole warp: 32 probes at a time.
+__device__ __forceinline__ int warp_find(const int32_t* begin, int n, int32_t x)
+{
+    const int lane = static_cast<int>(threadIdx.x & 31u);
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 31) >> 5, at = lane * step;
+        const bool below = at < n && __ldcg(begin + lo + at) <= x;
+        const int last = max(31 - __clz(__ballot_sync(0xffffffffu, below)), 0);
+        lo += last * step;
+        n = min(step, n - last * step);
+    }
+    return lo;
+}
+
+// K6s: pages -> tiles.  ecco_decompress_tma_kernel with another way in (a lane finds its token's block through the request's table)
+// and out (a piece leaves by one bulk copy of 1 KB).  Even CTAs decode K, odd ones V: both have the same number of tiles, no CTA
+// needs both sets of tables, and small calls decode K and V side by side.
+// Values are clamped to fp16's finite range (once per group, on the sixteen values of its table): weight zero times an infinity would
+// be NaN in rows that do not see the token.
+template <int kMaxWarps>
+__global__ void __launch_bounds__(kMaxWarps * 32, 1)
+ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const int which = static_cast<int>(blockIdx.x & 1u);
+    const uint32_t cta = blockIdx.x >> 1, ctas = gridDim.x >> 1;
+    const uint8_t* const d_meta = which ? kv.v_meta : kv.k_meta;
+    const uint32_t swz = ((lane >> 2) & 1u) << 4;
+    release_dependents();
+    const DecodeTables tb = plan_decode_tables(smem_u32(smem), d_meta, true);
+    issue_decode_tables(tb, d_meta);
+    const uint32_t tiles_base = (tb.warp_base + 1023u) & ~1023u;
+    const uint32_t nw = decode_warps(tb, kTmaWarpBytes, tiles_base - tb.warp_base);
+    const uint32_t stage = tiles_base + warp * 1024;
+    const uint32_t bits = tiles_base + nw * 1024 + warp * kBitBytes + lane * 4;
+    const uint32_t my_row = stage + lane * 32;
+    if (!finish_decode_tables(tb)) return;
+    dependency_wait();
+    const float T = tb.T;
+    const uint32_t n_tiles = static_cast<uint32_t>(paged_tiles(kv)), units = n_tiles * kv.heads;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+    const uint32_t tile_stride = balanced_warps(units, ctas * nw);
+    uint32_t u = warp * ctas + cta;
+    if (warp >= nw || u >= tile_stride) return;
+
+    const uint8_t* const blocks = which ? kv.v_blocks : kv.k_blocks;
+    // the block of this lane's token of unit u, NULL behind the request's last token
+    auto block_ptr = [&](uint32_t unit) -> const uint8_t* {
+        const uint32_t head = unit / n_tiles, tile = unit - head * n_tiles;
+        const int r = warp_find(kv.kv_tiles, kv.n_req, static_cast<int32_t>(tile));
+        const int64_t token = (static_cast<int64_t>(tile) - __ldcg(kv.kv_tiles + r)) * 32 + lane;
+        if (token < 0 || token >= __ldcg(kv.kv_lens + r)) return nullptr;
+        const int64_t e = token >> kv.page_shift;
+        const int32_t page = e < kv.stride ? __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + e) : -1;
+        if (page < 0 || page >= kv.n_pages) {
+            atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+            return nullptr;
+        }
+        const int64_t at = ((static_cast<int64_t>(page) * kv.all_heads + kv.head0 + head) << kv.page_shift) + (token & ((1 << kv.page_shift) - 1));
+        return blocks + at * kBlockBytes;
+    };
+    const uint8_t* next = block_ptr(u);
+    while (u < units) {
+        const uint32_t head = u / n_tiles;
+        uint8_t* const dst = staged_tile(kv, which, static_cast<int>(head), static_cast<int>(u - head * n_tiles));
+        Block blk;
+        const bool there = next != nullptr;
+        if (there) {
+            ldg_block(blk, next);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) blk.w[i] = 0;     // whatever it decodes to: finite, and a token that no row sees
+        }
+        LaneGroup lg = open_block<true>(blk, bits, tb, T);
+        u += tile_stride;
+        if (u < units) {
+            next = block_ptr(u);
+            if (next) prefetch_block_l2(next);
+        }
+        auto send_piece = [&](int piece) {
+            fence_async_smem();                            // generic-proxy writes -> visible to the engine
+            __syncwarp();
+            if (lane == 0) { bulk_s2g(dst + piece * kPieceBytes, stage, kPieceBytes); bulk_commit(); }
+        };
+        const uint32_t end = decode_group<kBlockBits, kBlockFreeSteps>(lg, bits, tb.pairs, [&](int i, uint32_t ranks, bool cutting, int n_ok) {
+            uint32_t v[4];
+            map_ranks(lg, ranks, v);
+            if (cutting) cut_values(v, n_ok);
+            if (!(i & 1)) {
+                if (lane == 0) bulk_wait_read0();          // the engine has read the previous piece
+                __syncwarp();
+                sts_v4(my_row + swz, v[0], v[1], v[2], v[3]);
+            } else {
+                sts_v4(my_row + (swz ^ 16u), v[0], v[1], v[2], v[3]);
+                if (i != 15) send_piece(i >> 1);
+            }
+        });
+        const int n_pad = pads_of(end);
+        const int n_max = __reduce_max_sync(0xffffffffu, n_pad);
+        if (n_max > 0) {
+            if (lane == 0) bulk_wait_all();                // pieces 0..6 of this tile are in memory
+            __syncwarp();
+#pragma unroll 1
+            for (int j = 0; j < n_max; ++j) {              // ascending: a later pad overrides an earlier one
+                if (j < n_pad) {
+                    const uint32_t f = pad_field(bits, j), loc = f & 127u, byte = ((loc & 15u) * 2) ^ swz;
+                    const float v = fminf(fmaxf(fp8_to_float(f >> 7) * T, -65504.0f), 65504.0f);
+                    if (loc >= 112u) sts_u16(my_row + byte, f2h_bits(v));
+                    else *reinterpret_cast<uint16_t*>(dst + (loc >> 4) * kPieceBytes + lane * 32 + byte) = static_cast<uint16_t>(f2h_bits(v));
+                }
+            }
+        }
+        send_piece(7);
+    }
+    if (lane == 0) bulk_wait_all();
+}
+
+// ---------------------------------------------------------------------------------------------
+// K6a: attention of requests of few rows (new tokens x query heads per KV head): single tokens, drafted tokens.
+// All tiles of all heads form one line, which is cut into equal runs, one per warp, whatever the requests' lengths: a warp is
+// alone from its first tile to its last.  It keeps a ring of tiles in shared memory, filled by bulk copies, and does
+//   S = Q K^T (16 rows x 32 tokens a tile, mma.sync), the softmax on the way in fp32, O += P V
+// with P taken from the scores' registers as they are.  A piece of a request that lies in one run as a whole is written out; the others
+// leave sums and maxima in the workspace and are joined by ecco_paged_combine_kernel.
+// Bound by memory: 512 bytes per token and KV head.
+// ---------------------------------------------------------------------------------------------
+struct PagedOut {
+    const __half* q;
+    int64_t q_stride;
+    float scale_log2;          // scale * log2(e)
+    int32_t q_per_kv, q_heads, causal;
+    int32_t row_from;          // first row of a request in this launch
+    __half* out;
+    float* lse;                // or NULL
+    float* part;               // partial sums [slot][rows][128]
+    float2* part_ml;           // maxima (log2) and sums of weights [slot][rows]
+};
+constexpr int kFewStages = 2;
+template <int kM> constexpr int kFewWarps = kM == 1 ? 6 : 5;
+template <int kM> constexpr uint32_t kFewWarpBytes = kFewStages * 2 * kKvTileBytes + kM * 4096;
+template <int kM> constexpr uint32_t kFewSmemBytes = kFewWarps<kM> * kFewWarpBytes<kM> + 1024;
+
+// Weights enter the tensor cores times 2^15: taken as they are, those below 6e-5 would lose bits and those below 3e-8 vanish.
+constexpr float kWeightLog2 = 15.0f;
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float log2_fast(float x)
+{
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// natural logarithm of a sum of weights that stands at l * 2^(m - offset)
+__device__ __forceinline__ float lse_of(float m, float l, float offset)
+{
+    return l > 0.0f ? (m - offset + log2f(l)) * 0.693147180559945309f : -INFINITY;
+}
+__device__ __forceinline__ uint32_t pack_h2(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// tokens that row i of a request sees
+__device__ __forceinline__ int32_t tokens_seen(const PagedReq& q, int32_t token, bool causal)
+{
+    return causal ? min(max(q.kv - q.rows + token + 1, 0), q.kv) : q.kv;
+}
+// bounded wait of a warp on one of its barriers
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
+{
+    bool done = false;
+    for (int i = 0; i < 2 * kWaitLimit && !done; ++i) done = mbar_try_wait(bar, parity);
+    done = __all_sync(0xffffffffu, done);
+    if (!done && (threadIdx.x & 31u) == 0) atomicExch(&g_device_status, ECCO_ERR_DEVICE_TIMEOUT);
+    return done;
+}
+
+template <int kM>
+__global__ void __launch_bounds__(kFewWarps<kM> * 32, 1)
+ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    constexpr unsigned full = 0xffffffffu;
+    constexpr int kRows = 16 * kM;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t mine = smem_u32(smem) + 1024 + warp * kFewWarpBytes<kM>, q_at = mine + kFewStages * 2 * kKvTileBytes;
+    const uint32_t bar = smem_u32(smem) + warp * kFewStages * 8;
+    release_dependents();
+    if (lane == 0)
+        for (int s = 0; s < kFewStages; ++s) mbar_init(bar + s * 8, 1);
+    __syncwarp();
+    dependency_wait();
+    const int32_t T = paged_tiles(kv);
+    const int W = static_cast<int>(gridDim.x) * kFewWarps<kM>, wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
+    const int64_t U = static_cast<int64_t>(T) * kv.heads;
+    const UnitSplit split(U, W);
+    const int64_t u0 = split.begin(wg), u1 = split.begin(wg + 1);
+
+    // a place in the run: unit u is tile `tile` of head `head`, which belongs to request r
+    struct Place { int64_t u, end; int32_t head, tile, r; PagedReq q; };
+    // moves to the first unit at or behind p.u whose request has rows for this kernel; p.end: the request's end in this run
+    auto seek = [&](Place& p) {
+        while (p.u < u1) {
+            p.head = static_cast<int32_t>(divide(static_cast<uint64_t>(p.u), static_cast<uint64_t>(T)));
+            p.tile = static_cast<int32_t>(p.u - static_cast<int64_t>(p.head) * T);
+            p.r = warp_find(kv.kv_tiles, kv.n_req, p.tile);
+            p.q = paged_req(kv, p.r, T);
+            // a request's tiles begin at or before this one and end behind it, unless the arrays are broken
+            const int64_t last = static_cast<int64_t>(p.head) * T + max(p.q.first + p.q.tiles, p.tile + 1);
+            p.end = min(last, u1);
+            if (static_cast<int64_t>(p.q.rows) * o.q_per_kv > o.row_from && p.q.first <= p.tile && p.tile < p.q.first + p.q.tiles) return;
+            p.u = p.end;
+        }
+    };
+    Place load = {};                                       // the next tile to ask for
+    load.u = u0;
+    seek(load);
+    Place at = load;                                       // the tile at hand
+    uint32_t asked = 0, taken = 0;
+    auto ask = [&]() {
+        if (load.u >= u1) return;
+        if (lane == 0) {
+            const uint32_t s = asked % kFewStages, b = bar + s * 8, dst = mine + s * 2 * kKvTileBytes;
+            mbar_expect_tx(b, 2 * kKvTileBytes);
+            bulk_g2s(dst, staged_tile(kv, 0, load.head, load.tile), kKvTileBytes, b);
+            bulk_g2s(dst + kKvTileBytes, staged_tile(kv, 1, load.head, load.tile), kKvTileBytes, b);
+        }
+        ++asked;
+        ++load.tile;
+        if (++load.u == load.end) seek(load);
+    };
+    for (int s = 0; s < kFewStages; ++s) ask();
+
+    const uint32_t col = (lane & 3u) * 2;
+    bool ok = true;
+    while (ok && at.u < u1) {
+        const PagedReq q = at.q;
+        const int R = min(q.rows * o.q_per_kv - o.row_from, kRows);
+        const bool whole = at.tile == q.first && at.end - at.u == q.tiles;
+        const int slot = 2 * wg + (at.u == u0 ? 0 : 1);
+        // the rows of q as tiles: rows beyond the last are zero
+        __syncwarp();
+        for (uint32_t c = lane; c < kRows * 16; c += 32) {
+            const uint32_t row = c >> 4, chunk = c & 15u;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (static_cast<int>(row) < R) {
+                const uint32_t i = (o.row_from + row) / o.q_per_kv, g = o.row_from + row - i * o.q_per_kv;
+                v = __ldcg(reinterpret_cast<const uint4*>(o.q + (q.row0 + i) * o.q_stride + (static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + g) * kGroup) + chunk);
+            }
+            sts_v4(q_at + (row >> 4) * 4096 + (chunk >> 1) * 512 + tile_byte(row & 15u, (chunk & 1u) * 8), v.x, v.y, v.z, v.w);
+        }
+        __syncwarp();
+        float acc[kM][16][4], m[kM][2], l[kM][2];
+        int32_t seen[kM][2];
+#pragma unroll
+        for (int t = 0; t < kM; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = t * 16 + static_cast<int>(lane >> 2) + 8 * i;
+                seen[t][i] = row < R ? tokens_seen(q, (o.row_from + row) / o.q_per_kv, o.causal) : 0;
+                m[t][i] = -INFINITY;
+                l[t][i] = 0.0f;
+            }
+#pragma unroll
+        for (int t = 0; t < kM; ++t)
+#pragma unroll
+            for (int n = 0; n < 16; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.0f;
+
+        for (; at.u < at.end; ++at.u, ++at.tile) {
+            const uint32_t s = taken % kFewStages, k_tile = mine + s * 2 * kKvTileBytes, v_tile = k_tile + kKvTileBytes;
+            ok = warp_wait(bar + s * 8, (taken / kFewStages) & 1u);
+            if (!ok) break;
+            ++taken;
+            // scores: rows x 8 tokens per fragment
+            float sc[kM][4][4];
+#pragma unroll
+            for (int t = 0; t < kM; ++t)
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[t][n][i] = 0.0f;
+            const uint32_t k_at = k_tile + tile_byte((lane & 7u) + ((lane >> 4) & 1u) * 8, ((lane >> 3) & 1u) * 8);
+            const uint32_t a_at = q_at + tile_byte((lane & 7u) + ((lane >> 3) & 1u) * 8, (lane >> 4) * 8);
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+                uint32_t b[2][4];
+                ldmatrix_x4(b[0], k_at + d * kPieceBytes);
+                ldmatrix_x4(b[1], k_at + d * kPieceBytes + 512);
+#pragma unroll
+                for (int t = 0; t < kM; ++t) {
+                    uint32_t a[4];
+                    ldmatrix_x4(a, a_at + t * 4096 + d * 512);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) mma_16816(sc[t][n], a, b[n >> 1][(n & 1) * 2], b[n >> 1][(n & 1) * 2 + 1]);
+                }
+            }
+            // softmax: relative to the largest score so far
+            const int32_t t0 = (at.tile - q.first) * 32 + static_cast<int32_t>(col);
+            uint32_t p[kM][2][4];                          // A fragments of 16 tokens each
+#pragma unroll
+            for (int t = 0; t < kM; ++t) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float top = m[t][i];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float& x = sc[t][n][2 * i + e];
+                            x = t0 + n * 8 + e < seen[t][i] ? x * o.scale_log2 : -INFINITY;
+                            top = fmaxf(top, x);
+                        }
+                    top = fmaxf(top, __shfl_xor_sync(full, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(full, top, 2));
+                    const float base = top == -INFINITY ? 0.0f : top;          // a row that has seen nothing: all weights zero
+                    const float f = exp2_fast(m[t][i] - base);
+                    if (__any_sync(full, top > m[t][i])) {
+                        l[t][i] *= f;
+#pragma unroll
+                        for (int n = 0; n < 16; ++n) { acc[t][n][2 * i] *= f; acc[t][n][2 * i + 1] *= f; }
+                    }
+                    m[t][i] = top;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float& x = sc[t][n][2 * i + e];
+                            x = exp2_fast(x - base + kWeightLog2);
+                            l[t][i] += x;
+                        }
+                }
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    p[t][n >> 1][(n & 1) * 2] = pack_h2(sc[t][n][0], sc[t][n][1]);
+                    p[t][n >> 1][(n & 1) * 2 + 1] = pack_h2(sc[t][n][2], sc[t][n][3]);
+                }
+            }
+            const uint32_t v_at = v_tile + tile_byte((lane & 7u) + ((lane >> 3) & 1u) * 8, (lane >> 4) * 8);
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    uint32_t b[4];
+                    ldmatrix_x4_trans(b, v_at + d * kPieceBytes + ks * 512);
+#pragma unroll
+                    for (int t = 0; t < kM; ++t) {
+                        mma_16816(acc[t][2 * d], p[t][ks], b[0], b[1]);
+                        mma_16816(acc[t][2 * d + 1], p[t][ks], b[2], b[3]);
+                    }
+                }
+            __syncwarp();                                  // the whole warp has read the tile
+            ask();
+        }
+        // out, or into a slot
+#pragma unroll
+        for (int t = 0; t < kM; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float sum = l[t][i];
+                sum += __shfl_xor_sync(full, sum, 1);
+                sum += __shfl_xor_sync(full, sum, 2);
+                const int row = t * 16 + static_cast<int>(lane >> 2) + 8 * i;
+                if (row >= R || !ok) continue;
+                if (whole) {
+                    const int token = (o.row_from + row) / o.q_per_kv, hq = (kv.head0 + at.head) * o.q_per_kv + o.row_from + row - token * o.q_per_kv;
+                    const int64_t at_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + hq;
+                    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                    uint32_t* const dst = reinterpret_cast<uint32_t*>(o.out + at_row * kGroup) + (lane & 3u);
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) dst[n * 4] = pack_h2(acc[t][n][2 * i] * inv, acc[t][n][2 * i + 1] * inv);
+                    if (o.lse && (lane & 3u) == 0) o.lse[at_row] = lse_of(m[t][i], sum, kWeightLog2);
+                } else {
+                    const int64_t at_row = static_cast<int64_t>(slot) * kRows + row;
+                    float2* const dst = reinterpret_cast<float2*>(o.part + at_row * kGroup) + (lane & 3u);
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) dst[n * 4] = make_float2(acc[t][n][2 * i], acc[t][n][2 * i + 1]);
+                    if ((lane & 3u) == 0) o.part_ml[at_row] = make_float2(m[t][i], sum);
+                }
+            }
+        if (ok) seek(at);
+    }
+    if (!ok)                                               // tiles on their way land before the warp leaves
+        for (; taken < asked; ++taken) warp_wait(bar + (taken % kFewStages) * 8, (taken / kFewStages) & 1u);
+}
+
+// Joins the pieces of rows whose request was cut, and writes the rows that see nothing.  `team` warps to a (new token, query head).
+template <int kM>
+__global__ void __launch_bounds__(256)
+ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, int few_ctas, int team)
+{
+    __shared__ float4 sums[8][32];
+    __shared__ float2 ml[8];
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5), sub = warp % team;
+    release_dependents();
+    dependency_wait();
+    const int slice_heads = kv.heads * o.q_per_kv;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * (8 / team) + warp / team;
+    const bool exists = item < static_cast<int64_t>(kv.n_tokens) * slice_heads;
+    const int token = exists ? static_cast<int>(item / slice_heads) : 0, hq = exists ? static_cast<int>(item - static_cast<int64_t>(token) * slice_heads) : 0;
+    const int32_t T = paged_tiles(kv);
+    const int r = warp_find(kv.cu_new, kv.n_req, token);
+    const PagedReq q = paged_req(kv, r, T);
+    const int i = token - q.row0;
+    const int head = hq / o.q_per_kv, row = i * o.q_per_kv + hq - head * o.q_per_kv - o.row_from;
+    const bool mine = exists && i >= 0 && i < q.rows && row >= 0 && row < 16 * kM;
+    const int64_t at_row = static_cast<int64_t>(token) * o.q_heads + kv.head0 * o.q_per_kv + hq;
+    int w_lo = 0, w_hi = -1;
+    bool first_slot = true;
+    if (mine && q.tiles > 0) {
+        const UnitSplit split(static_cast<int64_t>(T) * kv.heads, few_ctas * kFewWarps<kM>);
+        const int64_t f0 = static_cast<int64_t>(head) * T + q.first;
+        w_lo = split.owner(f0);
+        w_hi = split.owner(f0 + q.tiles - 1);
+        first_slot = split.begin(w_lo) == f0;
+    }
+    const bool joins = w_hi > w_lo;
+    float m = -INFINITY, l = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (joins) {
+        for (int w = w_lo + sub; w <= w_hi; w += team) {
+            const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && !first_slot ? 1 : 0)) * (16 * kM) + row;
+            const float2 x = __ldcg(o.part_ml + at);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
+            if (x.y == 0.0f) continue;                     // nothing seen there
+            const float top = fmaxf(m, x.x), f0 = exp2_fast(m - top), f1 = exp2_fast(x.x - top);
+            l = l * f0 + x.y * f1;
+            acc.x = acc.x * f0 + v.x * f1;
+            acc.y = acc.y * f0 + v.y * f1;
+            acc.z = acc.z * f0 + v.z * f1;
+            acc.w = acc.w * f0 + v.w * f1;
+            m = top;
+        }
+    }
+    if (team > 1) {
+        sums[warp][lane] = acc;
+        if (lane == 0) ml[warp] = make_float2(m, l);
+        __syncthreads();
+        if (sub == 0) {
+            for (int w = 1; w < team; ++w) {
+                const float2 x = ml[warp + w];
+                const float4 v = sums[warp + w][lane];
+                if (x.y == 0.0f) continue;
+                const float top = fmaxf(m, x.x), f0 = exp2_fast(m - top), f1 = exp2_fast(x.x - top);
+                l = l * f0 + x.y * f1;
+                acc.x = acc.x * f0 + v.x * f1;
+                acc.y = acc.y * f0 + v.y * f1;
+                acc.z = acc.z * f0 + v.z * f1;
+                acc.w = acc.w * f0 + v.w * f1;
+                m = top;
+            }
+        }
+    }
+    if (sub == 0 && mine && (joins || q.tiles == 0)) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        reinterpret_cast<uint2*>(o.out + at_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
+        if (o.lse && lane == 0) o.lse[at_row] = lse_of(m, l, kWeightLog2);
+    }
+}
+
+}  // namespace

@@ -1,0 +1,330 @@
+"""The paged KV cache: ecco_paged_plan, ecco_paged_append, ecco_paged_attn.
+
+Reference: plans in plain Python, blocks by the oracle's encoder, attention in 64 bits over what the oracle's decoder makes of the
+blocks.  Tolerances of the attention, per output, from the kernels' roundings:
+  scores: 128 products, exact in fp32, added on the tensor cores, which cut off: eps_s = 128 * 2^-23 * scale * max_t sum |q k|, and one
+          rounding each of scale * log2(e), of the product with it and of the difference to the maximum: 2^-22 * |s|;
+  weights: fp16, half a step 2^-11; exp2 2^-22; those below fp16's normal range 2^-40 of the largest weight each;
+  sums over n tokens on the tensor cores, sixteen a step: (n / 16 + 32) * 2^-23;
+  the output's own rounding: 2^-11 of it, or 2^-25.
+  |out - ref| <= 2^-11 |ref| + (2^-11 + 2 e_s + (n / 16 + 32) 2^-23 + n 2^-40) sum p |v| + 2^-25, e_s = eps_s + 2^-22 max |s| + 2^-22
+  |lse - ref| <= e_s + (n / 16 + 32) 2^-23 + 2^-22 |ref| + 2^-20.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from helpers import lib_meta_from_oracle
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="session")
+def B():
+    from paper_2505_06901_b200 import binding as b
+
+    b.lib()
+    return b
+
+
+@pytest.fixture(scope="session")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.fail("the gpu tests need a CUDA device")
+    return "cuda"
+
+
+def ints(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+# ------------------------------------------------------------------ refusals, on the CPU
+def test_argument_errors_without_a_gpu(B):
+    L, INV, ALIGN = B.lib(), B.ERR_INVALID_ARG, B.ERR_ALIGNMENT
+
+    def plan(page=16, pages=8, n_req=2, ctx=64, new=64, free=64, n_free=4, tables=64, stride=4, slots=64, n_slots=9, cu=64, lens=64, tiles=64, result=64):
+        return L.ecco_paged_plan(page, pages, n_req, ctx, new, free, n_free, tables, stride, slots, n_slots, cu, lens, tiles, result, None)
+
+    for bad in (dict(page=0), dict(page=12), dict(page=8192), dict(pages=0), dict(page=4096, pages=1 << 19), dict(n_req=-1), dict(n_req=65536), dict(n_free=-1),
+                dict(stride=-1), dict(n_slots=-1), dict(ctx=None), dict(new=None), dict(free=None), dict(tables=None), dict(slots=None), dict(cu=None),
+                dict(lens=None), dict(tiles=None), dict(result=None)):
+        assert plan(**bad) == INV, bad
+    for name in ("ctx", "new", "free", "tables", "slots", "cu", "lens", "tiles", "result"):
+        assert plan(**{name: 66}) == ALIGN, name
+
+    def cache(k_meta=64, v_meta=64, k=64, v=64, pages=8, heads=2, page=16):
+        return B.PagedCache(k_meta, v_meta, k, v, pages, heads, page)
+
+    def append(c=None, k=64, v=64, stride=256, slots=64, n=3):
+        return L.ecco_paged_append(ctypes.byref(c or cache()), k, v, stride, slots, n, None)
+
+    bad_caches = (dict(k_meta=None), dict(v_meta=None), dict(k=None), dict(v=None), dict(pages=0), dict(heads=0), dict(heads=65536), dict(page=3),
+                  dict(page=4096, pages=1 << 19))
+    assert append(n=0) == 0 and append(n=-1) == INV and L.ecco_paged_append(None, 64, 64, 256, 64, 3, None) == INV
+    for bad in bad_caches:
+        assert append(cache(**bad)) == INV, bad
+    for bad in (dict(k=None), dict(v=None), dict(slots=None), dict(stride=248)):
+        assert append(**bad) == INV, bad
+    for bad in (dict(c=cache(k=80)), dict(c=cache(v=80)), dict(c=cache(k_meta=72)), dict(c=cache(v_meta=72)), dict(k=72), dict(v=72), dict(slots=66), dict(stride=257)):
+        assert append(**bad) == ALIGN, bad
+
+    def batch(tables=64, cu=64, lens=64, tiles=64, stride=4, n_req=2, tokens=3, new=2, kv=60, n_tiles=4):
+        return B.PagedBatch(tables, cu, lens, tiles, stride, n_req, tokens, new, kv, n_tiles)
+
+    def attn(c=None, b=None, g=2, q=64, stride=512, scale=0.1, flags=1, out=64, lse=64, ws=64, ws_bytes=1 << 30):
+        return L.ecco_paged_attn(ctypes.byref(c or cache()), ctypes.byref(b or batch()), g, q, stride, ctypes.c_float(scale), flags, out, lse, ws, ws_bytes, None)
+
+    assert attn(b=batch(n_req=0)) == 0 and attn(b=batch(tokens=0)) == 0                        # nothing to do
+    for bad in bad_caches:
+        assert attn(cache(**bad)) == INV, bad
+    for bad in (dict(g=0), dict(g=17), dict(scale=math.nan), dict(scale=math.inf), dict(flags=2), dict(q=None), dict(out=None), dict(stride=504),
+                dict(b=batch(tables=None)), dict(b=batch(cu=None)), dict(b=batch(lens=None)), dict(b=batch(tiles=None)), dict(b=batch(stride=-1)),
+                dict(b=batch(n_req=65536)), dict(b=batch(tokens=-1)), dict(b=batch(new=-1)), dict(b=batch(kv=-1)), dict(b=batch(n_tiles=-1)),
+                dict(b=batch(n_tiles=1 << 30))):
+        assert attn(**bad) == INV, bad
+    for bad in (dict(q=72), dict(out=72), dict(lse=66), dict(stride=513), dict(b=batch(tables=66)), dict(b=batch(cu=66)), dict(b=batch(lens=66)),
+                dict(b=batch(tiles=66)), dict(c=cache(k=80))):
+        assert attn(**bad) == ALIGN, bad
+    need = lambda c, b, g: int(L.ecco_paged_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(b), g))  # noqa: E731
+    assert need(cache(), batch(), 2) >= 4 * 2 * 2 * 8192 and need(cache(), batch(), 0) == 0 and need(cache(), batch(n_tiles=-1), 2) == 0
+    assert need(cache(heads=1), batch(), 2) < need(cache(heads=8), batch(), 2)
+
+
+# ------------------------------------------------------------------ plan
+def plan_reference(page, n_pages, ctx, new, free, tables, n_slots):
+    tables, slots, taken = tables.copy(), np.full(n_slots, -1, np.int32), 0
+    cu, tiles, row = [0], [0], 0
+    for r, (c, n) in enumerate(zip(ctx, new)):
+        held, total = -(-c // page), -(-(c + n) // page)
+        tables[r, held:total] = free[taken:taken + total - held]
+        taken += total - held
+        for t in range(c, c + n):
+            e = tables[r, t // page]
+            slots[row] = e * page + t % page if 0 <= e < n_pages else -1
+            row += 1
+        cu.append(row)
+        tiles.append(tiles[-1] + -(-(c + n) // 32))
+    return tables, slots, np.array(cu), np.asarray(ctx, dtype=np.int64) + new, np.array(tiles), np.array([0, taken, row, tiles[-1]])
+
+
+def run_plan(B, page, n_pages, ctx, new, free, tables, n_slots):
+    n = len(ctx)
+    d_tables = ints(tables)
+    out = [torch.full((k,), -7, dtype=torch.int32, device="cuda") for k in (n_slots, n + 1, n, n + 1, 4)]
+    B.ecco_paged_plan(page, n_pages, n, ints(ctx), ints(new), ints(free), len(free), d_tables, tables.shape[1], out[0], n_slots, *out[1:])
+    torch.cuda.synchronize()
+    return [d_tables.cpu().numpy()] + [t.cpu().numpy() for t in out]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_req,page,max_ctx,max_new", [(1, 16, 0, 1), (1, 1, 0, 5000), (3, 16, 100, 40), (33, 64, 1000, 1), (1024, 16, 300, 9), (1025, 32, 50, 3),
+                                                        (2500, 8, 70, 5), (7, 4096, 9000, 5000), (40, 128, 0, 128), (300, 16, 64, 0)])
+def test_plan_matches_the_definition(B, dev, n_req, page, max_ctx, max_new):
+    rng = np.random.default_rng([n_req, page])
+    ctx, new = rng.integers(0, max_ctx + 1, n_req), rng.integers(0, max_new + 1, n_req)
+    if n_req > 2:
+        ctx[1] = ctx[1] // page * page                                         # a request that fills its last page
+        new[2] = 0
+    held, total = -(-ctx // page), -(-(ctx + new) // page)
+    need = int((total - held).sum())
+    n_pages = int(total.sum()) + 5
+    ids = rng.permutation(n_pages).astype(np.int32)
+    free, owned = ids[:need + 2], ids[need + 2:]
+    tables = rng.integers(-5, 1 << 30, (n_req, int(total.max()) + 2)).astype(np.int32)          # what is not the request's is arbitrary
+    at = 0
+    for r in range(n_req):
+        tables[r, :held[r]] = owned[at:at + held[r]]
+        at += held[r]
+    n_slots = int(new.sum()) + 13
+    want = plan_reference(page, n_pages, ctx, new, free, tables, n_slots)
+    got = run_plan(B, page, n_pages, ctx, new, free, tables, n_slots)
+    for name, w, g in zip(("tables", "slots", "cu_new", "kv_lens", "kv_tiles", "result"), want, got):
+        assert np.array_equal(w, g), name
+
+
+@pytest.mark.gpu
+def test_plan_without_requests_and_with_foreign_pages(B, dev):
+    out = [torch.full((k,), -7, dtype=torch.int32, device="cuda") for k in (3, 1, 1, 4)]
+    B.ecco_paged_plan(16, 4, 0, 0, 0, 0, 0, 0, 0, out[0], 3, out[1], 0, out[2], out[3])
+    assert out[0].tolist() == [-1] * 3 and out[1].tolist() == [0] and out[2].tolist() == [0] and out[3].tolist() == [0, 0, 0, 0]
+    # page ids that are not of the pool: the tokens get no slot
+    tables = np.array([[-1, 9], [7, 4]], np.int32)
+    got = run_plan(B, 4, 5, [2, 8], [3, 1], np.array([5, -3], np.int32), np.concatenate([tables, np.zeros((2, 1), np.int32)], 1), 6)
+    assert got[1].tolist() == [-1] * 6 and got[0].tolist() == [[-1, 5, 0], [7, 4, -3]] and got[5].tolist() == [0, 2, 4, 4 - 2]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", ["negative ctx", "negative new", "row too long", "no page", "no slot", "too many"])
+def test_plan_serves_all_or_none(B, dev, what):
+    ctx, new, free, n_slots, stride = [5, 17, 0], [1, 20, 3], np.arange(10, 14, dtype=np.int32), 24, 3
+    want = B.ERR_INVALID_ARG
+    if what == "negative ctx":
+        ctx[1] = -1
+    elif what == "negative new":
+        new[2] = -1
+    elif what == "row too long":
+        new[1], n_slots, free = 32, 100, np.arange(10, 20, dtype=np.int32)
+    elif what == "no page":
+        free, want = free[:1], B.ERR_WORKSPACE
+    elif what == "no slot":
+        n_slots, want = 23, B.ERR_WORKSPACE
+    else:
+        ctx, new, stride = [0] * 3, [2**31 - 1] * 3, 1 << 20
+        # the table is not touched, so only its stride is large
+        tables = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = [torch.full((k,), -7, dtype=torch.int32, device="cuda") for k in (5, 4, 3, 4, 4)]
+        B.ecco_paged_plan(4096, 10, 3, ints(ctx), ints(new), ints(free), 4, tables, stride, out[0], 5, *out[1:])
+        assert out[4].tolist() == [B.ERR_INVALID_ARG, 0, 0, 0] and out[0].tolist() == [-1] * 5
+        return
+    tables = np.arange(9, dtype=np.int32).reshape(3, 3)[:, :stride]
+    got = run_plan(B, 16, 20, ctx, new, free, tables, n_slots)
+    assert got[5].tolist() == [want, 0, 0, 0]
+    assert np.array_equal(got[0], tables) and (got[1] == -1).all() and not got[2].any() and not got[3].any() and not got[4].any()
+
+
+# ------------------------------------------------------------------ append
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,heads,page,extra", [(1, 1, 1, 0), (5, 3, 16, 8), (33, 8, 64, 0), (700, 32, 16, 4096), (4096, 8, 128, 1024), (9001, 1, 32, 24)])
+def test_append_writes_the_oracles_blocks_into_the_slots(B, dev, eo, kv_small, tokens, heads, page, extra):
+    """Small calls and calls of many groups; K and V in the rows of a projection, padding tokens, slots outside of the pool."""
+    rng = np.random.default_rng([tokens, heads])
+    meta_k, src = kv_small["meta"], kv_small["k"].reshape(-1, 128)
+    meta_v = eo.calibrate(kv_small["cal"].reshape(-1)[:128 * 512], S=16, H=4, seed=9, select=eo.SELECT_MINMAX)
+    n_pages = -(-tokens // page) + 3
+    slots = rng.permutation(n_pages * page)[:tokens].astype(np.int32)
+    if tokens > 4:
+        slots[[0, 3]] = -1
+        slots[1], slots[2] = n_pages * page, 2**31 - 1
+    rows = np.zeros((tokens, 2 * heads * 128 + extra), np.float16)
+    pick = rng.integers(0, len(src), (2, tokens, heads))
+    rows[:, :heads * 128] = src[pick[0]].reshape(tokens, -1)
+    rows[:, -heads * 128:] = src[pick[1]].reshape(tokens, -1)
+    old = rng.integers(0, 256, (2, n_pages, heads, page, 64), dtype=np.uint8)
+    want = old.copy()
+    for which, (meta, part) in enumerate(((meta_k, rows[:, :heads * 128]), (meta_v, rows[:, -heads * 128:]))):
+        there = (slots >= 0) & (slots < n_pages * page)
+        if there.any():
+            blocks, _ = eo.encode(meta, np.ascontiguousarray(part[there]), eo.SELECT_MINMAX)
+            want[which, slots[there] // page, :, slots[there] % page] = blocks.reshape(-1, heads, 64)
+    d_rows, d_pools = torch.from_numpy(rows).cuda(), torch.from_numpy(old).cuda()
+    d_meta = [B.meta_to_device(lib_meta_from_oracle(B, m)) for m in (meta_k, meta_v)]
+    cache = B.paged_cache(d_meta[0], d_meta[1], d_pools[0], d_pools[1], n_pages, heads, page)
+    at = d_rows.data_ptr()
+    B.ecco_paged_append(cache, at, at + 2 * (heads * 128 + extra), rows.shape[1], ints(slots), tokens)
+    assert np.array_equal(d_pools.cpu().numpy(), want)
+    assert B.ecco_device_status() == 0
+
+
+# ------------------------------------------------------------------ attention
+class Paged:
+    """Requests of given lengths over pools of blocks drawn from the oracle-encoded cache."""
+
+    def __init__(self, B, eo, metas, blocks, new, kv, heads, g, page, seed=0, q_extra=0):
+        rng = np.random.default_rng([seed, heads, g, page])
+        self.B, self.heads, self.g, self.page, self.new, self.kv = B, heads, g, page, list(new), list(kv)
+        n_req, held = len(new), [-(-k // page) for k in kv]
+        self.n_pages = sum(held) + 3
+        self.pools = [b[rng.integers(0, len(b), (self.n_pages, heads, page))] for b in blocks]
+        self.stride = max(held + [0]) + 2
+        self.tables = rng.integers(-3, 1 << 30, (n_req, self.stride)).astype(np.int32)           # arbitrary behind a request's pages
+        ids, at = rng.permutation(self.n_pages), 0
+        for r, h in enumerate(held):
+            self.tables[r, :h] = ids[at:at + h]
+            at += h
+        self.tokens = sum(new)
+        self.q_stride = heads * g * 128 + q_extra
+        self.q = rng.standard_normal((self.tokens, self.q_stride)).astype(np.float16)
+        self.decoded = []                                                     # per request [kv][heads][128], fp64
+        for pool, meta in zip(self.pools, metas):
+            self.decoded.append([])
+            for r, k in enumerate(kv):
+                t = np.arange(k)
+                b = pool[self.tables[r, t // page], :, t % page].reshape(-1, 64)
+                with np.errstate(over="ignore"):
+                    x = eo.decode(meta, b).astype(np.float64) if k else np.zeros((0, 128))
+                self.decoded[-1].append(np.clip(x, -65504, 65504).reshape(k, heads, 128))
+        self.d_meta = [B.meta_to_device(lib_meta_from_oracle(B, m)) for m in metas]
+        self.d_pools = [torch.from_numpy(p).cuda() for p in self.pools]
+        self.cache = B.paged_cache(self.d_meta[0], self.d_meta[1], self.d_pools[0], self.d_pools[1], self.n_pages, heads, page)
+        self.d_tables, self.d_q = ints(self.tables), torch.from_numpy(self.q).cuda()
+        tiles = np.concatenate([[0], np.cumsum([-(-k // 32) for k in kv])])
+        self.d_cu, self.d_lens, self.d_tiles = ints(np.concatenate([[0], np.cumsum(new)])), ints(kv), ints(tiles)
+        self.batch = B.paged_batch(self.d_tables, self.stride, self.d_cu, self.d_lens, self.d_tiles, n_req, self.tokens, max(new), max(kv), int(tiles[-1]))
+
+    def run(self, causal, scale=128 ** -0.5, ws_bytes=None, lse=True, spare=2):
+        B = self.B
+        full = B.ecco_paged_attn_workspace_bytes(self.cache, self.batch, self.g)
+        ws_bytes = full if ws_bytes is None else ws_bytes
+        ws = torch.full((ws_bytes,), 0xff, dtype=torch.uint8, device="cuda")  # NaN, whatever it is read as
+        out = torch.full((self.tokens + spare, self.heads * self.g, 128), 7.0, dtype=torch.float16, device="cuda")
+        d_lse = torch.full((self.tokens + spare, self.heads * self.g), 7.0, device="cuda") if lse else None
+        B.ecco_paged_attn(self.cache, self.batch, self.g, self.d_q, self.q_stride, scale, B.ATTN_CAUSAL if causal else 0, out, d_lse, ws, ws_bytes)
+        torch.cuda.synchronize()
+        assert (out[self.tokens:] == 7).all()                                  # rows behind the last request
+        return out[:self.tokens].cpu().numpy(), d_lse[:self.tokens].cpu().numpy() if lse else None
+
+    def check(self, out, lse, causal, scale=128 ** -0.5, rows=None):
+        at = 0
+        for r, (n, kv) in enumerate(zip(self.new, self.kv)):
+            k, v = self.decoded[0][r], self.decoded[1][r]
+            picked = range(n) if rows is None else [i for i in range(n) if (at + i) % rows == 0 or i == n - 1]
+            for i in picked:
+                see = min(max(kv - n + i + 1, 0), kv) if causal else kv
+                for hq in range(self.heads * self.g):
+                    got, got_lse = out[at + i, hq].astype(np.float64), None if lse is None else float(lse[at + i, hq])
+                    if see == 0:
+                        assert not got.any() and (lse is None or got_lse == -math.inf), (r, i, hq)
+                        continue
+                    q, kk, vv = self.q[at + i, hq * 128:(hq + 1) * 128].astype(np.float64), k[:see, hq // self.g], v[:see, hq // self.g]
+                    s = scale * (kk @ q)
+                    top = s.max()
+                    p = np.exp(s - top)
+                    ref, mass, ref_lse = p @ vv / p.sum(), p @ np.abs(vv) / p.sum(), top + math.log(p.sum())
+                    e_s = 128 * 2.0 ** -23 * abs(scale) * (np.abs(kk) @ np.abs(q)).max() + 2.0 ** -22 * (1 + np.abs(s).max())
+                    sums = (see / 16 + 32) * 2.0 ** -23
+                    tol = 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2 * e_s + sums + see * 2.0 ** -40) * mass + 2.0 ** -25
+                    assert (np.abs(got - ref) <= tol).all(), (r, i, hq, float((np.abs(got - ref) / tol).max()))
+                    if lse is not None:
+                        assert abs(got_lse - ref_lse) <= e_s + sums + 2.0 ** -22 * abs(ref_lse) + 2.0 ** -20, (r, i, hq, got_lse, ref_lse)
+            at += n
+
+
+@pytest.fixture(scope="session")
+def caches(eo, kv_small, synth):
+    """(metadata, blocks) of a K and of a V cache with tables of their own."""
+    v = synth.kv_cache(2, 2, 256, 1004, 3004)
+    meta_v = eo.calibrate(synth.kv_cache(2, 2, 256, 2004, 3004), S=64, H=4, seed=4, select=eo.SELECT_MINMAX)
+    blocks_v, _ = eo.encode(meta_v, v, eo.SELECT_MINMAX)
+    return (kv_small["meta"], meta_v), (kv_small["blocks"].reshape(-1, 64), blocks_v.reshape(-1, 64))
+
+
+SHAPES = [
+    # new tokens, cached tokens (new ones among them where causal), KV heads, query heads per KV head, page size
+    ([1], [1], 1, 1, 1),
+    ([1], [33], 2, 4, 16),
+    ([1, 1, 1], [777, 1, 64], 8, 4, 16),
+    ([1] * 40, [1 + 37 * i % 700 for i in range(40)], 2, 8, 32),
+    ([1, 0, 1, 1], [31, 50, 0, 32], 3, 16, 8),                                # no new token; no token at all
+    ([5, 3, 8], [100, 3, 4000], 2, 2, 64),
+    ([4, 1, 2], [129, 2, 1000], 2, 5, 128),
+    ([7, 2], [3, 300], 1, 4, 4),                                               # more new tokens than the cache holds: rows that see nothing
+    ([33, 1], [40, 2000], 2, 3, 16),
+    ([64, 17], [64, 500], 1, 16, 4096),
+    ([130, 1, 257], [700, 900, 257], 2, 4, 16),
+    ([100], [3000], 1, 1, 2),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shape", SHAPES, ids=[str(i) for i in range(len(SHAPES))])
+def test_attention_matches_64_bits(B, dev, eo, caches, shape, causal):
+    new, kv, heads, g, page = shape
+    p = Paged(B, eo, *caches, new, kv, heads, g, page, seed=len(new), q_extra=64 if g == 4 else 0)
+    out, lse = p.run(causal)
+    p.check(out, lse, causal)
+    assert B.ecco_device_status() == 0
+    again, _ = p.run(causal, lse=False)
+    assert np.array_equal(out.view(np.uint16), again.view(np.uint16))          # reproducible, with and without lse
