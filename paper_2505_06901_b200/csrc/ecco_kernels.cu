@@ -28,6 +28,7 @@
 //   ecco_act2x_kernels.cuh          2x activation codec
 //   ecco_kv_compress_kernel.cuh     online 4x compressor
 //   ecco_paged_kernels.cuh          paged KV cache: slots and block tables, pages into tiles, attention of few rows
+//   ecco_paged_many_kernel.cuh      attention of many rows over it, on tcgen05
 //   ecco_launch.cuh                 device query, overlapped launches, work plans
 //   this file                       the C ABI: argument checks and launches
 #include "ecco_device_core.cuh"
@@ -41,6 +42,7 @@
 #include "ecco_act2x_kernels.cuh"
 #include "ecco_kv_compress_kernel.cuh"
 #include "ecco_paged_kernels.cuh"
+#include "ecco_paged_many_kernel.cuh"
 
 
 // ---------------------------------------------------------------------------------------------
@@ -757,34 +759,56 @@ extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k,
 }
 
 namespace {
+// Workspace of a launch over some KV heads, all offsets multiples of 256:
+//   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks | few rows: sums, maxima | many rows: sums, maxima
 struct PagedAttnPlan {
-    int few_ctas, m;                   // CTAs of the kernel for few rows, its tiles of sixteen rows
-    size_t staged_bytes, part_bytes, ml_bytes;
-    size_t bytes() const { return staged_bytes + part_bytes + ml_bytes; }
+    int m, few_rows;                   // tiles of sixteen rows of ecco_paged_few_kernel, rows up to which a request is for it
+    bool many;                         // there may be requests of more rows
+    int few_ctas, many_ctas, max_blocks;
+    size_t few_tiles, block_tiles, blocks, n_blocks, few_part, few_ml, many_part, many_ml, bytes;
 };
-// of a launch over `heads` KV heads
 PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, int ctas_max)
 {
-    PagedAttnPlan p;
+    PagedAttnPlan p = {};
     const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
-    p.m = rows <= 16 ? 1 : 2;
+    p.m = rows > 16 && rows <= 32 ? 2 : 1;
+    p.few_rows = 16 * p.m;
+    p.many = rows > p.few_rows;
     p.few_ctas = std::max(1, spread_ctas(static_cast<int64_t>(b.max_tiles) * heads, ctas_max));
-    auto up = [](size_t v) { return (v + 255) & ~static_cast<size_t>(255); };
-    const size_t slots = static_cast<size_t>(p.few_ctas) * (p.m == 1 ? kFewWarps<1> : kFewWarps<2>) * 2 * 16 * p.m;
-    p.staged_bytes = static_cast<size_t>(b.max_tiles) * heads * 2 * kKvTileBytes;
-    p.part_bytes = up(slots * kGroup * sizeof(float));
-    p.ml_bytes = up(slots * sizeof(float2));
+    p.many_ctas = ctas_max;
+    p.max_blocks = p.many ? static_cast<int>(static_cast<int64_t>(b.n_tokens) * q_per_kv / kManyRows + std::min(b.n_req, b.n_tokens) + 1) : 0;
+    size_t at = static_cast<size_t>(b.max_tiles) * heads * 2 * kKvTileBytes;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at = (at + bytes + 255) & ~static_cast<size_t>(255);
+        return here;
+    };
+    const size_t few_slots = static_cast<size_t>(p.few_ctas) * (p.m == 1 ? kFewWarps<1> : kFewWarps<2>) * 2 * p.few_rows;
+    const size_t many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
+    p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
+    p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
+    p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
+    p.n_blocks = take(4);
+    p.few_part = take(few_slots * kGroup * sizeof(float));
+    p.few_ml = take(few_slots * sizeof(float2));
+    p.many_part = take(many_slots * kGroup * sizeof(float));
+    p.many_ml = take(many_slots * sizeof(float2));
+    p.bytes = at;
     return p;
 }
 bool paged_batch_fine(const ecco_paged_cache& c, const ecco_paged_batch& b, int q_per_kv)
 {
-    return b.n_req >= 0 && b.n_req <= 65535 && b.n_tokens >= 0 && b.table_stride >= 0 && b.max_new >= 0 && b.max_kv >= 0 && b.max_tiles >= 0 && q_per_kv >= 1 &&
-           q_per_kv <= 16 && static_cast<int64_t>(b.max_new) * q_per_kv <= INT32_MAX - 64 && static_cast<int64_t>(b.max_tiles) * c.n_kv_heads <= INT32_MAX / 2 && static_cast<int64_t>(c.n_kv_heads) * q_per_kv <= 65535 &&
-           static_cast<int64_t>(b.n_tokens) * c.n_kv_heads * q_per_kv <= INT32_MAX;
+    if (b.n_req < 0 || b.n_req > 65535 || b.n_tokens < 0 || b.table_stride < 0 || b.max_new < 0 || b.max_kv < 0 || b.max_tiles < 0) return false;
+    if (q_per_kv < 1 || q_per_kv > 16 || static_cast<int64_t>(c.n_kv_heads) * q_per_kv > 65535) return false;
+    if (static_cast<int64_t>(b.max_tiles) * c.n_kv_heads > INT32_MAX / 2 || static_cast<int64_t>(b.max_tiles) > INT32_MAX / 32) return false;
+    if (static_cast<int64_t>(b.n_tokens) * c.n_kv_heads * q_per_kv > INT32_MAX) return false;
+    // tiles of all blocks of rows together are counted in 32 bits
+    const int64_t blocks = static_cast<int64_t>(b.n_tokens) * q_per_kv / kManyRows + b.n_req + 1;
+    return blocks * (static_cast<int64_t>(b.max_kv) / kManyTokens + 1) <= INT32_MAX;
 }
 
 template <int kM>
-int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedAttnPlan& p, cudaStream_t s)
+int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
 {
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {
@@ -792,20 +816,32 @@ int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o,
         if (rc) return rc;
         configured[di.device] = true;
     }
-    int rc = launch_overlapped(ecco_paged_few_kernel<kM>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps<kM> * 32), kFewSmemBytes<kM>, s, kv, o);
+    int rc = launch_overlapped(ecco_paged_few_kernel<kM>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps<kM> * 32), kFewSmemBytes<kM>, s, kv, o, sc);
     if (rc) return rc;
     const int64_t rows = static_cast<int64_t>(kv.n_tokens) * kv.heads * o.q_per_kv;
     // warps to a row: by how many pieces a request of average length is cut into
     const int64_t pieces = static_cast<int64_t>(p.few_ctas) * kFewWarps<kM> / (static_cast<int64_t>(kv.n_req) * kv.heads);
     const int team = pieces > 16 ? 8 : 1;
-    return launch_overlapped(ecco_paged_combine_kernel<kM>, static_cast<unsigned>((rows * team + 7) / 8), 256u, 0, s, kv, o, p.few_ctas, team);
+    return launch_overlapped(ecco_paged_combine_kernel<kM>, static_cast<unsigned>((rows * team + 7) / 8), 256u, 0, s, kv, o, sc, p.few_ctas, team);
+}
+int launch_paged_many(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
+{
+    static thread_local bool configured[64] = {};
+    if (!configured[di.device]) {
+        const int rc = set_smem(ecco_paged_many_kernel, kManySmemBytes);
+        if (rc) return rc;
+        configured[di.device] = true;
+    }
+    const int rc = launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc);
+    if (rc || p.many_ctas == 1) return rc;
+    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>((p.many_ctas - 1) * kJoinParts), 256u, 0, s, kv, o, sc, p.many_ctas);
 }
 }  // namespace
 
 extern "C" size_t ecco_paged_attn_workspace_bytes(const ecco_paged_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv)
 {
     if (!cache || !batch || cache->n_kv_heads < 1 || cache->n_kv_heads > 65535 || !paged_batch_fine(*cache, *batch, q_per_kv)) return 0;
-    return paged_attn_plan(*batch, cache->n_kv_heads, q_per_kv, 256).bytes();
+    return paged_attn_plan(*batch, cache->n_kv_heads, q_per_kv, 256).bytes;
 }
 
 extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q, int64_t q_stride,
@@ -829,7 +865,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     const int ctas = di.sms < 256 ? di.sms : 256;
     // as many heads at a time as the workspace holds
     int heads = cache->n_kv_heads;
-    while (heads > 0 && paged_attn_plan(b, heads, q_per_kv, ctas).bytes() > workspace_bytes) --heads;
+    while (heads > 0 && paged_attn_plan(b, heads, q_per_kv, ctas).bytes > workspace_bytes) --heads;
     if (heads == 0) return ECCO_ERR_WORKSPACE;
     PagedKv kv = {};
     kv.k_meta = static_cast<const uint8_t*>(cache->d_k_meta); kv.v_meta = static_cast<const uint8_t*>(cache->d_v_meta);
@@ -837,6 +873,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     kv.tables = b.d_block_tables; kv.cu_new = b.d_cu_new; kv.kv_lens = b.d_kv_lens; kv.kv_tiles = b.d_kv_tiles;
     kv.n_pages = cache->n_pages; kv.page_shift = page_shift_of(cache->page_size); kv.all_heads = cache->n_kv_heads;
     kv.stride = b.table_stride; kv.n_req = b.n_req; kv.n_tokens = b.n_tokens; kv.max_tiles = b.max_tiles;
+    kv.max_new = b.max_new; kv.max_kv = b.max_kv;
     kv.staged = static_cast<uint8_t*>(d_workspace);
     PagedOut o = {};
     o.q = static_cast<const __half*>(d_q); o.q_stride = q_stride;
@@ -850,15 +887,26 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     for (kv.head0 = 0; kv.head0 < cache->n_kv_heads; kv.head0 += kv.heads) {
         kv.heads = std::min(heads, cache->n_kv_heads - kv.head0);
         const PagedAttnPlan p = paged_attn_plan(b, kv.heads, q_per_kv, ctas);
-        o.part = reinterpret_cast<float*>(kv.staged + p.staged_bytes);
-        o.part_ml = reinterpret_cast<float2*>(kv.staged + p.staged_bytes + p.part_bytes);
+        PagedSchedule sc = {};
+        sc.few_tiles = reinterpret_cast<int32_t*>(kv.staged + p.few_tiles);
+        sc.block_tiles = reinterpret_cast<int32_t*>(kv.staged + p.block_tiles);
+        sc.blocks = reinterpret_cast<int2*>(kv.staged + p.blocks);
+        sc.n_blocks = reinterpret_cast<int32_t*>(kv.staged + p.n_blocks);
+        sc.max_blocks = p.max_blocks;
+        sc.few_rows = p.few_rows;
         // an even number of CTAs: half of them for K, half for V
         const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
         const int pairs = std::max(1, spread_ctas(units, ctas / 2));
-        rc = launch_overlapped(ecco_paged_stage_kernel<32>, static_cast<unsigned>(2 * pairs), spread_threads(units, pairs, 32), kSmemCtaBytes, s, kv);
+        rc = launch_overlapped(ecco_paged_stage_kernel<32>, static_cast<unsigned>(2 * pairs), spread_threads(units, pairs, 32), kSmemCtaBytes, s, kv, sc, q_per_kv, o.causal);
         if (rc) return rc;
-        for (o.row_from = 0; o.row_from < static_cast<int64_t>(b.max_new) * q_per_kv; o.row_from += 16 * p.m) {
-            rc = p.m == 1 ? launch_paged_few<1>(di, kv, o, p, s) : launch_paged_few<2>(di, kv, o, p, s);
+        o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
+        o.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
+        rc = p.m == 1 ? launch_paged_few<1>(di, kv, o, sc, p, s) : launch_paged_few<2>(di, kv, o, sc, p, s);
+        if (rc) return rc;
+        if (p.many) {
+            o.part = reinterpret_cast<float*>(kv.staged + p.many_part);
+            o.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
+            rc = launch_paged_many(di, kv, o, sc, p, s);
             if (rc) return rc;
         }
     }

@@ -151,7 +151,7 @@ constexpr uint32_t kKvTileBytes = 8 * kPieceBytes;
 struct PagedKv {
     const uint8_t *k_meta, *v_meta, *k_blocks, *v_blocks;
     const int32_t *tables, *cu_new, *kv_lens, *kv_tiles;
-    int32_t n_pages, page_shift, all_heads, stride, n_req, n_tokens, max_tiles;
+    int32_t n_pages, page_shift, all_heads, stride, n_req, n_tokens, max_new, max_kv, max_tiles;
     int32_t head0, heads;      // KV heads of this launch
     uint8_t* staged;           // [K, V][heads][max_tiles] tiles
 };
@@ -170,7 +170,7 @@ __device__ __forceinline__ PagedReq paged_req(const PagedKv& kv, int r, int32_t 
     const int32_t t0 = __ldcg(kv.kv_tiles + r), t1 = __ldcg(kv.kv_tiles + r + 1), c0 = __ldcg(kv.cu_new + r), c1 = __ldcg(kv.cu_new + r + 1), len = __ldcg(kv.kv_lens + r);
     q.first = min(max(t0, 0), T);
     q.tiles = min(max(t1, q.first), T) - q.first;
-    q.kv = static_cast<int32_t>(min(static_cast<int64_t>(max(len, 0)), static_cast<int64_t>(q.tiles) * 32));
+    q.kv = static_cast<int32_t>(min(static_cast<int64_t>(min(max(len, 0), kv.max_kv)), static_cast<int64_t>(q.tiles) * 32));
     q.row0 = min(max(c0, 0), kv.n_tokens);
     q.rows = min(max(c1, q.row0), kv.n_tokens) - q.row0;
     return q;
@@ -190,6 +190,77 @@ __device__ __forceinline__ int warp_find(const int32_t* begin, int n, int32_t x)
     return lo;
 }
 
+constexpr int kManyRows = 256;                             // rows of a block of ecco_paged_many_kernel
+constexpr int kManyTokens = 128;                           // tokens of its tiles
+// What the attention kernels need to know of a batch, made by paged_schedule.
+struct PagedSchedule {
+    int32_t* few_tiles;        // [n_req + 1]: prefix sums of the tiles of the requests for ecco_paged_few_kernel
+    int32_t* block_tiles;      // [max_blocks + 1]: prefix sums of the 128-token tiles of all blocks
+    int2* blocks;              // [max_blocks]: request, block of the request
+    int32_t* n_blocks;
+    int32_t max_blocks, few_rows;
+};
+
+// tokens that row i of a request sees
+__device__ __forceinline__ int32_t tokens_seen(const PagedReq& q, int32_t token, bool causal)
+{
+    return causal ? min(max(q.kv - q.rows + token + 1, 0), q.kv) : q.kv;
+}
+// tokens that the rows of a block see together: those of its last row
+__device__ __forceinline__ int32_t block_tokens(const PagedReq& q, int32_t block, int32_t q_per_kv, bool causal)
+{
+    const int64_t last = min((static_cast<int64_t>(block) + 1) * kManyRows, static_cast<int64_t>(q.rows) * q_per_kv) - 1;
+    return tokens_seen(q, static_cast<int32_t>(last / q_per_kv), causal);
+}
+// By one warp: which requests are for which kernel, and the two lines of tiles.  A block that sees nothing counts as one tile, so that
+// somebody writes its rows.
+__device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSchedule& sc, int32_t q_per_kv, bool causal)
+{
+    constexpr unsigned full = 0xffffffffu;
+    const int lane = static_cast<int>(threadIdx.x & 31u);
+    const int32_t T = paged_tiles(kv);
+    auto scan = [&](int32_t v) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t x = __shfl_up_sync(full, v, o);
+            if (lane >= o) v += x;
+        }
+        return v;
+    };
+    int32_t few = 0, tiles = 0, n_blocks = 0;
+    if (lane == 0) { sc.few_tiles[0] = 0; sc.block_tiles[0] = 0; }
+    for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
+        const int r = r0 + lane;
+        PagedReq q = {};
+        if (r < kv.n_req) q = paged_req(kv, r, T);
+        const int64_t rows = static_cast<int64_t>(q.rows) * q_per_kv;
+        if (r < kv.n_req && (q.rows > kv.max_new || __ldcg(kv.kv_lens + r) != q.kv)) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        const bool many = rows > sc.few_rows;
+        const int32_t f = few + scan(!many && rows > 0 ? q.tiles : 0);
+        if (r < kv.n_req) sc.few_tiles[r + 1] = f;
+        few = __shfl_sync(full, f, 31);
+        for (unsigned left = __ballot_sync(full, many); left; left &= left - 1u) {
+            const int src = __ffs(left) - 1;
+            PagedReq one;
+            one.rows = __shfl_sync(full, q.rows, src);
+            one.kv = __shfl_sync(full, q.kv, src);
+            const int32_t blocks = static_cast<int32_t>((static_cast<int64_t>(one.rows) * q_per_kv + kManyRows - 1) / kManyRows);
+            for (int32_t b0 = 0; b0 < blocks && n_blocks < sc.max_blocks; b0 += 32) {
+                const int32_t b = b0 + lane, n = min(min(blocks - b0, 32), sc.max_blocks - n_blocks);
+                const int32_t mine = lane < n ? max((block_tokens(one, b, q_per_kv, causal) + kManyTokens - 1) / kManyTokens, 1) : 0;
+                const int32_t upto = tiles + scan(mine);
+                if (lane < n) {
+                    sc.blocks[n_blocks + lane] = make_int2(r0 + src, b);
+                    sc.block_tiles[n_blocks + lane + 1] = upto;
+                }
+                tiles = __shfl_sync(full, upto, 31);
+                n_blocks += n;
+            }
+        }
+    }
+    if (lane == 0) *sc.n_blocks = n_blocks;
+}
+
 // K6s: pages -> tiles.  ecco_decompress_tma_kernel with another way in (a lane finds its token's block through the request's table)
 // and out (a piece leaves by one bulk copy of 1 KB).  Even CTAs decode K, odd ones V: both have the same number of tiles, no CTA
 // needs both sets of tables, and small calls decode K and V side by side.
@@ -197,7 +268,7 @@ __device__ __forceinline__ int warp_find(const int32_t* begin, int n, int32_t x)
 // be NaN in rows that do not see the token.
 template <int kMaxWarps>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
-ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv)
+ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedSchedule sc, int32_t q_per_kv, int32_t causal)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -215,6 +286,8 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv)
     const uint32_t my_row = stage + lane * 32;
     if (!finish_decode_tables(tb)) return;
     dependency_wait();
+    // one warp, if possible one that has no room to decode, makes the schedule on the side
+    if (blockIdx.x == 0 && warp == (nw < blockDim.x >> 5 ? nw : 0u)) paged_schedule(kv, sc, q_per_kv, causal);
     const float T = tb.T;
     const uint32_t n_tiles = static_cast<uint32_t>(paged_tiles(kv)), units = n_tiles * kv.heads;
     if (blockIdx.x == 0 && threadIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
@@ -308,7 +381,6 @@ struct PagedOut {
     int64_t q_stride;
     float scale_log2;          // scale * log2(e)
     int32_t q_per_kv, q_heads, causal;
-    int32_t row_from;          // first row of a request in this launch
     __half* out;
     float* lse;                // or NULL
     float* part;               // partial sums [slot][rows][128]
@@ -343,11 +415,6 @@ __device__ __forceinline__ uint32_t pack_h2(float a, float b)
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-// tokens that row i of a request sees
-__device__ __forceinline__ int32_t tokens_seen(const PagedReq& q, int32_t token, bool causal)
-{
-    return causal ? min(max(q.kv - q.rows + token + 1, 0), q.kv) : q.kv;
-}
 // bounded wait of a warp on one of its barriers
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
 {
@@ -360,7 +427,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
 
 template <int kM>
 __global__ void __launch_bounds__(kFewWarps<kM> * 32, 1)
-ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o)
+ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     constexpr unsigned full = 0xffffffffu;
@@ -373,27 +440,23 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         for (int s = 0; s < kFewStages; ++s) mbar_init(bar + s * 8, 1);
     __syncwarp();
     dependency_wait();
-    const int32_t T = paged_tiles(kv);
+    const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);
     const int W = static_cast<int>(gridDim.x) * kFewWarps<kM>, wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
-    const int64_t U = static_cast<int64_t>(T) * kv.heads;
+    const int64_t U = static_cast<int64_t>(line) * kv.heads;
     const UnitSplit split(U, W);
     const int64_t u0 = split.begin(wg), u1 = split.begin(wg + 1);
 
-    // a place in the run: unit u is tile `tile` of head `head`, which belongs to request r
-    struct Place { int64_t u, end; int32_t head, tile, r; PagedReq q; };
-    // moves to the first unit at or behind p.u whose request has rows for this kernel; p.end: the request's end in this run
+    // a place in the run: unit u is tile `tile` of head `head`; the request it belongs to has units [begin, end), cut to the run's end
+    struct Place { int64_t u, begin, end; int32_t head, tile; PagedReq q; };
     auto seek = [&](Place& p) {
-        while (p.u < u1) {
-            p.head = static_cast<int32_t>(divide(static_cast<uint64_t>(p.u), static_cast<uint64_t>(T)));
-            p.tile = static_cast<int32_t>(p.u - static_cast<int64_t>(p.head) * T);
-            p.r = warp_find(kv.kv_tiles, kv.n_req, p.tile);
-            p.q = paged_req(kv, p.r, T);
-            // a request's tiles begin at or before this one and end behind it, unless the arrays are broken
-            const int64_t last = static_cast<int64_t>(p.head) * T + max(p.q.first + p.q.tiles, p.tile + 1);
-            p.end = min(last, u1);
-            if (static_cast<int64_t>(p.q.rows) * o.q_per_kv > o.row_from && p.q.first <= p.tile && p.tile < p.q.first + p.q.tiles) return;
-            p.u = p.end;
-        }
+        if (p.u >= u1) return;
+        p.head = static_cast<int32_t>(divide(static_cast<uint64_t>(p.u), static_cast<uint64_t>(line)));
+        const int64_t head_from = static_cast<int64_t>(p.head) * line;
+        const int r = warp_find(sc.few_tiles, kv.n_req, static_cast<int32_t>(p.u - head_from));
+        p.q = paged_req(kv, r, T);
+        p.begin = head_from + __ldcg(sc.few_tiles + r);
+        p.end = min(head_from + __ldcg(sc.few_tiles + r + 1), u1);
+        p.tile = p.q.first + static_cast<int32_t>(p.u - p.begin);
     };
     Place load = {};                                       // the next tile to ask for
     load.u = u0;
@@ -418,8 +481,8 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     bool ok = true;
     while (ok && at.u < u1) {
         const PagedReq q = at.q;
-        const int R = min(q.rows * o.q_per_kv - o.row_from, kRows);
-        const bool whole = at.tile == q.first && at.end - at.u == q.tiles;
+        const int R = min(q.rows * o.q_per_kv, kRows);
+        const bool whole = at.u == at.begin && at.end - at.u == q.tiles;
         const int slot = 2 * wg + (at.u == u0 ? 0 : 1);
         // the rows of q as tiles: rows beyond the last are zero
         __syncwarp();
@@ -427,7 +490,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
             const uint32_t row = c >> 4, chunk = c & 15u;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
             if (static_cast<int>(row) < R) {
-                const uint32_t i = (o.row_from + row) / o.q_per_kv, g = o.row_from + row - i * o.q_per_kv;
+                const uint32_t i = row / o.q_per_kv, g = row - i * o.q_per_kv;
                 v = __ldcg(reinterpret_cast<const uint4*>(o.q + (q.row0 + i) * o.q_stride + (static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + g) * kGroup) + chunk);
             }
             sts_v4(q_at + (row >> 4) * 4096 + (chunk >> 1) * 512 + tile_byte(row & 15u, (chunk & 1u) * 8), v.x, v.y, v.z, v.w);
@@ -440,7 +503,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int row = t * 16 + static_cast<int>(lane >> 2) + 8 * i;
-                seen[t][i] = row < R ? tokens_seen(q, (o.row_from + row) / o.q_per_kv, o.causal) : 0;
+                seen[t][i] = row < R ? tokens_seen(q, row / o.q_per_kv, o.causal) : 0;
                 m[t][i] = -INFINITY;
                 l[t][i] = 0.0f;
             }
@@ -547,7 +610,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
                 const int row = t * 16 + static_cast<int>(lane >> 2) + 8 * i;
                 if (row >= R || !ok) continue;
                 if (whole) {
-                    const int token = (o.row_from + row) / o.q_per_kv, hq = (kv.head0 + at.head) * o.q_per_kv + o.row_from + row - token * o.q_per_kv;
+                    const int token = row / o.q_per_kv, hq = (kv.head0 + at.head) * o.q_per_kv + row - token * o.q_per_kv;
                     const int64_t at_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + hq;
                     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
                     uint32_t* const dst = reinterpret_cast<uint32_t*>(o.out + at_row * kGroup) + (lane & 3u);
@@ -568,10 +631,19 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         for (; taken < asked; ++taken) warp_wait(bar + (taken % kFewStages) * 8, (taken / kFewStages) & 1u);
 }
 
+// adds a piece's sums v, with maximum and sum of weights x, to those at hand
+__device__ __forceinline__ void join_sums(float& m, float& l, float4& acc, float2 x, float4 v)
+{
+    if (x.y == 0.0f) return;                               // nothing seen there
+    const float top = fmaxf(m, x.x), f0 = exp2_fast(m - top), f1 = exp2_fast(x.x - top);
+    l = l * f0 + x.y * f1;
+    acc = make_float4(acc.x * f0 + v.x * f1, acc.y * f0 + v.y * f1, acc.z * f0 + v.z * f1, acc.w * f0 + v.w * f1);
+    m = top;
+}
 // Joins the pieces of rows whose request was cut, and writes the rows that see nothing.  `team` warps to a (new token, query head).
 template <int kM>
-__global__ void __launch_bounds__(256)
-ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, int few_ctas, int team)
+__global__ void __launch_bounds__(256, 4)
+ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int few_ctas, int team)
 {
     __shared__ float4 sums[8][32];
     __shared__ float2 ml[8];
@@ -586,14 +658,15 @@ ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_const
     const int r = warp_find(kv.cu_new, kv.n_req, token);
     const PagedReq q = paged_req(kv, r, T);
     const int i = token - q.row0;
-    const int head = hq / o.q_per_kv, row = i * o.q_per_kv + hq - head * o.q_per_kv - o.row_from;
-    const bool mine = exists && i >= 0 && i < q.rows && row >= 0 && row < 16 * kM;
+    const int head = hq / o.q_per_kv, row = i * o.q_per_kv + hq - head * o.q_per_kv;
+    const bool mine = exists && i >= 0 && i < q.rows && q.rows * static_cast<int64_t>(o.q_per_kv) <= sc.few_rows;
     const int64_t at_row = static_cast<int64_t>(token) * o.q_heads + kv.head0 * o.q_per_kv + hq;
     int w_lo = 0, w_hi = -1;
     bool first_slot = true;
     if (mine && q.tiles > 0) {
-        const UnitSplit split(static_cast<int64_t>(T) * kv.heads, few_ctas * kFewWarps<kM>);
-        const int64_t f0 = static_cast<int64_t>(head) * T + q.first;
+        const int32_t line = __ldcg(sc.few_tiles + kv.n_req);
+        const UnitSplit split(static_cast<int64_t>(line) * kv.heads, few_ctas * kFewWarps<kM>);
+        const int64_t f0 = static_cast<int64_t>(head) * line + __ldcg(sc.few_tiles + r);
         w_lo = split.owner(f0);
         w_hi = split.owner(f0 + q.tiles - 1);
         first_slot = split.begin(w_lo) == f0;
@@ -606,14 +679,7 @@ ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_const
             const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && !first_slot ? 1 : 0)) * (16 * kM) + row;
             const float2 x = __ldcg(o.part_ml + at);
             const float4 v = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
-            if (x.y == 0.0f) continue;                     // nothing seen there
-            const float top = fmaxf(m, x.x), f0 = exp2_fast(m - top), f1 = exp2_fast(x.x - top);
-            l = l * f0 + x.y * f1;
-            acc.x = acc.x * f0 + v.x * f1;
-            acc.y = acc.y * f0 + v.y * f1;
-            acc.z = acc.z * f0 + v.z * f1;
-            acc.w = acc.w * f0 + v.w * f1;
-            m = top;
+            join_sums(m, l, acc, x, v);
         }
     }
     if (team > 1) {
@@ -624,14 +690,7 @@ ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_const
             for (int w = 1; w < team; ++w) {
                 const float2 x = ml[warp + w];
                 const float4 v = sums[warp + w][lane];
-                if (x.y == 0.0f) continue;
-                const float top = fmaxf(m, x.x), f0 = exp2_fast(m - top), f1 = exp2_fast(x.x - top);
-                l = l * f0 + x.y * f1;
-                acc.x = acc.x * f0 + v.x * f1;
-                acc.y = acc.y * f0 + v.y * f1;
-                acc.z = acc.z * f0 + v.z * f1;
-                acc.w = acc.w * f0 + v.w * f1;
-                m = top;
+                join_sums(m, l, acc, x, v);
             }
         }
     }
