@@ -776,7 +776,7 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
     p.many = rows > p.few_rows;
     p.few_ctas = std::max(1, spread_ctas(static_cast<int64_t>(b.max_tiles) * heads, ctas_max));
     p.many_ctas = ctas_max;
-    p.max_blocks = p.many ? static_cast<int>(static_cast<int64_t>(b.n_tokens) * q_per_kv / kManyRows + std::min(b.n_req, b.n_tokens) + 1) : 0;
+    p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
     size_t at = static_cast<size_t>(b.max_tiles) * heads * 2 * kKvTileBytes;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -803,7 +803,7 @@ bool paged_batch_fine(const ecco_paged_cache& c, const ecco_paged_batch& b, int 
     if (static_cast<int64_t>(b.max_tiles) * c.n_kv_heads > INT32_MAX / 2 || static_cast<int64_t>(b.max_tiles) > INT32_MAX / 32) return false;
     if (static_cast<int64_t>(b.n_tokens) * c.n_kv_heads * q_per_kv > INT32_MAX) return false;
     // tiles of all blocks of rows together are counted in 32 bits
-    const int64_t blocks = static_cast<int64_t>(b.n_tokens) * q_per_kv / kManyRows + b.n_req + 1;
+    const int64_t blocks = static_cast<int64_t>(b.n_tokens) / (2 * tile_rows_tokens(q_per_kv)) + b.n_req + 1;
     return blocks * (static_cast<int64_t>(b.max_kv) / kManyTokens + 1) <= INT32_MAX;
 }
 
@@ -818,21 +818,47 @@ int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o,
     }
     int rc = launch_overlapped(ecco_paged_few_kernel<kM>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps<kM> * 32), kFewSmemBytes<kM>, s, kv, o, sc);
     if (rc) return rc;
-    const int64_t rows = static_cast<int64_t>(kv.n_tokens) * kv.heads * o.q_per_kv;
-    // warps to a row: by how many pieces a request of average length is cut into
-    const int64_t pieces = static_cast<int64_t>(p.few_ctas) * kFewWarps<kM> / (static_cast<int64_t>(kv.n_req) * kv.heads);
-    const int team = pieces > 16 ? 8 : 1;
-    return launch_overlapped(ecco_paged_combine_kernel<kM>, static_cast<unsigned>((rows * team + 7) / 8), 256u, 0, s, kv, o, sc, p.few_ctas, team);
+    const int64_t runs = static_cast<int64_t>(p.few_ctas) * kFewWarps<kM>, segments = static_cast<int64_t>(kv.n_req) * kv.heads;
+    if (runs == 1) return ECCO_OK;
+    // by how many pieces a request of average length is cut into
+    const int by_rows = runs / segments > 16 ? static_cast<int>(std::min<int64_t>(16 * kM, static_cast<int64_t>(kv.max_new) * o.q_per_kv)) : 0;
+    return launch_overlapped(ecco_paged_combine_kernel<kM>, static_cast<unsigned>(by_rows ? segments * by_rows : runs - 1), 256u, 0, s, kv, o, sc, p.few_ctas, by_rows);
+}
+// the tiles of a workspace as [piece][tile][1 KB]: a box of eight pieces of four tiles is a K or V operand of 128 tokens
+bool make_tile_map(CUtensorMap* map, const PagedKv& kv)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {kPieceBytes / 4, static_cast<cuuint64_t>(2) * kv.heads * kv.max_tiles, 8};
+    const cuuint64_t strides[2] = {kKvTileBytes, kPieceBytes};
+    const cuuint32_t box[3] = {kPieceBytes / 4, kManyTokens / 32, 8};
+    const cuuint32_t unit[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, kv.staged, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// q as [token][query head][dim]: a box is sixteen dims of a tile of rows, as an operand has them
+bool make_q_map(CUtensorMap* map, const PagedKv& kv, const PagedOut& o)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {kGroup, static_cast<cuuint64_t>(o.q_heads), static_cast<cuuint64_t>(kv.n_tokens)};
+    const cuuint64_t strides[2] = {kGroup * 2, static_cast<cuuint64_t>(o.q_stride) * 2};
+    const cuuint32_t box[3] = {16, static_cast<cuuint32_t>(o.q_per_kv), static_cast<cuuint32_t>(tile_rows_tokens(o.q_per_kv))};
+    const cuuint32_t unit[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<__half*>(o.q), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 int launch_paged_many(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
 {
+    CUtensorMap map, q_map;
+    if (!make_tile_map(&map, kv) || !make_q_map(&q_map, kv, o)) return ECCO_ERR_CUDA;
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {
         const int rc = set_smem(ecco_paged_many_kernel, kManySmemBytes);
         if (rc) return rc;
         configured[di.device] = true;
     }
-    const int rc = launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc);
+    const int rc = launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc, map, q_map);
     if (rc || p.many_ctas == 1) return rc;
     return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>((p.many_ctas - 1) * kJoinParts), 256u, 0, s, kv, o, sc, p.many_ctas);
 }
@@ -897,7 +923,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         // an even number of CTAs: half of them for K, half for V
         const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
         const int pairs = std::max(1, spread_ctas(units, ctas / 2));
-        rc = launch_overlapped(ecco_paged_stage_kernel<32>, static_cast<unsigned>(2 * pairs), spread_threads(units, pairs, 32), kSmemCtaBytes, s, kv, sc, q_per_kv, o.causal);
+        rc = launch_overlapped(ecco_paged_stage_kernel<32>, static_cast<unsigned>(2 * pairs), spread_threads(units, pairs, 32), kSmemCtaBytes, s, kv, o, sc);
         if (rc) return rc;
         o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
         o.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);

@@ -190,8 +190,9 @@ __device__ __forceinline__ int warp_find(const int32_t* begin, int n, int32_t x)
     return lo;
 }
 
-constexpr int kManyRows = 256;                             // rows of a block of ecco_paged_many_kernel
-constexpr int kManyTokens = 128;                           // tokens of its tiles
+constexpr int kManyRows = 256;                             // rows of a block of ecco_paged_many_kernel: two tiles of 128, as many whole tokens as these hold
+constexpr int kManyTokens = 128;                           // tokens of its tiles of K and V
+__host__ __device__ constexpr int32_t tile_rows_tokens(int32_t q_per_kv) { return 128 / q_per_kv; }      // new tokens of a tile of rows
 // What the attention kernels need to know of a batch, made by paged_schedule.
 struct PagedSchedule {
     int32_t* few_tiles;        // [n_req + 1]: prefix sums of the tiles of the requests for ecco_paged_few_kernel
@@ -201,21 +202,31 @@ struct PagedSchedule {
     int32_t max_blocks, few_rows;
 };
 
+struct PagedOut {
+    const __half* q;
+    int64_t q_stride;
+    float scale_log2;          // scale * log2(e)
+    int32_t q_per_kv, q_heads, causal;
+    __half* out;
+    float* lse;                // or NULL
+    float* part;               // partial sums [slot][rows][128]
+    float2* part_ml;           // maxima (log2) and sums of weights [slot][rows]
+};
 // tokens that row i of a request sees
 __device__ __forceinline__ int32_t tokens_seen(const PagedReq& q, int32_t token, bool causal)
 {
     return causal ? min(max(q.kv - q.rows + token + 1, 0), q.kv) : q.kv;
 }
 // tokens that the rows of a block see together: those of its last row
-__device__ __forceinline__ int32_t block_tokens(const PagedReq& q, int32_t block, int32_t q_per_kv, bool causal)
+__device__ __forceinline__ int32_t block_sees(const PagedReq& q, int32_t block, int32_t q_per_kv, bool causal)
 {
-    const int64_t last = min((static_cast<int64_t>(block) + 1) * kManyRows, static_cast<int64_t>(q.rows) * q_per_kv) - 1;
-    return tokens_seen(q, static_cast<int32_t>(last / q_per_kv), causal);
+    return tokens_seen(q, min((block + 1) * 2 * tile_rows_tokens(q_per_kv), q.rows) - 1, causal);
 }
 // By one warp: which requests are for which kernel, and the two lines of tiles.  A block that sees nothing counts as one tile, so that
 // somebody writes its rows.
-__device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSchedule& sc, int32_t q_per_kv, bool causal)
+__device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSchedule& sc, const PagedOut& o)
 {
+    const int32_t q_per_kv = o.q_per_kv;
     constexpr unsigned full = 0xffffffffu;
     const int lane = static_cast<int>(threadIdx.x & 31u);
     const int32_t T = paged_tiles(kv);
@@ -239,15 +250,25 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
         const int32_t f = few + scan(!many && rows > 0 ? q.tiles : 0);
         if (r < kv.n_req) sc.few_tiles[r + 1] = f;
         few = __shfl_sync(full, f, 31);
+        // requests without a token: nobody else comes to their rows
+        for (unsigned left = __ballot_sync(full, !many && rows > 0 && q.tiles == 0); left; left &= left - 1u) {
+            const int src = __ffs(left) - 1;
+            const int64_t row0 = __shfl_sync(full, q.row0, src), heads = kv.heads * q_per_kv, n = __shfl_sync(full, q.rows, src) * heads;
+            for (int64_t i = 0; i < n; ++i) {
+                const int64_t at = (row0 + i / heads) * o.q_heads + kv.head0 * q_per_kv + i % heads;
+                reinterpret_cast<uint2*>(o.out + at * kGroup)[lane] = make_uint2(0u, 0u);
+                if (o.lse && lane == 0) o.lse[at] = -INFINITY;
+            }
+        }
         for (unsigned left = __ballot_sync(full, many); left; left &= left - 1u) {
             const int src = __ffs(left) - 1;
             PagedReq one;
             one.rows = __shfl_sync(full, q.rows, src);
             one.kv = __shfl_sync(full, q.kv, src);
-            const int32_t blocks = static_cast<int32_t>((static_cast<int64_t>(one.rows) * q_per_kv + kManyRows - 1) / kManyRows);
+            const int32_t per_block = 2 * tile_rows_tokens(q_per_kv), blocks = (one.rows + per_block - 1) / per_block;
             for (int32_t b0 = 0; b0 < blocks && n_blocks < sc.max_blocks; b0 += 32) {
                 const int32_t b = b0 + lane, n = min(min(blocks - b0, 32), sc.max_blocks - n_blocks);
-                const int32_t mine = lane < n ? max((block_tokens(one, b, q_per_kv, causal) + kManyTokens - 1) / kManyTokens, 1) : 0;
+                const int32_t mine = lane < n ? max((block_sees(one, b, q_per_kv, o.causal) + kManyTokens - 1) / kManyTokens, 1) : 0;
                 const int32_t upto = tiles + scan(mine);
                 if (lane < n) {
                     sc.blocks[n_blocks + lane] = make_int2(r0 + src, b);
@@ -268,7 +289,7 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
 // be NaN in rows that do not see the token.
 template <int kMaxWarps>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
-ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedSchedule sc, int32_t q_per_kv, int32_t causal)
+ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -287,7 +308,7 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
     if (!finish_decode_tables(tb)) return;
     dependency_wait();
     // one warp, if possible one that has no room to decode, makes the schedule on the side
-    if (blockIdx.x == 0 && warp == (nw < blockDim.x >> 5 ? nw : 0u)) paged_schedule(kv, sc, q_per_kv, causal);
+    if (blockIdx.x == 0 && warp == (nw < blockDim.x >> 5 ? nw : 0u)) paged_schedule(kv, sc, o);
     const float T = tb.T;
     const uint32_t n_tiles = static_cast<uint32_t>(paged_tiles(kv)), units = n_tiles * kv.heads;
     if (blockIdx.x == 0 && threadIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
@@ -376,16 +397,6 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
 // leave sums and maxima in the workspace and are joined by ecco_paged_combine_kernel.
 // Bound by memory: 512 bytes per token and KV head.
 // ---------------------------------------------------------------------------------------------
-struct PagedOut {
-    const __half* q;
-    int64_t q_stride;
-    float scale_log2;          // scale * log2(e)
-    int32_t q_per_kv, q_heads, causal;
-    __half* out;
-    float* lse;                // or NULL
-    float* part;               // partial sums [slot][rows][128]
-    float2* part_ml;           // maxima (log2) and sums of weights [slot][rows]
-};
 constexpr int kFewStages = 2;
 template <int kM> constexpr int kFewWarps = kM == 1 ? 6 : 5;
 template <int kM> constexpr uint32_t kFewWarpBytes = kFewStages * 2 * kKvTileBytes + kM * 4096;
@@ -435,11 +446,11 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t mine = smem_u32(smem) + 1024 + warp * kFewWarpBytes<kM>, q_at = mine + kFewStages * 2 * kKvTileBytes;
     const uint32_t bar = smem_u32(smem) + warp * kFewStages * 8;
-    release_dependents();
     if (lane == 0)
         for (int s = 0; s < kFewStages; ++s) mbar_init(bar + s * 8, 1);
     __syncwarp();
     dependency_wait();
+    release_dependents();                                  // behind the wait: see ecco_paged_combine_kernel
     const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);
     const int W = static_cast<int>(gridDim.x) * kFewWarps<kM>, wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
     const int64_t U = static_cast<int64_t>(line) * kv.heads;
@@ -640,64 +651,75 @@ __device__ __forceinline__ void join_sums(float& m, float& l, float4& acc, float
     acc = make_float4(acc.x * f0 + v.x * f1, acc.y * f0 + v.y * f1, acc.z * f0 + v.z * f1, acc.w * f0 + v.w * f1);
     m = top;
 }
-// Joins the pieces of rows whose request was cut, and writes the rows that see nothing.  `team` warps to a (new token, query head).
+// Joins the pieces of requests that were cut.
+//   by_rows == 0   CTA c looks at the cut in front of run c + 1, and if it is the first one of its request (and head), a warp joins a row:
+//                  many requests, few pieces each
+//   by_rows > 0    a CTA to a (request, head, row < by_rows), its eight warps share the pieces: few requests, many pieces each
+// What it reads before its wait is older than ecco_paged_few_kernel, which lets it begin only when it has itself waited.
 template <int kM>
 __global__ void __launch_bounds__(256, 4)
-ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int few_ctas, int team)
+ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int few_ctas, int by_rows)
 {
     __shared__ float4 sums[8][32];
     __shared__ float2 ml[8];
-    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5), sub = warp % team;
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
     release_dependents();
-    dependency_wait();
-    const int slice_heads = kv.heads * o.q_per_kv;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * (8 / team) + warp / team;
-    const bool exists = item < static_cast<int64_t>(kv.n_tokens) * slice_heads;
-    const int token = exists ? static_cast<int>(item / slice_heads) : 0, hq = exists ? static_cast<int>(item - static_cast<int64_t>(token) * slice_heads) : 0;
-    const int32_t T = paged_tiles(kv);
-    const int r = warp_find(kv.cu_new, kv.n_req, token);
-    const PagedReq q = paged_req(kv, r, T);
-    const int i = token - q.row0;
-    const int head = hq / o.q_per_kv, row = i * o.q_per_kv + hq - head * o.q_per_kv;
-    const bool mine = exists && i >= 0 && i < q.rows && q.rows * static_cast<int64_t>(o.q_per_kv) <= sc.few_rows;
-    const int64_t at_row = static_cast<int64_t>(token) * o.q_heads + kv.head0 * o.q_per_kv + hq;
-    int w_lo = 0, w_hi = -1;
-    bool first_slot = true;
-    if (mine && q.tiles > 0) {
-        const int32_t line = __ldcg(sc.few_tiles + kv.n_req);
-        const UnitSplit split(static_cast<int64_t>(line) * kv.heads, few_ctas * kFewWarps<kM>);
-        const int64_t f0 = static_cast<int64_t>(head) * line + __ldcg(sc.few_tiles + r);
-        w_lo = split.owner(f0);
-        w_hi = split.owner(f0 + q.tiles - 1);
-        first_slot = split.begin(w_lo) == f0;
+    const int32_t line = __ldcg(sc.few_tiles + kv.n_req);
+    const int64_t U = static_cast<int64_t>(line) * kv.heads;
+    const UnitSplit split(U, few_ctas * kFewWarps<kM>);
+    int head, r, row = warp;
+    int64_t cut = 0;
+    if (by_rows) {
+        row = static_cast<int>(blockIdx.x) % by_rows;
+        head = static_cast<int>(blockIdx.x) / by_rows % kv.heads;
+        r = static_cast<int>(blockIdx.x) / by_rows / kv.heads;
+    } else {
+        cut = split.begin(static_cast<int>(blockIdx.x) + 1);
+        if (cut >= U) { dependency_wait(); return; }
+        head = static_cast<int>(divide(static_cast<uint64_t>(cut), static_cast<uint64_t>(line)));
+        r = warp_find(sc.few_tiles, kv.n_req, static_cast<int32_t>(cut - static_cast<int64_t>(head) * line));
     }
-    const bool joins = w_hi > w_lo;
-    float m = -INFINITY, l = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (joins) {
-        for (int w = w_lo + sub; w <= w_hi; w += team) {
-            const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && !first_slot ? 1 : 0)) * (16 * kM) + row;
+    const int32_t at0 = __ldcg(sc.few_tiles + r);
+    const int64_t first = static_cast<int64_t>(head) * line + at0, end = first + __ldcg(sc.few_tiles + r + 1) - at0;
+    const PagedReq q = paged_req(kv, r, paged_tiles(kv));
+    const int R = min(q.rows * o.q_per_kv, 16 * kM);
+    bool joins = end > first && row < R;
+    int w_lo = 0, w_hi = 0;
+    if (by_rows) {
+        if (joins) { w_lo = split.owner(first); w_hi = split.owner(end - 1); }
+        joins = w_hi > w_lo;
+    } else {
+        w_lo = static_cast<int>(blockIdx.x);
+        joins = first < cut && split.begin(w_lo) <= first;
+        if (joins) w_hi = split.owner(end - 1);
+    }
+    const bool second = joins && split.begin(w_lo) != first;           // the piece in run w_lo is in its second slot
+    dependency_wait();
+    if (!joins) return;                                    // by_rows: the whole CTA
+    const int step = by_rows ? 8 : 1;
+    for (; row < R; row += 8) {
+        float m = -INFINITY, l = 0.0f;
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int w = w_lo + (by_rows ? warp : 0); w <= w_hi; w += step) {
+            const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && second ? 1 : 0)) * (16 * kM) + row;
             const float2 x = __ldcg(o.part_ml + at);
             const float4 v = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
             join_sums(m, l, acc, x, v);
         }
-    }
-    if (team > 1) {
-        sums[warp][lane] = acc;
-        if (lane == 0) ml[warp] = make_float2(m, l);
-        __syncthreads();
-        if (sub == 0) {
-            for (int w = 1; w < team; ++w) {
-                const float2 x = ml[warp + w];
-                const float4 v = sums[warp + w][lane];
-                join_sums(m, l, acc, x, v);
-            }
+        if (by_rows) {
+            sums[warp][lane] = acc;
+            if (lane == 0) ml[warp] = make_float2(m, l);
+            __syncthreads();
+            if (warp) return;
+            for (int w = 1; w < 8; ++w) join_sums(m, l, acc, ml[w], sums[w][lane]);
         }
-    }
-    if (sub == 0 && mine && (joins || q.tiles == 0)) {
+        const int token = row / o.q_per_kv, g = row - token * o.q_per_kv;
+        const int64_t at_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + (kv.head0 + head) * o.q_per_kv + g;
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
         reinterpret_cast<uint2*>(o.out + at_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
         if (o.lse && lane == 0) o.lse[at_row] = lse_of(m, l, kWeightLog2);
+        if (by_rows) return;
     }
 }
 

@@ -6,24 +6,33 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // K6m: pieces of prompts: a request's rows (new tokens x query heads per KV head, query heads innermost) in blocks of 256.
+// (as many whole tokens as two tiles of 128 rows hold)
 //   S = Q K^T    128 x 128 per tile of rows and tile of tokens; Q and K from shared memory, S to tensor memory
 //   P = 2^(scale S - m)   in registers, a thread to a row; fp16, back to tensor memory over S
 //   O += P V     P from tensor memory, V from shared memory, O in tensor memory
 // Two tiles of rows share every K and V tile, and while one's products run, the other's softmax does.
-// Warps 0-3 and 4-7: softmax of the first and of the second tile of rows; warp 8: loads; warp 9: one thread issues the products.
+// Warps 0-3 and 4-7: softmax of the first and of the second tile of rows; warp 8: K and V; warp 9 issues the
+// products; warp 10: Q, and what there is to do (ManyTask); warp 11 only gives its registers away.
 // m is the row's maximum when it was last taken; a larger one is taken only when it is more than 2^8 larger (the weights are fp16
 // times 2^7, at most 2^15), so O is rescaled now and then instead of with every tile.
 //
 // All blocks' tiles of all heads form one line, which is cut into equal runs, one per CTA (see paged_schedule): a block that is cut leaves
 // its sums in the workspace and ecco_paged_join_kernel joins them.
 // ---------------------------------------------------------------------------------------------
-constexpr int kManyThreads = 384;                          // warps 10 and 11 only give their registers away
+constexpr int kManyThreads = 384;
 constexpr uint32_t kOperandBytes = 8 * 4096;               // eight pieces of [128][16] fp16, 32-byte swizzle
 constexpr int kManyStages = 5;                             // tiles of K and V in flight
 constexpr uint32_t kManySmemBytes = 1024 + (2 + kManyStages) * kOperandBytes;
 static_assert(kManySmemBytes <= kSmemCtaBytes, "fits an SM");
 constexpr float kManyWeightLog2 = 7.0f, kLazyLog2 = 8.0f;
 
+// 3-D tiled bulk load global -> shared through a tensor map (TMA); what lies outside of the tensor reads as zero
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x),
+                 "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_ld32(uint32_t* r, uint32_t at)
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -44,11 +53,42 @@ __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// arrives when all products issued so far by this thread are done
+// one arrival for the whole warp (32 at one address go one after the other)
+__device__ __forceinline__ void warp_arrive(uint32_t bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31u) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// by a converged warp: arrives when all products that it has issued so far are done
 __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\t@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ uint64_t pack_f2(float a, float b)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void unpack_f2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float v;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(a), "f"(b), "f"(c));
+    return v;
 }
 // Shared-memory operand with 32-byte swizzle: rows of 32 bytes, blocks of eight rows `stride` bytes apart; `lead`: what is 16 elements on
 // in the direction of the rows' bytes, where the operand is wider than that (MN-major only).
@@ -58,17 +98,45 @@ __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t lead, uint32_t
 }
 // 128 x 128 x 16, fp16 x fp16 -> fp32; b_mn: B's contiguous direction is N
 __host__ __device__ constexpr uint32_t mma_shape(bool b_mn) { return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((128u >> 3) << 17) | ((128u >> 4) << 24); }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
+// One lane of a converged warp issues the products; what they get as operands has to be the same in all lanes, and known to the compiler
+// to be (see same_in_warp): it lies in uniform registers then, and an instruction takes as long to issue as the tensor core takes to do
+// it.  With one lane in a branch of its own it was some 130 clocks against 64.
+__device__ __forceinline__ int same_in_warp(int v) { return __reduce_max_sync(0xffffffffu, v); }
+// S = Q K^T of a tile: eight steps of 16 dims, 4096 bytes apart in both operands
+__device__ __forceinline__ void mma_scores(uint32_t d, uint64_t a, uint64_t b)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(shape),
-                 "r"(static_cast<uint32_t>(add))
-                 : "memory");
+    asm volatile(
+        "{\n\t.reg .pred p, f, t;\n\t.reg .b64 a, b;\n\telect.sync _|p, 0xffffffff;\n\tsetp.ne.u32 f, 0, 0;\n\tsetp.eq.u32 t, 0, 0;\n\tmov.b64 a, %1;\n\tmov.b64 b, %2;\n\t"
+        "@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, f;\n\t"
+        "add.u64 a, a, 256;\n\tadd.u64 b, b, 256;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+        "add.u64 a, a, 256;\n\tadd.u64 b, b, 256;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+        "add.u64 a, a, 256;\n\tadd.u64 b, b, 256;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+        "add.u64 a, a, 256;\n\tadd.u64 b, b, 256;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+        "add.u64 a, a, 256;\n\tadd.u64 b, b, 256;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+        "add.u64 a, a, 256;\n\tadd.u64 b, b, 256;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+        "add.u64 a, a, 256;\n\tadd.u64 b, b, 256;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(mma_shape(false))
+        : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add)
+// O (+)= P V over 64 tokens: four steps, eight columns of P and 512 bytes of V apart
+__device__ __forceinline__ void mma_values4(uint32_t d, uint32_t a, uint64_t b, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(shape),
-                 "r"(static_cast<uint32_t>(add))
-                 : "memory");
+    asm volatile(
+        "{\n\t.reg .pred p, q, t;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\telect.sync _|p, 0xffffffff;\n\tsetp.ne.u32 q, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\tmov.b32 a, %1;\n\tmov.b64 b, %2;\n\t"
+        "@p tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, q;\n\t"
+        "add.u32 a, a, 8;\n\tadd.u64 b, b, 32;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+        "add.u32 a, a, 8;\n\tadd.u64 b, b, 32;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+        "add.u32 a, a, 8;\n\tadd.u64 b, b, 32;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(mma_shape(true)), "r"(static_cast<uint32_t>(add))
+        : "memory");
+}
+// the same over 16 tokens
+__device__ __forceinline__ void mma_values(uint32_t d, uint32_t a, uint64_t b, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\telect.sync _|p, 0xffffffff;\n\tsetp.ne.u32 q, %4, 0;\n\t@p tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, q;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(mma_shape(true)), "r"(static_cast<uint32_t>(add))
+        : "memory");
 }
 
 // a piece of a block: tiles [from, to) of the `tiles` tiles of block `block` of request r, for head `head`
@@ -90,19 +158,31 @@ __device__ __forceinline__ ManyPiece many_piece(const PagedSchedule& sc, int32_t
     return p;
 }
 
+// what the other warps need to know of a piece, for a tile of its rows (read from shared memory)
+struct ManyTask {
+    int32_t used;              // the tile has rows
+    int32_t from, to, tiles;   // of 128 tokens; of 32 tokens: the request's
+    int32_t head, r_row0, r_rows, r_kv;   // KV head, the request's rows of q and tokens
+    int32_t token;             // the tile's first new token of the request
+    int32_t whole, slot;       // the piece is its block; else: place of its sums
+};
+
 __global__ void __launch_bounds__(kManyThreads, 1)
-ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
+ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc,
+                       const __grid_constant__ CUtensorMap tile_map, const __grid_constant__ CUtensorMap q_map)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, base = smem_u32(smem);
     // barriers: tiles have come / are free again, Q there, S there, P there, O there
-    const uint32_t full_at = base, free_at = base + 8 * kManyStages, q_bar = base + 128, s_bar = base + 144, p_bar = base + 160, o_bar = base + 176, end_bar = base + 192;
+    const uint32_t full_at = base, free_at = base + 8 * kManyStages, q_bar = base + 128, s_bar = base + 144, p_bar = base + 160 /* halves, tiles of rows */, o_bar = base + 192, q_free = base + 208, end_bar = base + 224;
     const uint32_t q_smem = base + 1024, ring = q_smem + 2 * kOperandBytes;
     uint32_t* const tmem_word = reinterpret_cast<uint32_t*>(smem + 256);
     volatile int* const failed = reinterpret_cast<volatile int*>(smem + 264);
+    ManyTask* const tasks = reinterpret_cast<ManyTask*>(smem + 320);       // [two pieces][tile of rows]
+    static_assert(320 + 4 * sizeof(ManyTask) <= 1024, "tasks fit");
     if (threadIdx.x == 0) {
         for (int i = 0; i < kManyStages; ++i) { mbar_init(full_at + 8 * i, 1); mbar_init(free_at + 8 * i, 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(q_bar + 8 * x, 128); mbar_init(s_bar + 8 * x, 1); mbar_init(p_bar + 8 * x, 128); mbar_init(o_bar + 8 * x, 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(q_bar + 8 * x, 1); mbar_init(q_free + 8 * x, 5); mbar_init(s_bar + 8 * x, 1); mbar_init(p_bar + 8 * x, 4); mbar_init(p_bar + 16 + 8 * x, 4); mbar_init(o_bar + 8 * x, 1); }
         mbar_init(end_bar, 1);
         *failed = 0;
     }
@@ -121,15 +201,18 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     const int64_t u0 = split.begin(static_cast<int>(blockIdx.x)), u1 = split.begin(static_cast<int>(blockIdx.x) + 1);
     const int32_t T = paged_tiles(kv);
     const bool causal = o.causal;
-    // a wait that has run out makes all others run out at once
+    // The whole warp waits; one vote decides, so that the branches are the warp's.  (A loop of each lane's own took 250 clocks to see a barrier
+    // that had long been passed, this one 50.)  A wait that has run out makes all others run out at once.
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        bool done = false;
-        for (int i = 0; i < 2 * kWaitLimit && !done; ++i) {
-            done = mbar_try_wait(bar, parity);
-            if (!done && (i & 63) == 63 && *failed) break;
+        constexpr unsigned full = 0xffffffffu;
+        if (__all_sync(full, mbar_try_wait(bar, parity))) return true;
+        for (int i = 0; i < 2 * kWaitLimit; ++i) {
+            if (__all_sync(full, mbar_try_wait(bar, parity))) return true;
+            if ((i & 63) == 63 && __any_sync(full, *failed)) break;
         }
-        if (!done) { *failed = 1; atomicExch(&g_device_status, ECCO_ERR_DEVICE_TIMEOUT); }
-        return done;
+        *failed = 1;
+        atomicExch(&g_device_status, ECCO_ERR_DEVICE_TIMEOUT);
+        return false;
     };
 
     // 384 threads x 168 registers = 128 x 40 + 256 x 232
@@ -138,37 +221,27 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     if (warp < 8) {
         // softmax: thread t of tile x holds row 128 x + t
         const uint32_t x = warp >> 2, t = threadIdx.x & 127u, s_at = tmem + ((warp & 3u) << 21) + x * 128, o_at = s_at + 256;
-        uint32_t n_s = 0, n_o = 0;                         // S and O waited for
+        const int32_t in_tile = static_cast<int32_t>(t) / o.q_per_kv, g = static_cast<int32_t>(t) - in_tile * o.q_per_kv;       // new token, query head
+        // a scale of zero as a small one: times minus infinity it is still minus infinity
+        const float scale = fabsf(o.scale_log2) < 1e-30f ? 1e-30f : o.scale_log2, unseen = scale > 0.0f ? -INFINITY : INFINITY;
+        uint32_t n_piece = 0, n_s = 0, n_o = 0;            // pieces, S and O waited for
         bool ok = true;
         for (int64_t u = u0; u < u1 && ok;) {
-            const ManyPiece pc = many_piece(sc, n_blocks, total, u, u1);
-            const PagedReq q = paged_req(kv, pc.r, T);
-            const int slot = 2 * static_cast<int>(blockIdx.x) + (u == u0 ? 0 : 1);
-            u = pc.next;
-            const int64_t rows = static_cast<int64_t>(q.rows) * o.q_per_kv, row = static_cast<int64_t>(pc.block) * kManyRows + x * 128 + t;
-            if (x == 1 && rows <= static_cast<int64_t>(pc.block) * kManyRows + 128) continue;             // one tile of rows only
-            const bool exists = row < rows;
-            const int32_t token = static_cast<int32_t>((exists ? row : 0) / o.q_per_kv), g = static_cast<int32_t>(row - static_cast<int64_t>(token) * o.q_per_kv);
-            const int64_t out_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + g;
-            const int32_t seen = exists ? tokens_seen(q, token, causal) : 0;
-            {
-                // a negative scale is taken as its size, with q negated
-                const uint4* const src = reinterpret_cast<const uint4*>(o.q + (q.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + pc.head) * o.q_per_kv + g) * kGroup);
-                const uint32_t flip = o.scale_log2 < 0.0f ? 0x80008000u : 0u, dst = q_smem + x * kOperandBytes + t * 32;
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (exists) v = __ldcg(src + c);
-                    sts_v4(dst + (c >> 1) * 4096 + (((c & 1) ^ ((t >> 2) & 1u)) << 4), v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
-                }
-                fence_async_smem();
-                mbar_arrive(q_bar + 8 * x);
-            }
-            const float scale = fabsf(o.scale_log2);
+            ok = wait(q_bar + 8 * x, n_piece & 1u);
+            if (!ok) break;
+            const ManyTask pc = tasks[(n_piece & 1u) * 2 + x];
+            ++n_piece;
+            warp_arrive(q_free + 8 * x);                   // the task has been read: with the products' arrival the next may come
+            u += pc.to - pc.from;
+            if (!pc.used) continue;
+            const int32_t token = pc.token + in_tile;
+            const bool exists = in_tile < tile_rows_tokens(o.q_per_kv) && token < pc.r_rows;
+            const int64_t out_row = static_cast<int64_t>(pc.r_row0 + token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + g;
+            const int32_t seen = exists ? tokens_seen(PagedReq{0, 0, pc.r_kv, 0, pc.r_rows}, token, causal) : 0;
             float m = -INFINITY, l = 0.0f;                 // m in units of log2, the weights stand at 2^(s - m + kManyWeightLog2)
             for (int32_t j = pc.from; j < pc.to; ++j) {
                 ok = wait(s_bar + 8 * x, n_s++ & 1u);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                if (!ok) break;
                 tmem_fence_after();
                 float s[128];
 #pragma unroll
@@ -177,13 +250,20 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 const int32_t left = seen - j * kManyTokens;           // columns that the row sees
                 if (__any_sync(0xffffffffu, left < kManyTokens)) {
 #pragma unroll
-                    for (int c = 0; c < 128; ++c) s[c] = c < left ? s[c] : -INFINITY;
+                    for (int c = 0; c < 128; ++c) s[c] = c < left ? s[c] : unseen;
                 }
-                float top = s[0];
+                float top;
+                if (scale > 0.0f) {
+                    float top4[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
 #pragma unroll
-                for (int c = 1; c < 128; ++c) top = fmaxf(top, s[c]);
-                top *= scale;
-                if (left <= 0) top = -INFINITY;            // also where the scale is zero
+                    for (int c = 8; c < 128; c += 2) top4[(c >> 1) & 3] = max3(top4[(c >> 1) & 3], s[c], s[c + 1]);
+                    top = fmaxf(max3(top4[0], top4[1], top4[2]), top4[3]) * scale;
+                } else {
+                    top = s[0];
+#pragma unroll
+                    for (int c = 1; c < 128; ++c) top = fminf(top, s[c]);
+                    top *= scale;
+                }
                 const bool grow = top > m + kLazyLog2;     // -inf + 8 is -inf
                 if (__any_sync(0xffffffffu, grow)) {
                     const float m_new = grow ? top : m, f = grow ? exp2_fast(m - top) : 1.0f;
@@ -202,29 +282,37 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                     }
                 }
                 const float sub = kManyWeightLog2 - (m == -INFINITY ? 0.0f : m);
-                float sum0 = 0.0f, sum1 = 0.0f;
-                uint32_t p[64];
+                // in two halves: the products of the first begin while the second is formed
+                const uint64_t scale2 = pack_f2(scale, scale), sub2 = pack_f2(sub, sub);
+                uint64_t sums[2] = {0, 0};                 // pairs of zeros
 #pragma unroll
-                for (int c = 0; c < 64; ++c) {
-                    const float a = exp2_fast(fmaf(s[2 * c], scale, sub)), b = exp2_fast(fmaf(s[2 * c + 1], scale, sub));
-                    sum0 += a;
-                    sum1 += b;
-                    p[c] = pack_h2(a, b);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        float a, b;
+                        unpack_f2(fma_f2(pack_f2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), scale2, sub2), a, b);
+                        a = exp2_fast(a);
+                        b = exp2_fast(b);
+                        sums[c & 1] = add_f2(sums[c & 1], pack_f2(a, b));
+                        p[c] = pack_h2(a, b);
+                    }
+                    tmem_st32(s_at + 32 * h, p);
+                    tmem_wait_st();
+                    tmem_fence_before();
+                    warp_arrive(p_bar + 16 * h + 8 * x);
                 }
-                l += sum0 + sum1;
-                tmem_st32(s_at, p);
-                tmem_st32(s_at + 32, p + 32);
-                tmem_wait_st();
-                tmem_fence_before();
-                mbar_arrive(p_bar + 8 * x);
+                float sum_a, sum_b;
+                unpack_f2(add_f2(sums[0], sums[1]), sum_a, sum_b);
+                l += sum_a + sum_b;
             }
             if (!ok) break;
             ok = wait(o_bar + 8 * x, n_o++ & 1u);
-            if (!__all_sync(0xffffffffu, ok)) break;
+            if (!ok) break;
             tmem_fence_after();
-            const bool whole = pc.from == 0 && pc.to == pc.tiles;
+            const bool whole = pc.whole;
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            float* const part = o.part + (static_cast<int64_t>(slot) * kManyRows + x * 128 + t) * kGroup;
+            float* const part = o.part + (static_cast<int64_t>(pc.slot) * kManyRows + x * 128 + t) * kGroup;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t v[32];
@@ -244,7 +332,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             }
             if (exists) {
                 if (whole) { if (o.lse) o.lse[out_row] = lse_of(m, l, kManyWeightLog2); }
-                else o.part_ml[static_cast<int64_t>(slot) * kManyRows + x * 128 + t] = make_float2(m, l);
+                else o.part_ml[static_cast<int64_t>(pc.slot) * kManyRows + x * 128 + t] = make_float2(m, l);
             }
             tmem_fence_before();                           // O has been read before the next block's P arrives
         }
@@ -257,18 +345,17 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             const PagedReq q = paged_req(kv, pc.r, T);
             u = pc.next;
             for (int32_t j = pc.from; j < pc.to && ok; ++j) {
-                const int32_t tiles = min(max(q.tiles - 4 * j, 0), 4);         // of 32 tokens
                 for (int which = 0; which < 2; ++which) {
-                    const uint32_t st = n % kManyStages, bar = full_at + 8 * st, dst = ring + st * kOperandBytes;
-                    if (n >= kManyStages) ok = __all_sync(0xffffffffu, wait(free_at + 8 * st, (n / kManyStages - 1) & 1u));
+                    const uint32_t st = n % kManyStages, bar = full_at + 8 * st;
+                    if (n >= kManyStages) ok = wait(free_at + 8 * st, (n / kManyStages - 1) & 1u);
                     if (!ok) break;
                     ++n;
-                    if (lane == 0) mbar_expect_tx(bar, tiles * kKvTileBytes);
+                    if (lane == 0) {
+                        mbar_expect_tx(bar, kOperandBytes);
+                        // four tiles of 32 tokens, their pieces side by side; tiles that are not the request's are not used
+                        tma_load_3d(ring + st * kOperandBytes, &tile_map, 0, (which * kv.heads + pc.head) * kv.max_tiles + q.first + 4 * j, 0, bar);
+                    }
                     __syncwarp();
-                    // piece lane % 8 of tile lane / 8
-                    if (static_cast<int32_t>(lane >> 3) < tiles)
-                        bulk_g2s(dst + (lane & 7u) * 4096 + (lane >> 3) * kPieceBytes,
-                                 staged_tile(kv, which, pc.head, q.first + 4 * j + static_cast<int32_t>(lane >> 3)) + (lane & 7u) * kPieceBytes, kPieceBytes, bar);
                 }
             }
         }
@@ -276,61 +363,94 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             for (uint32_t i = n < kManyStages ? 0 : n - kManyStages; i < n; ++i)
                 for (int k = 0; k < kWaitLimit && !mbar_try_wait(full_at + 8 * (i % kManyStages), (i / kManyStages) & 1u); ++k) {}
     } else if (warp == 9) {
-        // products: one thread issues them
-        uint32_t n = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+        // products: of one tile of the rows while the other's softmax runs
+        const uint32_t tmem_u = static_cast<uint32_t>(same_in_warp(static_cast<int>(tmem)));
+        const uint64_t q_op = operand(q_smem, 16, 256), k_op = operand(ring, 16, 256), v_op = operand(ring, 4096, 256);
+        constexpr uint64_t kStep = kOperandBytes >> 4;     // from one tile to the next, in an operand's units
+        int n_q = 0, n_p[2] = {0, 0};                      // rows of Q and weights waited for
+        int st = 0, turn = 0;                              // place in the ring, times around
         bool ok = true;
+        auto advance = [&]() { if (++st == kManyStages) { st = 0; ++turn; } };
         for (int64_t u = u0; u < u1 && ok;) {
-            const ManyPiece pc = many_piece(sc, n_blocks, total, u, u1);
-            const PagedReq q = paged_req(kv, pc.r, T);
-            u = pc.next;
-            const int n_x = static_cast<int64_t>(q.rows) * o.q_per_kv > static_cast<int64_t>(pc.block) * kManyRows + 128 ? 2 : 1;
-            if (lane == 0) {
-                auto scores = [&](int x, uint32_t st) {
+            ok = wait(q_bar, n_q & 1) && wait(q_bar + 8, n_q & 1) && wait(full_at + 8 * st, turn & 1);
+            if (!ok) break;
+            const ManyTask* const pc = tasks + (n_q & 1) * 2;
+            ++n_q;
+            const bool two = same_in_warp(pc[1].used) != 0;
+            const int n_tiles = same_in_warp(pc->to - pc->from), steps_left = same_in_warp(max(pc->tiles - 4 * pc->from, 0) * 2);
+            u += n_tiles;
+            tmem_fence_after();
 #pragma unroll
-                    for (int d = 0; d < 8; ++d)
-                        mma_ss(tmem + x * 128, operand(q_smem + x * kOperandBytes + d * 4096, 16, 256), operand(ring + st * kOperandBytes + d * 4096, 16, 256), mma_shape(false), d > 0);
-                    mma_commit(s_bar + 8 * x);
-                };
-                auto come = [&](uint32_t i) {
-                    ok = ok && wait(full_at + 8 * (i % kManyStages), (i / kManyStages) & 1u);
-                    return i % kManyStages;
-                };
-                uint32_t k_st = come(n);
-                for (int x = 0; x < n_x && ok; ++x) {
-                    ok = wait(q_bar + 8 * x, n_q[x]++ & 1u);
-                    tmem_fence_after();
-                    if (ok) scores(x, k_st);
-                }
-                if (ok) mma_commit(free_at + 8 * k_st);
-                for (int32_t j = pc.from; j < pc.to && ok; ++j) {
-                    const bool more = j + 1 < pc.to;
-                    const uint32_t v_st = come(n + 1);
-                    n += 2;
-                    // sixteen tokens at a time, as far as there are tiles
-                    const int steps = min(max(q.tiles - 4 * j, 0), 4) * 2;
-                    for (int x = 0; x < n_x && ok; ++x) {
-                        ok = wait(p_bar + 8 * x, n_p[x]++ & 1u);
+            for (int x = 0; x < 2; ++x) {
+                if (x && !two) break;
+                mma_scores(tmem_u + x * 128, q_op + x * kStep, k_op + st * kStep);
+                mma_commit(s_bar + 8 * x);
+            }
+            if (n_tiles == 1) { mma_commit(q_free); mma_commit(q_free + 8); }
+            mma_commit(free_at + 8 * st);
+            advance();
+            for (int j = 0; j < n_tiles && ok; ++j) {
+                const int v_st = st, steps = min(steps_left - 8 * j, 8);        // sixteen tokens at a time, as far as there are tiles
+                const bool more = j + 1 < n_tiles;
+                ok = wait(full_at + 8 * st, turn & 1);
+                advance();
+                if (ok && more) ok = wait(full_at + 8 * st, turn & 1);           // the next K tile: not to be waited for behind the products
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (x && !two) break;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (ok) ok = wait(p_bar + 16 * h + 8 * x, n_p[x] & 1);
                         if (!ok) break;
                         tmem_fence_after();
-                        for (int ks = 0; ks < steps; ++ks)
-                            mma_ts(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, operand(ring + v_st * kOperandBytes + ks * 512, 4096, 256), mma_shape(true), j > pc.from || ks > 0);
-                        if (x == n_x - 1) mma_commit(free_at + 8 * v_st);
-                        if (more) {
-                            if (x == 0) k_st = come(n);
-                            if (ok) scores(x, k_st);
-                            if (x == n_x - 1) mma_commit(free_at + 8 * k_st);
-                        } else {
-                            mma_commit(o_bar + 8 * x);
-                        }
+                        const uint64_t v_half = v_op + v_st * kStep + h * 128;
+                        if (steps == 8) mma_values4(tmem_u + 256 + x * 128, tmem_u + x * 128 + h * 32, v_half, j > 0 || h > 0);
+                        else
+#pragma unroll 1
+                            for (int ks = 0; ks < min(4, steps - 4 * h); ++ks)
+                                mma_values(tmem_u + 256 + x * 128, tmem_u + x * 128 + h * 32 + ks * 8, v_half + ks * 32, j > 0 || h > 0 || ks > 0);
+                    }
+                    if (!ok) break;
+                    ++n_p[x];
+                    if (more) {
+                        mma_scores(tmem_u + x * 128, q_op + x * kStep, k_op + st * kStep);
+                        mma_commit(s_bar + 8 * x);
+                    } else {
+                        mma_commit(o_bar + 8 * x);
                     }
                 }
-                if (!ok) {                                 // what has been issued ends before tensor memory is given back
-                    mma_commit(end_bar);
-                    for (int k = 0; k < kWaitLimit && !mbar_try_wait(end_bar, 0); ++k) {}
-                }
+                if (!ok) break;
+                mma_commit(free_at + 8 * v_st);
+                if (more) { mma_commit(free_at + 8 * st); advance(); }
+                if (j + 2 == n_tiles) { mma_commit(q_free); mma_commit(q_free + 8); }       // the piece's last scores are on their way
             }
-            ok = __shfl_sync(0xffffffffu, ok, 0);
+        }
+        if (!ok) {                                         // what has been issued ends before tensor memory is given back
+            mma_commit(end_bar);
+            for (int k = 0; k < kWaitLimit && !mbar_try_wait(end_bar, 0); ++k) {}
+        }
+    } else if (warp == 10) {
+        // what there is to do, and the rows of Q: the next piece's while the last products of this one run
+        const int32_t tokens = tile_rows_tokens(o.q_per_kv);
+        uint32_t n = 0;
+        for (int64_t u = u0; u < u1;) {
+            const ManyPiece pc = many_piece(sc, n_blocks, total, u, u1);
+            const PagedReq q = paged_req(kv, pc.r, T);
+            if (n && !(wait(q_free, (n - 1) & 1u) && wait(q_free + 8, (n - 1) & 1u))) break;
+            if (lane < 2) {                                // a lane to a tile of rows
+                const uint32_t x = lane, bar = q_bar + 8 * x;
+                const int32_t token = (2 * pc.block + static_cast<int32_t>(x)) * tokens;
+                const bool used = token < q.rows;
+                tasks[(n & 1u) * 2 + x] = ManyTask{used, pc.from, pc.to, q.tiles, pc.head, q.row0, q.rows, q.kv, token, pc.from == 0 && pc.to == pc.tiles,
+                                                   2 * static_cast<int>(blockIdx.x) + (u == u0 ? 0 : 1)};
+                mbar_expect_tx(bar, used ? 8 * 32 * tokens * o.q_per_kv : 0);
+                if (used)
+                    for (int d = 0; d < 8; ++d)
+                        tma_load_3d(q_smem + x * kOperandBytes + d * 4096, &q_map, 16 * d, (kv.head0 + pc.head) * o.q_per_kv, q.row0 + token, bar);
+            }
             __syncwarp();
+            ++n;
+            u = pc.next;
         }
     }
     tmem_fence_before();
@@ -340,30 +460,32 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
 }
 
 // Joins the pieces of blocks that were cut: CTA (c, part) looks at the cut in front of run c, and if it is its block's first one
-// joins 32 of the block's rows.  A warp to a row.
-constexpr int kJoinParts = kManyRows / 32;
+// joins sixteen of the block's rows, a warp to a row.  What it reads before its wait is older than ecco_paged_many_kernel, which lets it begin
+// only when it has itself waited for the kernels before it.
+constexpr int kJoinRows = 16, kJoinParts = kManyRows / kJoinRows;
 __global__ void __launch_bounds__(256)
 ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int many_ctas)
 {
     release_dependents();
     const int c = static_cast<int>(blockIdx.x) / kJoinParts + 1, part = static_cast<int>(blockIdx.x) % kJoinParts;
     const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
-    dependency_wait();
     const int32_t n_blocks = __ldcg(sc.n_blocks), total = n_blocks > 0 ? __ldcg(sc.block_tiles + n_blocks) : 0;
     const int64_t U = static_cast<int64_t>(total) * kv.heads;
     const UnitSplit split(U, many_ctas);
     const int64_t cut = split.begin(c);
-    if (cut >= U) return;
+    if (cut >= U) { dependency_wait(); return; }
     const ManyPiece pc = many_piece(sc, n_blocks, total, cut, U);
     const int64_t first = cut - pc.from, end = first + pc.tiles;
-    if (pc.from == 0 || split.begin(c - 1) > first) return;        // not inside of a block, or not its first cut
+    if (pc.from == 0 || split.begin(c - 1) > first) { dependency_wait(); return; }        // not inside of a block, or not its first cut
     const int w_lo = c - 1, w_hi = split.owner(end - 1);
     const bool second = split.begin(w_lo) != first;        // the piece in run w_lo is in its second slot
     const PagedReq q = paged_req(kv, pc.r, paged_tiles(kv));
-    for (int i = warp; i < 32; i += 8) {
-        const int in_block = part * 32 + i;
-        const int64_t row = static_cast<int64_t>(pc.block) * kManyRows + in_block;
-        if (row >= static_cast<int64_t>(q.rows) * o.q_per_kv) return;
+    dependency_wait();
+#pragma unroll
+    for (int i = warp; i < kJoinRows; i += 8) {
+        const int in_block = part * kJoinRows + i, t = in_block & 127, in_tile = t / o.q_per_kv, g = t - in_tile * o.q_per_kv;
+        const int32_t tokens = tile_rows_tokens(o.q_per_kv), token = (2 * pc.block + (in_block >> 7)) * tokens + in_tile;
+        if (in_tile >= tokens || token >= q.rows) continue;
         float m = -INFINITY, l = 0.0f;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         for (int w = w_lo; w <= w_hi; ++w) {
@@ -372,7 +494,6 @@ ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             const float4 v = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
             join_sums(m, l, acc, x, v);
         }
-        const int32_t token = static_cast<int32_t>(row / o.q_per_kv), g = static_cast<int32_t>(row - static_cast<int64_t>(token) * o.q_per_kv);
         const int64_t out_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + g;
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
         reinterpret_cast<uint2*>(o.out + out_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
