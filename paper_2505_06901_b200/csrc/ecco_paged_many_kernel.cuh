@@ -49,6 +49,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t* r)
                  "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
                  : "memory");
 }
+// what was loaded is used behind this point only: the compiler does not see that the wait in front concerns these registers
+__device__ __forceinline__ void tie32(uint32_t* r)
+{
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                      "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                      "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]));
+    asm volatile("" : "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -247,6 +255,8 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(reinterpret_cast<uint32_t*>(s) + 32 * c, s_at + 32 * c);
                 tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tie32(reinterpret_cast<uint32_t*>(s) + 32 * c);
                 const int32_t left = seen - j * kManyTokens;           // columns that the row sees
                 if (__any_sync(0xffffffffu, left < kManyTokens)) {
 #pragma unroll
@@ -275,6 +285,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                             uint32_t v[32];
                             tmem_ld32(v, o_at + 32 * c);
                             tmem_wait_ld();
+                            tie32(v);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
                             tmem_st32(o_at + 32 * c, v);
@@ -285,23 +296,30 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 // in two halves: the products of the first begin while the second is formed
                 const uint64_t scale2 = pack_f2(scale, scale), sub2 = pack_f2(sub, sub);
                 uint64_t sums[2] = {0, 0};                 // pairs of zeros
+                uint32_t p[32];
+                auto weights = [&](int from, int to) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t p[32];
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
+                    for (int c = from; c < to; ++c) {
                         float a, b;
-                        unpack_f2(fma_f2(pack_f2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), scale2, sub2), a, b);
+                        unpack_f2(fma_f2(pack_f2(s[2 * c], s[2 * c + 1]), scale2, sub2), a, b);
                         a = exp2_fast(a);
                         b = exp2_fast(b);
                         sums[c & 1] = add_f2(sums[c & 1], pack_f2(a, b));
-                        p[c] = pack_h2(a, b);
+                        p[c & 31] = pack_h2(a, b);
                     }
-                    tmem_st32(s_at + 32 * h, p);
+                };
+                auto sent = [&](int h) {
                     tmem_wait_st();
                     tmem_fence_before();
                     warp_arrive(p_bar + 16 * h + 8 * x);
-                }
+                };
+                weights(0, 32);
+                tmem_st32(s_at, p);
+                weights(32, 40);                           // while the first half is on its way
+                sent(0);
+                weights(40, 64);
+                tmem_st32(s_at + 32, p);
+                sent(1);
                 float sum_a, sum_b;
                 unpack_f2(add_f2(sums[0], sums[1]), sum_a, sum_b);
                 l += sum_a + sum_b;
@@ -318,6 +336,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 uint32_t v[32];
                 tmem_ld32(v, o_at + 32 * c);
                 tmem_wait_ld();
+                tie32(v);
                 if (exists && whole) {
                     uint4* const dst = reinterpret_cast<uint4*>(o.out + out_row * kGroup) + 4 * c;
                     // a row that has seen nothing: O may not have been written at all
