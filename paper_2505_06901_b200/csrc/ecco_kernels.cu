@@ -759,11 +759,12 @@ extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k,
 }
 
 namespace {
+// Tiles per warp (of each kind) from which on every CTA decodes both kinds.
+constexpr int kStageBothTiles = 3;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
 //   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks | few rows: sums, maxima | many rows: sums, maxima
 struct PagedAttnPlan {
-    int m, few_rows;                   // tiles of sixteen rows of ecco_paged_few_kernel, rows up to which a request is for it
-    bool many;                         // there may be requests of more rows
+    bool many;                         // there may be requests of more than kFewRows rows
     int few_ctas, many_ctas, max_blocks;
     size_t few_tiles, block_tiles, blocks, n_blocks, few_part, few_ml, many_part, many_ml, bytes;
 };
@@ -771,9 +772,7 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
 {
     PagedAttnPlan p = {};
     const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
-    p.m = rows > 16 && rows <= 32 ? 2 : 1;
-    p.few_rows = 16 * p.m;
-    p.many = rows > p.few_rows;
+    p.many = rows > kFewRows;
     p.few_ctas = std::max(1, spread_ctas(static_cast<int64_t>(b.max_tiles) * heads, ctas_max));
     p.many_ctas = ctas_max;
     p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
@@ -783,7 +782,7 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
         at = (at + bytes + 255) & ~static_cast<size_t>(255);
         return here;
     };
-    const size_t few_slots = static_cast<size_t>(p.few_ctas) * (p.m == 1 ? kFewWarps<1> : kFewWarps<2>) * 2 * p.few_rows;
+    const size_t few_slots = static_cast<size_t>(p.few_ctas) * kFewWarps * 2 * kFewRows;
     const size_t many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
     p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
     p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
@@ -807,22 +806,15 @@ bool paged_batch_fine(const ecco_paged_cache& c, const ecco_paged_batch& b, int 
     return blocks * (static_cast<int64_t>(b.max_kv) / kManyTokens + 1) <= INT32_MAX;
 }
 
-template <int kM>
 int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
 {
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {
-        const int rc = set_smem(ecco_paged_few_kernel<kM>, kFewSmemBytes<kM>);
+        const int rc = set_smem(ecco_paged_few_kernel, kFewSmemBytes);
         if (rc) return rc;
         configured[di.device] = true;
     }
-    int rc = launch_overlapped(ecco_paged_few_kernel<kM>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps<kM> * 32), kFewSmemBytes<kM>, s, kv, o, sc);
-    if (rc) return rc;
-    const int64_t runs = static_cast<int64_t>(p.few_ctas) * kFewWarps<kM>, segments = static_cast<int64_t>(kv.n_req) * kv.heads;
-    if (runs == 1) return ECCO_OK;
-    // by how many pieces a request of average length is cut into
-    const int by_rows = runs / segments > 16 ? static_cast<int>(std::min<int64_t>(16 * kM, static_cast<int64_t>(kv.max_new) * o.q_per_kv)) : 0;
-    return launch_overlapped(ecco_paged_combine_kernel<kM>, static_cast<unsigned>(by_rows ? segments * by_rows : runs - 1), 256u, 0, s, kv, o, sc, p.few_ctas, by_rows);
+    return launch_overlapped(ecco_paged_few_kernel, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps * 32), kFewSmemBytes, s, kv, o, sc);
 }
 // the tiles of a workspace as [piece][tile][1 KB]: a box of eight pieces of four tiles is a K or V operand of 128 tokens
 bool make_tile_map(CUtensorMap* map, const PagedKv& kv)
@@ -858,9 +850,17 @@ int launch_paged_many(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o
         if (rc) return rc;
         configured[di.device] = true;
     }
-    const int rc = launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc, map, q_map);
-    if (rc || p.many_ctas == 1) return rc;
-    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>((p.many_ctas - 1) * kJoinParts), 256u, 0, s, kv, o, sc, p.many_ctas);
+    return launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc, map, q_map);
+}
+int launch_paged_join(const PagedKv& kv, const PagedOut& few, const PagedOut& many, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
+{
+    const int64_t runs = static_cast<int64_t>(p.few_ctas) * kFewWarps, segments = static_cast<int64_t>(kv.n_req) * kv.heads;
+    // by how many pieces a request of average length is cut into
+    const int64_t by_rows = runs / segments > 16 ? std::min<int64_t>(kFewRows, static_cast<int64_t>(kv.max_new) * few.q_per_kv) : 0;
+    const int64_t few_items = by_rows ? segments * by_rows : runs - 1, many_items = p.many ? static_cast<int64_t>(p.many_ctas - 1) * kJoinParts : 0;
+    if (few_items + many_items == 0) return ECCO_OK;
+    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(few_items + many_items), 256u, 0, s, kv, few, many, sc, static_cast<int>(few_items), p.few_ctas,
+                             static_cast<int>(by_rows), p.many_ctas);
 }
 }  // namespace
 
@@ -908,8 +908,12 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     o.out = static_cast<__half*>(d_out); o.lse = d_lse;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     static thread_local bool configured[64] = {};
-    rc = want_all_smem(ecco_paged_stage_kernel<32>, &configured[di.device]);
-    if (rc) return rc;
+    if (!configured[di.device]) {
+        rc = set_smem(ecco_paged_stage_kernel<32, false>, kSmemCtaBytes);
+        if (!rc) rc = set_smem(ecco_paged_stage_kernel<32, true>, kSmemCtaBytes);
+        if (rc) return rc;
+        configured[di.device] = true;
+    }
     for (kv.head0 = 0; kv.head0 < cache->n_kv_heads; kv.head0 += kv.heads) {
         kv.heads = std::min(heads, cache->n_kv_heads - kv.head0);
         const PagedAttnPlan p = paged_attn_plan(b, kv.heads, q_per_kv, ctas);
@@ -919,22 +923,27 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         sc.blocks = reinterpret_cast<int2*>(kv.staged + p.blocks);
         sc.n_blocks = reinterpret_cast<int32_t*>(kv.staged + p.n_blocks);
         sc.max_blocks = p.max_blocks;
-        sc.few_rows = p.few_rows;
-        // an even number of CTAs: half of them for K, half for V
+        sc.few_rows = kFewRows;
+        // both kinds one after the other in every CTA where a warp has several tiles of each; else half of the CTAs for K, half for V
         const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
-        const int pairs = std::max(1, spread_ctas(units, ctas / 2));
-        rc = launch_overlapped(ecco_paged_stage_kernel<32>, static_cast<unsigned>(2 * pairs), spread_threads(units, pairs, 32), kSmemCtaBytes, s, kv, o, sc);
+        const bool both = units >= static_cast<int64_t>(kStageBothTiles) * 31 * di.sms;
+        const int ctas_k = std::max(1, spread_ctas(units, both ? di.sms : di.sms / 2));
+        rc = launch_overlapped(both ? ecco_paged_stage_kernel<32, true> : ecco_paged_stage_kernel<32, false>, static_cast<unsigned>(both ? ctas_k : 2 * ctas_k),
+                               spread_threads(units, ctas_k, 32), kSmemCtaBytes, s, kv, o, sc);
         if (rc) return rc;
         o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
         o.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
-        rc = p.m == 1 ? launch_paged_few<1>(di, kv, o, sc, p, s) : launch_paged_few<2>(di, kv, o, sc, p, s);
+        rc = launch_paged_few(di, kv, o, sc, p, s);
         if (rc) return rc;
+        PagedOut many = o;
         if (p.many) {
-            o.part = reinterpret_cast<float*>(kv.staged + p.many_part);
-            o.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
-            rc = launch_paged_many(di, kv, o, sc, p, s);
+            many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
+            many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
+            rc = launch_paged_many(di, kv, many, sc, p, s);
             if (rc) return rc;
         }
+        rc = launch_paged_join(kv, o, many, sc, p, s);
+        if (rc) return rc;
     }
     return ECCO_OK;
 }

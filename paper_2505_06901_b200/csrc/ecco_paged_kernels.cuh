@@ -283,109 +283,136 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
 }
 
 // K6s: pages -> tiles.  ecco_decompress_tma_kernel with another way in (a lane finds its token's block through the request's table)
-// and out (a piece leaves by one bulk copy of 1 KB).  Even CTAs decode K, odd ones V: both have the same number of tiles, no CTA
-// needs both sets of tables, and small calls decode K and V side by side.
+// and out (a piece leaves by one bulk copy of 1 KB).
+//   kBoth = false: even CTAs decode K, odd ones V: no CTA needs both sets of tables, and small calls decode K and V side by side.
+//   kBoth = true: every CTA decodes its share of K, then of V: another 4 us for the second set of tables, but caches
+//   whose blocks take differently long leave no CTA waiting (2.1 M groups of K and of V, 178 and 146 us alone: 377 -> 345 us).
 // Values are clamped to fp16's finite range (once per group, on the sixteen values of its table): weight zero times an infinity would
 // be NaN in rows that do not see the token.
-template <int kMaxWarps>
+constexpr int kStageTiles = 224;                           // prefix sums of this many requests are kept in the misc area
+template <int kMaxWarps, bool kBoth>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const int which = static_cast<int>(blockIdx.x & 1u);
-    const uint32_t cta = blockIdx.x >> 1, ctas = gridDim.x >> 1;
-    const uint8_t* const d_meta = which ? kv.v_meta : kv.k_meta;
+    const uint32_t cta = kBoth ? blockIdx.x : blockIdx.x >> 1, ctas = kBoth ? gridDim.x : gridDim.x >> 1;
     const uint32_t swz = ((lane >> 2) & 1u) << 4;
+    int32_t* const firsts = reinterpret_cast<int32_t*>(smem + 64);
+    static_assert(64 + (kStageTiles + 1) * 4 <= kMisc, "the prefix sums fit the misc area");
     release_dependents();
-    const DecodeTables tb = plan_decode_tables(smem_u32(smem), d_meta, true);
-    issue_decode_tables(tb, d_meta);
-    const uint32_t tiles_base = (tb.warp_base + 1023u) & ~1023u;
-    const uint32_t nw = decode_warps(tb, kTmaWarpBytes, tiles_base - tb.warp_base);
-    const uint32_t stage = tiles_base + warp * 1024;
-    const uint32_t bits = tiles_base + nw * 1024 + warp * kBitBytes + lane * 4;
-    const uint32_t my_row = stage + lane * 32;
-    if (!finish_decode_tables(tb)) return;
-    dependency_wait();
-    // one warp, if possible one that has no room to decode, makes the schedule on the side
-    if (blockIdx.x == 0 && warp == (nw < blockDim.x >> 5 ? nw : 0u)) paged_schedule(kv, sc, o);
-    const float T = tb.T;
-    const uint32_t n_tiles = static_cast<uint32_t>(paged_tiles(kv)), units = n_tiles * kv.heads;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-    const uint32_t tile_stride = balanced_warps(units, ctas * nw);
-    uint32_t u = warp * ctas + cta;
-    if (warp >= nw || u >= tile_stride) return;
+    for (int phase = 0; phase < (kBoth ? 2 : 1); ++phase) {
+        const int which = kBoth ? phase : static_cast<int>(blockIdx.x & 1u);
+        const uint8_t* const d_meta = which ? kv.v_meta : kv.k_meta;
+        const DecodeTables tb = plan_decode_tables(smem_u32(smem), d_meta, true);
+        if (phase) {                                           // see ecco_decompress_tma_kernel
+            fence_async_smem();
+            __syncthreads();
+        }
+        issue_decode_tables(tb, d_meta, phase == 0);
+        const uint32_t tiles_base = (tb.warp_base + 1023u) & ~1023u;
+        const uint32_t nw = decode_warps(tb, kTmaWarpBytes, tiles_base - tb.warp_base);
+        const uint32_t stage = tiles_base + warp * 1024;
+        const uint32_t bits = tiles_base + nw * 1024 + warp * kBitBytes + lane * 4;
+        const uint32_t my_row = stage + lane * 32;
+        if (!finish_decode_tables(tb, static_cast<uint32_t>(phase))) return;
+        if (phase == 0) {
+            dependency_wait();
+            if (kv.n_req <= kStageTiles)
+                for (int i = static_cast<int>(threadIdx.x); i <= kv.n_req; i += static_cast<int>(blockDim.x)) firsts[i] = __ldcg(kv.kv_tiles + i);
+            __syncthreads();
+            // one warp, if possible one that has no room to decode, makes the schedule on the side
+            if (blockIdx.x == 0 && warp == (nw < blockDim.x >> 5 ? nw : 0u)) paged_schedule(kv, sc, o);
+            if (blockIdx.x == 0 && threadIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        }
+        const float T = tb.T;
+        const uint32_t n_tiles = static_cast<uint32_t>(paged_tiles(kv)), units = n_tiles * kv.heads;
+        const uint32_t tile_stride = balanced_warps(units, ctas * nw);
+        uint32_t u = warp * ctas + cta;
+        if (warp >= nw || u >= tile_stride) u = units;
 
-    const uint8_t* const blocks = which ? kv.v_blocks : kv.k_blocks;
-    // the block of this lane's token of unit u, NULL behind the request's last token
-    auto block_ptr = [&](uint32_t unit) -> const uint8_t* {
-        const uint32_t head = unit / n_tiles, tile = unit - head * n_tiles;
-        const int r = warp_find(kv.kv_tiles, kv.n_req, static_cast<int32_t>(tile));
-        const int64_t token = (static_cast<int64_t>(tile) - __ldcg(kv.kv_tiles + r)) * 32 + lane;
-        if (token < 0 || token >= __ldcg(kv.kv_lens + r)) return nullptr;
-        const int64_t e = token >> kv.page_shift;
-        const int32_t page = e < kv.stride ? __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + e) : -1;
-        if (page < 0 || page >= kv.n_pages) {
-            atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-            return nullptr;
-        }
-        const int64_t at = ((static_cast<int64_t>(page) * kv.all_heads + kv.head0 + head) << kv.page_shift) + (token & ((1 << kv.page_shift) - 1));
-        return blocks + at * kBlockBytes;
-    };
-    const uint8_t* next = block_ptr(u);
-    while (u < units) {
-        const uint32_t head = u / n_tiles;
-        uint8_t* const dst = staged_tile(kv, which, static_cast<int>(head), static_cast<int>(u - head * n_tiles));
-        Block blk;
-        const bool there = next != nullptr;
-        if (there) {
-            ldg_block(blk, next);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) blk.w[i] = 0;     // whatever it decodes to: finite, and a token that no row sees
-        }
-        LaneGroup lg = open_block<true>(blk, bits, tb, T);
-        u += tile_stride;
-        if (u < units) {
-            next = block_ptr(u);
-            if (next) prefetch_block_l2(next);
-        }
-        auto send_piece = [&](int piece) {
-            fence_async_smem();                            // generic-proxy writes -> visible to the engine
-            __syncwarp();
-            if (lane == 0) { bulk_s2g(dst + piece * kPieceBytes, stage, kPieceBytes); bulk_commit(); }
-        };
-        const uint32_t end = decode_group<kBlockBits, kBlockFreeSteps>(lg, bits, tb.pairs, [&](int i, uint32_t ranks, bool cutting, int n_ok) {
-            uint32_t v[4];
-            map_ranks(lg, ranks, v);
-            if (cutting) cut_values(v, n_ok);
-            if (!(i & 1)) {
-                if (lane == 0) bulk_wait_read0();          // the engine has read the previous piece
-                __syncwarp();
-                sts_v4(my_row + swz, v[0], v[1], v[2], v[3]);
+        const uint8_t* const blocks = which ? kv.v_blocks : kv.k_blocks;
+        // the block of this lane's token of unit u, NULL behind the request's last token
+        auto block_ptr = [&](uint32_t unit) -> const uint8_t* {
+            const uint32_t head = unit / n_tiles;
+            const int32_t tile = static_cast<int32_t>(unit - head * n_tiles);
+            int r = 0;
+            int64_t token;
+            if (kv.n_req <= kStageTiles) {                     // the last request that begins at or before the tile
+                for (int n = kv.n_req; n > 1;) {
+                    const int half = n >> 1;
+                    if (firsts[r + half] <= tile) { r += half; n -= half; } else n = half;
+                }
+                token = (static_cast<int64_t>(tile) - firsts[r]) * 32 + lane;
             } else {
-                sts_v4(my_row + (swz ^ 16u), v[0], v[1], v[2], v[3]);
-                if (i != 15) send_piece(i >> 1);
+                r = warp_find(kv.kv_tiles, kv.n_req, tile);
+                token = (static_cast<int64_t>(tile) - __ldcg(kv.kv_tiles + r)) * 32 + lane;
             }
-        });
-        const int n_pad = pads_of(end);
-        const int n_max = __reduce_max_sync(0xffffffffu, n_pad);
-        if (n_max > 0) {
-            if (lane == 0) bulk_wait_all();                // pieces 0..6 of this tile are in memory
-            __syncwarp();
+            const int64_t e = token >> kv.page_shift;
+            const int32_t len = __ldcg(kv.kv_lens + r), page = e >= 0 && e < kv.stride ? __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + e) : -1;
+            if (token < 0 || token >= len) return nullptr;
+            if (page < 0 || page >= kv.n_pages) {
+                atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+                return nullptr;
+            }
+            const int64_t at = ((static_cast<int64_t>(page) * kv.all_heads + kv.head0 + head) << kv.page_shift) + (token & ((1 << kv.page_shift) - 1));
+            return blocks + at * kBlockBytes;
+        };
+        const uint8_t* next = u < units ? block_ptr(u) : nullptr;
+        while (u < units) {
+            const uint32_t head = u / n_tiles;
+            uint8_t* const dst = staged_tile(kv, which, static_cast<int>(head), static_cast<int>(u - head * n_tiles));
+            Block blk;
+            const bool there = next != nullptr;
+            if (there) {
+                ldg_block(blk, next);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) blk.w[i] = 0;     // whatever it decodes to: finite, and a token that no row sees
+            }
+            LaneGroup lg = open_block<true>(blk, bits, tb, T);
+            u += tile_stride;
+            if (u < units) {
+                next = block_ptr(u);
+                if (next) prefetch_block_l2(next);
+            }
+            auto send_piece = [&](int piece) {
+                fence_async_smem();                            // generic-proxy writes -> visible to the engine
+                __syncwarp();
+                if (lane == 0) { bulk_s2g(dst + piece * kPieceBytes, stage, kPieceBytes); bulk_commit(); }
+            };
+            const uint32_t end = decode_group<kBlockBits, kBlockFreeSteps>(lg, bits, tb.pairs, [&](int i, uint32_t ranks, bool cutting, int n_ok) {
+                uint32_t v[4];
+                map_ranks(lg, ranks, v);
+                if (cutting) cut_values(v, n_ok);
+                if (!(i & 1)) {
+                    if (lane == 0) bulk_wait_read0();          // the engine has read the previous piece
+                    __syncwarp();
+                    sts_v4(my_row + swz, v[0], v[1], v[2], v[3]);
+                } else {
+                    sts_v4(my_row + (swz ^ 16u), v[0], v[1], v[2], v[3]);
+                    if (i != 15) send_piece(i >> 1);
+                }
+            });
+            const int n_pad = pads_of(end);
+            const int n_max = __reduce_max_sync(0xffffffffu, n_pad);
+            if (n_max > 0) {
+                if (lane == 0) bulk_wait_all();                // pieces 0..6 of this tile are in memory
+                __syncwarp();
 #pragma unroll 1
-            for (int j = 0; j < n_max; ++j) {              // ascending: a later pad overrides an earlier one
-                if (j < n_pad) {
-                    const uint32_t f = pad_field(bits, j), loc = f & 127u, byte = ((loc & 15u) * 2) ^ swz;
-                    const float v = fminf(fmaxf(fp8_to_float(f >> 7) * T, -65504.0f), 65504.0f);
-                    if (loc >= 112u) sts_u16(my_row + byte, f2h_bits(v));
-                    else *reinterpret_cast<uint16_t*>(dst + (loc >> 4) * kPieceBytes + lane * 32 + byte) = static_cast<uint16_t>(f2h_bits(v));
+                for (int j = 0; j < n_max; ++j) {              // ascending: a later pad overrides an earlier one
+                    if (j < n_pad) {
+                        const uint32_t f = pad_field(bits, j), loc = f & 127u, byte = ((loc & 15u) * 2) ^ swz;
+                        const float v = fminf(fmaxf(fp8_to_float(f >> 7) * T, -65504.0f), 65504.0f);
+                        if (loc >= 112u) sts_u16(my_row + byte, f2h_bits(v));
+                        else *reinterpret_cast<uint16_t*>(dst + (loc >> 4) * kPieceBytes + lane * 32 + byte) = static_cast<uint16_t>(f2h_bits(v));
+                    }
                 }
             }
+            send_piece(7);
         }
-        send_piece(7);
+        if (lane == 0) bulk_wait_all();                        // the staging piece may lie elsewhere in the next phase
     }
-    if (lane == 0) bulk_wait_all();
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -397,10 +424,14 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
 // leave sums and maxima in the workspace and are joined by ecco_paged_combine_kernel.
 // Bound by memory: 512 bytes per token and KV head.
 // ---------------------------------------------------------------------------------------------
-constexpr int kFewStages = 2;
-template <int kM> constexpr int kFewWarps = kM == 1 ? 6 : 5;
-template <int kM> constexpr uint32_t kFewWarpBytes = kFewStages * 2 * kKvTileBytes + kM * 4096;
-template <int kM> constexpr uint32_t kFewSmemBytes = kFewWarps<kM> * kFewWarpBytes<kM> + 1024;
+constexpr int kFewRows = 16, kFewStages = 2, kFewWarps = 6;
+constexpr uint32_t kFewWarpBytes = kFewStages * 2 * kKvTileBytes + kFewRows * 256, kFewSmemBytes = kFewWarps * kFewWarpBytes + 1024;
+// Runs of the line: one per warp, but none shorter than this many tiles, or the joining costs more than the waiting.
+constexpr int kFewRunTiles = 3;
+__device__ __forceinline__ UnitSplit few_split(int64_t units, int ctas)
+{
+    return UnitSplit(units, static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(ctas) * kFewWarps, units / kFewRunTiles))));
+}
 
 // Weights enter the tensor cores times 2^15: taken as they are, those below 6e-5 would lose bits and those below 3e-8 vanish.
 constexpr float kWeightLog2 = 15.0f;
@@ -436,26 +467,24 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
     return done;
 }
 
-template <int kM>
-__global__ void __launch_bounds__(kFewWarps<kM> * 32, 1)
+__global__ void __launch_bounds__(kFewWarps * 32, 1)
 ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     constexpr unsigned full = 0xffffffffu;
-    constexpr int kRows = 16 * kM;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t mine = smem_u32(smem) + 1024 + warp * kFewWarpBytes<kM>, q_at = mine + kFewStages * 2 * kKvTileBytes;
+    const uint32_t mine = smem_u32(smem) + 1024 + warp * kFewWarpBytes, q_at = mine + kFewStages * 2 * kKvTileBytes;
     const uint32_t bar = smem_u32(smem) + warp * kFewStages * 8;
     if (lane == 0)
         for (int s = 0; s < kFewStages; ++s) mbar_init(bar + s * 8, 1);
     __syncwarp();
     dependency_wait();
-    release_dependents();                                  // behind the wait: see ecco_paged_combine_kernel
+    release_dependents();                                  // behind the wait: see ecco_paged_join_kernel
     const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);
-    const int W = static_cast<int>(gridDim.x) * kFewWarps<kM>, wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
+    const int wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
     const int64_t U = static_cast<int64_t>(line) * kv.heads;
-    const UnitSplit split(U, W);
-    const int64_t u0 = split.begin(wg), u1 = split.begin(wg + 1);
+    const UnitSplit split = few_split(U, static_cast<int>(gridDim.x));
+    const int64_t u0 = min(split.begin(wg), U), u1 = min(split.begin(wg + 1), U);     // warps beyond the runs: nothing
 
     // a place in the run: unit u is tile `tile` of head `head`; the request it belongs to has units [begin, end), cut to the run's end
     struct Place { int64_t u, begin, end; int32_t head, tile; PagedReq q; };
@@ -492,12 +521,12 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     bool ok = true;
     while (ok && at.u < u1) {
         const PagedReq q = at.q;
-        const int R = min(q.rows * o.q_per_kv, kRows);
+        const int R = min(q.rows * o.q_per_kv, kFewRows);
         const bool whole = at.u == at.begin && at.end - at.u == q.tiles;
         const int slot = 2 * wg + (at.u == u0 ? 0 : 1);
         // the rows of q as tiles: rows beyond the last are zero
         __syncwarp();
-        for (uint32_t c = lane; c < kRows * 16; c += 32) {
+        for (uint32_t c = lane; c < kFewRows * 16; c += 32) {
             const uint32_t row = c >> 4, chunk = c & 15u;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
             if (static_cast<int>(row) < R) {
@@ -507,23 +536,19 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
             sts_v4(q_at + (row >> 4) * 4096 + (chunk >> 1) * 512 + tile_byte(row & 15u, (chunk & 1u) * 8), v.x, v.y, v.z, v.w);
         }
         __syncwarp();
-        float acc[kM][16][4], m[kM][2], l[kM][2];
-        int32_t seen[kM][2];
+        float acc[16][4], m[2], l[2];
+        int32_t seen[2];
 #pragma unroll
-        for (int t = 0; t < kM; ++t)
+        for (int i = 0; i < 2; ++i) {
+            const int row = static_cast<int>(lane >> 2) + 8 * i;
+            seen[i] = row < R ? tokens_seen(q, row / o.q_per_kv, o.causal) : 0;
+            m[i] = -INFINITY;
+            l[i] = 0.0f;
+        }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int row = t * 16 + static_cast<int>(lane >> 2) + 8 * i;
-                seen[t][i] = row < R ? tokens_seen(q, row / o.q_per_kv, o.causal) : 0;
-                m[t][i] = -INFINITY;
-                l[t][i] = 0.0f;
-            }
+        for (int n = 0; n < 16; ++n)
 #pragma unroll
-        for (int t = 0; t < kM; ++t)
-#pragma unroll
-            for (int n = 0; n < 16; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.0f;
+            for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
 
         for (; at.u < at.end; ++at.u, ++at.tile) {
             const uint32_t s = taken % kFewStages, k_tile = mine + s * 2 * kKvTileBytes, v_tile = k_tile + kKvTileBytes;
@@ -531,13 +556,11 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
             if (!ok) break;
             ++taken;
             // scores: rows x 8 tokens per fragment
-            float sc[kM][4][4];
+            float s4[4][4];
 #pragma unroll
-            for (int t = 0; t < kM; ++t)
+            for (int n = 0; n < 4; ++n)
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[t][n][i] = 0.0f;
+                for (int i = 0; i < 4; ++i) s4[n][i] = 0.0f;
             const uint32_t k_at = k_tile + tile_byte((lane & 7u) + ((lane >> 4) & 1u) * 8, ((lane >> 3) & 1u) * 8);
             const uint32_t a_at = q_at + tile_byte((lane & 7u) + ((lane >> 3) & 1u) * 8, (lane >> 4) * 8);
 #pragma unroll
@@ -545,54 +568,48 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
                 uint32_t b[2][4];
                 ldmatrix_x4(b[0], k_at + d * kPieceBytes);
                 ldmatrix_x4(b[1], k_at + d * kPieceBytes + 512);
+                uint32_t a[4];
+                ldmatrix_x4(a, a_at + d * 512);
 #pragma unroll
-                for (int t = 0; t < kM; ++t) {
-                    uint32_t a[4];
-                    ldmatrix_x4(a, a_at + t * 4096 + d * 512);
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) mma_16816(sc[t][n], a, b[n >> 1][(n & 1) * 2], b[n >> 1][(n & 1) * 2 + 1]);
-                }
+                for (int n = 0; n < 4; ++n) mma_16816(s4[n], a, b[n >> 1][(n & 1) * 2], b[n >> 1][(n & 1) * 2 + 1]);
             }
             // softmax: relative to the largest score so far
             const int32_t t0 = (at.tile - q.first) * 32 + static_cast<int32_t>(col);
-            uint32_t p[kM][2][4];                          // A fragments of 16 tokens each
+            uint32_t p[2][4];                              // A fragments of 16 tokens each
 #pragma unroll
-            for (int t = 0; t < kM; ++t) {
+            for (int i = 0; i < 2; ++i) {
+                float top = m[i];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float top = m[t][i];
+                for (int n = 0; n < 4; ++n)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float& x = sc[t][n][2 * i + e];
-                            x = t0 + n * 8 + e < seen[t][i] ? x * o.scale_log2 : -INFINITY;
-                            top = fmaxf(top, x);
-                        }
-                    top = fmaxf(top, __shfl_xor_sync(full, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(full, top, 2));
-                    const float base = top == -INFINITY ? 0.0f : top;          // a row that has seen nothing: all weights zero
-                    const float f = exp2_fast(m[t][i] - base);
-                    if (__any_sync(full, top > m[t][i])) {
-                        l[t][i] *= f;
-#pragma unroll
-                        for (int n = 0; n < 16; ++n) { acc[t][n][2 * i] *= f; acc[t][n][2 * i + 1] *= f; }
+                    for (int e = 0; e < 2; ++e) {
+                        float& x = s4[n][2 * i + e];
+                        x = t0 + n * 8 + e < seen[i] ? x * o.scale_log2 : -INFINITY;
+                        top = fmaxf(top, x);
                     }
-                    m[t][i] = top;
+                top = fmaxf(top, __shfl_xor_sync(full, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(full, top, 2));
+                const float base = top == -INFINITY ? 0.0f : top;              // a row that has seen nothing: all weights zero
+                if (__any_sync(full, top > m[i])) {
+                    const float f = exp2_fast(m[i] - base);
+                    l[i] *= f;
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float& x = sc[t][n][2 * i + e];
-                            x = exp2_fast(x - base + kWeightLog2);
-                            l[t][i] += x;
-                        }
+                    for (int n = 0; n < 16; ++n) { acc[n][2 * i] *= f; acc[n][2 * i + 1] *= f; }
                 }
+                m[i] = top;
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    p[t][n >> 1][(n & 1) * 2] = pack_h2(sc[t][n][0], sc[t][n][1]);
-                    p[t][n >> 1][(n & 1) * 2 + 1] = pack_h2(sc[t][n][2], sc[t][n][3]);
-                }
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float& x = s4[n][2 * i + e];
+                        x = exp2_fast(x - base + kWeightLog2);
+                        l[i] += x;
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                p[n >> 1][(n & 1) * 2] = pack_h2(s4[n][0], s4[n][1]);
+                p[n >> 1][(n & 1) * 2 + 1] = pack_h2(s4[n][2], s4[n][3]);
             }
             const uint32_t v_at = v_tile + tile_byte((lane & 7u) + ((lane >> 3) & 1u) * 8, (lane >> 4) * 8);
 #pragma unroll
@@ -601,80 +618,69 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
                 for (int ks = 0; ks < 2; ++ks) {
                     uint32_t b[4];
                     ldmatrix_x4_trans(b, v_at + d * kPieceBytes + ks * 512);
-#pragma unroll
-                    for (int t = 0; t < kM; ++t) {
-                        mma_16816(acc[t][2 * d], p[t][ks], b[0], b[1]);
-                        mma_16816(acc[t][2 * d + 1], p[t][ks], b[2], b[3]);
-                    }
+                    mma_16816(acc[2 * d], p[ks], b[0], b[1]);
+                    mma_16816(acc[2 * d + 1], p[ks], b[2], b[3]);
                 }
             __syncwarp();                                  // the whole warp has read the tile
             ask();
         }
         // out, or into a slot
 #pragma unroll
-        for (int t = 0; t < kM; ++t)
+        for (int i = 0; i < 2; ++i) {
+            float sum = l[i];
+            sum += __shfl_xor_sync(full, sum, 1);
+            sum += __shfl_xor_sync(full, sum, 2);
+            const int row = static_cast<int>(lane >> 2) + 8 * i;
+            if (row >= R || !ok) continue;
+            if (whole) {
+                const int token = row / o.q_per_kv, hq = (kv.head0 + at.head) * o.q_per_kv + row - token * o.q_per_kv;
+                const int64_t at_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + hq;
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                uint32_t* const dst = reinterpret_cast<uint32_t*>(o.out + at_row * kGroup) + (lane & 3u);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float sum = l[t][i];
-                sum += __shfl_xor_sync(full, sum, 1);
-                sum += __shfl_xor_sync(full, sum, 2);
-                const int row = t * 16 + static_cast<int>(lane >> 2) + 8 * i;
-                if (row >= R || !ok) continue;
-                if (whole) {
-                    const int token = row / o.q_per_kv, hq = (kv.head0 + at.head) * o.q_per_kv + row - token * o.q_per_kv;
-                    const int64_t at_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + hq;
-                    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-                    uint32_t* const dst = reinterpret_cast<uint32_t*>(o.out + at_row * kGroup) + (lane & 3u);
+                for (int n = 0; n < 16; ++n) dst[n * 4] = pack_h2(acc[n][2 * i] * inv, acc[n][2 * i + 1] * inv);
+                if (o.lse && (lane & 3u) == 0) o.lse[at_row] = lse_of(m[i], sum, kWeightLog2);
+            } else {
+                const int64_t at_row = static_cast<int64_t>(slot) * kFewRows + row;
+                float2* const dst = reinterpret_cast<float2*>(o.part + at_row * kGroup) + (lane & 3u);
 #pragma unroll
-                    for (int n = 0; n < 16; ++n) dst[n * 4] = pack_h2(acc[t][n][2 * i] * inv, acc[t][n][2 * i + 1] * inv);
-                    if (o.lse && (lane & 3u) == 0) o.lse[at_row] = lse_of(m[t][i], sum, kWeightLog2);
-                } else {
-                    const int64_t at_row = static_cast<int64_t>(slot) * kRows + row;
-                    float2* const dst = reinterpret_cast<float2*>(o.part + at_row * kGroup) + (lane & 3u);
-#pragma unroll
-                    for (int n = 0; n < 16; ++n) dst[n * 4] = make_float2(acc[t][n][2 * i], acc[t][n][2 * i + 1]);
-                    if ((lane & 3u) == 0) o.part_ml[at_row] = make_float2(m[t][i], sum);
-                }
+                for (int n = 0; n < 16; ++n) dst[n * 4] = make_float2(acc[n][2 * i], acc[n][2 * i + 1]);
+                if ((lane & 3u) == 0) o.part_ml[at_row] = make_float2(m[i], sum);
             }
+        }
         if (ok) seek(at);
     }
     if (!ok)                                               // tiles on their way land before the warp leaves
         for (; taken < asked; ++taken) warp_wait(bar + (taken % kFewStages) * 8, (taken / kFewStages) & 1u);
 }
 
-// adds a piece's sums v, with maximum and sum of weights x, to those at hand
+// adds a piece's sums v, with maximum and sum of weights x, to those at hand; a piece that has seen nothing has sums of zero
 __device__ __forceinline__ void join_sums(float& m, float& l, float4& acc, float2 x, float4 v)
 {
-    if (x.y == 0.0f) return;                               // nothing seen there
-    const float top = fmaxf(m, x.x), f0 = exp2_fast(m - top), f1 = exp2_fast(x.x - top);
+    const float top = fmaxf(m, x.y == 0.0f ? -INFINITY : x.x), base = top == -INFINITY ? 0.0f : top;
+    const float f0 = exp2_fast(m - base), f1 = x.y == 0.0f ? 0.0f : exp2_fast(x.x - base);
     l = l * f0 + x.y * f1;
     acc = make_float4(acc.x * f0 + v.x * f1, acc.y * f0 + v.y * f1, acc.z * f0 + v.z * f1, acc.w * f0 + v.w * f1);
     m = top;
 }
-// Joins the pieces of requests that were cut.
-//   by_rows == 0   CTA c looks at the cut in front of run c + 1, and if it is the first one of its request (and head), a warp joins a row:
+// Joins the pieces of a request of few rows that was cut, part of ecco_paged_join_kernel (see there for the waits).
+//   by_rows == 0   item c looks at the cut in front of run c + 1, and if it is the first one of its request (and head), a warp joins a row:
 //                  many requests, few pieces each
-//   by_rows > 0    a CTA to a (request, head, row < by_rows), its eight warps share the pieces: few requests, many pieces each
-// What it reads before its wait is older than ecco_paged_few_kernel, which lets it begin only when it has itself waited.
-template <int kM>
-__global__ void __launch_bounds__(256, 4)
-ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int few_ctas, int by_rows)
+//   by_rows > 0    an item to a (request, head, row < by_rows), the CTA's eight warps share the pieces: few requests, many pieces each
+__device__ __forceinline__ void join_few(const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, int item, int few_ctas, int by_rows, float4 (*sums)[32], float2* ml)
 {
-    __shared__ float4 sums[8][32];
-    __shared__ float2 ml[8];
     const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
-    release_dependents();
     const int32_t line = __ldcg(sc.few_tiles + kv.n_req);
     const int64_t U = static_cast<int64_t>(line) * kv.heads;
-    const UnitSplit split(U, few_ctas * kFewWarps<kM>);
+    const UnitSplit split = few_split(U, few_ctas);
     int head, r, row = warp;
     int64_t cut = 0;
     if (by_rows) {
-        row = static_cast<int>(blockIdx.x) % by_rows;
-        head = static_cast<int>(blockIdx.x) / by_rows % kv.heads;
-        r = static_cast<int>(blockIdx.x) / by_rows / kv.heads;
+        row = item % by_rows;
+        head = item / by_rows % kv.heads;
+        r = item / by_rows / kv.heads;
     } else {
-        cut = split.begin(static_cast<int>(blockIdx.x) + 1);
+        cut = split.begin(item + 1);
         if (cut >= U) { dependency_wait(); return; }
         head = static_cast<int>(divide(static_cast<uint64_t>(cut), static_cast<uint64_t>(line)));
         r = warp_find(sc.few_tiles, kv.n_req, static_cast<int32_t>(cut - static_cast<int64_t>(head) * line));
@@ -682,15 +688,15 @@ ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_const
     const int32_t at0 = __ldcg(sc.few_tiles + r);
     const int64_t first = static_cast<int64_t>(head) * line + at0, end = first + __ldcg(sc.few_tiles + r + 1) - at0;
     const PagedReq q = paged_req(kv, r, paged_tiles(kv));
-    const int R = min(q.rows * o.q_per_kv, 16 * kM);
+    const int R = min(q.rows * o.q_per_kv, kFewRows);
     bool joins = end > first && row < R;
     int w_lo = 0, w_hi = 0;
     if (by_rows) {
         if (joins) { w_lo = split.owner(first); w_hi = split.owner(end - 1); }
         joins = w_hi > w_lo;
     } else {
-        w_lo = static_cast<int>(blockIdx.x);
-        joins = first < cut && split.begin(w_lo) <= first;
+        w_lo = item;
+        joins = joins && first < cut && split.begin(w_lo) <= first;
         if (joins) w_hi = split.owner(end - 1);
     }
     const bool second = joins && split.begin(w_lo) != first;           // the piece in run w_lo is in its second slot
@@ -702,7 +708,7 @@ ecco_paged_combine_kernel(const __grid_constant__ PagedKv kv, const __grid_const
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
         for (int w = w_lo + (by_rows ? warp : 0); w <= w_hi; w += step) {
-            const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && second ? 1 : 0)) * (16 * kM) + row;
+            const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && second ? 1 : 0)) * kFewRows + row;
             const float2 x = __ldcg(o.part_ml + at);
             const float4 v = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
             join_sums(m, l, acc, x, v);

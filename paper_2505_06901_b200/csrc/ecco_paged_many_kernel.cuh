@@ -478,15 +478,12 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
-// Joins the pieces of blocks that were cut: CTA (c, part) looks at the cut in front of run c, and if it is its block's first one
-// joins sixteen of the block's rows, a warp to a row.  What it reads before its wait is older than ecco_paged_many_kernel, which lets it begin
-// only when it has itself waited for the kernels before it.
+// Joins the pieces of blocks that were cut: item (c, part) looks at the cut in front of run c, and if it is its block's first one
+// joins sixteen of the block's rows, a warp to a row.
 constexpr int kJoinRows = 16, kJoinParts = kManyRows / kJoinRows;
-__global__ void __launch_bounds__(256)
-ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int many_ctas)
+__device__ __forceinline__ void join_many(const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, int item, int many_ctas)
 {
-    release_dependents();
-    const int c = static_cast<int>(blockIdx.x) / kJoinParts + 1, part = static_cast<int>(blockIdx.x) % kJoinParts;
+    const int c = item / kJoinParts + 1, part = item % kJoinParts;
     const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
     const int32_t n_blocks = __ldcg(sc.n_blocks), total = n_blocks > 0 ? __ldcg(sc.block_tiles + n_blocks) : 0;
     const int64_t U = static_cast<int64_t>(total) * kv.heads;
@@ -518,6 +515,20 @@ ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         reinterpret_cast<uint2*>(o.out + out_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
         if (o.lse && lane == 0) o.lse[out_row] = lse_of(m, l, kManyWeightLog2);
     }
+}
+
+// Joins what the attention kernels have cut: few_items CTAs for the requests of few rows, the others for blocks.  What it reads before its
+// wait is older than the kernel in front of it, which lets it begin only when it has itself waited for the kernels before.
+__global__ void __launch_bounds__(256, 4)
+ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedOut many, const __grid_constant__ PagedSchedule sc,
+                       int few_items, int few_ctas, int by_rows, int many_ctas)
+{
+    __shared__ float4 sums[8][32];
+    __shared__ float2 ml[8];
+    release_dependents();
+    const int item = static_cast<int>(blockIdx.x);
+    if (item < few_items) join_few(kv, o, sc, item, few_ctas, by_rows, sums, ml);
+    else join_many(kv, many, sc, item - few_items, many_ctas);
 }
 
 }  // namespace
