@@ -762,11 +762,11 @@ namespace {
 // Tiles per warp (of each kind) from which on every CTA decodes both kinds.
 constexpr int kStageBothTiles = 3;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
-//   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks | few rows: sums, maxima | many rows: sums, maxima
+//   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks, tickets | few rows: sums, maxima | many rows: sums, maxima
 struct PagedAttnPlan {
     bool many;                         // there may be requests of more than kFewRows rows
     int few_ctas, many_ctas, max_blocks;
-    size_t few_tiles, block_tiles, blocks, n_blocks, few_part, few_ml, many_part, many_ml, bytes;
+    size_t few_tiles, block_tiles, blocks, n_blocks, tickets, few_part, few_ml, many_part, many_ml, bytes;
 };
 PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, int ctas_max)
 {
@@ -788,6 +788,7 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
     p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
     p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
     p.n_blocks = take(4);
+    p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
     p.few_part = take(few_slots * kGroup * sizeof(float));
     p.few_ml = take(few_slots * sizeof(float2));
     p.many_part = take(many_slots * kGroup * sizeof(float));
@@ -806,16 +807,6 @@ bool paged_batch_fine(const ecco_paged_cache& c, const ecco_paged_batch& b, int 
     return blocks * (static_cast<int64_t>(b.max_kv) / kManyTokens + 1) <= INT32_MAX;
 }
 
-int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
-{
-    static thread_local bool configured[64] = {};
-    if (!configured[di.device]) {
-        const int rc = set_smem(ecco_paged_few_kernel, kFewSmemBytes);
-        if (rc) return rc;
-        configured[di.device] = true;
-    }
-    return launch_overlapped(ecco_paged_few_kernel, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps * 32), kFewSmemBytes, s, kv, o, sc);
-}
 // the tiles of a workspace as [piece][tile][1 KB]: a box of eight pieces of four tiles is a K or V operand of 128 tokens
 bool make_tile_map(CUtensorMap* map, const PagedKv& kv)
 {
@@ -852,15 +843,20 @@ int launch_paged_many(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o
     }
     return launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc, map, q_map);
 }
-int launch_paged_join(const PagedKv& kv, const PagedOut& few, const PagedOut& many, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
+int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
 {
+    static thread_local bool configured[64] = {};
+    if (!configured[di.device]) {
+        const int rc = set_smem(ecco_paged_few_kernel, kFewSmemBytes);
+        if (rc) return rc;
+        configured[di.device] = true;
+    }
+    const int rc = launch_overlapped(ecco_paged_few_kernel, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps * 32), kFewSmemBytes, s, kv, o, sc);
+    if (rc) return rc;
     const int64_t runs = static_cast<int64_t>(p.few_ctas) * kFewWarps, segments = static_cast<int64_t>(kv.n_req) * kv.heads;
     // by how many pieces a request of average length is cut into
-    const int64_t by_rows = runs / segments > 16 ? std::min<int64_t>(kFewRows, static_cast<int64_t>(kv.max_new) * few.q_per_kv) : 0;
-    const int64_t few_items = by_rows ? segments * by_rows : runs - 1, many_items = p.many ? static_cast<int64_t>(p.many_ctas - 1) * kJoinParts : 0;
-    if (few_items + many_items == 0) return ECCO_OK;
-    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(few_items + many_items), 256u, 0, s, kv, few, many, sc, static_cast<int>(few_items), p.few_ctas,
-                             static_cast<int>(by_rows), p.many_ctas);
+    const int64_t by_rows = runs / segments > 16 ? std::min<int64_t>(kFewRows, static_cast<int64_t>(kv.max_new) * o.q_per_kv) : 0;
+    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(by_rows ? segments * by_rows : runs - 1), 256u, 0, s, kv, o, sc, p.few_ctas, static_cast<int>(by_rows));
 }
 }  // namespace
 
@@ -924,6 +920,8 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         sc.n_blocks = reinterpret_cast<int32_t*>(kv.staged + p.n_blocks);
         sc.max_blocks = p.max_blocks;
         sc.few_rows = kFewRows;
+        sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
+        sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
         // both kinds one after the other in every CTA where a warp has several tiles of each; else half of the CTAs for K, half for V
         const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
         const bool both = units >= static_cast<int64_t>(kStageBothTiles) * 31 * di.sms;
@@ -933,16 +931,14 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         if (rc) return rc;
         o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
         o.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
-        rc = launch_paged_few(di, kv, o, sc, p, s);
-        if (rc) return rc;
-        PagedOut many = o;
         if (p.many) {
+            PagedOut many = o;
             many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
             many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
             rc = launch_paged_many(di, kv, many, sc, p, s);
             if (rc) return rc;
         }
-        rc = launch_paged_join(kv, o, many, sc, p, s);
+        rc = launch_paged_few(di, kv, o, sc, p, s);
         if (rc) return rc;
     }
     return ECCO_OK;

@@ -200,6 +200,8 @@ struct PagedSchedule {
     int2* blocks;              // [max_blocks]: request, block of the request
     int32_t* n_blocks;
     int32_t max_blocks, few_rows;
+    int32_t* tickets;          // [n_tickets]: zero when ecco_paged_many_kernel begins
+    int32_t n_tickets;
 };
 
 struct PagedOut {
@@ -240,6 +242,7 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
     };
     int32_t few = 0, tiles = 0, n_blocks = 0;
     if (lane == 0) { sc.few_tiles[0] = 0; sc.block_tiles[0] = 0; }
+    for (int i = lane; i < sc.n_tickets; i += 32) sc.tickets[i] = 0;
     for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
         const int r = r0 + lane;
         PagedReq q = {};
@@ -663,12 +666,18 @@ __device__ __forceinline__ void join_sums(float& m, float& l, float4& acc, float
     acc = make_float4(acc.x * f0 + v.x * f1, acc.y * f0 + v.y * f1, acc.z * f0 + v.z * f1, acc.w * f0 + v.w * f1);
     m = top;
 }
-// Joins the pieces of a request of few rows that was cut, part of ecco_paged_join_kernel (see there for the waits).
-//   by_rows == 0   item c looks at the cut in front of run c + 1, and if it is the first one of its request (and head), a warp joins a row:
+// Joins the pieces of requests that were cut.
+//   by_rows == 0   CTA c looks at the cut in front of run c + 1, and if it is the first one of its request (and head), a warp joins a row:
 //                  many requests, few pieces each
-//   by_rows > 0    an item to a (request, head, row < by_rows), the CTA's eight warps share the pieces: few requests, many pieces each
-__device__ __forceinline__ void join_few(const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, int item, int few_ctas, int by_rows, float4 (*sums)[32], float2* ml)
+//   by_rows > 0    a CTA to a (request, head, row < by_rows), its eight warps share the pieces: few requests, many pieces each
+// What it reads before its wait is older than ecco_paged_few_kernel, which lets it begin only when it has itself waited for the kernels before.
+__global__ void __launch_bounds__(256, 3)
+ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int few_ctas, int by_rows)
 {
+    __shared__ float4 sums[8][32];
+    __shared__ float2 ml[8];
+    release_dependents();
+    const int item = static_cast<int>(blockIdx.x);
     const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
     const int32_t line = __ldcg(sc.few_tiles + kv.n_req);
     const int64_t U = static_cast<int64_t>(line) * kv.heads;
@@ -706,12 +715,20 @@ __device__ __forceinline__ void join_few(const PagedKv& kv, const PagedOut& o, c
     for (; row < R; row += 8) {
         float m = -INFINITY, l = 0.0f;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int w = w_lo + (by_rows ? warp : 0); w <= w_hi; w += step) {
-            const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && second ? 1 : 0)) * kFewRows + row;
-            const float2 x = __ldcg(o.part_ml + at);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
-            join_sums(m, l, acc, x, v);
+#pragma unroll 1
+        for (int w0 = w_lo + (by_rows ? warp : 0); w0 <= w_hi; w0 += 8 * step) {            // eight pieces on their way together
+            float2 x[8];
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int w = min(w0 + k * step, w_hi);
+                const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && second ? 1 : 0)) * kFewRows + row;
+                x[k] = __ldcg(o.part_ml + at);
+                v[k] = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (w0 + k * step <= w_hi) join_sums(m, l, acc, x[k], v[k]);
         }
         if (by_rows) {
             sums[warp][lane] = acc;

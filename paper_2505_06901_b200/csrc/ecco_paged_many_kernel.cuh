@@ -16,8 +16,8 @@ namespace {
 // m is the row's maximum when it was last taken; a larger one is taken only when it is more than 2^8 larger (the weights are fp16
 // times 2^7, at most 2^15), so O is rescaled now and then instead of with every tile.
 //
-// All blocks' tiles of all heads form one line, which is cut into equal runs, one per CTA (see paged_schedule): a block that is cut leaves
-// its sums in the workspace and ecco_paged_join_kernel joins them.
+// All blocks' tiles of all heads form one line, which is cut into equal runs, one per CTA (see paged_schedule).  A block that is cut leaves
+// its sums in the workspace, and whoever comes last joins them, in the order of the runs.
 // ---------------------------------------------------------------------------------------------
 constexpr int kManyThreads = 384;
 constexpr uint32_t kOperandBytes = 8 * 4096;               // eight pieces of [128][16] fp16, 32-byte swizzle
@@ -172,7 +172,8 @@ struct ManyTask {
     int32_t from, to, tiles;   // of 128 tokens; of 32 tokens: the request's
     int32_t head, r_row0, r_rows, r_kv;   // KV head, the request's rows of q and tokens
     int32_t token;             // the tile's first new token of the request
-    int32_t whole, slot;       // the piece is its block; else: place of its sums
+    int32_t whole, slot;       // the piece is its block; else: place of its sums,
+    int32_t run_lo, run_hi, second;    // the runs that have pieces of the block; the first of them has it in its second slot
 };
 
 __global__ void __launch_bounds__(kManyThreads, 1)
@@ -187,7 +188,8 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     uint32_t* const tmem_word = reinterpret_cast<uint32_t*>(smem + 256);
     volatile int* const failed = reinterpret_cast<volatile int*>(smem + 264);
     ManyTask* const tasks = reinterpret_cast<ManyTask*>(smem + 320);       // [two pieces][tile of rows]
-    static_assert(320 + 4 * sizeof(ManyTask) <= 1024, "tasks fit");
+    static_assert(320 + 4 * sizeof(ManyTask) <= 1008, "tasks fit");
+    volatile int* const last_in = reinterpret_cast<volatile int*>(smem + 1008);          // [tile of rows]
     if (threadIdx.x == 0) {
         for (int i = 0; i < kManyStages; ++i) { mbar_init(full_at + 8 * i, 1); mbar_init(free_at + 8 * i, 1); }
         for (int x = 0; x < 2; ++x) { mbar_init(q_bar + 8 * x, 1); mbar_init(q_free + 8 * x, 5); mbar_init(s_bar + 8 * x, 1); mbar_init(p_bar + 8 * x, 4); mbar_init(p_bar + 16 + 8 * x, 4); mbar_init(o_bar + 8 * x, 1); }
@@ -354,6 +356,49 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 else o.part_ml[static_cast<int64_t>(pc.slot) * kManyRows + x * 128 + t] = make_float2(m, l);
             }
             tmem_fence_before();                           // O has been read before the next block's P arrives
+            if (!whole) {
+                // the tile's four warps count themselves in; the last run's read all pieces, a warp to a row
+                __threadfence();
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + x) : "memory");
+                if (t == 0) last_in[x] = atomicAdd(sc.tickets + 2 * pc.run_lo + x, 1) == pc.run_hi - pc.run_lo;
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + x) : "memory");
+                if (last_in[x]) {
+                    __threadfence();
+                    // eight rows at a time, so that their loads are on their way together
+                    const int n_rows = min(tile_rows_tokens(o.q_per_kv), pc.r_rows - pc.token) * o.q_per_kv;
+#pragma unroll 1
+                    for (int i0 = static_cast<int>(warp & 3u) * 8; i0 < n_rows; i0 += 32) {
+                        float jm[8], jl[8];
+                        float4 acc[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) { jm[k] = -INFINITY; jl[k] = 0.0f; acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+#pragma unroll 1
+                        for (int w = pc.run_lo; w <= pc.run_hi; ++w) {
+                            const int64_t at = (2 * static_cast<int64_t>(w) + (w == pc.run_lo ? pc.second : 0)) * kManyRows + x * 128 + i0;
+                            float2 ml[8];
+                            float4 v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const int64_t r = at + min(k, n_rows - 1 - i0);
+                                ml[k] = __ldcg(o.part_ml + r);
+                                v[k] = __ldcg(reinterpret_cast<const float4*>(o.part + r * kGroup) + lane);
+                            }
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) join_sums(jm[k], jl[k], acc[k], ml[k], v[k]);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (i0 + k >= n_rows) break;
+                            const int tile_token = (i0 + k) / o.q_per_kv, i_g = i0 + k - tile_token * o.q_per_kv;
+                            const int64_t to = static_cast<int64_t>(pc.r_row0 + pc.token + tile_token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + i_g;
+                            const float j_inv = jl[k] > 0.0f ? 1.0f / jl[k] : 0.0f;
+                            reinterpret_cast<uint2*>(o.out + to * kGroup)[lane] =
+                                make_uint2(pack_h2(acc[k].x * j_inv, acc[k].y * j_inv), pack_h2(acc[k].z * j_inv, acc[k].w * j_inv));
+                            if (o.lse && lane == 0) o.lse[to] = lse_of(jm[k], jl[k], kManyWeightLog2);
+                        }
+                    }
+                }
+            }
         }
     } else if (warp == 8) {
         // loads: K and V tiles in the order in which they are used
@@ -455,13 +500,15 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         for (int64_t u = u0; u < u1;) {
             const ManyPiece pc = many_piece(sc, n_blocks, total, u, u1);
             const PagedReq q = paged_req(kv, pc.r, T);
+            const int64_t first = u - pc.from;             // the block's first unit
+            const int run_lo = split.owner(first), run_hi = split.owner(first + pc.tiles - 1);
             if (n && !(wait(q_free, (n - 1) & 1u) && wait(q_free + 8, (n - 1) & 1u))) break;
             if (lane < 2) {                                // a lane to a tile of rows
                 const uint32_t x = lane, bar = q_bar + 8 * x;
                 const int32_t token = (2 * pc.block + static_cast<int32_t>(x)) * tokens;
                 const bool used = token < q.rows;
                 tasks[(n & 1u) * 2 + x] = ManyTask{used, pc.from, pc.to, q.tiles, pc.head, q.row0, q.rows, q.kv, token, pc.from == 0 && pc.to == pc.tiles,
-                                                   2 * static_cast<int>(blockIdx.x) + (u == u0 ? 0 : 1)};
+                                                   2 * static_cast<int>(blockIdx.x) + (u == u0 ? 0 : 1), run_lo, run_hi, split.begin(run_lo) != first};
                 mbar_expect_tx(bar, used ? 8 * 32 * tokens * o.q_per_kv : 0);
                 if (used)
                     for (int d = 0; d < 8; ++d)
@@ -476,59 +523,6 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     __syncthreads();
     tmem_fence_after();
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-}
-
-// Joins the pieces of blocks that were cut: item (c, part) looks at the cut in front of run c, and if it is its block's first one
-// joins sixteen of the block's rows, a warp to a row.
-constexpr int kJoinRows = 16, kJoinParts = kManyRows / kJoinRows;
-__device__ __forceinline__ void join_many(const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, int item, int many_ctas)
-{
-    const int c = item / kJoinParts + 1, part = item % kJoinParts;
-    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
-    const int32_t n_blocks = __ldcg(sc.n_blocks), total = n_blocks > 0 ? __ldcg(sc.block_tiles + n_blocks) : 0;
-    const int64_t U = static_cast<int64_t>(total) * kv.heads;
-    const UnitSplit split(U, many_ctas);
-    const int64_t cut = split.begin(c);
-    if (cut >= U) { dependency_wait(); return; }
-    const ManyPiece pc = many_piece(sc, n_blocks, total, cut, U);
-    const int64_t first = cut - pc.from, end = first + pc.tiles;
-    if (pc.from == 0 || split.begin(c - 1) > first) { dependency_wait(); return; }        // not inside of a block, or not its first cut
-    const int w_lo = c - 1, w_hi = split.owner(end - 1);
-    const bool second = split.begin(w_lo) != first;        // the piece in run w_lo is in its second slot
-    const PagedReq q = paged_req(kv, pc.r, paged_tiles(kv));
-    dependency_wait();
-#pragma unroll
-    for (int i = warp; i < kJoinRows; i += 8) {
-        const int in_block = part * kJoinRows + i, t = in_block & 127, in_tile = t / o.q_per_kv, g = t - in_tile * o.q_per_kv;
-        const int32_t tokens = tile_rows_tokens(o.q_per_kv), token = (2 * pc.block + (in_block >> 7)) * tokens + in_tile;
-        if (in_tile >= tokens || token >= q.rows) continue;
-        float m = -INFINITY, l = 0.0f;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int w = w_lo; w <= w_hi; ++w) {
-            const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && second ? 1 : 0)) * kManyRows + in_block;
-            const float2 x = __ldcg(o.part_ml + at);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
-            join_sums(m, l, acc, x, v);
-        }
-        const int64_t out_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + g;
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        reinterpret_cast<uint2*>(o.out + out_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
-        if (o.lse && lane == 0) o.lse[out_row] = lse_of(m, l, kManyWeightLog2);
-    }
-}
-
-// Joins what the attention kernels have cut: few_items CTAs for the requests of few rows, the others for blocks.  What it reads before its
-// wait is older than the kernel in front of it, which lets it begin only when it has itself waited for the kernels before.
-__global__ void __launch_bounds__(256, 4)
-ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedOut many, const __grid_constant__ PagedSchedule sc,
-                       int few_items, int few_ctas, int by_rows, int many_ctas)
-{
-    __shared__ float4 sums[8][32];
-    __shared__ float2 ml[8];
-    release_dependents();
-    const int item = static_cast<int>(blockIdx.x);
-    if (item < few_items) join_few(kv, o, sc, item, few_ctas, by_rows, sums, ml);
-    else join_many(kv, many, sc, item - few_items, many_ctas);
 }
 
 }  // namespace
