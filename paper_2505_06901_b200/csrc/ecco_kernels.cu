@@ -762,11 +762,11 @@ namespace {
 // Tiles per warp (of each kind) from which on every CTA decodes both kinds.
 constexpr int kStageBothTiles = 3;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
-//   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks, tickets | few rows: sums, maxima | many rows: sums, maxima
+//   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks, tickets, cuts | few rows: sums, maxima | many rows: sums, maxima
 struct PagedAttnPlan {
     bool many;                         // there may be requests of more than kFewRows rows
     int few_ctas, many_ctas, max_blocks;
-    size_t few_tiles, block_tiles, blocks, n_blocks, tickets, few_part, few_ml, many_part, many_ml, bytes;
+    size_t few_tiles, block_tiles, blocks, n_blocks, tickets, cuts, few_part, few_ml, many_part, many_ml, bytes;
 };
 PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, int ctas_max)
 {
@@ -789,6 +789,7 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
     p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
     p.n_blocks = take(4);
     p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
+    p.cuts = take(static_cast<size_t>(p.few_ctas) * kFewWarps * sizeof(FewCut));
     p.few_part = take(few_slots * kGroup * sizeof(float));
     p.few_ml = take(few_slots * sizeof(float2));
     p.many_part = take(many_slots * kGroup * sizeof(float));
@@ -853,10 +854,8 @@ int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o,
     }
     const int rc = launch_overlapped(ecco_paged_few_kernel, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps * 32), kFewSmemBytes, s, kv, o, sc);
     if (rc) return rc;
-    const int64_t runs = static_cast<int64_t>(p.few_ctas) * kFewWarps, segments = static_cast<int64_t>(kv.n_req) * kv.heads;
-    // by how many pieces a request of average length is cut into
-    const int64_t by_rows = runs / segments > 16 ? std::min<int64_t>(kFewRows, static_cast<int64_t>(kv.max_new) * o.q_per_kv) : 0;
-    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(by_rows ? segments * by_rows : runs - 1), 256u, 0, s, kv, o, sc, p.few_ctas, static_cast<int>(by_rows));
+    const int runs = p.few_ctas * kFewWarps;
+    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(runs), 256u, 0, s, o, kv.head0);
 }
 }  // namespace
 
@@ -931,6 +930,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         if (rc) return rc;
         o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
         o.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
+        o.cuts = reinterpret_cast<FewCut*>(kv.staged + p.cuts);
         if (p.many) {
             PagedOut many = o;
             many.part = reinterpret_cast<float*>(kv.staged + p.many_part);

@@ -204,6 +204,9 @@ struct PagedSchedule {
     int32_t n_tickets;
 };
 
+// A request of few rows that begins in a run and goes on in the next ones, as ecco_paged_join_kernel needs it: rows (0: there is none), KV
+// head, first row of q, place of the first piece, run of the last one.
+struct alignas(16) FewCut { int32_t rows, head, row0, slot, last_run, unused[3]; };
 struct PagedOut {
     const __half* q;
     int64_t q_stride;
@@ -213,6 +216,7 @@ struct PagedOut {
     float* lse;                // or NULL
     float* part;               // partial sums [slot][rows][128]
     float2* part_ml;           // maxima (log2) and sums of weights [slot][rows]
+    FewCut* cuts;              // [run]
 };
 // tokens that row i of a request sees
 __device__ __forceinline__ int32_t tokens_seen(const PagedReq& q, int32_t token, bool causal)
@@ -482,7 +486,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         for (int s = 0; s < kFewStages; ++s) mbar_init(bar + s * 8, 1);
     __syncwarp();
     dependency_wait();
-    release_dependents();                                  // behind the wait: see ecco_paged_join_kernel
+    release_dependents();
     const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);
     const int wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
     const int64_t U = static_cast<int64_t>(line) * kv.heads;
@@ -521,23 +525,27 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     for (int s = 0; s < kFewStages; ++s) ask();
 
     const uint32_t col = (lane & 3u) * 2;
+    FewCut cut = {};                                       // at most one request begins here and goes on in the next run
     bool ok = true;
     while (ok && at.u < u1) {
         const PagedReq q = at.q;
         const int R = min(q.rows * o.q_per_kv, kFewRows);
         const bool whole = at.u == at.begin && at.end - at.u == q.tiles;
+        const bool starts = at.u == at.begin;              // the request begins in this run
         const int slot = 2 * wg + (at.u == u0 ? 0 : 1);
+        if (starts && !whole) cut = FewCut{R, at.head, q.row0, slot, split.owner(at.begin + q.tiles - 1), {0, 0, 0}};
         // the rows of q as tiles: rows beyond the last are zero
         __syncwarp();
-        for (uint32_t c = lane; c < kFewRows * 16; c += 32) {
-            const uint32_t row = c >> 4, chunk = c & 15u;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (static_cast<int>(row) < R) {
-                const uint32_t i = row / o.q_per_kv, g = row - i * o.q_per_kv;
-                v = __ldcg(reinterpret_cast<const uint4*>(o.q + (q.row0 + i) * o.q_stride + (static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + g) * kGroup) + chunk);
-            }
-            sts_v4(q_at + (row >> 4) * 4096 + (chunk >> 1) * 512 + tile_byte(row & 15u, (chunk & 1u) * 8), v.x, v.y, v.z, v.w);
+        uint4 rows[8];                                     // sixteen lanes to a row, two rows at a time, all on their way together
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = 2 * i + static_cast<int>(lane >> 4), token = row / o.q_per_kv, g = row - token * o.q_per_kv;
+            rows[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (row < R) rows[i] = __ldcg(reinterpret_cast<const uint4*>(o.q + (q.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + g) * kGroup) + (lane & 15u));
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            sts_v4(q_at + ((lane & 15u) >> 1) * 512 + tile_byte(2 * i + (lane >> 4), (lane & 1u) * 8), rows[i].x, rows[i].y, rows[i].z, rows[i].w);
         __syncwarp();
         float acc[16][4], m[2], l[2];
         int32_t seen[2];
@@ -653,6 +661,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         }
         if (ok) seek(at);
     }
+    if (lane == 0) o.cuts[wg] = ok ? cut : FewCut{};
     if (!ok)                                               // tiles on their way land before the warp leaves
         for (; taken < asked; ++taken) warp_wait(bar + (taken % kFewStages) * 8, (taken / kFewStages) & 1u);
 }
@@ -666,83 +675,54 @@ __device__ __forceinline__ void join_sums(float& m, float& l, float4& acc, float
     acc = make_float4(acc.x * f0 + v.x * f1, acc.y * f0 + v.y * f1, acc.z * f0 + v.z * f1, acc.w * f0 + v.w * f1);
     m = top;
 }
-// Joins the pieces of requests that were cut.
-//   by_rows == 0   CTA c looks at the cut in front of run c + 1, and if it is the first one of its request (and head), a warp joins a row:
-//                  many requests, few pieces each
-//   by_rows > 0    a CTA to a (request, head, row < by_rows), its eight warps share the pieces: few requests, many pieces each
-// What it reads before its wait is older than ecco_paged_few_kernel, which lets it begin only when it has itself waited for the kernels before.
+// Joins the pieces of the request that begins in run blockIdx.x and goes on in the next ones, if there is one.  A row has as many warps as
+// there are for it, and these share the pieces.
 __global__ void __launch_bounds__(256, 3)
-ecco_paged_join_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int few_ctas, int by_rows)
+ecco_paged_join_kernel(const __grid_constant__ PagedOut o, int32_t head0)
 {
     __shared__ float4 sums[8][32];
     __shared__ float2 ml[8];
-    release_dependents();
-    const int item = static_cast<int>(blockIdx.x);
     const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
-    const int32_t line = __ldcg(sc.few_tiles + kv.n_req);
-    const int64_t U = static_cast<int64_t>(line) * kv.heads;
-    const UnitSplit split = few_split(U, few_ctas);
-    int head, r, row = warp;
-    int64_t cut = 0;
-    if (by_rows) {
-        row = item % by_rows;
-        head = item / by_rows % kv.heads;
-        r = item / by_rows / kv.heads;
-    } else {
-        cut = split.begin(item + 1);
-        if (cut >= U) { dependency_wait(); return; }
-        head = static_cast<int>(divide(static_cast<uint64_t>(cut), static_cast<uint64_t>(line)));
-        r = warp_find(sc.few_tiles, kv.n_req, static_cast<int32_t>(cut - static_cast<int64_t>(head) * line));
-    }
-    const int32_t at0 = __ldcg(sc.few_tiles + r);
-    const int64_t first = static_cast<int64_t>(head) * line + at0, end = first + __ldcg(sc.few_tiles + r + 1) - at0;
-    const PagedReq q = paged_req(kv, r, paged_tiles(kv));
-    const int R = min(q.rows * o.q_per_kv, kFewRows);
-    bool joins = end > first && row < R;
-    int w_lo = 0, w_hi = 0;
-    if (by_rows) {
-        if (joins) { w_lo = split.owner(first); w_hi = split.owner(end - 1); }
-        joins = w_hi > w_lo;
-    } else {
-        w_lo = item;
-        joins = joins && first < cut && split.begin(w_lo) <= first;
-        if (joins) w_hi = split.owner(end - 1);
-    }
-    const bool second = joins && split.begin(w_lo) != first;           // the piece in run w_lo is in its second slot
+    release_dependents();
     dependency_wait();
-    if (!joins) return;                                    // by_rows: the whole CTA
-    const int step = by_rows ? 8 : 1;
-    for (; row < R; row += 8) {
+    const int4* const from = reinterpret_cast<const int4*>(o.cuts + blockIdx.x);
+    const int4 c0 = __ldcg(from), c1 = __ldcg(from + 1);
+    const int R = c0.x, head = c0.y, row0 = c0.z, w_lo = static_cast<int>(blockIdx.x), w_hi = c1.x;
+    const int team = R <= 1 ? 8 : R <= 2 ? 4 : R <= 4 ? 2 : 1, sub = warp % team;
+    for (int first = 0; first < R; first += 8 / team) {    // the same number of turns for all warps
+        const int row = first + warp / team;
         float m = -INFINITY, l = 0.0f;
         float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
-        for (int w0 = w_lo + (by_rows ? warp : 0); w0 <= w_hi; w0 += 8 * step) {            // eight pieces on their way together
+        for (int w0 = w_lo + sub; w0 <= w_hi && row < R; w0 += 8 * team) {           // eight pieces on their way together
             float2 x[8];
             float4 v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const int w = min(w0 + k * step, w_hi);
-                const int64_t at = (2 * static_cast<int64_t>(w) + (w == w_lo && second ? 1 : 0)) * kFewRows + row;
+                const int w = min(w0 + k * team, w_hi);
+                const int64_t at = static_cast<int64_t>(w == w_lo ? c0.w : 2 * w) * kFewRows + row;
                 x[k] = __ldcg(o.part_ml + at);
                 v[k] = __ldcg(reinterpret_cast<const float4*>(o.part + at * kGroup) + lane);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (w0 + k * step <= w_hi) join_sums(m, l, acc, x[k], v[k]);
+                if (w0 + k * team <= w_hi) join_sums(m, l, acc, x[k], v[k]);
         }
-        if (by_rows) {
+        if (team > 1) {
             sums[warp][lane] = acc;
             if (lane == 0) ml[warp] = make_float2(m, l);
             __syncthreads();
-            if (warp) return;
-            for (int w = 1; w < 8; ++w) join_sums(m, l, acc, ml[w], sums[w][lane]);
+            if (sub == 0)
+                for (int w = warp + 1; w < warp + team; ++w) join_sums(m, l, acc, ml[w], sums[w][lane]);
+            __syncthreads();
         }
-        const int token = row / o.q_per_kv, g = row - token * o.q_per_kv;
-        const int64_t at_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + (kv.head0 + head) * o.q_per_kv + g;
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        reinterpret_cast<uint2*>(o.out + at_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
-        if (o.lse && lane == 0) o.lse[at_row] = lse_of(m, l, kWeightLog2);
-        if (by_rows) return;
+        if (sub == 0 && row < R) {
+            const int token = row / o.q_per_kv, g = row - token * o.q_per_kv;
+            const int64_t at_row = static_cast<int64_t>(row0 + token) * o.q_heads + (head0 + head) * o.q_per_kv + g;
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            reinterpret_cast<uint2*>(o.out + at_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
+            if (o.lse && lane == 0) o.lse[at_row] = lse_of(m, l, kWeightLog2);
+        }
     }
 }
 
