@@ -737,6 +737,9 @@ extern "C" int ecco_paged_plan(int32_t page_size, int32_t n_pages, int32_t n_req
                              static_cast<cudaStream_t>(stream), p);
 }
 
+// Groups from which on K and V are compressed one after the other, each by all CTAs: they rarely take equally long, and half of the
+// CTAs would wait for the others.
+constexpr uint64_t kAppendTwoGroups = 65536;
 extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k, const void* d_v, int64_t token_stride, const int32_t* d_slots,
                                  int32_t n_tokens, void* stream)
 {
@@ -749,13 +752,19 @@ extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k,
     DeviceInfo di;
     rc = device_info(&di);
     if (rc) return rc;
-    PagedGroups g = {};
-    g.k_image = static_cast<const uint8_t*>(cache->d_k_meta); g.v_image = static_cast<const uint8_t*>(cache->d_v_meta);
-    g.k = static_cast<const __half*>(d_k); g.v = static_cast<const __half*>(d_v);
-    g.k_blocks = cache->d_k_blocks; g.v_blocks = cache->d_v_blocks;
-    g.slots = d_slots; g.token_stride = token_stride;
-    g.heads = cache->n_kv_heads; g.page_shift = page_shift_of(cache->page_size); g.n_slots = cache->n_pages * cache->page_size;
-    return launch_kv_compress(di, g, static_cast<uint64_t>(n_tokens) * cache->n_kv_heads, 2, static_cast<cudaStream_t>(stream));
+    const uint64_t n_groups = static_cast<uint64_t>(n_tokens) * cache->n_kv_heads;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    auto launch = [&](auto g, int kinds) {
+        g.k_image = static_cast<const uint8_t*>(cache->d_k_meta); g.v_image = static_cast<const uint8_t*>(cache->d_v_meta);
+        g.k = static_cast<const __half*>(d_k); g.v = static_cast<const __half*>(d_v);
+        g.k_blocks = cache->d_k_blocks; g.v_blocks = cache->d_v_blocks;
+        g.slots = d_slots; g.token_stride = token_stride;
+        g.heads = cache->n_kv_heads; g.page_shift = page_shift_of(cache->page_size); g.n_slots = cache->n_pages * cache->page_size;
+        return launch_kv_compress(di, g, n_groups, kinds, s);
+    };
+    if (n_groups < kAppendTwoGroups) return launch(PagedGroups<2>{}, 2);
+    rc = launch(PagedGroups<0>{}, 1);
+    return rc ? rc : launch(PagedGroups<1>{}, 1);
 }
 
 namespace {

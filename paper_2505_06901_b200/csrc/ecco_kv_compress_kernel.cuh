@@ -19,41 +19,48 @@
 // ---------------------------------------------------------------------------------------------
 namespace {
 
-// Where the groups of a call lie and where their blocks go.  cta of ctas: this CTA among those that share its groups.
+// Where the groups of a call lie and where their blocks go.  cta of ctas: this CTA among those that share its groups.  A place is what both
+// follow from.
 struct DenseGroups {                                       // one after the other
+    using Place = uint64_t;
     const uint8_t* image;
     const __half* x;
     uint8_t* blocks;
     __device__ __forceinline__ const uint8_t* meta() const { return image; }
     __device__ __forceinline__ uint32_t cta() const { return blockIdx.x; }
     __device__ __forceinline__ uint32_t ctas() const { return gridDim.x; }
-    __device__ __forceinline__ const __half* source(uint64_t g) const { return x + g * kGroup; }
-    __device__ __forceinline__ uint8_t* block(uint64_t g) const { return blocks + g * kBlockBytes; }
+    __device__ __forceinline__ Place place(uint64_t g) const { return g; }
+    __device__ __forceinline__ const __half* source(Place g) const { return x + g * kGroup; }
+    __device__ __forceinline__ uint8_t* block(Place g) const { return blocks + g * kBlockBytes; }
 };
-// New tokens of a paged cache: group g is head g % heads of token g / heads.  Even CTAs encode K, odd ones V.
+// New tokens of a paged cache: group g is head g % heads of token g / heads.  kKind 0: K, 1: V, 2: even CTAs K, odd ones V.
+template <int kKind>
 struct PagedGroups {
+    struct Place { uint32_t token, head; };
     const uint8_t *k_image, *v_image;
     const __half *k, *v;
     uint8_t *k_blocks, *v_blocks;
     const int32_t* slots;
     int64_t token_stride;
     int32_t heads, page_shift, n_slots;
-    __device__ __forceinline__ bool is_v() const { return blockIdx.x & 1u; }
+    __device__ __forceinline__ bool is_v() const { return kKind == 2 ? blockIdx.x & 1u : kKind; }
     __device__ __forceinline__ const uint8_t* meta() const { return is_v() ? v_image : k_image; }
-    __device__ __forceinline__ uint32_t cta() const { return blockIdx.x >> 1; }
-    __device__ __forceinline__ uint32_t ctas() const { return gridDim.x >> 1; }
-    __device__ __forceinline__ const __half* source(uint64_t g) const
+    __device__ __forceinline__ uint32_t cta() const { return kKind == 2 ? blockIdx.x >> 1 : blockIdx.x; }
+    __device__ __forceinline__ uint32_t ctas() const { return kKind == 2 ? gridDim.x >> 1 : gridDim.x; }
+    __device__ __forceinline__ Place place(uint64_t g) const
     {
-        const uint32_t token = static_cast<uint32_t>(divide(g, static_cast<uint64_t>(heads))), head = static_cast<uint32_t>(g - static_cast<uint64_t>(token) * heads);
-        return (is_v() ? v : k) + token * token_stride + head * kGroup;
+        Place p;
+        p.token = static_cast<uint32_t>(divide(g, static_cast<uint64_t>(heads)));
+        p.head = static_cast<uint32_t>(g - static_cast<uint64_t>(p.token) * heads);
+        return p;
     }
+    __device__ __forceinline__ const __half* source(Place p) const { return (is_v() ? v : k) + p.token * token_stride + p.head * kGroup; }
     // NULL: the token is left out
-    __device__ __forceinline__ uint8_t* block(uint64_t g) const
+    __device__ __forceinline__ uint8_t* block(Place p) const
     {
-        const uint32_t token = static_cast<uint32_t>(divide(g, static_cast<uint64_t>(heads))), head = static_cast<uint32_t>(g - static_cast<uint64_t>(token) * heads);
-        const int32_t slot = __ldcg(slots + token), page = slot >> page_shift;
+        const int32_t slot = __ldcg(slots + p.token), page = slot >> page_shift;
         if (slot < 0 || slot >= n_slots) return nullptr;
-        return (is_v() ? v_blocks : k_blocks) + (((static_cast<int64_t>(page) * heads + head) << page_shift) + (slot - (page << page_shift))) * kBlockBytes;
+        return (is_v() ? v_blocks : k_blocks) + (((static_cast<int64_t>(page) * heads + p.head) << page_shift) + (slot - (page << page_shift))) * kBlockBytes;
     }
 };
 
@@ -88,9 +95,10 @@ ecco_kv_compress_kernel(const __grid_constant__ Groups groups, uint64_t n_groups
     auto fp8 = [&](float v) { return static_cast<uint32_t>(__nv_cvt_float_to_fp8(v * invT, __NV_SATFINITE, __NV_E4M3)); };
 
     for (uint64_t g = static_cast<uint64_t>(groups.cta()) * kKvWarps + warp; g < n_groups; g += static_cast<uint64_t>(groups.ctas()) * kKvWarps) {
-        uint8_t* const block = groups.block(g);
+        const typename Groups::Place place = groups.place(g);
+        uint8_t* const block = groups.block(place);
         if (!block) continue;
-        const uint2 raw = __ldcg(reinterpret_cast<const uint2*>(groups.source(g)) + lane);
+        const uint2 raw = __ldcg(reinterpret_cast<const uint2*>(groups.source(place)) + lane);
         const uint32_t h16[4] = {raw.x & 0xffffu, raw.x >> 16, raw.y & 0xffffu, raw.y >> 16};
         float x[4];
         uint32_t key[4];                                   // |x| then low index first
@@ -367,9 +375,10 @@ ecco_kv_compress_many_kernel(const __grid_constant__ Groups groups, uint64_t n_g
     const uint64_t n_units = (n_groups + 3) / 4;
     for (uint64_t unit = static_cast<uint64_t>(warp) * groups.ctas() + groups.cta(); unit < n_units; unit += static_cast<uint64_t>(groups.ctas()) * kKvManyWarps) {
         const uint64_t g = min(unit * 4 + grp, n_groups - 1);            // past the end: the last group again, not stored
+        const typename Groups::Place place = groups.place(g);
         uint32_t h[8];                                     // x is 16-byte aligned: two loads
         {
-            const uint4* const src = reinterpret_cast<const uint4*>(groups.source(g) + sub * 16);
+            const uint4* const src = reinterpret_cast<const uint4*>(groups.source(place) + sub * 16);
             const uint4 a = __ldcg(src), b = __ldcg(src + 1);
             h[0] = a.x; h[1] = a.y; h[2] = a.z; h[3] = a.w; h[4] = b.x; h[5] = b.y; h[6] = b.z; h[7] = b.w;
         }
@@ -576,7 +585,7 @@ ecco_kv_compress_many_kernel(const __grid_constant__ Groups groups, uint64_t n_g
             }
         }
         __syncwarp();
-        uint8_t* const block = unit * 4 + grp < n_groups ? groups.block(g) : nullptr;
+        uint8_t* const block = unit * 4 + grp < n_groups ? groups.block(place) : nullptr;
         if (block) reinterpret_cast<uint2*>(block)[sub] = make_uint2(blk[sub * 2], blk[sub * 2 + 1]);
         __syncwarp();
     }
