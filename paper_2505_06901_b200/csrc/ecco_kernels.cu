@@ -785,7 +785,7 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
     p.few_ctas = std::max(1, spread_ctas(static_cast<int64_t>(b.max_tiles) * heads, ctas_max));
     p.many_ctas = ctas_max;
     p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
-    size_t at = static_cast<size_t>(b.max_tiles) * heads * 2 * kKvTileBytes;
+    size_t at = static_cast<size_t>(std::max(b.max_tiles, 1)) * heads * 2 * kKvTileBytes;          // one at least: the tensor map has to have some
     auto take = [&](size_t bytes) {
         const size_t here = at;
         at = (at + bytes + 255) & ~static_cast<size_t>(255);
@@ -884,7 +884,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     if (b.n_req == 0 || b.n_tokens == 0) return ECCO_OK;
     const int q_heads = cache->n_kv_heads * q_per_kv;
     if (!b.d_cu_new || !b.d_kv_lens || !b.d_kv_tiles || (b.table_stride && !b.d_block_tables) || !d_q || !d_out) return ECCO_ERR_INVALID_ARG;
-    if (q_stride < static_cast<int64_t>(q_heads) * kGroup) return ECCO_ERR_INVALID_ARG;
+    if (q_stride < static_cast<int64_t>(q_heads) * kGroup || q_stride >= 1ll << 38) return ECCO_ERR_INVALID_ARG;
     if (!aligned16(d_q) || q_stride % 8 || !aligned16(d_out) || !aligned_to(d_lse, 4)) return ECCO_ERR_ALIGNMENT;
     for (const int32_t* p : {b.d_block_tables, b.d_cu_new, b.d_kv_lens, b.d_kv_tiles})
         if (!aligned_to(p, 4)) return ECCO_ERR_ALIGNMENT;
@@ -902,7 +902,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     kv.k_blocks = cache->d_k_blocks; kv.v_blocks = cache->d_v_blocks;
     kv.tables = b.d_block_tables; kv.cu_new = b.d_cu_new; kv.kv_lens = b.d_kv_lens; kv.kv_tiles = b.d_kv_tiles;
     kv.n_pages = cache->n_pages; kv.page_shift = page_shift_of(cache->page_size); kv.all_heads = cache->n_kv_heads;
-    kv.stride = b.table_stride; kv.n_req = b.n_req; kv.n_tokens = b.n_tokens; kv.max_tiles = b.max_tiles;
+    kv.stride = b.table_stride; kv.n_req = b.n_req; kv.n_tokens = b.n_tokens; kv.max_tiles = std::max(b.max_tiles, 1);
     kv.max_new = b.max_new; kv.max_kv = b.max_kv;
     kv.staged = static_cast<uint8_t*>(d_workspace);
     PagedOut o = {};
@@ -910,6 +910,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     o.scale_log2 = scale * 1.4426950408889634f;
     o.q_per_kv = q_per_kv; o.q_heads = q_heads; o.causal = flags & ECCO_ATTN_CAUSAL;
     o.out = static_cast<__half*>(d_out); o.lse = d_lse;
+    o.discard = aligned_to(d_workspace, 128);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {

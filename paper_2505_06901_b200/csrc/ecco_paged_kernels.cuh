@@ -217,6 +217,7 @@ struct PagedOut {
     float* part;               // partial sums [slot][rows][128]
     float2* part_ml;           // maxima (log2) and sums of weights [slot][rows]
     FewCut* cuts;              // [run]
+    int32_t discard;           // the tiles begin at multiples of 128 bytes
 };
 // tokens that row i of a request sees
 __device__ __forceinline__ int32_t tokens_seen(const PagedReq& q, int32_t token, bool causal)
@@ -247,10 +248,13 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
     int32_t few = 0, tiles = 0, n_blocks = 0;
     if (lane == 0) { sc.few_tiles[0] = 0; sc.block_tiles[0] = 0; }
     for (int i = lane; i < sc.n_tickets; i += 32) sc.tickets[i] = 0;
+    PagedReq next = {};
+    if (lane < kv.n_req) next = paged_req(kv, lane, T);
     for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
         const int r = r0 + lane;
-        PagedReq q = {};
-        if (r < kv.n_req) q = paged_req(kv, r, T);
+        const PagedReq q = next;
+        next = {};
+        if (r + 32 < kv.n_req) next = paged_req(kv, r + 32, T);        // on their way while these are dealt with
         const int64_t rows = static_cast<int64_t>(q.rows) * q_per_kv;
         if (r < kv.n_req && (q.rows > kv.max_new || __ldcg(kv.kv_lens + r) != q.kv)) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
         const bool many = rows > sc.few_rows;
@@ -433,14 +437,14 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewRows = 16, kFewStages = 2, kFewWarps = 6;
 constexpr uint32_t kFewWarpBytes = kFewStages * 2 * kKvTileBytes + kFewRows * 256, kFewSmemBytes = kFewWarps * kFewWarpBytes + 1024;
-// Runs of the line: one per warp, but of at least three tiles once every SM has three of them, or joining costs more than waiting: 16
-// requests of 4 to 8 drafted tokens, 2048 tiles, 158 us with runs of two or three tiles, 145 with three; 2 requests of 780 tokens, 400 tiles,
-// 24.4 us with runs of three, 20.4 with runs of one.
+// Runs of the line: one per warp, but of three tiles, or joining costs more than waiting (16 requests of 4 to 8 drafted tokens, 2048 tiles: 158
+// us with runs of two or three tiles, 145 with three), unless there are so few tiles that every run has just one (2 requests of 780 tokens,
+// 400 tiles: 24.4 us with runs of three, 20.4 with runs of one).
 constexpr int kFewRunTiles = 3;
 __device__ __forceinline__ UnitSplit few_split(int64_t units, int ctas)
 {
-    const int64_t least = min(units, static_cast<int64_t>(ctas) * 3);
-    return UnitSplit(units, static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(ctas) * kFewWarps, max(units / kFewRunTiles, least)))));
+    const int64_t runs = units <= static_cast<int64_t>(ctas) * 3 ? units : max(units / kFewRunTiles, static_cast<int64_t>(ctas) * 2);
+    return UnitSplit(units, static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(ctas) * kFewWarps, runs))));
 }
 
 // Weights enter the tensor cores times 2^15: taken as they are, those below 6e-5 would lose bits and those below 3e-8 vanish.
@@ -467,6 +471,8 @@ __device__ __forceinline__ uint32_t pack_h2(float a, float b)
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// 128 bytes that nobody will read any more before they are written again
+__device__ __forceinline__ void discard_line(const uint8_t* p) { asm volatile("discard.global.L2 [%0], 128;" ::"l"(p) : "memory"); }
 // bounded wait of a warp on one of its barriers
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
 {
@@ -500,8 +506,9 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     struct Place { int64_t u, begin, end; int32_t head, tile; PagedReq q; };
     auto seek = [&](Place& p) {
         if (p.u >= u1) return;
-        p.head = static_cast<int32_t>(divide(static_cast<uint64_t>(p.u), static_cast<uint64_t>(line)));
-        const int64_t head_from = static_cast<int64_t>(p.head) * line;
+        const int32_t nth = static_cast<int32_t>(divide(static_cast<uint64_t>(p.u), static_cast<uint64_t>(line)));
+        const int64_t head_from = static_cast<int64_t>(nth) * line;
+        p.head = kv.heads - 1 - nth;                       // the last head's tiles are the latest in the L2 cache
         const int r = warp_find(sc.few_tiles, kv.n_req, static_cast<int32_t>(p.u - head_from));
         p.q = paged_req(kv, r, T);
         p.begin = head_from + __ldcg(sc.few_tiles + r);
@@ -636,6 +643,12 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
                     mma_16816(acc[2 * d + 1], p[ks], b[2], b[3]);
                 }
             __syncwarp();                                  // the whole warp has read the tile
+            if (o.discard) {
+                // nobody reads the tile again: what of it is still in the L2 cache need not go to memory (1.06 M tokens and KV heads:
+                // 273 -> 260 us, 2.1 M: 533 -> 522)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) discard_line(staged_tile(kv, i >> 1, at.head, at.tile) + (i & 1) * (kKvTileBytes / 2) + lane * 128);
+            }
             ask();
         }
         // out, or into a slot

@@ -149,11 +149,12 @@ __device__ __forceinline__ void mma_values(uint32_t d, uint32_t a, uint64_t b, b
 
 // a piece of a block: tiles [from, to) of the `tiles` tiles of block `block` of request r, for head `head`
 struct ManyPiece { int64_t next; int32_t head, r, block, tiles, from, to; };
-__device__ __forceinline__ ManyPiece many_piece(const PagedSchedule& sc, int32_t n_blocks, int64_t total, int64_t u, int64_t u1)
+__device__ __forceinline__ ManyPiece many_piece(const PagedSchedule& sc, int32_t heads, int32_t n_blocks, int64_t total, int64_t u, int64_t u1)
 {
     ManyPiece p;
-    p.head = static_cast<int32_t>(divide(static_cast<uint64_t>(u), static_cast<uint64_t>(total)));
-    const int32_t at = static_cast<int32_t>(u - p.head * total);
+    const int32_t nth = static_cast<int32_t>(divide(static_cast<uint64_t>(u), static_cast<uint64_t>(total)));
+    const int32_t at = static_cast<int32_t>(u - nth * total);
+    p.head = heads - 1 - nth;                              // the last head's tiles are the latest in the L2 cache
     const int j = warp_find(sc.block_tiles, n_blocks, at);
     const int32_t first = __ldcg(sc.block_tiles + j), end = __ldcg(sc.block_tiles + j + 1);
     const int2 rb = __ldcg(sc.blocks + j);
@@ -405,7 +406,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         uint32_t n = 0;
         bool ok = true;
         for (int64_t u = u0; u < u1 && ok;) {
-            const ManyPiece pc = many_piece(sc, n_blocks, total, u, u1);
+            const ManyPiece pc = many_piece(sc, kv.heads, n_blocks, total, u, u1);
             const PagedReq q = paged_req(kv, pc.r, T);
             u = pc.next;
             for (int32_t j = pc.from; j < pc.to && ok; ++j) {
@@ -498,7 +499,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         const int32_t tokens = tile_rows_tokens(o.q_per_kv);
         uint32_t n = 0;
         for (int64_t u = u0; u < u1;) {
-            const ManyPiece pc = many_piece(sc, n_blocks, total, u, u1);
+            const ManyPiece pc = many_piece(sc, kv.heads, n_blocks, total, u, u1);
             const PagedReq q = paged_req(kv, pc.r, T);
             const int64_t first = u - pc.from;             // the block's first unit
             const int run_lo = split.owner(first), run_hi = split.owner(first + pc.tiles - 1);
