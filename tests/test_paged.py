@@ -79,7 +79,8 @@ def test_argument_errors_without_a_gpu(B):
     assert attn(b=batch(n_req=0)) == 0 and attn(b=batch(tokens=0)) == 0                        # nothing to do
     for bad in bad_caches:
         assert attn(cache(**bad)) == INV, bad
-    for bad in (dict(g=0), dict(g=17), dict(scale=math.nan), dict(scale=math.inf), dict(flags=2), dict(q=None), dict(out=None), dict(stride=504),
+    for bad in (dict(g=0), dict(g=17), dict(scale=math.nan), dict(scale=math.inf), dict(flags=2), dict(q=None), dict(out=None), dict(stride=504), dict(stride=1 << 38),
+                dict(b=batch(tokens=1 << 26, kv=1 << 26)),
                 dict(b=batch(tables=None)), dict(b=batch(cu=None)), dict(b=batch(lens=None)), dict(b=batch(tiles=None)), dict(b=batch(stride=-1)),
                 dict(b=batch(n_req=65536)), dict(b=batch(tokens=-1)), dict(b=batch(new=-1)), dict(b=batch(kv=-1)), dict(b=batch(n_tiles=-1)),
                 dict(b=batch(n_tiles=1 << 30))):
@@ -253,8 +254,9 @@ class Paged:
         self.d_cu, self.d_lens, self.d_tiles = ints(np.concatenate([[0], np.cumsum(new)])), ints(kv), ints(tiles)
         self.batch = B.paged_batch(self.d_tables, self.stride, self.d_cu, self.d_lens, self.d_tiles, n_req, self.tokens, max(new), max(kv), int(tiles[-1]))
 
-    def run(self, causal, scale=128 ** -0.5, ws_bytes=None, lse=True, spare=2):
-        B = self.B
+    def run(self, causal, scale=128 ** -0.5, ws_bytes=None, lse=True, spare=2, batch=None):
+        B, own = self.B, self.batch
+        self.batch = batch or own
         full = B.ecco_paged_attn_workspace_bytes(self.cache, self.batch, self.g)
         ws_bytes = full if ws_bytes is None else ws_bytes
         ws = torch.full((ws_bytes,), 0xff, dtype=torch.uint8, device="cuda")  # NaN, whatever it is read as
@@ -262,6 +264,7 @@ class Paged:
         d_lse = torch.full((self.tokens + spare, self.heads * self.g), 7.0, device="cuda") if lse else None
         B.ecco_paged_attn(self.cache, self.batch, self.g, self.d_q, self.q_stride, scale, B.ATTN_CAUSAL if causal else 0, out, d_lse, ws, ws_bytes)
         torch.cuda.synchronize()
+        self.batch = own
         assert (out[self.tokens:] == 7).all()                                  # rows behind the last request
         return out[:self.tokens].cpu().numpy(), d_lse[:self.tokens].cpu().numpy() if lse else None
 
@@ -314,6 +317,10 @@ SHAPES = [
     ([64, 17], [64, 500], 1, 16, 4096),
     ([130, 1, 257], [700, 900, 257], 2, 4, 16),
     ([100], [3000], 1, 1, 2),
+    ([61, 40], [200, 129], 1, 7, 32),                                          # heads that do not divide 128: blocks of whole tokens
+    ([50], [333], 2, 13, 16),
+    ([20, 1, 18], [0, 0, 5], 1, 2, 16),                                        # many rows and no token at all; one tile
+    ([128, 129], [128, 1025], 1, 2, 64),                                       # a block that is just full, and one row more
 ]
 
 
@@ -328,3 +335,294 @@ def test_attention_matches_64_bits(B, dev, eo, caches, shape, causal):
     assert B.ecco_device_status() == 0
     again, _ = p.run(causal, lse=False)
     assert np.array_equal(out.view(np.uint16), again.view(np.uint16))          # reproducible, with and without lse
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.0, -0.11, 1.0, 1e-42])
+def test_attention_scales(B, dev, eo, caches, scale):
+    """Zero (all tokens alike), negative, sharp, below fp32's normal range; few rows and many."""
+    p = Paged(B, eo, *caches, [1, 40, 3], [100, 300, 2], 2, 2, 16, seed=7)
+    for causal in (True, False):
+        out, lse = p.run(causal, scale=scale)
+        p.check(out, lse, causal, scale=float(np.float32(scale)))
+
+
+@pytest.mark.gpu
+def test_attention_takes_some_heads_at_a_time(B, dev, eo, caches):
+    p = Paged(B, eo, *caches, [1, 70, 4], [500, 90, 64], 5, 3, 16, seed=8)
+    sizes = []
+    for heads in (1, 2, 3, 5):
+        c = B.paged_cache(p.d_meta[0], p.d_meta[1], p.d_pools[0], p.d_pools[1], p.n_pages, heads, p.page)
+        sizes.append(B.ecco_paged_attn_workspace_bytes(c, p.batch, p.g))
+    assert sizes == sorted(sizes) and sizes[0] < sizes[-1]
+    for n in sizes:
+        out, lse = p.run(True, ws_bytes=n)
+        p.check(out, lse, True, rows=3)
+
+    def launches(n):
+        before = B.ecco_kernel_launch_count()
+        out, lse = p.run(True, ws_bytes=n)
+        p.check(out, lse, True, rows=7)
+        return B.ecco_kernel_launch_count() - before
+
+    low, high = 0, sizes[0]                                                    # what one head needs on this device: at most what the call says
+    while high - low > 16:
+        mid = (low + high) // 2
+        try:
+            p.run(True, ws_bytes=mid)
+            high = mid
+        except B.EccoError as e:
+            assert e.code == B.ERR_WORKSPACE
+            low = mid
+    assert low > 2 * 20 * 8192 and launches(high) == 5 * launches(sizes[-1])
+    with pytest.raises(B.EccoError) as ei:
+        B.ecco_paged_attn(p.cache, p.batch, p.g, p.d_q, p.q_stride, 0.1, 0, p.d_q, None, None, 1 << 40)
+    assert ei.value.code == B.ERR_WORKSPACE
+
+
+@pytest.mark.gpu
+def test_attention_of_a_padded_batch(B, dev, eo, caches):
+    """Sizes that the host passes are upper bounds: spare rows, requests without tokens at the end, generous maxima; an odd workspace address."""
+    p = Paged(B, eo, *caches, [1, 30, 0, 0], [70, 64, 0, 0], 2, 4, 16, seed=9)
+    for new, kv, tiles in ((30, 70, 5), (900, 5000, 300), (31, 71, 6)):
+        b = B.paged_batch(p.d_tables, p.stride, p.d_cu, p.d_lens, p.d_tiles, 4, p.tokens + 2, new, kv, tiles)
+        q = torch.cat([p.d_q, torch.full((2, p.q_stride), math.nan, dtype=torch.float16, device="cuda")])
+        ws = torch.full((B.ecco_paged_attn_workspace_bytes(p.cache, b, p.g) + 16,), 0xff, dtype=torch.uint8, device="cuda")[16:]
+        out = torch.full((p.tokens + 2, 8, 128), 7.0, dtype=torch.float16, device="cuda")
+        lse = torch.full((p.tokens + 2, 8), 7.0, device="cuda")
+        B.ecco_paged_attn(p.cache, b, p.g, q, p.q_stride, 0.1, B.ATTN_CAUSAL, out, lse, ws, ws.numel())
+        assert (out[p.tokens:] == 7).all() and (lse[p.tokens:] == 7).all()
+        p.check(out[:p.tokens].cpu().numpy(), lse[:p.tokens].cpu().numpy(), True, scale=0.1)
+    assert B.ecco_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_attention_of_more_requests_than_shared_memory_keeps(B, dev, eo, caches):
+    rng = np.random.default_rng(10)
+    new = rng.integers(0, 4, 300)
+    new[[5, 77, 299]] = [40, 9, 130]
+    kv = new + rng.integers(0, 60, 300)
+    p = Paged(B, eo, *caches, new.tolist(), kv.tolist(), 1, 2, 8, seed=10)
+    out, lse = p.run(True)
+    p.check(out, lse, True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [[1, 2], [40, 30]])
+def test_values_beyond_fp16_do_not_leave_their_rows(B, dev, eo, caches, new):
+    """V values beyond fp16's range enter as +-65504; a row that does not see them has nothing of them."""
+    metas, blocks = caches
+    big = eo.Meta()
+    ctypes.memmove(ctypes.byref(big), ctypes.byref(metas[1]), ctypes.sizeof(big))
+    big.e = 16
+    p = Paged(B, eo, (metas[0], big), blocks, new, [50, 40], 2, 2, 16, seed=11)
+    assert (np.abs(p.decoded[1][0]) == 65504).any()
+    out, lse = p.run(True)
+    p.check(out, lse, True)
+    # and a q that is not finite stays in the rows of its token
+    clean = out.copy()
+    p.d_q[0, :256] = math.inf
+    out, _ = p.run(True)
+    assert np.array_equal(out[1:].view(np.uint16), clean[1:].view(np.uint16)) and np.array_equal(out[0, 2:].view(np.uint16), clean[0, 2:].view(np.uint16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [[1, 2, 1], [30, 33, 60]])
+def test_bad_pages_and_lengths_are_reported(B, dev, eo, caches, new):
+    """The requests beside a broken one keep their results, and nothing outside of the buffers is touched."""
+    def make():
+        return Paged(B, eo, *caches, new, [100, 90, 200], 2, 2, 16, seed=12)
+
+    p = make()
+    for page in (-1, p.n_pages, 2**31 - 1, -2**31):
+        p.d_tables[1, 2] = page
+        out, lse = p.run(True)
+        assert B.ecco_device_status() == B.ERR_INVALID_ARG
+        q = make()
+        q.new, q.kv = p.new, p.kv
+        keep = np.r_[0:new[0], new[0] + new[1]:sum(new)]
+        want, want_lse = q.run(True)
+        assert np.array_equal(out[keep].view(np.uint16), want[keep].view(np.uint16)) and np.array_equal(lse[keep], want_lse[keep])
+    # lengths and prefix sums that say more than the bounds, or anything at all
+    rng = np.random.default_rng(13)
+    for name in ("d_lens", "d_tiles", "d_cu", "d_tables"):
+        for trial in range(6):
+            p = make()
+            t = getattr(p, name)
+            t.copy_(torch.from_numpy(rng.integers(-2**31, 2**31, t.shape) if trial < 3 else rng.integers(-50, 300, t.shape)).int())
+            p.run(True, spare=0)
+            assert B.ecco_device_status() in (0, B.ERR_INVALID_ARG)
+    p = make()
+    out, lse = p.run(True)
+    p.check(out, lse, True, rows=5)
+    assert B.ecco_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_pools_beyond_32_bits(B, dev, eo, caches):
+    """Pages on both sides of byte 2^32 of a pool; append and attention."""
+    heads, page = 32, 64
+    n_pages = (1 << 32) // (heads * page * 64) + 40
+    pool = torch.empty((n_pages, heads, page, 64), dtype=torch.uint8, device="cuda")
+    (meta, _), _ = caches
+    d_meta = B.meta_to_device(lib_meta_from_oracle(B, meta))
+    cache = B.paged_cache(d_meta, d_meta, pool, pool, n_pages, heads, page)
+    ids = [n_pages - 1, 3, n_pages - 39, n_pages - 41]
+    kv = 3 * page + 5
+    slots = np.concatenate([np.arange(e * page, e * page + page) for e in ids])[:kv]
+    rng = np.random.default_rng(14)
+    x = rng.standard_normal((kv, heads * 128)).astype(np.float16)
+    B.ecco_paged_append(cache, torch.from_numpy(x).cuda(), torch.from_numpy(x).cuda(), heads * 128, ints(slots), kv)
+    blocks, _ = eo.encode(meta, x, eo.SELECT_MINMAX)
+    got = pool[torch.from_numpy(slots // page).cuda(), :, torch.from_numpy(slots % page).cuda()].cpu().numpy()
+    assert np.array_equal(got.reshape(-1, 64), blocks)
+    values = eo.decode(meta, blocks).astype(np.float64).reshape(kv, heads, 128)
+    q = rng.standard_normal((2, heads * 128)).astype(np.float16)
+    batch = B.paged_batch(ints([ids]), 4, ints([0, 2]), ints([kv]), ints([0, -(-kv // 32)]), 1, 2, 2, kv, -(-kv // 32))
+    n = B.ecco_paged_attn_workspace_bytes(cache, batch, 1)
+    out = torch.empty((2, heads, 128), dtype=torch.float16, device="cuda")
+    B.ecco_paged_attn(cache, batch, 1, torch.from_numpy(q).cuda(), heads * 128, 0.1, 0, out, None, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    for h in range(heads):
+        s = 0.1 * (q[:, h * 128:(h + 1) * 128].astype(np.float64) @ values[:, h].T)
+        w = np.exp(s - s.max(1, keepdims=True))
+        w /= w.sum(1, keepdims=True)
+        ref, mass = w @ values[:, h], w @ np.abs(values[:, h])
+        assert (np.abs(out[:, h].cpu().numpy() - ref) <= 2.0 ** -11 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -14) * mass + 2.0 ** -25).all(), h
+
+
+# ------------------------------------------------------------------ the three together
+class Server:
+    """Requests that grow: every step plans, appends and attends, on fixed buffers."""
+
+    def __init__(self, B, eo, caches, n_req, heads, g, page, max_kv, seed):
+        (self.metas, _), self.B, self.eo = caches, B, eo
+        self.heads, self.g, self.page, self.rng = heads, g, page, np.random.default_rng(seed)
+        self.stride = max_kv // page + 1
+        self.n_pages = n_req * self.stride
+        self.max_new, self.max_kv = 48, max_kv
+        self.n_tokens = n_req * self.max_new
+        z = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype, device="cuda")  # noqa: E731
+        self.ctx, self.new, self.tables = z(n_req), z(n_req), z(n_req, self.stride)
+        self.free = torch.from_numpy(self.rng.permutation(self.n_pages)).int().cuda()
+        self.used = 0
+        self.slots, self.cu, self.lens, self.tiles, self.result = z(self.n_tokens), z(n_req + 1), z(n_req), z(n_req + 1), z(4)
+        self.qkv = z(self.n_tokens, heads * (g + 2), 128, dtype=torch.float16)
+        self.pools = [z(self.n_pages, heads, page, 64, dtype=torch.uint8) for _ in range(2)]
+        self.d_meta = [B.meta_to_device(lib_meta_from_oracle(B, m)) for m in self.metas]
+        self.cache = B.paged_cache(self.d_meta[0], self.d_meta[1], self.pools[0], self.pools[1], self.n_pages, heads, page)
+        self.batch = B.paged_batch(self.tables, self.stride, self.cu, self.lens, self.tiles, n_req, self.n_tokens, self.max_new, max_kv, n_req * (max_kv // 32 + 1))
+        self.ws_bytes = B.ecco_paged_attn_workspace_bytes(self.cache, self.batch, g)
+        self.ws = z(self.ws_bytes, dtype=torch.uint8)
+        self.out, self.lse = z(self.n_tokens, heads * g, 128, dtype=torch.float16), z(self.n_tokens, heads * g, dtype=torch.float32)
+        self.free_now = self.free.clone()
+        self.rows = [[] for _ in range(n_req)]                                # K and V values of every request so far
+
+    def feed(self, new):
+        """The host's part of a step: lengths and rows of the projection."""
+        x = self.rng.standard_normal((self.n_tokens, self.heads * (self.g + 2), 128)).astype(np.float16)
+        self.new.copy_(ints(new))
+        self.qkv.copy_(torch.from_numpy(x))
+        self.free_now[:self.n_pages - self.used] = self.free[self.used:]
+        at = 0
+        for r, n in enumerate(new):
+            self.rows[r].append(x[at:at + n, self.heads * self.g:])
+            at += n
+        self.x = x
+
+    def step(self):
+        B, row = self.B, self.qkv.data_ptr()
+        stride = self.heads * (self.g + 2) * 128
+        B.ecco_paged_plan(self.page, self.n_pages, len(self.ctx), self.ctx, self.new, self.free_now, self.n_pages, self.tables, self.stride, self.slots,
+                          self.n_tokens, self.cu, self.lens, self.tiles, self.result)
+        B.ecco_paged_append(self.cache, row + self.heads * self.g * 256, row + self.heads * (self.g + 1) * 256, stride, self.slots, self.n_tokens)
+        B.ecco_paged_attn(self.cache, self.batch, self.g, self.qkv.data_ptr(), stride, 128 ** -0.5, B.ATTN_CAUSAL, self.out, self.lse, self.ws, self.ws_bytes)
+
+    def done(self):
+        torch.cuda.synchronize()
+        assert self.B.ecco_device_status() == 0 and self.result[0].item() == 0
+        self.used += self.result[1].item()
+        self.ctx.copy_(self.lens)
+        return self.out.cpu().numpy(), self.lse.cpu().numpy()
+
+    def check(self, out, lse, new):
+        """A request's rows against 64 bits over all that it was ever given."""
+        at = 0
+        for r, n in enumerate(new):
+            kv = np.concatenate(self.rows[r])
+            if n and r % 3 == 0:
+                p = Paged.__new__(Paged)
+                p.heads, p.g, p.new, p.kv = self.heads, self.g, [n], [len(kv)]
+                p.q = self.x[at:at + n, :self.heads * self.g].reshape(n, -1)
+                p.decoded = []
+                for which in range(2):
+                    part = np.ascontiguousarray(kv[:, which * self.heads:(which + 1) * self.heads])
+                    blocks, _ = self.eo.encode(self.metas[which], part, self.eo.SELECT_MINMAX)
+                    p.decoded.append([self.eo.decode(self.metas[which], blocks).astype(np.float64).reshape(-1, self.heads, 128)])
+                p.check(out[at:at + n], lse[at:at + n], True, rows=4)
+            at += n
+
+
+def steps_of(n_req):
+    return [[37 - r % 30 for r in range(n_req)], [1] * n_req, [(r * 7) % 5 for r in range(n_req)], [0] * n_req, [48 if r == 1 else 1 for r in range(n_req)]]
+
+
+@pytest.mark.gpu
+def test_a_server_step_by_step(B, dev, eo, caches):
+    s = Server(B, eo, caches, 6, 2, 2, 16, 160, 21)
+    for new in steps_of(6):
+        s.feed(new)
+        s.step()
+        out, lse = s.done()
+        s.check(out, lse, new)
+
+
+@pytest.mark.gpu
+def test_captured_steps_replay_with_other_lengths(B, dev, eo, caches):
+    """One step captured into a graph and replayed with other lengths, against the same steps issued one by one; two servers' graphs,
+    each with a workspace of its own, on two streams at once."""
+    eager = [Server(B, eo, caches, 6, 2, 2, 16, 160, seed) for seed in (22, 23)]
+    graphed = [Server(B, eo, caches, 6, 2, 2, 16, 160, seed) for seed in (22, 23)]
+    want = []
+    for s in eager:
+        want.append([])
+        for new in steps_of(6):
+            s.feed(new)
+            s.step()
+            want[-1].append(s.done())
+    streams, graphs = [torch.cuda.Stream() for _ in graphed], []
+    for s, stream in zip(graphed, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            s.step()
+        graphs.append(g)
+    for i, new in enumerate(steps_of(6)):
+        for s in graphed:
+            s.feed(new)
+        torch.cuda.synchronize()
+        for g, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                g.replay()
+        for k, s in enumerate(graphed):
+            out, lse = s.done()
+            n = sum(new)
+            assert np.array_equal(out[:n].view(np.uint16), want[k][i][0][:n].view(np.uint16)), (i, k)
+            assert np.array_equal(lse[:n], want[k][i][1][:n]), (i, k)
+
+
+@pytest.mark.gpu
+def test_paged_and_dense_caches_agree(B, dev, eo, caches):
+    """One token each over equal lengths: ecco_attn_scores and ecco_attn_values over the same blocks in one piece."""
+    heads, g, kv, batch = 2, 4, 333, 3
+    p = Paged(B, eo, *caches, [1] * batch, [kv] * batch, heads, g, 16, seed=31)
+    out, _ = p.run(True)
+    dense = [torch.from_numpy(np.stack([np.stack([pool[p.tables[r, np.arange(kv) // 16], h, np.arange(kv) % 16] for h in range(heads)]) for r in range(batch)])).cuda()
+             for pool in p.pools]
+    scores = torch.empty((batch, heads * g, kv), device="cuda")
+    B.ecco_attn_scores(p.d_meta[0], dense[0], batch, heads, kv, g, p.d_q.view(batch, -1)[:, :heads * g * 128].contiguous(), 128 ** -0.5, scores)
+    n = B.ecco_attn_values_workspace_bytes(batch, heads, kv, g)
+    want = torch.empty((batch, heads * g, 128), device="cuda")
+    B.ecco_attn_values(p.d_meta[1], dense[1], batch, heads, kv, g, scores, want, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    want = want.cpu().numpy().astype(np.float64)
+    # both rounded: the tolerance of the paged call, with the largest |V| for the weighted mean
+    top = max(np.abs(v).max() for v in p.decoded[1])
+    assert (np.abs(out - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -10 * top).all()
