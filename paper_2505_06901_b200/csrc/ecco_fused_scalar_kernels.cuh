@@ -58,10 +58,12 @@ __device__ __forceinline__ float sum_of(const float (&a)[kChains]) { return a[0]
 // decode one group and accumulate its kV dot products against the slice at shared address xs
 // keep = false: the products are not wanted.  The lanes past the end of a row decode its last group again; with 23 copies of a
 // group of many outliers to deal, one warp held up a whole call (scores of 2 x 8 x 777 tokens 14.6 instead of 9.0 us).
-template <int kV, bool kDeal>
+// kFinite: values beyond fp16's range are +-65504 instead of infinities
+template <int kV, bool kDeal, bool kFinite = false>
 __device__ __forceinline__ void fused_group(const Block& blk, const DecodeTables& tb, uint32_t bits, float T, uint32_t xs, bool keep, float (&acc)[kV][kChains])
 {
-    LaneGroup g = open_block(blk, bits, tb, T);
+    LaneGroup g = open_block<kFinite>(blk, bits, tb, T);
+    auto finite = [](float v) { return kFinite ? fminf(fmaxf(v, -65504.0f), 65504.0f) : v; };
     if (kDeal) sts_u32(bits + 18 * 128, blk.w[0]);                    // the ranks will lie over the block's first words
     const uint32_t ranks_at = bits - kRankRows * 128;
     const uint32_t end = decode_group<kBlockBits, kBlockFreeSteps>(g, bits, tb.pairs, [&](int i, uint32_t ranks, bool cutting, int n_ok) {
@@ -94,7 +96,7 @@ __device__ __forceinline__ void fused_group(const Block& blk, const DecodeTables
             }
             seen |= bit;
             const float mapped = rank_value(g, (lds_u32(ranks_at + (loc >> 3) * 128) >> ((loc & 7u) * 4)) & 15u);
-            const float outlier = __half2float(__float2half_rn(fp8_to_float(f >> 7) * T));
+            const float outlier = finite(__half2float(__float2half_rn(fp8_to_float(f >> 7) * T)));
 #pragma unroll
             for (int b = 0; b < kV; ++b) {
                 const float x = __half2float(__ushort_as_half(static_cast<unsigned short>(lds_u16(xs + b * (kGroup * 2) + loc * 2))));
@@ -106,8 +108,8 @@ __device__ __forceinline__ void fused_group(const Block& blk, const DecodeTables
         deal_outliers(bits, list, n_pad, [&](uint32_t slot, uint32_t owner, uint32_t f, bool valid) {
             const uint32_t loc = f & 127u;
             const uint32_t rank = (lds_u32(ranks_at - lane4 + owner * 4 + (loc >> 3) * 128) >> ((loc & 7u) * 4)) & 15u;
-            const float mapped = value_of(lds_u32(bits0 + 18 * 128 + owner * 4), rank, tb, T);
-            const float outlier = __half2float(__float2half_rn(fp8_to_float(f >> 7) * T));
+            const float mapped = finite(value_of(lds_u32(bits0 + 18 * 128 + owner * 4), rank, tb, T));
+            const float outlier = finite(__half2float(__float2half_rn(fp8_to_float(f >> 7) * T)));
 #pragma unroll
             for (int b = 0; b < kV; ++b) {
                 const float x = __half2float(__ushort_as_half(static_cast<unsigned short>(lds_u16(xs + b * (kGroup * 2) + loc * 2))));

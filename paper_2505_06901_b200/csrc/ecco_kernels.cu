@@ -768,6 +768,7 @@ extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k,
 }
 
 namespace {
+constexpr float kLog2E = 1.4426950408889634f;
 // Tiles per warp (of each kind) from which on every CTA decodes both kinds.
 constexpr int kStageBothTiles = 3;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
@@ -853,18 +854,39 @@ int launch_paged_many(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o
     }
     return launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc, map, q_map);
 }
+template <bool kScores>
 int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
 {
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {
-        const int rc = set_smem(ecco_paged_few_kernel, kFewSmemBytes);
+        const int rc = set_smem(ecco_paged_few_kernel<kScores>, kFewSmemBytes<kScores>);
         if (rc) return rc;
         configured[di.device] = true;
     }
-    const int rc = launch_overlapped(ecco_paged_few_kernel, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps * 32), kFewSmemBytes, s, kv, o, sc);
+    const int rc = launch_overlapped(ecco_paged_few_kernel<kScores>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps * 32), kFewSmemBytes<kScores>, s, kv, o, sc);
     if (rc) return rc;
     const int runs = p.few_ctas * kFewWarps;
     return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(runs), 256u, 0, s, o, kv.head0);
+}
+template <StageKind kKind>
+int launch_paged_stage(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, int64_t units, cudaStream_t s)
+{
+    static thread_local bool configured[64] = {};
+    auto kernel = ecco_paged_stage_kernel<32, kKind>;
+    int rc = want_all_smem(kernel, &configured[di.device]);
+    if (rc) return rc;
+    const int ctas = std::max(1, spread_ctas(units, kKind == kHalves ? di.sms / 2 : di.sms));
+    return launch_overlapped(kernel, static_cast<unsigned>(kKind == kHalves ? 2 * ctas : ctas), spread_threads(units, ctas, 32), kSmemCtaBytes, s, kv, o, sc);
+}
+template <int kV>
+int launch_paged_scores(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, float* scores, int64_t units, cudaStream_t s)
+{
+    static thread_local bool configured[64] = {};
+    auto kernel = ecco_paged_scores_kernel<kV, fused_warps(kV)>;
+    int rc = want_all_smem(kernel, &configured[di.device]);
+    if (rc) return rc;
+    const int ctas = std::max(1, spread_ctas(units, di.sms));
+    return launch_overlapped(kernel, static_cast<unsigned>(ctas), spread_threads(units, ctas, fused_warps(kV)), kSmemCtaBytes, s, kv, o, scores);
 }
 }  // namespace
 
@@ -879,7 +901,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
 {
     int rc = check_paged_cache(cache);
     if (rc) return rc;
-    if (!batch || !paged_batch_fine(*cache, *batch, q_per_kv) || (flags & ~ECCO_ATTN_CAUSAL) || !(scale - scale == 0.0f)) return ECCO_ERR_INVALID_ARG;
+    if (!batch || !paged_batch_fine(*cache, *batch, q_per_kv) || (flags & ~ECCO_ATTN_CAUSAL) || !std::isfinite(scale * kLog2E)) return ECCO_ERR_INVALID_ARG;
     const ecco_paged_batch& b = *batch;
     if (b.n_req == 0 || b.n_tokens == 0) return ECCO_OK;
     const int q_heads = cache->n_kv_heads * q_per_kv;
@@ -907,18 +929,11 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     kv.staged = static_cast<uint8_t*>(d_workspace);
     PagedOut o = {};
     o.q = static_cast<const __half*>(d_q); o.q_stride = q_stride;
-    o.scale_log2 = scale * 1.4426950408889634f;
+    o.scale_log2 = scale * kLog2E;
     o.q_per_kv = q_per_kv; o.q_heads = q_heads; o.causal = flags & ECCO_ATTN_CAUSAL;
     o.out = static_cast<__half*>(d_out); o.lse = d_lse;
     o.discard = aligned_to(d_workspace, 128);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    static thread_local bool configured[64] = {};
-    if (!configured[di.device]) {
-        rc = set_smem(ecco_paged_stage_kernel<32, false>, kSmemCtaBytes);
-        if (!rc) rc = set_smem(ecco_paged_stage_kernel<32, true>, kSmemCtaBytes);
-        if (rc) return rc;
-        configured[di.device] = true;
-    }
     for (kv.head0 = 0; kv.head0 < cache->n_kv_heads; kv.head0 += kv.heads) {
         kv.heads = std::min(heads, cache->n_kv_heads - kv.head0);
         const PagedAttnPlan p = paged_attn_plan(b, kv.heads, q_per_kv, ctas);
@@ -931,12 +946,22 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         sc.few_rows = kFewRows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
         sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
-        // both kinds one after the other in every CTA where a warp has several tiles of each; else half of the CTAs for K, half for V
+        // Small calls decode K in half of the CTAs and V in the other half.  Large ones decode both in every CTA, or, for one or two rows
+        // to a request, take the products with K at once.
         const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
-        const bool both = units >= static_cast<int64_t>(kStageBothTiles) * 31 * di.sms;
-        const int ctas_k = std::max(1, spread_ctas(units, both ? di.sms : di.sms / 2));
-        rc = launch_overlapped(both ? ecco_paged_stage_kernel<32, true> : ecco_paged_stage_kernel<32, false>, static_cast<unsigned>(both ? ctas_k : 2 * ctas_k),
-                               spread_threads(units, ctas_k, 32), kSmemCtaBytes, s, kv, o, sc);
+        const bool large = units >= static_cast<int64_t>(kStageBothTiles) * 31 * di.sms;
+        const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
+        const bool scores = large && (rows == 1 || rows == 2);
+        if (scores) {
+            // where K's tiles would be
+            float* const at = reinterpret_cast<float*>(kv.staged + static_cast<size_t>(kv.heads) * kv.max_tiles * kKvTileBytes);
+            o.scores = at;
+            o.score_rows = static_cast<int32_t>(rows);
+            rc = rows == 1 ? launch_paged_scores<1>(di, kv, o, at, units, s) : launch_paged_scores<2>(di, kv, o, at, units, s);
+            if (!rc) rc = launch_paged_stage<kOnlyV>(di, kv, o, sc, units, s);
+        } else {
+            rc = large ? launch_paged_stage<kBoth>(di, kv, o, sc, units, s) : launch_paged_stage<kHalves>(di, kv, o, sc, units, s);
+        }
         if (rc) return rc;
         o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
         o.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
@@ -947,8 +972,9 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
             many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
             rc = launch_paged_many(di, kv, many, sc, p, s);
             if (rc) return rc;
+            o.early = 1;
         }
-        rc = launch_paged_few(di, kv, o, sc, p, s);
+        rc = scores ? launch_paged_few<true>(di, kv, o, sc, p, s) : launch_paged_few<false>(di, kv, o, sc, p, s);
         if (rc) return rc;
     }
     return ECCO_OK;

@@ -218,6 +218,9 @@ struct PagedOut {
     float2* part_ml;           // maxima (log2) and sums of weights [slot][rows]
     FewCut* cuts;              // [run]
     int32_t discard;           // the tiles begin at multiples of 128 bytes
+    const float* scores;       // [heads][max_tiles][score_rows][32]: products of q and K, see ecco_paged_scores_kernel
+    int32_t score_rows;
+    int32_t early;             // ecco_paged_few_kernel comes behind ecco_paged_many_kernel
 };
 // tokens that row i of a request sees
 __device__ __forceinline__ int32_t tokens_seen(const PagedReq& q, int32_t token, bool causal)
@@ -293,27 +296,66 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
     if (lane == 0) *sc.n_blocks = n_blocks;
 }
 
+// The request that a tile belongs to, and the tile's first token in it: from the prefix sums in the misc area (`firsts`) or, of more requests
+// than find room there, in memory.
+constexpr int kStageTiles = 224;
+__device__ __forceinline__ void fetch_firsts(const PagedKv& kv, int32_t* firsts)
+{
+    if (kv.n_req <= kStageTiles)
+        for (int i = static_cast<int>(threadIdx.x); i <= kv.n_req; i += static_cast<int>(blockDim.x)) firsts[i] = __ldcg(kv.kv_tiles + i);
+    __syncthreads();
+}
+__device__ __forceinline__ int request_of(const PagedKv& kv, const int32_t* firsts, int32_t tile, int32_t& first)
+{
+    int r = 0;
+    if (kv.n_req <= kStageTiles) {                         // the last request that begins at or before the tile
+        for (int n = kv.n_req; n > 1;) {
+            const int half = n >> 1;
+            if (firsts[r + half] <= tile) { r += half; n -= half; } else n = half;
+        }
+        first = firsts[r];
+    } else {
+        r = warp_find(kv.kv_tiles, kv.n_req, tile);
+        first = __ldcg(kv.kv_tiles + r);
+    }
+    return r;
+}
+// The block of a request's token for a KV head of the launch, NULL where there is none.
+__device__ __forceinline__ const uint8_t* paged_block(const PagedKv& kv, const uint8_t* blocks, int r, int64_t token, int32_t head)
+{
+    const int64_t e = token >> kv.page_shift;
+    const int32_t len = __ldcg(kv.kv_lens + r), page = e >= 0 && e < kv.stride ? __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + e) : -1;
+    if (token < 0 || token >= len) return nullptr;
+    if (page < 0 || page >= kv.n_pages) {
+        atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        return nullptr;
+    }
+    const int64_t at = ((static_cast<int64_t>(page) * kv.all_heads + kv.head0 + head) << kv.page_shift) + (token & ((1 << kv.page_shift) - 1));
+    return blocks + at * kBlockBytes;
+}
+
 // K6s: pages -> tiles.  ecco_decompress_tma_kernel with another way in (a lane finds its token's block through the request's table)
 // and out (a piece leaves by one bulk copy of 1 KB).
-//   kBoth = false: even CTAs decode K, odd ones V: no CTA needs both sets of tables, and small calls decode K and V side by side.
-//   kBoth = true: every CTA decodes its share of K, then of V: another 4 us for the second set of tables, but caches
+//   kHalves: even CTAs decode K, odd ones V: no CTA needs both sets of tables, and small calls decode K and V side by side.
+//   kBoth: every CTA decodes its share of K, then of V: another 4 us for the second set of tables, but caches
 //   whose blocks take differently long leave no CTA waiting (2.1 M groups of K and of V, 178 and 146 us alone: 377 -> 345 us).
 // Values are clamped to fp16's finite range (once per group, on the sixteen values of its table): weight zero times an infinity would
 // be NaN in rows that do not see the token.
-constexpr int kStageTiles = 224;                           // prefix sums of this many requests are kept in the misc area
-template <int kMaxWarps, bool kBoth>
+//   kOnlyV: V alone, see ecco_paged_scores_kernel.
+enum StageKind { kHalves, kBoth, kOnlyV };
+template <int kMaxWarps, StageKind kKind>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t cta = kBoth ? blockIdx.x : blockIdx.x >> 1, ctas = kBoth ? gridDim.x : gridDim.x >> 1;
+    const uint32_t cta = kKind == kHalves ? blockIdx.x >> 1 : blockIdx.x, ctas = kKind == kHalves ? gridDim.x >> 1 : gridDim.x;
     const uint32_t swz = ((lane >> 2) & 1u) << 4;
     int32_t* const firsts = reinterpret_cast<int32_t*>(smem + 64);
     static_assert(64 + (kStageTiles + 1) * 4 <= kMisc, "the prefix sums fit the misc area");
     release_dependents();
-    for (int phase = 0; phase < (kBoth ? 2 : 1); ++phase) {
-        const int which = kBoth ? phase : static_cast<int>(blockIdx.x & 1u);
+    for (int phase = 0; phase < (kKind == kBoth ? 2 : 1); ++phase) {
+        const int which = kKind == kBoth ? phase : kKind == kOnlyV ? 1 : static_cast<int>(blockIdx.x & 1u);
         const uint8_t* const d_meta = which ? kv.v_meta : kv.k_meta;
         const DecodeTables tb = plan_decode_tables(smem_u32(smem), d_meta, true);
         if (phase) {                                           // see ecco_decompress_tma_kernel
@@ -329,9 +371,7 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
         if (!finish_decode_tables(tb, static_cast<uint32_t>(phase))) return;
         if (phase == 0) {
             dependency_wait();
-            if (kv.n_req <= kStageTiles)
-                for (int i = static_cast<int>(threadIdx.x); i <= kv.n_req; i += static_cast<int>(blockDim.x)) firsts[i] = __ldcg(kv.kv_tiles + i);
-            __syncthreads();
+            fetch_firsts(kv, firsts);
             // one warp, if possible one that has no room to decode, makes the schedule on the side
             if (blockIdx.x == 0 && warp == (nw < blockDim.x >> 5 ? nw : 0u)) paged_schedule(kv, sc, o);
             if (blockIdx.x == 0 && threadIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
@@ -343,36 +383,17 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
         if (warp >= nw || u >= tile_stride) u = units;
 
         const uint8_t* const blocks = which ? kv.v_blocks : kv.k_blocks;
-        // the block of this lane's token of unit u, NULL behind the request's last token
-        auto block_ptr = [&](uint32_t unit) -> const uint8_t* {
+        auto block_ptr = [&](uint32_t unit) {
             const uint32_t head = unit / n_tiles;
             const int32_t tile = static_cast<int32_t>(unit - head * n_tiles);
-            int r = 0;
-            int64_t token;
-            if (kv.n_req <= kStageTiles) {                     // the last request that begins at or before the tile
-                for (int n = kv.n_req; n > 1;) {
-                    const int half = n >> 1;
-                    if (firsts[r + half] <= tile) { r += half; n -= half; } else n = half;
-                }
-                token = (static_cast<int64_t>(tile) - firsts[r]) * 32 + lane;
-            } else {
-                r = warp_find(kv.kv_tiles, kv.n_req, tile);
-                token = (static_cast<int64_t>(tile) - __ldcg(kv.kv_tiles + r)) * 32 + lane;
-            }
-            const int64_t e = token >> kv.page_shift;
-            const int32_t len = __ldcg(kv.kv_lens + r), page = e >= 0 && e < kv.stride ? __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + e) : -1;
-            if (token < 0 || token >= len) return nullptr;
-            if (page < 0 || page >= kv.n_pages) {
-                atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-                return nullptr;
-            }
-            const int64_t at = ((static_cast<int64_t>(page) * kv.all_heads + kv.head0 + head) << kv.page_shift) + (token & ((1 << kv.page_shift) - 1));
-            return blocks + at * kBlockBytes;
+            int32_t first;
+            const int r = request_of(kv, firsts, tile, first);
+            return paged_block(kv, blocks, r, (static_cast<int64_t>(tile) - first) * 32 + lane, static_cast<int32_t>(head));
         };
         const uint8_t* next = u < units ? block_ptr(u) : nullptr;
         while (u < units) {
             const uint32_t head = u / n_tiles;
-            uint8_t* const dst = staged_tile(kv, which, static_cast<int>(head), static_cast<int>(u - head * n_tiles));
+            uint8_t* const dst = staged_tile(kv, kKind == kOnlyV ? 0 : which, static_cast<int>(head), static_cast<int>(u - head * n_tiles));
             Block blk;
             const bool there = next != nullptr;
             if (there) {
@@ -426,6 +447,77 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
     }
 }
 
+// K6k: products of K with one or two rows of q per request (a token each without grouped heads), instead of K in tiles: ecco_attn_scores_kernel with
+// another way to the blocks.  As fast as decoding K is, and half of the tiles need neither be written nor read (8 requests of 4048 tokens,
+// 32 heads: 261 us with K in tiles).
+template <int kV, int kMaxWarps>
+__global__ void __launch_bounds__(kMaxWarps * 32, 1)
+ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, float* __restrict__ d_scores)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    int32_t* const firsts = reinterpret_cast<int32_t*>(smem + 64);
+    release_dependents();
+    const DecodeTables tb = plan_decode_tables(smem_u32(smem), kv.k_meta, true);
+    const int nw = static_cast<int>(decode_warps(tb, scalar_warp_bytes(kV)));
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
+    const uint32_t xs = tb.warp_base + warp * scalar_warp_bytes(kV);             // this warp's rows of q [kV][128] fp16
+    const uint32_t bits = xs + kV * kGroup * 2 + kRankRows * 128 + lane * 4;
+    issue_decode_tables(tb, kv.k_meta);
+    if (!finish_decode_tables(tb)) return;
+    dependency_wait();
+    fetch_firsts(kv, firsts);
+    const int32_t n_tiles = paged_tiles(kv);
+    const int64_t U = static_cast<int64_t>(n_tiles) * kv.heads;
+    const int wg = warp < nw ? warp * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x) : INT_MAX;
+    const int W = static_cast<int>(balanced_warps(static_cast<uint64_t>(U), gridDim.x * static_cast<uint32_t>(nw)));
+    if (wg >= W) return;
+    const UnitSplit split(U, W);
+    const int64_t u0 = split.begin(wg), u1 = split.begin(wg + 1);
+    const float T = tb.T;
+
+    int32_t head = static_cast<int32_t>(divide(static_cast<uint64_t>(u0), static_cast<uint64_t>(n_tiles))), tile = static_cast<int32_t>(u0 - static_cast<int64_t>(head) * n_tiles);
+    int32_t first;
+    int r = request_of(kv, firsts, tile, first), of_head = -1, of_request = -1;
+    auto block_ptr = [&]() { return paged_block(kv, kv.k_blocks, r, (static_cast<int64_t>(tile) - first) * 32 + lane, head); };
+    const uint8_t* next = block_ptr();
+    for (int64_t u = u0; u < u1; ++u) {
+        if (head != of_head || r != of_request) {
+            // lane l brings elements 4l .. 4l+3 of every row; rows that there are not are zero
+            const PagedReq q = paged_req(kv, r, n_tiles);
+            __syncwarp();                                  // every lane is done with the rows before
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                const int token = i / o.q_per_kv, g = i - token * o.q_per_kv;
+                uint2 raw = make_uint2(0u, 0u);
+                if (token < q.rows) raw = __ldcg(reinterpret_cast<const uint2*>(o.q + (q.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + head) * o.q_per_kv + g) * kGroup) + lane);
+                sts_v2(xs + i * (kGroup * 2) + lane * 8, raw.x, raw.y);
+            }
+            __syncwarp();
+            of_head = head;
+            of_request = r;
+        }
+        Block cur;
+        const bool there = next != nullptr;
+        if (there) {
+            ldg_block(cur, next);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) cur.w[i] = 0;
+        }
+        float* const dst = d_scores + (static_cast<int64_t>(head) * kv.max_tiles + tile) * (kV * 32) + lane;
+        if (u + 1 < u1) {
+            if (++tile == n_tiles) { tile = 0; ++head; }
+            r = request_of(kv, firsts, tile, first);
+            next = block_ptr();
+            if (next) prefetch_block_l2(next);
+        }
+        float acc[kV][kChains] = {};
+        fused_group<kV, true, true>(cur, tb, bits, T, xs, there, acc);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) dst[i * 32] = sum_of(acc[i]);
+    }
+}
+
 // ---------------------------------------------------------------------------------------------
 // K6a: attention of requests of few rows (new tokens x query heads per KV head): single tokens, drafted tokens.
 // All tiles of all heads form one line, which is cut into equal runs, one per warp, whatever the requests' lengths: a warp is
@@ -435,8 +527,12 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
 // leave sums and maxima in the workspace and are joined by ecco_paged_combine_kernel.
 // Bound by memory: 512 bytes per token and KV head.
 // ---------------------------------------------------------------------------------------------
-constexpr int kFewRows = 16, kFewStages = 2, kFewWarps = 6;
-constexpr uint32_t kFewWarpBytes = kFewStages * 2 * kKvTileBytes + kFewRows * 256, kFewSmemBytes = kFewWarps * kFewWarpBytes + 1024;
+constexpr int kFewRows = 16, kFewWarps = 6;
+// Of a stage of a warp's ring, and their number: K and V, or scores of up to two rows and V.
+template <bool kScores> constexpr uint32_t kFewTileBytes = kScores ? kKvTileBytes + 256 : 2 * kKvTileBytes;
+template <bool kScores> constexpr int kFewStages = kScores ? 4 : 2;
+template <bool kScores> constexpr uint32_t kFewWarpBytes = kFewStages<kScores> * kFewTileBytes<kScores> + (kScores ? 0 : kFewRows * 256);
+template <bool kScores> constexpr uint32_t kFewSmemBytes = kFewWarps * kFewWarpBytes<kScores> + 1024;
 // Runs of the line: one per warp, but of three tiles, or joining costs more than waiting (16 requests of 4 to 8 drafted tokens, 2048 tiles: 158
 // us with runs of two or three tiles, 145 with three), unless there are so few tiles that every run has just one (2 requests of 780 tokens,
 // 400 tiles: 24.4 us with runs of three, 20.4 with runs of one).
@@ -483,18 +579,22 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
     return done;
 }
 
+// kScores: the products with K are there already (ecco_paged_scores_kernel), only V is in tiles.
+template <bool kScores>
 __global__ void __launch_bounds__(kFewWarps * 32, 1)
 ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     constexpr unsigned full = 0xffffffffu;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t mine = smem_u32(smem) + 1024 + warp * kFewWarpBytes, q_at = mine + kFewStages * 2 * kKvTileBytes;
-    const uint32_t bar = smem_u32(smem) + warp * kFewStages * 8;
+    const uint32_t mine = smem_u32(smem) + 1024 + warp * kFewWarpBytes<kScores>, q_at = mine + kFewStages<kScores> * kFewTileBytes<kScores>;
+    const uint32_t bar = smem_u32(smem) + warp * kFewStages<kScores> * 8;
     if (lane == 0)
-        for (int s = 0; s < kFewStages; ++s) mbar_init(bar + s * 8, 1);
+        for (int s = 0; s < kFewStages<kScores>; ++s) mbar_init(bar + s * 8, 1);
     __syncwarp();
-    dependency_wait();
+    // Behind ecco_paged_many_kernel, which lets this one begin only when it has itself waited for the tiles, there is nothing to wait for: the two
+    // have nothing in common.  The next kernel relies on this one for that one's completion all the same, so the wait comes at the end.
+    if (!o.early) dependency_wait();
     release_dependents();
     const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);
     const int wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
@@ -523,16 +623,22 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     auto ask = [&]() {
         if (load.u >= u1) return;
         if (lane == 0) {
-            const uint32_t s = asked % kFewStages, b = bar + s * 8, dst = mine + s * 2 * kKvTileBytes;
-            mbar_expect_tx(b, 2 * kKvTileBytes);
-            bulk_g2s(dst, staged_tile(kv, 0, load.head, load.tile), kKvTileBytes, b);
-            bulk_g2s(dst + kKvTileBytes, staged_tile(kv, 1, load.head, load.tile), kKvTileBytes, b);
+            const uint32_t s = asked % kFewStages<kScores>, b = bar + s * 8, dst = mine + s * kFewTileBytes<kScores>;
+            if (kScores) {
+                mbar_expect_tx(b, kKvTileBytes + o.score_rows * 128);
+                bulk_g2s(dst, staged_tile(kv, 0, load.head, load.tile), kKvTileBytes, b);
+                bulk_g2s(dst + kKvTileBytes, o.scores + (static_cast<int64_t>(load.head) * kv.max_tiles + load.tile) * o.score_rows * 32, o.score_rows * 128, b);
+            } else {
+                mbar_expect_tx(b, 2 * kKvTileBytes);
+                bulk_g2s(dst, staged_tile(kv, 0, load.head, load.tile), kKvTileBytes, b);
+                bulk_g2s(dst + kKvTileBytes, staged_tile(kv, 1, load.head, load.tile), kKvTileBytes, b);
+            }
         }
         ++asked;
         ++load.tile;
         if (++load.u == load.end) seek(load);
     };
-    for (int s = 0; s < kFewStages; ++s) ask();
+    for (int s = 0; s < kFewStages<kScores>; ++s) ask();
 
     const uint32_t col = (lane & 3u) * 2;
     FewCut cut = {};                                       // at most one request begins here and goes on in the next run
@@ -544,19 +650,21 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         const bool starts = at.u == at.begin;              // the request begins in this run
         const int slot = 2 * wg + (at.u == u0 ? 0 : 1);
         if (starts && !whole) cut = FewCut{R, at.head, q.row0, slot, split.owner(at.begin + q.tiles - 1), {0, 0, 0}};
-        // the rows of q as tiles: rows beyond the last are zero
-        __syncwarp();
-        uint4 rows[8];                                     // sixteen lanes to a row, two rows at a time, all on their way together
+        if (!kScores) {
+            // the rows of q as tiles: rows beyond the last are zero
+            __syncwarp();
+            uint4 rows[8];                                     // sixteen lanes to a row, two rows at a time, all on their way together
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = 2 * i + static_cast<int>(lane >> 4), token = row / o.q_per_kv, g = row - token * o.q_per_kv;
-            rows[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (row < R) rows[i] = __ldcg(reinterpret_cast<const uint4*>(o.q + (q.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + g) * kGroup) + (lane & 15u));
+            for (int i = 0; i < 8; ++i) {
+                const int row = 2 * i + static_cast<int>(lane >> 4), token = row / o.q_per_kv, g = row - token * o.q_per_kv;
+                rows[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (row < R) rows[i] = __ldcg(reinterpret_cast<const uint4*>(o.q + (q.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + g) * kGroup) + (lane & 15u));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                sts_v4(q_at + ((lane & 15u) >> 1) * 512 + tile_byte(2 * i + (lane >> 4), (lane & 1u) * 8), rows[i].x, rows[i].y, rows[i].z, rows[i].w);
+            __syncwarp();
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            sts_v4(q_at + ((lane & 15u) >> 1) * 512 + tile_byte(2 * i + (lane >> 4), (lane & 1u) * 8), rows[i].x, rows[i].y, rows[i].z, rows[i].w);
-        __syncwarp();
         float acc[16][4], m[2], l[2];
         int32_t seen[2];
 #pragma unroll
@@ -572,8 +680,8 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
             for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
 
         for (; at.u < at.end; ++at.u, ++at.tile) {
-            const uint32_t s = taken % kFewStages, k_tile = mine + s * 2 * kKvTileBytes, v_tile = k_tile + kKvTileBytes;
-            ok = warp_wait(bar + s * 8, (taken / kFewStages) & 1u);
+            const uint32_t s = taken % kFewStages<kScores>, k_tile = mine + s * kFewTileBytes<kScores>, v_tile = kScores ? k_tile : k_tile + kKvTileBytes;
+            ok = warp_wait(bar + s * 8, (taken / kFewStages<kScores>) & 1u);
             if (!ok) break;
             ++taken;
             // scores: rows x 8 tokens per fragment
@@ -582,17 +690,25 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
             for (int n = 0; n < 4; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s4[n][i] = 0.0f;
-            const uint32_t k_at = k_tile + tile_byte((lane & 7u) + ((lane >> 4) & 1u) * 8, ((lane >> 3) & 1u) * 8);
-            const uint32_t a_at = q_at + tile_byte((lane & 7u) + ((lane >> 3) & 1u) * 8, (lane >> 4) * 8);
+            if (kScores) {
+                const uint32_t row = lane >> 2;            // the scores of rows that there are not are not looked at
+                if (row < static_cast<uint32_t>(o.score_rows))
 #pragma unroll
-            for (int d = 0; d < 8; ++d) {
-                uint32_t b[2][4];
-                ldmatrix_x4(b[0], k_at + d * kPieceBytes);
-                ldmatrix_x4(b[1], k_at + d * kPieceBytes + 512);
-                uint32_t a[4];
-                ldmatrix_x4(a, a_at + d * 512);
+                    for (int n = 0; n < 4; ++n)
+                        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(s4[n][0]), "=f"(s4[n][1]) : "r"(k_tile + kKvTileBytes + row * 128 + (n * 8 + col) * 4));
+            } else {
+                const uint32_t k_at = k_tile + tile_byte((lane & 7u) + ((lane >> 4) & 1u) * 8, ((lane >> 3) & 1u) * 8);
+                const uint32_t a_at = q_at + tile_byte((lane & 7u) + ((lane >> 3) & 1u) * 8, (lane >> 4) * 8);
 #pragma unroll
-                for (int n = 0; n < 4; ++n) mma_16816(s4[n], a, b[n >> 1][(n & 1) * 2], b[n >> 1][(n & 1) * 2 + 1]);
+                for (int d = 0; d < 8; ++d) {
+                    uint32_t b[2][4];
+                    ldmatrix_x4(b[0], k_at + d * kPieceBytes);
+                    ldmatrix_x4(b[1], k_at + d * kPieceBytes + 512);
+                    uint32_t a[4];
+                    ldmatrix_x4(a, a_at + d * 512);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) mma_16816(s4[n], a, b[n >> 1][(n & 1) * 2], b[n >> 1][(n & 1) * 2 + 1]);
+                }
             }
             // softmax: relative to the largest score so far
             const int32_t t0 = (at.tile - q.first) * 32 + static_cast<int32_t>(col);
@@ -647,7 +763,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
                 // nobody reads the tile again: what of it is still in the L2 cache need not go to memory (1.06 M tokens and KV heads:
                 // 273 -> 260 us, 2.1 M: 533 -> 522)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) discard_line(staged_tile(kv, i >> 1, at.head, at.tile) + (i & 1) * (kKvTileBytes / 2) + lane * 128);
+                for (int i = 0; i < (kScores ? 2 : 4); ++i) discard_line(staged_tile(kv, i >> 1, at.head, at.tile) + (i & 1) * (kKvTileBytes / 2) + lane * 128);
             }
             ask();
         }
@@ -678,8 +794,9 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         if (ok) seek(at);
     }
     if (lane == 0) o.cuts[wg] = ok ? cut : FewCut{};
+    if (o.early) dependency_wait();
     if (!ok)                                               // tiles on their way land before the warp leaves
-        for (; taken < asked; ++taken) warp_wait(bar + (taken % kFewStages) * 8, (taken / kFewStages) & 1u);
+        for (; taken < asked; ++taken) warp_wait(bar + (taken % kFewStages<kScores>) * 8, (taken / kFewStages<kScores>) & 1u);
 }
 
 // adds a piece's sums v, with maximum and sum of weights x, to those at hand; a piece that has seen nothing has sums of zero

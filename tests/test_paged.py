@@ -79,7 +79,7 @@ def test_argument_errors_without_a_gpu(B):
     assert attn(b=batch(n_req=0)) == 0 and attn(b=batch(tokens=0)) == 0                        # nothing to do
     for bad in bad_caches:
         assert attn(cache(**bad)) == INV, bad
-    for bad in (dict(g=0), dict(g=17), dict(scale=math.nan), dict(scale=math.inf), dict(flags=2), dict(q=None), dict(out=None), dict(stride=504), dict(stride=1 << 38),
+    for bad in (dict(g=0), dict(g=17), dict(scale=math.nan), dict(scale=math.inf), dict(scale=3e38), dict(flags=2), dict(q=None), dict(out=None), dict(stride=504), dict(stride=1 << 38),
                 dict(b=batch(tokens=1 << 26, kv=1 << 26)),
                 dict(b=batch(tables=None)), dict(b=batch(cu=None)), dict(b=batch(lens=None)), dict(b=batch(tiles=None)), dict(b=batch(stride=-1)),
                 dict(b=batch(n_req=65536)), dict(b=batch(tokens=-1)), dict(b=batch(new=-1)), dict(b=batch(kv=-1)), dict(b=batch(n_tiles=-1)),
@@ -397,6 +397,23 @@ def test_attention_of_a_padded_batch(B, dev, eo, caches):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("new,kv,heads,g", [([1, 1, 1], [300, 1, 64], 3, 1), ([1, 0, 1, 1], [2000, 5, 0, 33], 2, 1), ([1, 1], [70, 129], 2, 2), ([2, 1, 2], [90, 1, 2], 1, 1),
+                                            ([1] * 260, list(range(260)), 1, 2), ([2, 1], [40, 64], 2, 4), ([20, 1], [100, 300], 1, 3)])
+def test_attention_of_large_calls(B, dev, eo, caches, new, kv, heads, g, causal):
+    """The ways of a call whose bounds say that it is large: K and V in every CTA, and, for one or two rows to a request, products with K
+    instead of K in tiles."""
+    p = Paged(B, eo, *caches, new, kv, heads, g, 16, seed=41)
+    b = B.paged_batch(p.d_tables, p.stride, p.d_cu, p.d_lens, p.d_tiles, len(new), p.tokens, max(new), max(kv), 14000 // heads + 1)
+    out, lse = p.run(causal, batch=b)
+    p.check(out, lse, causal)
+    small, _ = p.run(causal)
+    assert B.ecco_device_status() == 0
+    top = max(np.abs(v).max() for v in p.decoded[1] if len(v))
+    assert (np.abs(out.astype(np.float64) - small) <= 2.0 ** -10 * np.abs(small) + 2.0 ** -10 * top).all()
+
+
+@pytest.mark.gpu
 def test_attention_of_more_requests_than_shared_memory_keeps(B, dev, eo, caches):
     rng = np.random.default_rng(10)
     new = rng.integers(0, 4, 300)
@@ -419,6 +436,12 @@ def test_values_beyond_fp16_do_not_leave_their_rows(B, dev, eo, caches, new):
     assert (np.abs(p.decoded[1][0]) == 65504).any()
     out, lse = p.run(True)
     p.check(out, lse, True)
+    # K beyond fp16's range, in tiles and taken at once: scores are what finite numbers give
+    k = Paged(B, eo, (big, metas[1]), (blocks[1], blocks[1]), [1, 2], [50, 40], 2, 1, 16, seed=15)
+    assert (np.abs(k.decoded[0][0]) == 65504).any()
+    for tiles in (4, 7000):
+        got, got_lse = k.run(True, scale=1e-6, batch=B.paged_batch(k.d_tables, k.stride, k.d_cu, k.d_lens, k.d_tiles, 2, k.tokens, 2, 50, tiles))
+        k.check(got, got_lse, True, scale=float(np.float32(1e-6)))
     # and a q that is not finite stays in the rows of its token
     clean = out.copy()
     p.d_q[0, :256] = math.inf
