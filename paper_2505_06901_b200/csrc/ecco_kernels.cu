@@ -760,6 +760,7 @@ extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k,
         g.k_blocks = cache->d_k_blocks; g.v_blocks = cache->d_v_blocks;
         g.slots = d_slots; g.token_stride = token_stride;
         g.heads = cache->n_kv_heads; g.page_shift = page_shift_of(cache->page_size); g.n_slots = cache->n_pages * cache->page_size;
+        g.inverse = static_cast<uint32_t>(std::min<uint64_t>((1ull << 32) / static_cast<uint64_t>(g.heads), UINT32_MAX));
         return launch_kv_compress(di, g, n_groups, kinds, s);
     };
     if (n_groups < kAppendTwoGroups) return launch(PagedGroups<2>{}, 2);

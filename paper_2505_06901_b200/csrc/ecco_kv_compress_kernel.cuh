@@ -31,7 +31,12 @@ struct DenseGroups {                                       // one after the othe
     __device__ __forceinline__ uint32_t ctas() const { return gridDim.x; }
     __device__ __forceinline__ Place place(uint64_t g) const { return g; }
     __device__ __forceinline__ const __half* source(Place g) const { return x + g * kGroup; }
-    __device__ __forceinline__ uint8_t* block(Place g) const { return blocks + g * kBlockBytes; }
+    __device__ __forceinline__ uint8_t* block(Place g) const
+    {
+        uint8_t* const p = blocks + g * kBlockBytes;
+        __builtin_assume(p != nullptr);                    // none is left out
+        return p;
+    }
 };
 // New tokens of a paged cache: group g is head g % heads of token g / heads.  kKind 0: K, 1: V, 2: even CTAs K, odd ones V.
 template <int kKind>
@@ -43,6 +48,7 @@ struct PagedGroups {
     const int32_t* slots;
     int64_t token_stride;
     int32_t heads, page_shift, n_slots;
+    uint32_t inverse;          // floor(2^32 / heads), one less for one head
     __device__ __forceinline__ bool is_v() const { return kKind == 2 ? blockIdx.x & 1u : kKind; }
     __device__ __forceinline__ const uint8_t* meta() const { return is_v() ? v_image : k_image; }
     __device__ __forceinline__ uint32_t cta() const { return kKind == 2 ? blockIdx.x >> 1 : blockIdx.x; }
@@ -50,8 +56,16 @@ struct PagedGroups {
     __device__ __forceinline__ Place place(uint64_t g) const
     {
         Place p;
-        p.token = static_cast<uint32_t>(divide(g, static_cast<uint64_t>(heads)));
-        p.head = static_cast<uint32_t>(g - static_cast<uint64_t>(p.token) * heads);
+        if (g >> 32) {
+            p.token = static_cast<uint32_t>(g / static_cast<uint32_t>(heads));
+            p.head = static_cast<uint32_t>(g - static_cast<uint64_t>(p.token) * heads);
+        } else {
+            // inverse is at most one below 2^32 / heads, so the product's upper half is the quotient or one less
+            const uint32_t n = static_cast<uint32_t>(g), d = static_cast<uint32_t>(heads);
+            p.token = __umulhi(n, inverse);
+            p.head = n - p.token * d;
+            if (p.head >= d) { ++p.token; p.head -= d; }
+        }
         return p;
     }
     __device__ __forceinline__ const __half* source(Place p) const { return (is_v() ? v : k) + p.token * token_stride + p.head * kGroup; }
@@ -68,7 +82,7 @@ constexpr int kKvWarps = 8;
 
 template <class Groups>
 __global__ void __launch_bounds__(kKvWarps * 32)
-ecco_kv_compress_kernel(const __grid_constant__ Groups groups, uint64_t n_groups)
+ecco_kv_compress_kernel(const Groups groups, uint64_t n_groups)
 {
     const uint8_t* const __restrict__ d_meta = groups.meta();
     __shared__ __align__(16) uint16_t pat_s[kMaxPatterns * 16];
@@ -307,7 +321,7 @@ __device__ __forceinline__ uint32_t kv_key(uint32_t half, int pos) { return ((ha
 
 template <class Groups>
 __global__ void __launch_bounds__(kKvManyWarps * 32, 1)
-ecco_kv_compress_many_kernel(const __grid_constant__ Groups groups, uint64_t n_groups)
+ecco_kv_compress_many_kernel(const Groups groups, uint64_t n_groups)
 {
     const uint8_t* const __restrict__ d_meta = groups.meta();
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -585,8 +599,10 @@ ecco_kv_compress_many_kernel(const __grid_constant__ Groups groups, uint64_t n_g
             }
         }
         __syncwarp();
-        uint8_t* const block = unit * 4 + grp < n_groups ? groups.block(place) : nullptr;
-        if (block) reinterpret_cast<uint2*>(block)[sub] = make_uint2(blk[sub * 2], blk[sub * 2 + 1]);
+        if (unit * 4 + grp < n_groups) {
+            uint8_t* const block = groups.block(place);
+            if (block) reinterpret_cast<uint2*>(block)[sub] = make_uint2(blk[sub * 2], blk[sub * 2 + 1]);
+        }
         __syncwarp();
     }
 }
