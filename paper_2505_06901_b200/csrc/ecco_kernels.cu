@@ -813,7 +813,7 @@ bool paged_batch_fine(const ecco_paged_cache& c, const ecco_paged_batch& b, int 
     if (b.n_req < 0 || b.n_req > 65535 || b.n_tokens < 0 || b.table_stride < 0 || b.max_new < 0 || b.max_kv < 0 || b.max_tiles < 0) return false;
     if (q_per_kv < 1 || q_per_kv > 16 || static_cast<int64_t>(c.n_kv_heads) * q_per_kv > 65535) return false;
     if (static_cast<int64_t>(b.max_tiles) * c.n_kv_heads > INT32_MAX / 2 || static_cast<int64_t>(b.max_tiles) > INT32_MAX / 32) return false;
-    if (static_cast<int64_t>(b.n_tokens) * c.n_kv_heads * q_per_kv > INT32_MAX) return false;
+    if (static_cast<int64_t>(b.n_tokens) * c.n_kv_heads * q_per_kv > INT32_MAX - 1024) return false;
     // tiles of all blocks of rows together are counted in 32 bits
     const int64_t blocks = static_cast<int64_t>(b.n_tokens) / (2 * tile_rows_tokens(q_per_kv)) + b.n_req + 1;
     return blocks * (static_cast<int64_t>(b.max_kv) / kManyTokens + 1) <= INT32_MAX;

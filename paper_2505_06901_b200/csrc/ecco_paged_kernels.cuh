@@ -338,7 +338,7 @@ __device__ __forceinline__ const uint8_t* paged_block(const PagedKv& kv, const u
 // and out (a piece leaves by one bulk copy of 1 KB).
 //   kHalves: even CTAs decode K, odd ones V: no CTA needs both sets of tables, and small calls decode K and V side by side.
 //   kBoth: every CTA decodes its share of K, then of V: another 4 us for the second set of tables, but caches
-//   whose blocks take differently long leave no CTA waiting (2.1 M groups of K and of V, 178 and 146 us alone: 377 -> 345 us).
+//   whose blocks take differently long leave no CTA waiting (2.1 M groups of K and of V, 178 and 146 us by ecco_decompress: 377 -> 362 us).
 // Values are clamped to fp16's finite range (once per group, on the sixteen values of its table): weight zero times an infinity would
 // be NaN in rows that do not see the token.
 //   kOnlyV: V alone, see ecco_paged_scores_kernel.
@@ -449,7 +449,7 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
 
 // K6k: products of K with one or two rows of q per request (a token each without grouped heads), instead of K in tiles: ecco_attn_scores_kernel with
 // another way to the blocks.  As fast as decoding K is, and half of the tiles need neither be written nor read (8 requests of 4048 tokens,
-// 32 heads: 261 us with K in tiles).
+// 32 heads: 261 -> 223 us).  With three rows and more the decoder slows down by as much as the tiles would take.
 template <int kV, int kMaxWarps>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, float* __restrict__ d_scores)
@@ -525,7 +525,8 @@ ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 //   S = Q K^T (16 rows x 32 tokens a tile, mma.sync), the softmax on the way in fp32, O += P V
 // with P taken from the scores' registers as they are.  A piece of a request that lies in one run as a whole is written out; the others
 // leave sums and maxima in the workspace and are joined by ecco_paged_combine_kernel.
-// Bound by memory: 512 bytes per token and KV head.
+// Bound by memory: 512 bytes per token and KV head (1.09 GB in 165 us, the copy rate); the products take as long at sixteen rows, mma.sync being
+// slow here, so requests of more rows are for ecco_paged_many_kernel (20 to 32 rows: 57 us here with two tiles of rows, 42 there).
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewRows = 16, kFewWarps = 6;
 // Of a stage of a warp's ring, and their number: K and V, or scores of up to two rows and V.

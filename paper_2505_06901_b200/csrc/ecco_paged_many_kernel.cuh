@@ -13,6 +13,12 @@ namespace {
 // Two tiles of rows share every K and V tile, and while one's products run, the other's softmax does.
 // Warps 0-3 and 4-7: softmax of the first and of the second tile of rows; warp 8: K and V; warp 9 issues the
 // products; warp 10: Q, and what there is to do (ManyTask); warp 11 only gives its registers away.
+// What carries it: operands that lie in uniform registers, waits that one vote decides (see below), weights sent in two halves, the
+// next block's Q and first scores under way while this one's sums are written out.  A tile of tokens takes two tiles of rows some 3100 clocks,
+// 2048 of them products: a thread's softmax (1.7 thousand clocks, 128 exponentials in it) and the products behind its last weights follow
+// one another.  2 x 2048 tokens x 32 heads over 8192 tokens, 469 GFLOP: 422 us = 1.11 PFLOP/s, at 1.6 of 1.9 GHz under the power limit.
+// (Measured equal or slower: the maximum searched for beside the first weights, an eighth or a quarter of the exponentials as polynomials, a warp
+// of products for each tile of rows, the tokens of a block of one tile of rows shared out between both tiles' warps.)
 // m is the row's maximum when it was last taken; a larger one is taken only when it is more than 2^8 larger (the weights are fp16
 // times 2^7, at most 2^15), so O is rescaled now and then instead of with every tile.
 //
@@ -184,7 +190,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, base = smem_u32(smem);
     // barriers: tiles have come / are free again, Q there, S there, P there, O there
-    const uint32_t full_at = base, free_at = base + 8 * kManyStages, q_bar = base + 128, s_bar = base + 144, p_bar = base + 160 /* halves, tiles of rows */, o_bar = base + 192, q_free = base + 208, end_bar = base + 224;
+    const uint32_t full_at = base, free_at = base + 8 * kManyStages, q_bar = base + 128, s_bar = base + 144, p_bar = base + 160 /* halves, tiles of rows */, o_bar = base + 192, q_free = base + 208, end_bar = base + 224, in_bar = base + 272, told_bar = base + 288;
     const uint32_t q_smem = base + 1024, ring = q_smem + 2 * kOperandBytes;
     uint32_t* const tmem_word = reinterpret_cast<uint32_t*>(smem + 256);
     volatile int* const failed = reinterpret_cast<volatile int*>(smem + 264);
@@ -194,6 +200,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     if (threadIdx.x == 0) {
         for (int i = 0; i < kManyStages; ++i) { mbar_init(full_at + 8 * i, 1); mbar_init(free_at + 8 * i, 1); }
         for (int x = 0; x < 2; ++x) { mbar_init(q_bar + 8 * x, 1); mbar_init(q_free + 8 * x, 5); mbar_init(s_bar + 8 * x, 1); mbar_init(p_bar + 8 * x, 4); mbar_init(p_bar + 16 + 8 * x, 4); mbar_init(o_bar + 8 * x, 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(in_bar + 8 * x, 4); mbar_init(told_bar + 8 * x, 1); }
         mbar_init(end_bar, 1);
         *failed = 0;
     }
@@ -235,7 +242,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         const int32_t in_tile = static_cast<int32_t>(t) / o.q_per_kv, g = static_cast<int32_t>(t) - in_tile * o.q_per_kv;       // new token, query head
         // a scale of zero as a small one: times minus infinity it is still minus infinity
         const float scale = fabsf(o.scale_log2) < 1e-30f ? 1e-30f : o.scale_log2, unseen = scale > 0.0f ? -INFINITY : INFINITY;
-        uint32_t n_piece = 0, n_s = 0, n_o = 0;            // pieces, S and O waited for
+        uint32_t n_piece = 0, n_s = 0, n_o = 0, n_join = 0;        // pieces, S, O and joins waited for
         bool ok = true;
         for (int64_t u = u0; u < u1 && ok;) {
             ok = wait(q_bar + 8 * x, n_piece & 1u);
@@ -358,11 +365,16 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             }
             tmem_fence_before();                           // O has been read before the next block's P arrives
             if (!whole) {
-                // the tile's four warps count themselves in; the last run's read all pieces, a warp to a row
+                // The tile's four warps count themselves in; the last run's read all pieces, a warp to eight rows.  (They meet at barriers whose
+                // waits are bounded: a warp that has given up does not come.)
                 __threadfence();
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + x) : "memory");
-                if (t == 0) last_in[x] = atomicAdd(sc.tickets + 2 * pc.run_lo + x, 1) == pc.run_hi - pc.run_lo;
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + x) : "memory");
+                warp_arrive(in_bar + 8 * x);
+                if ((warp & 3u) == 0 && wait(in_bar + 8 * x, n_join & 1u)) {
+                    if (lane == 0) last_in[x] = atomicAdd(sc.tickets + 2 * pc.run_lo + x, 1) == pc.run_hi - pc.run_lo;
+                    warp_arrive(told_bar + 8 * x);
+                }
+                ok = wait(told_bar + 8 * x, n_join++ & 1u);
+                if (!ok) break;
                 if (last_in[x]) {
                     __threadfence();
                     // eight rows at a time, so that their loads are on their way together
@@ -519,6 +531,9 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             ++n;
             u = pc.next;
         }
+        if (n && *failed)                                  // what is on its way lands before the CTA leaves
+            for (uint32_t x = 0; x < 2; ++x)
+                for (int k = 0; k < kWaitLimit && !mbar_try_wait(q_bar + 8 * x, (n - 1) & 1u); ++k) {}
     }
     tmem_fence_before();
     __syncthreads();
