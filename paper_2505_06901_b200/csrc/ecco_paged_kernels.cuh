@@ -70,7 +70,7 @@ ecco_paged_plan_kernel(const PagedPlan p)
         lengths(r, ctx, added);
         if (r == tid) { ctx0 = ctx; added0 = added; }
         const long long kv = static_cast<long long>(ctx) + added;
-        fine = fine && ctx >= 0 && added >= 0 && kv <= static_cast<long long>(p.stride) << p.page_shift;
+        fine = fine && ctx >= 0 && added >= 0 && kv <= INT32_MAX && kv <= static_cast<long long>(p.stride) << p.page_shift;
         sum[0] += added;
         sum[1] += ((kv + page_size - 1) >> p.page_shift) - ((static_cast<long long>(ctx) + page_size - 1) >> p.page_shift);
         sum[2] += (kv + 31) >> 5;
@@ -141,7 +141,7 @@ ecco_paged_plan_kernel(const PagedPlan p)
 //   eight [32 tokens][16 dims] fp16 pieces of 1 KB, the 16-byte halves of a 32-byte row swapped in every second block of four rows
 // which is what the decoder's staging pieces look like in shared memory, what ldmatrix reads without conflicts, and, for tcgen05, the
 // canonical layout of both a K operand (contraction over dims, K-major) and a V operand (contraction over tokens, MN-major)
-// with 32-byte swizzle.  One layout for all, moved by plain bulk copies.
+// with 32-byte swizzle.  One layout for all, moved by bulk copies.
 // Decoding inside of the attention kernel instead leaves the decoder 17 warps (9.6 KB of tiles per warp and two sets of tables) instead
 // of 31 and one symbol per lookup instead of two, and decodes again for every row tile.
 // ---------------------------------------------------------------------------------------------
@@ -358,7 +358,7 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
         const int which = kKind == kBoth ? phase : kKind == kOnlyV ? 1 : static_cast<int>(blockIdx.x & 1u);
         const uint8_t* const d_meta = which ? kv.v_meta : kv.k_meta;
         const DecodeTables tb = plan_decode_tables(smem_u32(smem), d_meta, true);
-        if (phase) {                                           // see ecco_decompress_tma_kernel
+        if (phase) {                                       // see ecco_decompress_tma_kernel
             fence_async_smem();
             __syncthreads();
         }
@@ -524,7 +524,7 @@ ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 // alone from its first tile to its last.  It keeps a ring of tiles in shared memory, filled by bulk copies, and does
 //   S = Q K^T (16 rows x 32 tokens a tile, mma.sync), the softmax on the way in fp32, O += P V
 // with P taken from the scores' registers as they are.  A piece of a request that lies in one run as a whole is written out; the others
-// leave sums and maxima in the workspace and are joined by ecco_paged_combine_kernel.
+// leave sums and maxima in the workspace and are joined by ecco_paged_join_kernel.
 // Bound by memory: 512 bytes per token and KV head (1.09 GB in 165 us, the copy rate); the products take as long at sixteen rows, mma.sync being
 // slow here, so requests of more rows are for ecco_paged_many_kernel (20 to 32 rows: 57 us here with two tiles of rows, 42 there).
 // ---------------------------------------------------------------------------------------------
@@ -550,12 +550,6 @@ __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float log2_fast(float x)
-{
-    float y;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 // natural logarithm of a sum of weights that stands at l * 2^(m - offset)
@@ -654,7 +648,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         if (!kScores) {
             // the rows of q as tiles: rows beyond the last are zero
             __syncwarp();
-            uint4 rows[8];                                     // sixteen lanes to a row, two rows at a time, all on their way together
+            uint4 rows[8];                                 // sixteen lanes to a row, two rows at a time, all on their way together
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int row = 2 * i + static_cast<int>(lane >> 4), token = row / o.q_per_kv, g = row - token * o.q_per_kv;
