@@ -770,8 +770,10 @@ extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k,
 
 namespace {
 constexpr float kLog2E = 1.4426950408889634f;
-// Tiles per warp (of each kind) from which on every CTA decodes both kinds.
-constexpr int kStageBothTiles = 3;
+// Tiles per warp (of each kind) from which on every CTA decodes both kinds (between one and three it makes no difference), and from
+// which on one or two rows to a request take the products with K at once (8 requests of 1600 tokens, 32 heads, 2.8 tiles: 118 -> 106 us;
+// of 1024, 1.8 tiles: 80 -> 75; of 800, 1.4 tiles: 67 -> 66).
+constexpr int kStageBothTiles = 3, kScoresTiles = 1;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
 //   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks, tickets, cuts | few rows: sums, maxima | many rows: sums, maxima
 struct PagedAttnPlan {
@@ -950,9 +952,8 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         // Small calls decode K in half of the CTAs and V in the other half.  Large ones decode both in every CTA, or, for one or two rows
         // to a request, take the products with K at once.
         const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
-        const bool large = units >= static_cast<int64_t>(kStageBothTiles) * 31 * di.sms;
-        const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
-        const bool scores = large && (rows == 1 || rows == 2);
+        const int64_t per_warp = units / (31 * di.sms), rows = static_cast<int64_t>(b.max_new) * q_per_kv;
+        const bool scores = per_warp >= kScoresTiles && (rows == 1 || rows == 2);
         if (scores) {
             // where K's tiles would be
             float* const at = reinterpret_cast<float*>(kv.staged + static_cast<size_t>(kv.heads) * kv.max_tiles * kKvTileBytes);
@@ -961,7 +962,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
             rc = rows == 1 ? launch_paged_scores<1>(di, kv, o, at, units, s) : launch_paged_scores<2>(di, kv, o, at, units, s);
             if (!rc) rc = launch_paged_stage<kOnlyV>(di, kv, o, sc, units, s);
         } else {
-            rc = large ? launch_paged_stage<kBoth>(di, kv, o, sc, units, s) : launch_paged_stage<kHalves>(di, kv, o, sc, units, s);
+            rc = per_warp >= kStageBothTiles ? launch_paged_stage<kBoth>(di, kv, o, sc, units, s) : launch_paged_stage<kHalves>(di, kv, o, sc, units, s);
         }
         if (rc) return rc;
         o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
