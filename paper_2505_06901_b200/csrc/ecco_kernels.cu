@@ -795,14 +795,15 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
         at = (at + bytes + 255) & ~static_cast<size_t>(255);
         return here;
     };
-    const size_t few_slots = static_cast<size_t>(p.few_ctas) * kFewWarps * 2 * kFewRows;
+    static_assert(kFewWarps<true> >= kFewWarps<false>, "places for either");
+    const size_t few_slots = static_cast<size_t>(p.few_ctas) * kFewWarps<true> * 2 * kFewRows;
     const size_t many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
     p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
     p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
     p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
     p.n_blocks = take(4);
     p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
-    p.cuts = take(static_cast<size_t>(p.few_ctas) * kFewWarps * sizeof(FewCut));
+    p.cuts = take(static_cast<size_t>(p.few_ctas) * kFewWarps<true> * sizeof(FewCut));
     p.few_part = take(few_slots * kGroup * sizeof(float));
     p.few_ml = take(few_slots * sizeof(float2));
     p.many_part = take(many_slots * kGroup * sizeof(float));
@@ -866,9 +867,9 @@ int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o,
         if (rc) return rc;
         configured[di.device] = true;
     }
-    const int rc = launch_overlapped(ecco_paged_few_kernel<kScores>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps * 32), kFewSmemBytes<kScores>, s, kv, o, sc);
+    const int rc = launch_overlapped(ecco_paged_few_kernel<kScores>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps<kScores> * 32), kFewSmemBytes<kScores>, s, kv, o, sc);
     if (rc) return rc;
-    const int runs = p.few_ctas * kFewWarps;
+    const int runs = p.few_ctas * kFewWarps<kScores>;
     return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(runs), 256u, 0, s, o, kv.head0);
 }
 template <StageKind kKind>

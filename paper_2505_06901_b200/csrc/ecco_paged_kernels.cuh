@@ -528,20 +528,22 @@ ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 // Bound by memory: 512 bytes per token and KV head (1.09 GB in 165 us, the copy rate); the products take as long at sixteen rows, mma.sync being
 // slow here, so requests of more rows are for ecco_paged_many_kernel (20 to 32 rows: 57 us here with two tiles of rows, 42 there).
 // ---------------------------------------------------------------------------------------------
-constexpr int kFewRows = 16, kFewWarps = 6;
+constexpr int kFewRows = 16;
+template <bool kScores> constexpr int kFewWarps = kScores ? 8 : 6;
 // Of a stage of a warp's ring, and their number: K and V, or scores of up to two rows and V.
 template <bool kScores> constexpr uint32_t kFewTileBytes = kScores ? kKvTileBytes + 256 : 2 * kKvTileBytes;
-template <bool kScores> constexpr int kFewStages = kScores ? 4 : 2;
+template <bool kScores> constexpr int kFewStages = kScores ? 3 : 2;
 template <bool kScores> constexpr uint32_t kFewWarpBytes = kFewStages<kScores> * kFewTileBytes<kScores> + (kScores ? 0 : kFewRows * 256);
-template <bool kScores> constexpr uint32_t kFewSmemBytes = kFewWarps * kFewWarpBytes<kScores> + 1024;
+template <bool kScores> constexpr uint32_t kFewSmemBytes = kFewWarps<kScores> * kFewWarpBytes<kScores> + 1024;
 // Runs of the line: one per warp, but of three tiles, or joining costs more than waiting (16 requests of 4 to 8 drafted tokens, 2048 tiles: 158
 // us with runs of two or three tiles, 145 with three), unless there are so few tiles that every run has just one (2 requests of 780 tokens,
 // 400 tiles: 24.4 us with runs of three, 20.4 with runs of one).
 constexpr int kFewRunTiles = 3;
+template <bool kScores>
 __device__ __forceinline__ UnitSplit few_split(int64_t units, int ctas)
 {
     const int64_t runs = units <= static_cast<int64_t>(ctas) * 3 ? units : max(units / kFewRunTiles, static_cast<int64_t>(ctas) * 2);
-    return UnitSplit(units, static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(ctas) * kFewWarps, runs))));
+    return UnitSplit(units, static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(ctas) * kFewWarps<kScores>, runs))));
 }
 
 // Weights enter the tensor cores times 2^15: taken as they are, those below 6e-5 would lose bits and those below 3e-8 vanish.
@@ -576,7 +578,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
 
 // kScores: the products with K are there already (ecco_paged_scores_kernel), only V is in tiles.
 template <bool kScores>
-__global__ void __launch_bounds__(kFewWarps * 32, 1)
+__global__ void __launch_bounds__(kFewWarps<kScores> * 32, 1)
 ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -594,7 +596,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);
     const int wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
     const int64_t U = static_cast<int64_t>(line) * kv.heads;
-    const UnitSplit split = few_split(U, static_cast<int>(gridDim.x));
+    const UnitSplit split = few_split<kScores>(U, static_cast<int>(gridDim.x));
     const int64_t u0 = min(split.begin(wg), U), u1 = min(split.begin(wg + 1), U);     // warps beyond the runs: nothing
 
     // a place in the run: unit u is tile `tile` of head `head`; the request it belongs to has units [begin, end), cut to the run's end
