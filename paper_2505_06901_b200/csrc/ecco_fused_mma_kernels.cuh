@@ -20,12 +20,12 @@ namespace {
 __device__ __forceinline__ void load_vfrag(uint32_t (&vfrag)[16], const __half* base, size_t col_stride, int n_cols);
 
 // kDeal, keep: see decode_to_tiles (the scores of lanes past the end of a row are not wanted)
-template <bool kDeal, class FetchVectors>
+template <bool kDeal, bool kFinite = false, class FetchVectors>
 __device__ __forceinline__ void row_dot_mma(const Block& blk, const DecodeTables& tb, uint32_t tiles, float T, bool keep,
                                             FetchVectors&& fetch_vectors, float (&acc)[2][4])
 {
     const uint32_t lane = threadIdx.x & 31u;
-    decode_to_tiles<true, kDeal>(blk, tb, tiles, T, keep);
+    decode_to_tiles<true, kDeal, kFinite>(blk, tb, tiles, T, keep);
     uint32_t vfrag[16];
     fetch_vectors(vfrag);
     const uint32_t a_at = tiles + tile_byte(((lane >> 3) & 1u) * 8 + (lane & 7u), (lane >> 4) * 8);

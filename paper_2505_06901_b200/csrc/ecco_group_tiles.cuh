@@ -53,13 +53,14 @@ __device__ __forceinline__ uint32_t tile_byte(uint32_t r, uint32_t c) { return r
 
 // One group per lane, outliers in place; a lane with keep = false contributes zeros.  The tiles are complete when this returns.
 // kDeal: deal_outliers (caches) or every lane its own (weights).
-template <bool kSpread, bool kDeal>
+// kFinite: values beyond fp16's range are +-65504 instead of infinities.
+template <bool kSpread, bool kDeal, bool kFinite = false>
 __device__ __forceinline__ void decode_to_tiles(const Block& blk, const DecodeTables& tb, uint32_t tiles, float T, bool keep)
 {
     const uint32_t lane = threadIdx.x & 31u, bits = tiles + 7 * kTileBytes + lane * 4;
     const uint32_t my_row = tiles + lane * 32, swz = ((lane >> 2) & 1u) << 4;
     __syncwarp();                                          // the tiles of the previous groups have been read
-    LaneGroup g = open_block(blk, bits, tb, T);
+    LaneGroup g = open_block<kFinite>(blk, bits, tb, T);
     uint32_t even[4] = {0, 0, 0, 0};
     const uint32_t end = decode_group_by_one<kBlockBits, kBlockFreeSteps>(g, bits, [&](int i, uint32_t ranks, bool cutting, int n_ok) {
         uint32_t v[4];
@@ -82,7 +83,8 @@ __device__ __forceinline__ void decode_to_tiles(const Block& blk, const DecodeTa
     // outliers of a complete group replace the mapped values in the tiles
     auto put = [&](uint32_t owner, uint32_t f) {
         const uint32_t loc = f & 127u, i = loc & 15u;
-        sts_u16(tiles + (loc >> 4) * kTileBytes + tile_byte(owner, kSpread ? tile_column(i) : i), f2h_bits(fp8_to_float(f >> 7) * T));
+        sts_u16(tiles + (loc >> 4) * kTileBytes + tile_byte(owner, kSpread ? tile_column(i) : i),
+                f2h_bits(kFinite ? fminf(fmaxf(fp8_to_float(f >> 7) * T, -65504.0f), 65504.0f) : fp8_to_float(f >> 7) * T));
     };
     const int n_pad = keep ? pads_of(end) : 0;
     if (!kDeal) {

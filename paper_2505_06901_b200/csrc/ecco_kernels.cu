@@ -772,8 +772,9 @@ namespace {
 constexpr float kLog2E = 1.4426950408889634f;
 // Tiles per warp (of each kind) from which on every CTA decodes both kinds (between one and three it makes no difference), and from
 // which on one or two rows to a request take the products with K at once (8 requests of 1600 tokens, 32 heads, 2.8 tiles: 118 -> 106 us;
-// of 1024, 1.8 tiles: 80 -> 75; of 800, 1.4 tiles: 67 -> 66).
-constexpr int kStageBothTiles = 3, kScoresTiles = 1;
+// of 1024, 1.8 tiles: 80 -> 75; of 800, 1.4 tiles: 67 -> 66).  With three to eight rows that pays later: 8 requests, 8 heads, three / eight
+// rows, 2.1 tiles: 99 / 101 -> 103 / 106; 4.1 tiles: 163 / 167 -> 164 / 170; 6.1 tiles: 234 / 234 -> 225 / 234; 13.6 tiles: 530 / 531 -> 506 / 520.
+constexpr int kStageBothTiles = 3, kScoresTiles = 1, kScoresMmaTiles = 6;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
 //   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks, tickets, cuts | few rows: sums, maxima | many rows: sums, maxima
 struct PagedAttnPlan {
@@ -892,6 +893,15 @@ int launch_paged_scores(const DeviceInfo& di, const PagedKv& kv, const PagedOut&
     const int ctas = std::max(1, spread_ctas(units, di.sms));
     return launch_overlapped(kernel, static_cast<unsigned>(ctas), spread_threads(units, ctas, fused_warps(kV)), kSmemCtaBytes, s, kv, o, scores);
 }
+int launch_paged_scores_mma(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, float* scores, int64_t units, cudaStream_t s)
+{
+    static thread_local bool configured[64] = {};
+    auto kernel = ecco_paged_scores_mma_kernel<kMmaWarps>;
+    int rc = want_all_smem(kernel, &configured[di.device]);
+    if (rc) return rc;
+    const int ctas = std::max(1, spread_ctas(units, di.sms));
+    return launch_overlapped(kernel, static_cast<unsigned>(ctas), spread_threads(units, ctas, kMmaWarps), kSmemCtaBytes, s, kv, o, scores);
+}
 }  // namespace
 
 extern "C" size_t ecco_paged_attn_workspace_bytes(const ecco_paged_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv)
@@ -950,17 +960,19 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         sc.few_rows = kFewRows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
         sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
-        // Small calls decode K in half of the CTAs and V in the other half.  Large ones decode both in every CTA, or, for one or two rows
-        // to a request, take the products with K at once.
+        // Small calls decode K in half of the CTAs and V in the other half.  Large ones decode both in every CTA, or, for up to eight
+        // rows to a request, take the products with K at once.
         const int64_t units = static_cast<int64_t>(b.max_tiles) * kv.heads;
         const int64_t per_warp = units / (31 * di.sms), rows = static_cast<int64_t>(b.max_new) * q_per_kv;
-        const bool scores = per_warp >= kScoresTiles && (rows == 1 || rows == 2);
+        const bool scores = rows >= 1 && rows <= kScoreRows && per_warp >= (rows <= 2 ? kScoresTiles : kScoresMmaTiles);
         if (scores) {
             // where K's tiles would be
             float* const at = reinterpret_cast<float*>(kv.staged + static_cast<size_t>(kv.heads) * kv.max_tiles * kKvTileBytes);
             o.scores = at;
             o.score_rows = static_cast<int32_t>(rows);
-            rc = rows == 1 ? launch_paged_scores<1>(di, kv, o, at, units, s) : launch_paged_scores<2>(di, kv, o, at, units, s);
+            rc = rows == 1   ? launch_paged_scores<1>(di, kv, o, at, units, s)
+                 : rows == 2 ? launch_paged_scores<2>(di, kv, o, at, units, s)
+                             : launch_paged_scores_mma(di, kv, o, at, units, s);
             if (!rc) rc = launch_paged_stage<kOnlyV>(di, kv, o, sc, units, s);
         } else {
             rc = per_warp >= kStageBothTiles ? launch_paged_stage<kBoth>(di, kv, o, sc, units, s) : launch_paged_stage<kHalves>(di, kv, o, sc, units, s);

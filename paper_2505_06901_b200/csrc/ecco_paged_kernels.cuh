@@ -218,7 +218,7 @@ struct PagedOut {
     float2* part_ml;           // maxima (log2) and sums of weights [slot][rows]
     FewCut* cuts;              // [run]
     int32_t discard;           // the tiles begin at multiples of 128 bytes
-    const float* scores;       // [heads][max_tiles][score_rows][32]: products of q and K, see ecco_paged_scores_kernel
+    const float* scores;       // [heads][max_tiles][score_rows][32]: products of q and K, see K6k
     int32_t score_rows;
     int32_t early;             // ecco_paged_few_kernel comes behind ecco_paged_many_kernel
 };
@@ -447,9 +447,57 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
     }
 }
 
-// K6k: products of K with one or two rows of q per request (a token each without grouped heads), instead of K in tiles: ecco_attn_scores_kernel with
-// another way to the blocks.  As fast as decoding K is, and half of the tiles need neither be written nor read (8 requests of 4048 tokens,
-// 32 heads: 261 -> 223 us).  With three rows and more the decoder slows down by as much as the tiles would take.
+// K6k: products of K with one to eight rows of q per request (new tokens x query heads per KV head), instead of K in tiles:
+// ecco_attn_scores_kernel and ecco_attn_scores_mma_kernel with another way to the blocks.  Half of the tiles need neither be written nor read.
+// One or two rows are as fast as decoding K is (8 requests of 4048 tokens, 32 heads: 261 -> 223 us).  Three to eight go through the warp's
+// own tiles to the tensor cores, with 20 warps and one symbol per lookup: slower than the decoder alone, but by less than K's way through
+// memory takes (32 requests of 1 to 16384 tokens, 8 heads, three / eight rows: 530 / 531 -> 506 / 520 us).
+//
+// The walk over a warp's tiles: tile by tile of head by head; use(block, there, head, tile, request, whether the request or the head is another one)
+template <class Use>
+__device__ __forceinline__ void walk_tiles(const PagedKv& kv, const int32_t* firsts, int nw, Use&& use)
+{
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
+    const int32_t n_tiles = paged_tiles(kv);
+    const int64_t U = static_cast<int64_t>(n_tiles) * kv.heads;
+    const int wg = warp < nw ? warp * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x) : INT_MAX;
+    const int W = static_cast<int>(balanced_warps(static_cast<uint64_t>(U), gridDim.x * static_cast<uint32_t>(nw)));
+    if (wg >= W) return;
+    const UnitSplit split(U, W);
+    const int64_t u0 = split.begin(wg);
+    int32_t head = static_cast<int32_t>(divide(static_cast<uint64_t>(u0), static_cast<uint64_t>(n_tiles))), tile = static_cast<int32_t>(u0 - static_cast<int64_t>(head) * n_tiles);
+    int32_t first;
+    int r = request_of(kv, firsts, tile, first), of_head = -1, of_request = -1;
+    auto block_ptr = [&]() { return paged_block(kv, kv.k_blocks, r, (static_cast<int64_t>(tile) - first) * 32 + lane, head); };
+    const uint8_t* next = block_ptr();
+    for (int left = static_cast<int>(split.begin(wg + 1) - u0); left > 0; --left) {
+        const int32_t this_head = head, this_tile = tile;
+        const int this_r = r;
+        Block cur;
+        const bool there = next != nullptr;
+        if (there) {
+            ldg_block(cur, next);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) cur.w[i] = 0;
+        }
+        if (left > 1) {
+            if (++tile == n_tiles) { tile = 0; ++head; }
+            r = request_of(kv, firsts, tile, first);
+            next = block_ptr();
+            if (next) prefetch_block_l2(next);
+        }
+        use(cur, there, this_head, this_tile, this_r, this_head != of_head || this_r != of_request);
+        of_head = this_head;
+        of_request = this_r;
+    }
+}
+// Row i of a request's q for a head of the launch, NULL where there is none.
+__device__ __forceinline__ const __half* paged_row(const PagedKv& kv, const PagedOut& o, const PagedReq& q, int32_t head, int i)
+{
+    const int token = i / o.q_per_kv, g = i - token * o.q_per_kv;
+    return token < q.rows ? o.q + (q.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + head) * o.q_per_kv + g) * kGroup : nullptr;
+}
 template <int kV, int kMaxWarps>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1)
 ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, float* __restrict__ d_scores)
@@ -466,56 +514,71 @@ ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
     if (!finish_decode_tables(tb)) return;
     dependency_wait();
     fetch_firsts(kv, firsts);
-    const int32_t n_tiles = paged_tiles(kv);
-    const int64_t U = static_cast<int64_t>(n_tiles) * kv.heads;
-    const int wg = warp < nw ? warp * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x) : INT_MAX;
-    const int W = static_cast<int>(balanced_warps(static_cast<uint64_t>(U), gridDim.x * static_cast<uint32_t>(nw)));
-    if (wg >= W) return;
-    const UnitSplit split(U, W);
-    const int64_t u0 = split.begin(wg), u1 = split.begin(wg + 1);
     const float T = tb.T;
-
-    int32_t head = static_cast<int32_t>(divide(static_cast<uint64_t>(u0), static_cast<uint64_t>(n_tiles))), tile = static_cast<int32_t>(u0 - static_cast<int64_t>(head) * n_tiles);
-    int32_t first;
-    int r = request_of(kv, firsts, tile, first), of_head = -1, of_request = -1;
-    auto block_ptr = [&]() { return paged_block(kv, kv.k_blocks, r, (static_cast<int64_t>(tile) - first) * 32 + lane, head); };
-    const uint8_t* next = block_ptr();
-    for (int64_t u = u0; u < u1; ++u) {
-        if (head != of_head || r != of_request) {
+    walk_tiles(kv, firsts, nw, [&](const Block& cur, bool there, int32_t head, int32_t tile, int r, bool other) {
+        if (other) {
             // lane l brings elements 4l .. 4l+3 of every row; rows that there are not are zero
-            const PagedReq q = paged_req(kv, r, n_tiles);
+            const PagedReq q = paged_req(kv, r, paged_tiles(kv));
             __syncwarp();                                  // every lane is done with the rows before
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
-                const int token = i / o.q_per_kv, g = i - token * o.q_per_kv;
-                uint2 raw = make_uint2(0u, 0u);
-                if (token < q.rows) raw = __ldcg(reinterpret_cast<const uint2*>(o.q + (q.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + head) * o.q_per_kv + g) * kGroup) + lane);
+                const __half* const row = paged_row(kv, o, q, head, i);
+                const uint2 raw = row ? __ldcg(reinterpret_cast<const uint2*>(row) + lane) : make_uint2(0u, 0u);
                 sts_v2(xs + i * (kGroup * 2) + lane * 8, raw.x, raw.y);
             }
             __syncwarp();
-            of_head = head;
-            of_request = r;
-        }
-        Block cur;
-        const bool there = next != nullptr;
-        if (there) {
-            ldg_block(cur, next);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) cur.w[i] = 0;
-        }
-        float* const dst = d_scores + (static_cast<int64_t>(head) * kv.max_tiles + tile) * (kV * 32) + lane;
-        if (u + 1 < u1) {
-            if (++tile == n_tiles) { tile = 0; ++head; }
-            r = request_of(kv, firsts, tile, first);
-            next = block_ptr();
-            if (next) prefetch_block_l2(next);
         }
         float acc[kV][kChains] = {};
         fused_group<kV, true, true>(cur, tb, bits, T, xs, there, acc);
+        float* const dst = d_scores + (static_cast<int64_t>(head) * kv.max_tiles + tile) * (kV * 32) + lane;
 #pragma unroll
         for (int i = 0; i < kV; ++i) dst[i * 32] = sum_of(acc[i]);
-    }
+    });
+}
+template <int kMaxWarps>
+__global__ void __launch_bounds__(kMaxWarps * 32, 1)
+ecco_paged_scores_mma_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, float* __restrict__ d_scores)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    int32_t* const firsts = reinterpret_cast<int32_t*>(smem + 64);
+    release_dependents();
+    const DecodeTables tb = plan_decode_tables(smem_u32(smem), kv.k_meta, false);    // one symbol per lookup: the tiles need the room
+    const int nw = static_cast<int>(decode_warps(tb, kTiledWarpBytes));
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5);
+    const uint32_t tiles_at = tb.warp_base + warp * kTiledWarpBytes;
+    issue_decode_tables(tb, kv.k_meta);
+    if (!finish_decode_tables(tb)) return;
+    dependency_wait();
+    fetch_firsts(kv, firsts);
+    const float T = tb.T;
+    uint32_t vfrag[16];                                    // as load_vfrag has them: row lane / 4
+    walk_tiles(kv, firsts, nw, [&](const Block& cur, bool there, int32_t head, int32_t tile, int r, bool other) {
+        if (other) {
+            const PagedReq q = paged_req(kv, r, paged_tiles(kv));
+            const __half* const row = (lane >> 2) < o.score_rows ? paged_row(kv, o, q, head, lane >> 2) : nullptr;
+            const uint2* const p = reinterpret_cast<const uint2*>(row) + (lane & 3);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const uint2 v = row ? __ldcg(p + c * 4) : make_uint2(0u, 0u);
+                vfrag[2 * c] = v.x;
+                vfrag[2 * c + 1] = v.y;
+            }
+        }
+        float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        row_dot_mma<true, true>(cur, tb, tiles_at, T, there,
+                                [&](uint32_t (&v)[16]) {
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) v[i] = vfrag[i];
+                                }, acc);
+        float* const dst = d_scores + (static_cast<int64_t>(head) * kv.max_tiles + tile) * (o.score_rows * 32);
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 16 * mt + (lane >> 2) + (i >= 2 ? 8 : 0), row = (lane & 3) * 2 + (i & 1);
+                if (row < o.score_rows) dst[row * 32 + t] = acc[mt][i];
+            }
+    });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -530,8 +593,9 @@ ecco_paged_scores_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewRows = 16;
 template <bool kScores> constexpr int kFewWarps = kScores ? 8 : 6;
-// Of a stage of a warp's ring, and their number: K and V, or scores of up to two rows and V.
-template <bool kScores> constexpr uint32_t kFewTileBytes = kScores ? kKvTileBytes + 256 : 2 * kKvTileBytes;
+// Of a stage of a warp's ring, and their number: K and V, or V and scores of up to eight rows.
+constexpr int kScoreRows = 8;
+template <bool kScores> constexpr uint32_t kFewTileBytes = kScores ? kKvTileBytes + kScoreRows * 128 : 2 * kKvTileBytes;
 template <bool kScores> constexpr int kFewStages = kScores ? 3 : 2;
 template <bool kScores> constexpr uint32_t kFewWarpBytes = kFewStages<kScores> * kFewTileBytes<kScores> + (kScores ? 0 : kFewRows * 256);
 template <bool kScores> constexpr uint32_t kFewSmemBytes = kFewWarps<kScores> * kFewWarpBytes<kScores> + 1024;
@@ -576,7 +640,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity)
     return done;
 }
 
-// kScores: the products with K are there already (ecco_paged_scores_kernel), only V is in tiles.
+// kScores: the products with K are there already (K6k), only V is in tiles.
 template <bool kScores>
 __global__ void __launch_bounds__(kFewWarps<kScores> * 32, 1)
 ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc)

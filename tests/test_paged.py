@@ -401,12 +401,14 @@ def test_attention_of_a_padded_batch(B, dev, eo, caches):
 @pytest.mark.gpu
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("new,kv,heads,g", [([1, 1, 1], [300, 1, 64], 3, 1), ([1, 0, 1, 1], [2000, 5, 0, 33], 2, 1), ([1, 1], [70, 129], 2, 2), ([2, 1, 2], [90, 1, 2], 1, 1),
-                                            ([1] * 260, list(range(260)), 1, 2), ([2, 1], [40, 64], 2, 4), ([20, 1], [100, 300], 1, 3)])
+                                            ([1] * 260, list(range(260)), 1, 2), ([2, 1], [40, 64], 2, 4), ([20, 1], [100, 300], 1, 3),
+                                            ([1, 0, 1], [700, 3, 31], 2, 3), ([2, 1, 0, 2], [33, 500, 0, 2], 3, 3), ([3, 1], [3, 77], 1, 2), ([5, 7], [64, 7], 1, 1),
+                                            ([1] * 260, list(range(260)), 1, 8), ([3, 1], [90, 300], 2, 3)])
 def test_attention_of_large_calls(B, dev, eo, caches, new, kv, heads, g, causal):
-    """The ways of a call whose bounds say that it is large: K and V in every CTA, and, for one or two rows to a request, products with K
+    """The ways of a call whose bounds say that it is large: K and V in every CTA, and, for up to eight rows to a request, products with K
     instead of K in tiles."""
     p = Paged(B, eo, *caches, new, kv, heads, g, 16, seed=41)
-    b = B.paged_batch(p.d_tables, p.stride, p.d_cu, p.d_lens, p.d_tiles, len(new), p.tokens, max(new), max(kv), 14000 // heads + 1)
+    b = B.paged_batch(p.d_tables, p.stride, p.d_cu, p.d_lens, p.d_tiles, len(new), p.tokens, max(new), max(kv), 28000 // heads + 1)
     out, lse = p.run(causal, batch=b)
     p.check(out, lse, causal)
     small, _ = p.run(causal)
@@ -441,8 +443,8 @@ def test_values_beyond_fp16_do_not_leave_their_rows(B, dev, eo, caches, new):
     # K beyond fp16's range, in tiles and taken at once: scores are what finite numbers give
     k = Paged(B, eo, (big, metas[1]), (blocks[1], blocks[1]), [1, 2], [50, 40], 2, 1, 16, seed=15)
     assert (np.abs(k.decoded[0][0]) == 65504).any()
-    for tiles in (4, 7000):
-        got, got_lse = k.run(True, scale=1e-6, batch=B.paged_batch(k.d_tables, k.stride, k.d_cu, k.d_lens, k.d_tiles, 2, k.tokens, 2, 50, tiles))
+    for bound, tiles in ((2, 4), (2, 7000), (3, 14000)):
+        got, got_lse = k.run(True, scale=1e-6, batch=B.paged_batch(k.d_tables, k.stride, k.d_cu, k.d_lens, k.d_tiles, 2, k.tokens, bound, 50, tiles))
         k.check(got, got_lse, True, scale=float(np.float32(1e-6)))
     # and a q that is not finite stays in the rows of its token
     clean = out.copy()
