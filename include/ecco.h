@@ -292,7 +292,7 @@ int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k_fp16, const
  * cu_new[n_req] are left as they are.  q_per_kv in 1..16; q_stride a multiple of 8.
  * Scores, maxima, sums of weights and the sums over tokens are held in fp32; weights enter the tensor cores as fp16 (rounding
  * 2^-11 of each weight, or 2^-32 of the row's largest).  A decoded value beyond fp16's range enters as +-65504.  A q that is not finite
- * spoils the rows of its own token only; scale, times log2(e), is finite.  The result does not depend on scheduling.  d_out and d_lse overlap
+ * spoils the rows of its own token only (NaN gives NaN); scale, times log2(e), is finite.  The result does not depend on scheduling.  d_out and d_lse overlap
  * neither q nor the pools nor the workspace.
  * Upper bounds that the host knows: max_new and max_kv of one request's new tokens and of its length, max_tiles of
  * d_kv_tiles[n_req].  What exceeds them, and tokens whose page is not one of the pool, give unspecified values for the request and make

@@ -725,6 +725,8 @@ extern "C" int ecco_paged_plan(int32_t page_size, int32_t n_pages, int32_t n_req
                           static_cast<const void*>(d_block_tables), static_cast<const void*>(d_slots), static_cast<const void*>(d_cu_new),
                           static_cast<const void*>(d_kv_lens), static_cast<const void*>(d_kv_tiles), static_cast<const void*>(d_result)})
         if (!aligned_to(p, 4)) return ECCO_ERR_ALIGNMENT;
+    // in place it cannot be done: every CTA reads all lengths, whatever the others have written
+    if (n_req && (d_kv_lens == d_ctx_lens || d_kv_lens == d_new_lens)) return ECCO_ERR_INVALID_ARG;
     DeviceInfo di;
     const int rc = device_info(&di);
     if (rc) return rc;
@@ -924,6 +926,8 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
     if (!aligned16(d_q) || q_stride % 8 || !aligned16(d_out) || !aligned_to(d_lse, 4)) return ECCO_ERR_ALIGNMENT;
     for (const int32_t* p : {b.d_block_tables, b.d_cu_new, b.d_kv_lens, b.d_kv_tiles})
         if (!aligned_to(p, 4)) return ECCO_ERR_ALIGNMENT;
+    // in place it cannot be done: a row of q is read by whoever has tokens that it sees, at any time
+    if (d_workspace && (d_out == d_q || d_out == d_workspace || d_q == d_workspace)) return ECCO_ERR_INVALID_ARG;
     DeviceInfo di;
     rc = device_info(&di);
     if (rc) return rc;

@@ -368,14 +368,15 @@ ecco_paged_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constan
         const uint32_t stage = tiles_base + warp * 1024;
         const uint32_t bits = tiles_base + nw * 1024 + warp * kBitBytes + lane * 4;
         const uint32_t my_row = stage + lane * 32;
-        if (!finish_decode_tables(tb, static_cast<uint32_t>(phase))) return;
-        if (phase == 0) {
+        const bool ready = finish_decode_tables(tb, static_cast<uint32_t>(phase));
+        if (phase == 0) {                                  // without tables too: the next kernels rely on the schedule
             dependency_wait();
             fetch_firsts(kv, firsts);
             // one warp, if possible one that has no room to decode, makes the schedule on the side
             if (blockIdx.x == 0 && warp == (nw < blockDim.x >> 5 ? nw : 0u)) paged_schedule(kv, sc, o);
             if (blockIdx.x == 0 && threadIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
         }
+        if (!ready) return;
         const float T = tb.T;
         const uint32_t n_tiles = static_cast<uint32_t>(paged_tiles(kv)), units = n_tiles * kv.heads;
         const uint32_t tile_stride = balanced_warps(units, ctas * nw);
@@ -618,11 +619,13 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// natural logarithm of a sum of weights that stands at l * 2^(m - offset)
+// natural logarithm of a sum of weights that stands at l * 2^(m - offset); NaN where the scores were
 __device__ __forceinline__ float lse_of(float m, float l, float offset)
 {
-    return l > 0.0f ? (m - offset + log2f(l)) * 0.693147180559945309f : -INFINITY;
+    return l == 0.0f ? -INFINITY : (m - offset + log2f(l)) * 0.693147180559945309f;
 }
+// what a row's sums are multiplied by: zero for a row that has seen nothing
+__device__ __forceinline__ float inverse_of(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ uint32_t pack_h2(float a, float b)
 {
     const __half2 h = __floats2half2_rn(a, b);
@@ -839,7 +842,7 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
             if (whole) {
                 const int token = row / o.q_per_kv, hq = (kv.head0 + at.head) * o.q_per_kv + row - token * o.q_per_kv;
                 const int64_t at_row = static_cast<int64_t>(q.row0 + token) * o.q_heads + hq;
-                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                const float inv = inverse_of(sum);
                 uint32_t* const dst = reinterpret_cast<uint32_t*>(o.out + at_row * kGroup) + (lane & 3u);
 #pragma unroll
                 for (int n = 0; n < 16; ++n) dst[n * 4] = pack_h2(acc[n][2 * i] * inv, acc[n][2 * i + 1] * inv);
@@ -913,7 +916,7 @@ ecco_paged_join_kernel(const __grid_constant__ PagedOut o, int32_t head0)
         if (sub == 0 && row < R) {
             const int token = row / o.q_per_kv, g = row - token * o.q_per_kv;
             const int64_t at_row = static_cast<int64_t>(row0 + token) * o.q_heads + (head0 + head) * o.q_per_kv + g;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inv = inverse_of(l);
             reinterpret_cast<uint2*>(o.out + at_row * kGroup)[lane] = make_uint2(pack_h2(acc.x * inv, acc.y * inv), pack_h2(acc.z * inv, acc.w * inv));
             if (o.lse && lane == 0) o.lse[at_row] = lse_of(m, l, kWeightLog2);
         }

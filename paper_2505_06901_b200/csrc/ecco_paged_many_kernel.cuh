@@ -339,7 +339,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             if (!ok) break;
             tmem_fence_after();
             const bool whole = pc.whole;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inv = inverse_of(l);
             float* const part = o.part + (static_cast<int64_t>(pc.slot) * kManyRows + x * 128 + t) * kGroup;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -350,7 +350,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 if (exists && whole) {
                     uint4* const dst = reinterpret_cast<uint4*>(o.out + out_row * kGroup) + 4 * c;
                     // a row that has seen nothing: O may not have been written at all
-                    auto two = [&](int i) { return l > 0.0f ? pack_h2(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv) : 0u; };
+                    auto two = [&](int i) { return l != 0.0f ? pack_h2(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv) : 0u; };
 #pragma unroll
                     for (int i = 0; i < 4; ++i) dst[i] = make_uint4(two(8 * i), two(8 * i + 2), two(8 * i + 4), two(8 * i + 6));
                 } else if (exists) {
@@ -404,7 +404,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                             if (i0 + k >= n_rows) break;
                             const int tile_token = (i0 + k) / o.q_per_kv, i_g = i0 + k - tile_token * o.q_per_kv;
                             const int64_t to = static_cast<int64_t>(pc.r_row0 + pc.token + tile_token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + i_g;
-                            const float j_inv = jl[k] > 0.0f ? 1.0f / jl[k] : 0.0f;
+                            const float j_inv = inverse_of(jl[k]);
                             reinterpret_cast<uint2*>(o.out + to * kGroup)[lane] =
                                 make_uint2(pack_h2(acc[k].x * j_inv, acc[k].y * j_inv), pack_h2(acc[k].z * j_inv, acc[k].w * j_inv));
                             if (o.lse && lane == 0) o.lse[to] = lse_of(jm[k], jl[k], kManyWeightLog2);

@@ -54,6 +54,7 @@ def test_argument_errors_without_a_gpu(B):
         assert plan(**bad) == INV, bad
     for name in ("ctx", "new", "free", "tables", "slots", "cu", "lens", "tiles", "result"):
         assert plan(**{name: 66}) == ALIGN, name
+    assert plan(ctx=128) == INV and plan(new=128) == INV                       # the new lengths over the ones that they come from
 
     def cache(k_meta=64, v_meta=64, k=64, v=64, pages=8, heads=2, page=16):
         return B.PagedCache(k_meta, v_meta, k, v, pages, heads, page)
@@ -89,6 +90,7 @@ def test_argument_errors_without_a_gpu(B):
     for bad in (dict(q=72), dict(out=72), dict(lse=66), dict(stride=513), dict(b=batch(tables=66)), dict(b=batch(cu=66)), dict(b=batch(lens=66)),
                 dict(b=batch(tiles=66)), dict(c=cache(k=80))):
         assert attn(**bad) == ALIGN, bad
+    assert attn(ws=128) == INV and attn(out=128) == INV and attn(q=128) == INV                  # two of the three are one
     need = lambda c, b, g: int(L.ecco_paged_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(b), g))  # noqa: E731
     assert need(cache(), batch(), 2) >= 4 * 2 * 2 * 8192 and need(cache(), batch(), 0) == 0 and need(cache(), batch(n_tiles=-1), 2) == 0
     assert need(cache(heads=1), batch(), 2) < need(cache(heads=8), batch(), 2)
@@ -451,6 +453,23 @@ def test_values_beyond_fp16_do_not_leave_their_rows(B, dev, eo, caches, new):
     p.d_q[0, :256] = math.inf
     out, _ = p.run(True)
     assert np.array_equal(out[1:].view(np.uint16), clean[1:].view(np.uint16)) and np.array_equal(out[0, 2:].view(np.uint16), clean[0, 2:].view(np.uint16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new,g,tiles", [([1, 2], 2, 0), ([1, 2], 1, 14000), ([1, 2], 2, 14000), ([1, 2], 4, 7000), ([40, 30], 2, 0), ([150, 3], 2, 0)])
+def test_a_q_that_is_no_number_gives_none(B, dev, eo, caches, new, g, tiles):
+    """In requests that one run of tiles holds and in cut ones; the other tokens' rows stay as they are."""
+    for kv in ([150, 200], [5000, 3000]):
+        p = Paged(B, eo, *caches, new, kv, 2, g, 16, seed=19)
+        bound = B.paged_batch(p.d_tables, p.stride, p.d_cu, p.d_lens, p.d_tiles, 2, p.tokens, max(new), max(kv), tiles) if tiles else None
+        want, want_lse = p.run(True, batch=bound)
+        p.d_q[new[0], 5] = math.nan                        # the first query head of the second request's first token
+        out, lse = p.run(True, batch=bound)
+        assert np.isnan(out[new[0], 0]).all() and np.isnan(lse[new[0], 0])
+        rest = np.ones(out.shape[:2], bool)
+        rest[new[0], 0] = False
+        assert np.array_equal(out[rest].view(np.uint16), want[rest].view(np.uint16)) and np.array_equal(lse[rest], want_lse[rest])
+    assert B.ecco_device_status() == 0
 
 
 @pytest.mark.gpu
