@@ -804,9 +804,9 @@ PagedAttnPlan paged_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv
     p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
     p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
     p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
-    p.n_blocks = take(4);
+    p.n_blocks = take(8);                                  // and the number of rows to join
     p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
-    p.cuts = take(static_cast<size_t>(p.few_ctas) * kFewWarps<true> * sizeof(FewCut));
+    p.cuts = take(static_cast<size_t>(p.few_ctas) * kFewWarps<true> * kFewRows * sizeof(FewCut));
     p.few_part = take(few_slots * kGroup * sizeof(float));
     p.few_ml = take(few_slots * sizeof(float2));
     p.many_part = take(many_slots * kGroup * sizeof(float));
@@ -872,8 +872,7 @@ int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o,
     }
     const int rc = launch_overlapped(ecco_paged_few_kernel<kScores>, static_cast<unsigned>(p.few_ctas), static_cast<unsigned>(kFewWarps<kScores> * 32), kFewSmemBytes<kScores>, s, kv, o, sc);
     if (rc) return rc;
-    const int runs = p.few_ctas * kFewWarps<kScores>;
-    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(runs), 256u, 0, s, o, kv.head0);
+    return launch_overlapped(ecco_paged_join_kernel, static_cast<unsigned>(std::min(p.few_ctas * kFewWarps<kScores>, di.sms * kJoinCtas)), 256u, 0, s, o);
 }
 template <StageKind kKind>
 int launch_paged_stage(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, int64_t units, cudaStream_t s)
@@ -960,6 +959,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         sc.block_tiles = reinterpret_cast<int32_t*>(kv.staged + p.block_tiles);
         sc.blocks = reinterpret_cast<int2*>(kv.staged + p.blocks);
         sc.n_blocks = reinterpret_cast<int32_t*>(kv.staged + p.n_blocks);
+        sc.n_cuts = sc.n_blocks + 1;
         sc.max_blocks = p.max_blocks;
         sc.few_rows = kFewRows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
@@ -985,6 +985,7 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         o.part = reinterpret_cast<float*>(kv.staged + p.few_part);
         o.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
         o.cuts = reinterpret_cast<FewCut*>(kv.staged + p.cuts);
+        o.n_cuts = sc.n_cuts;
         if (p.many) {
             PagedOut many = o;
             many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
