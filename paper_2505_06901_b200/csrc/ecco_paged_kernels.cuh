@@ -663,7 +663,8 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     if (!o.early) dependency_wait();
     release_dependents();
     const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);
-    const int wg = static_cast<int>(warp * gridDim.x + blockIdx.x);
+    // Fewer runs than warps are spread over the CTAs, but behind ecco_paged_many_kernel they go to the first CTAs, which begin earlier.
+    const int wg = static_cast<int>(o.early ? blockIdx.x * kFewWarps<kScores> + warp : warp * gridDim.x + blockIdx.x);
     const int64_t U = static_cast<int64_t>(line) * kv.heads;
     const UnitSplit split = few_split<kScores>(U, static_cast<int>(gridDim.x));
     const int64_t u0 = min(split.begin(wg), U), u1 = min(split.begin(wg + 1), U);     // warps beyond the runs: nothing
