@@ -306,11 +306,12 @@ def ecco_decompress(d_meta, d_blocks, n_groups: int, d_out_fp16, stream=None) ->
 
 def decompress_items(items):
     """The host array ecco_decompress_batch reads, from a sequence of (d_meta, d_blocks, n_groups, d_out_fp16).  A
-    caller that issues the same batch again and again builds it once and passes it instead of the sequence."""
+    caller that issues the same batch again and again builds it once and passes it instead of the sequence.  It
+    keeps the tensors alive whose addresses it holds."""
     arr = (DecompressItem * max(len(items), 1))()
     for i, (d_meta, d_blocks, n_groups, d_out) in enumerate(items):
         arr[i].d_meta, arr[i].d_blocks, arr[i].n_groups, arr[i].d_out_fp16 = _ptr(d_meta), _ptr(d_blocks), n_groups, _ptr(d_out)
-    arr.n_items = len(items)
+    arr.n_items, arr.keeps = len(items), list(items)
     return arr
 
 
@@ -334,12 +335,13 @@ def ecco_gemv(d_meta, d_blocks, n_out: int, k: int, d_x_fp16, batch: int, d_y, d
 
 def gemv_items(items):
     """The host array ecco_gemv_batch reads, from a sequence of (d_meta, d_blocks, n_out, k, d_x_fp16, d_y).  A caller
-    that issues the same group again and again builds it once and passes it instead of the sequence."""
+    that issues the same group again and again builds it once and passes it instead of the sequence.  It keeps the
+    tensors alive whose addresses it holds."""
     arr = (GemvItem * max(len(items), 1))()
     for i, (d_meta, d_blocks, n_out, k, d_x, d_y) in enumerate(items):
         arr[i].d_meta, arr[i].d_blocks, arr[i].n_out, arr[i].k = _ptr(d_meta), _ptr(d_blocks), n_out, k
         arr[i].d_x_fp16, arr[i].d_y = _ptr(d_x), _ptr(d_y)
-    arr.n_items = len(items)
+    arr.n_items, arr.keeps = len(items), list(items)
     return arr
 
 
@@ -396,15 +398,21 @@ def ecco_kv_compress(d_meta, d_x_fp16, n_groups: int, d_blocks, stream=None) -> 
 
 
 def paged_cache(d_k_meta, d_v_meta, d_k_blocks, d_v_blocks, n_pages: int, n_kv_heads: int, page_size: int) -> PagedCache:
-    """The pools of a paged cache as ecco_paged_append and ecco_paged_attn take them; built once and kept, like the tensors."""
-    return PagedCache(_ptr(d_k_meta), _ptr(d_v_meta), _ptr(d_k_blocks), _ptr(d_v_blocks), n_pages, n_kv_heads, page_size)
+    """The pools of a paged cache as ecco_paged_append and ecco_paged_attn take them.  Built once and kept; it keeps the
+    tensors alive whose addresses it holds."""
+    cache = PagedCache(_ptr(d_k_meta), _ptr(d_v_meta), _ptr(d_k_blocks), _ptr(d_v_blocks), n_pages, n_kv_heads, page_size)
+    cache.keeps = (d_k_meta, d_v_meta, d_k_blocks, d_v_blocks)
+    return cache
 
 
 def paged_batch(d_block_tables, table_stride: int, d_cu_new, d_kv_lens, d_kv_tiles, n_req: int, n_tokens: int, max_new: int,
                 max_kv: int, max_tiles: int) -> PagedBatch:
-    """A batch of requests as ecco_paged_attn takes it: the arrays that ecco_paged_plan writes, and upper bounds of what they hold."""
-    return PagedBatch(_ptr(d_block_tables), _ptr(d_cu_new), _ptr(d_kv_lens), _ptr(d_kv_tiles), table_stride, n_req, n_tokens, max_new, max_kv,
-                      max_tiles)
+    """A batch of requests as ecco_paged_attn takes it: the arrays that ecco_paged_plan writes, and upper bounds of what they hold.
+    It keeps the tensors alive whose addresses it holds."""
+    batch = PagedBatch(_ptr(d_block_tables), _ptr(d_cu_new), _ptr(d_kv_lens), _ptr(d_kv_tiles), table_stride, n_req, n_tokens, max_new, max_kv,
+                       max_tiles)
+    batch.keeps = (d_block_tables, d_cu_new, d_kv_lens, d_kv_tiles)
+    return batch
 
 
 def ecco_paged_plan(page_size: int, n_pages: int, n_req: int, d_ctx_lens, d_new_lens, d_free_pages, n_free: int, d_block_tables,
