@@ -294,9 +294,10 @@ int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k_fp16, const
  * 2^-11 of each weight, or 2^-32 of the row's largest).  A decoded value beyond fp16's range enters as +-65504.  A q that is not finite
  * spoils the rows of its own token only (NaN gives NaN); scale, times log2(e), is finite.  The result does not depend on scheduling.  d_out and d_lse overlap
  * neither q nor the pools nor the workspace.
- * Upper bounds that the host knows: max_new and max_kv of one request's new tokens and of its length, max_tiles of
- * d_kv_tiles[n_req].  What exceeds them, and tokens whose page is not one of the pool, give unspecified values for the request and make
- * ecco_device_status() report ECCO_ERR_INVALID_ARG.
+ * Upper bounds that the host knows: n_tokens of d_cu_new[n_req] (the rows of q and out), max_new and max_kv of one request's new tokens and
+ * of its length, max_tiles of d_kv_tiles[n_req].  What exceeds them, prefix sums that are negative or fall, lengths that do not fit their
+ * tiles, and tokens whose page is not one of the pool, give unspecified values for the request and make ecco_device_status() report
+ * ECCO_ERR_INVALID_ARG.
  * The blocks are decoded once per call, into 512 bytes of the workspace per token and KV head.  A workspace that is smaller than
  * ecco_paged_attn_workspace_bytes (for the same arguments), down to what that gives for n_kv_heads = 1, makes the call
  * take some heads at a time.  16-byte aligned; contents irrelevant before and undefined after; calls sharing a workspace must

@@ -162,8 +162,9 @@ __device__ __forceinline__ uint8_t* staged_tile(const PagedKv& kv, int which, in
 // tiles of all requests, cut to what the workspace was made for
 __device__ __forceinline__ int32_t paged_tiles(const PagedKv& kv) { return min(max(__ldcg(kv.kv_tiles + kv.n_req), 0), kv.max_tiles); }
 
-// Where a request's tiles and rows are, whatever the arrays hold: inside of the workspace and of q.
-struct PagedReq { int32_t first, tiles, kv, row0, rows; };
+// Where a request's tiles and rows are, whatever the arrays hold: inside of the workspace and of q.  cut: the arrays say something else, which
+// paged_schedule reports (with fewer rows than the request has, for one, the causal mask of those that are left would be another one).
+struct PagedReq { int32_t first, tiles, kv, row0, rows; bool cut; };
 __device__ __forceinline__ PagedReq paged_req(const PagedKv& kv, int r, int32_t T)
 {
     PagedReq q;
@@ -173,6 +174,7 @@ __device__ __forceinline__ PagedReq paged_req(const PagedKv& kv, int r, int32_t 
     q.kv = static_cast<int32_t>(min(static_cast<int64_t>(min(max(len, 0), kv.max_kv)), static_cast<int64_t>(q.tiles) * 32));
     q.row0 = min(max(c0, 0), kv.n_tokens);
     q.rows = min(max(c1, q.row0), kv.n_tokens) - q.row0;
+    q.cut = q.first != t0 || q.first + q.tiles != t1 || q.kv != len || q.row0 != c0 || q.row0 + q.rows != c1;
     return q;
 }
 // The last r in 0 .. n - 1 with begin[r] <= x (0 if there is none), by the whole warp: 32 probes at a time.
@@ -261,7 +263,7 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
         next = {};
         if (r + 32 < kv.n_req) next = paged_req(kv, r + 32, T);        // on their way while these are dealt with
         const int64_t rows = static_cast<int64_t>(q.rows) * q_per_kv;
-        if (r < kv.n_req && (q.rows > kv.max_new || __ldcg(kv.kv_lens + r) != q.kv)) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        if (r < kv.n_req && (q.rows > kv.max_new || q.cut)) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
         const bool many = rows > sc.few_rows;
         const int32_t f = few + scan(!many && rows > 0 ? q.tiles : 0);
         if (r < kv.n_req) sc.few_tiles[r + 1] = f;

@@ -255,7 +255,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             const int32_t token = pc.token + in_tile;
             const bool exists = in_tile < tile_rows_tokens(o.q_per_kv) && token < pc.r_rows;
             const int64_t out_row = static_cast<int64_t>(pc.r_row0 + token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + g;
-            const int32_t seen = exists ? tokens_seen(PagedReq{0, 0, pc.r_kv, 0, pc.r_rows}, token, causal) : 0;
+            const int32_t seen = exists ? tokens_seen(PagedReq{0, 0, pc.r_kv, 0, pc.r_rows, false}, token, causal) : 0;
             float m = -INFINITY, l = 0.0f;                 // m in units of log2, the weights stand at 2^(s - m + kManyWeightLog2)
             for (int32_t j = pc.from; j < pc.to; ++j) {
                 ok = wait(s_bar + 8 * x, n_s++ & 1u);

@@ -672,3 +672,36 @@ def test_paged_and_dense_caches_agree(B, dev, eo, caches):
     # both rounded: the tolerance of the paged call, with the largest |V| for the weighted mean
     top = max(np.abs(v).max() for v in p.decoded[1])
     assert (np.abs(out - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -10 * top).all()
+
+
+# ------------------------------------------------------------------ arrays that say more than the bounds
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [[2, 1, 3], [40, 33, 70]])
+@pytest.mark.parametrize("what", ["more tokens than rows", "a request beyond the rows", "falling rows", "negative rows", "falling tiles", "negative tiles"])
+def test_whatever_the_bounds_cut_off_is_reported(B, dev, eo, caches, new, what):
+    """Rows of a request that were cut off would move the causal mask of those that are left: the status says so, the requests in front keep
+    their results, and the rows behind the bound stay as they are."""
+    p = Paged(B, eo, *caches, new, [100, 90, 200], 2, 2, 16, seed=51)
+    want, want_lse = p.run(True)
+    assert B.ecco_device_status() == 0
+    n = p.tokens
+    if what == "more tokens than rows":
+        n -= 1
+    elif what == "a request beyond the rows":
+        n -= new[2]
+    elif what == "falling rows":
+        p.d_cu[2] = new[0] - 1
+    elif what == "negative rows":
+        p.d_cu[0] = -1
+    elif what == "falling tiles":                                              # of a request without a token, so its own length still fits
+        p.d_lens[1] = 0
+        p.d_tiles[2] = 3
+    else:
+        p.d_tiles[0] = -1
+    b = B.paged_batch(p.d_tables, p.stride, p.d_cu, p.d_lens, p.d_tiles, 3, n, max(new) + 2, 200, p.batch.max_tiles)
+    out, lse = p.run(True, batch=b)
+    assert B.ecco_device_status() == B.ERR_INVALID_ARG
+    if "negative" not in what:
+        assert np.array_equal(out[:new[0] - 1].view(np.uint16), want[:new[0] - 1].view(np.uint16)) and np.array_equal(lse[:new[0] - 1], want_lse[:new[0] - 1])
+    assert (out[n:] == 7).all() and (lse[n:] == 7).all()
+    assert B.ecco_device_status() == 0                                         # told once
