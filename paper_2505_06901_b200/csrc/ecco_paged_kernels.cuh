@@ -197,7 +197,7 @@ constexpr int kManyTokens = 128;                           // tokens of its tile
 __host__ __device__ constexpr int32_t tile_rows_tokens(int32_t q_per_kv) { return 128 / q_per_kv; }      // new tokens of a tile of rows
 // What the attention kernels need to know of a batch, made by paged_schedule.
 struct PagedSchedule {
-    int32_t* few_tiles;        // [n_req + 1]: prefix sums of the tiles of the requests for ecco_paged_few_kernel
+    int32_t* few_tiles;        // [n_req + 1]: prefix sums of the tiles of the requests for ecco_paged_few_kernel, at most all tiles that there are
     int32_t* block_tiles;      // [max_blocks + 1]: prefix sums of the 128-token tiles of all blocks
     int2* blocks;              // [max_blocks]: request, block of the request
     int32_t* n_blocks;
@@ -265,7 +265,9 @@ __device__ __forceinline__ void paged_schedule(const PagedKv& kv, const PagedSch
         const int64_t rows = static_cast<int64_t>(q.rows) * q_per_kv;
         if (r < kv.n_req && (q.rows > kv.max_new || q.cut)) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
         const bool many = rows > sc.few_rows;
-        const int32_t f = few + scan(!many && rows > 0 ? q.tiles : 0);
+        // Requests that share no tile have T together at most.  Prefix sums that go up and down could give any number: beyond T there is
+        // nothing, so that no place in the line passes 32 bits.  (Such a request is cut, and reported; 32 times T is below 2^31.)
+        const int32_t f = static_cast<int32_t>(min(static_cast<int64_t>(few) + scan(!many && rows > 0 ? q.tiles : 0), static_cast<int64_t>(T)));
         if (r < kv.n_req) sc.few_tiles[r + 1] = f;
         few = __shfl_sync(full, f, 31);
         // requests without a token: nobody else comes to their rows
@@ -680,8 +682,10 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
         p.head = kv.heads - 1 - nth;                       // the last head's tiles are the latest in the L2 cache
         const int r = warp_find(sc.few_tiles, kv.n_req, static_cast<int32_t>(p.u - head_from));
         p.q = paged_req(kv, r, T);
-        p.begin = head_from + __ldcg(sc.few_tiles + r);
-        p.end = min(head_from + __ldcg(sc.few_tiles + r + 1), u1);
+        const int32_t from = __ldcg(sc.few_tiles + r), to = __ldcg(sc.few_tiles + r + 1);
+        p.q.tiles = to - from;                             // as many as the line has: the run that has the last of them is one that there is
+        p.begin = head_from + from;
+        p.end = min(head_from + to, u1);
         p.tile = p.q.first + static_cast<int32_t>(p.u - p.begin);
     };
     Place load = {};                                       // the next tile to ask for

@@ -705,3 +705,34 @@ def test_whatever_the_bounds_cut_off_is_reported(B, dev, eo, caches, new, what):
         assert np.array_equal(out[:new[0] - 1].view(np.uint16), want[:new[0] - 1].view(np.uint16)) and np.array_equal(lse[:new[0] - 1], want_lse[:new[0] - 1])
     assert (out[n:] == 7).all() and (lse[n:] == 7).all()
     assert B.ecco_device_status() == 0                                         # told once
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("g", [1, 16])
+def test_prefix_sums_whose_lengths_pass_32_bits(B, dev, eo, caches, g):
+    """65535 requests that all say that they have 70000 tiles or none, 2.3e9 in all: the line of tiles ends at the 70000 that there are.
+    Everything that the call may write lies between guards."""
+    (meta, _), (blocks, _) = caches
+    n, tiles = 65535, 70000
+    d_meta = B.meta_to_device(lib_meta_from_oracle(B, meta))
+    pool = torch.from_numpy(blocks[:64].reshape(1, 1, 64, 64).copy()).cuda()
+    cache = B.paged_cache(d_meta, d_meta, pool, pool, 1, 1, 64)
+    sums = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    sums[1::2] = tiles
+    assert int(sums.diff().clamp(min=0).sum(dtype=torch.int64)) > 2**31
+    batch = B.paged_batch(torch.zeros((n, 1), dtype=torch.int32, device="cuda"), 1, torch.arange(n + 1, dtype=torch.int32, device="cuda"),
+                          torch.full((n,), 64, dtype=torch.int32, device="cuda"), sums, n, n, 1, 64, tiles)
+    need = B.ecco_paged_attn_workspace_bytes(cache, batch, g)
+    ws = torch.full((need + 8192,), 0xa5, dtype=torch.uint8, device="cuda")
+    out = torch.full((n + 16, g, 128), 7.0, dtype=torch.float16, device="cuda")
+    lse = torch.full((n + 16, g), 7.0, device="cuda")
+    q = torch.randn((n, g, 128), device="cuda").half()
+    B.ecco_paged_attn(cache, batch, g, q, g * 128, 0.1, 0, out[8:], lse[8:], ws[4096:], need)
+    assert B.ecco_device_status() == B.ERR_INVALID_ARG
+    assert (ws[:4096] == 0xa5).all() and (ws[4096 + need:] == 0xa5).all()
+    assert all((t[:8] == 7).all() and (t[n + 8:] == 7).all() for t in (out, lse))
+    assert np.array_equal(pool.cpu().numpy().reshape(-1, 64), blocks[:64])
+    p = Paged(B, eo, *caches, [1, 3], [300, 70], 2, 2, 16, seed=52)             # and the next call is as ever
+    got, got_lse = p.run(True)
+    p.check(got, got_lse, True)
+    assert B.ecco_device_status() == 0
