@@ -185,6 +185,10 @@ __device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, int 
 // A grid that ends without having waited breaks the chain: the kernel behind it waits for this grid only and could start on data that
 // the one before it is still writing.  So a way out that every CTA may take leads through dependency_wait(), too.
 // release_dependents() lets the next kernel of the stream do the same with respect to this one.
+// One kernel reads memory before it waits: ecco_paged_few_kernel behind ecco_paged_many_kernel.  What it reads was written by kernels in front of
+// that one, which releases its dependents only when it has itself waited (every one of its threads waits first): these grids have ended and
+// their writes have arrived in L2 by then.  It reads through L2 alone (__ldcg, bulk copies), no L1 line can be older than its start, and
+// it neither reads what the kernel in front writes nor writes what that reads.  It waits before it ends, for the kernels behind it.
 __device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void release_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

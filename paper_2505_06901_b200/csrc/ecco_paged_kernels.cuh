@@ -662,8 +662,11 @@ ecco_paged_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant_
     if (lane == 0)
         for (int s = 0; s < kFewStages<kScores>; ++s) mbar_init(bar + s * 8, 1);
     __syncwarp();
-    // Behind ecco_paged_many_kernel, which lets this one begin only when it has itself waited for the tiles, there is nothing to wait for: the two
-    // have nothing in common.  The next kernel relies on this one for that one's completion all the same, so the wait comes at the end.
+    // Behind ecco_paged_many_kernel the wait comes at the end, where the next kernel needs it: that kernel releases this one only when all its
+    // threads have waited, so the tiles, the schedule, q and the batch's arrays are in L2, where every read before the wait goes (__ldcg and bulk
+    // copies, no plain loads), and the two kernels write nothing that the other reads or writes.  Waiting here instead, a CTA would begin
+    // when the last one of the other kernel has ended and not when its SM is free (24 requests of which six are pieces of prompts: 177 -> 196 us; 8 of
+    // 3 to 64 rows over 700 to 1500 tokens: 77 -> 91).
     if (!o.early) dependency_wait();
     release_dependents();
     const int32_t T = paged_tiles(kv), line = __ldcg(sc.few_tiles + kv.n_req);

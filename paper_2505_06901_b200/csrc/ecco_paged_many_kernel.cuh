@@ -213,7 +213,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     tmem_fence_after();
     const uint32_t tmem = *tmem_word;                      // columns 0, 128: S and P; 256, 384: O
     dependency_wait();
-    release_dependents();
+    release_dependents();                                  // not before the wait: ecco_paged_few_kernel relies on the order of the two
     const int32_t n_blocks = __ldcg(sc.n_blocks), total = n_blocks > 0 ? __ldcg(sc.block_tiles + n_blocks) : 0;
     const UnitSplit split(static_cast<int64_t>(total) * kv.heads, static_cast<int>(gridDim.x));
     const int64_t u0 = split.begin(static_cast<int>(blockIdx.x)), u1 = split.begin(static_cast<int>(blockIdx.x) + 1);

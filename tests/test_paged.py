@@ -736,3 +736,78 @@ def test_prefix_sums_whose_lengths_pass_32_bits(B, dev, eo, caches, g):
     got, got_lse = p.run(True)
     p.check(got, got_lse, True)
     assert B.ecco_device_status() == 0
+
+
+# ------------------------------------------------------------------ calls behind one another
+class Layers:
+    """Layers of one step: append and attention of each, its rows the output of the one before; one workspace for all."""
+
+    def __init__(self, B, eo, caches, n, new, kv, heads, g, page, tiles=0, small=False, seed=60):
+        self.B, self.g, self.row = B, g, heads * g * 128
+        self.p = [Paged(B, eo, *caches, new, kv, heads, g, page, seed=seed + i) for i in range(n)]
+        p = self.p[0]
+        self.heads = heads
+        self.slots = [ints([q.tables[r, t // page] * page + t % page for r in range(len(new)) for t in range(kv[r] - new[r], kv[r])]) for q in self.p]
+        assert g >= 2                                                          # K and V of a layer are parts of its rows
+        self.first = torch.from_numpy(p.q[:, :self.row].copy()).cuda()
+        self.batch = [B.paged_batch(q.d_tables, q.stride, q.d_cu, q.d_lens, q.d_tiles, len(new), q.tokens, max(new), max(kv), tiles or q.batch.max_tiles) for q in self.p]
+        one = B.paged_cache(p.d_meta[0], p.d_meta[1], p.d_pools[0], p.d_pools[1], p.n_pages, 1, page)
+        self.ws_bytes = B.ecco_paged_attn_workspace_bytes(one if small else p.cache, self.batch[0], g)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device="cuda")
+        self.outs = [torch.empty((p.tokens, heads * g, 128), dtype=torch.float16, device="cuda") for _ in range(n)]
+
+    def reset(self):
+        for q in self.p:
+            for d, h in zip(q.d_pools, q.pools):
+                d.copy_(torch.from_numpy(h))
+        for o in self.outs:
+            o.fill_(math.nan)
+        self.ws.fill_(0xff)
+
+    def step(self, after=lambda: None):
+        x = self.first
+        for q, batch, slots, out in zip(self.p, self.batch, self.slots, self.outs):
+            self.B.ecco_paged_append(q.cache, x.data_ptr(), x.data_ptr() + self.heads * 256, self.row, slots, q.tokens)
+            after()
+            self.B.ecco_paged_attn(q.cache, batch, self.g, x, self.row, 0.3, self.B.ATTN_CAUSAL, out, None, self.ws, self.ws_bytes)
+            after()
+            x = out
+
+    def results(self):
+        return [t.cpu().numpy().view(np.uint8) for t in self.outs + [d for q in self.p for d in q.d_pools]]
+
+
+LAYERS = {
+    "few rows": dict(new=[1, 2, 1, 3], kv=[700, 90, 3000, 3], heads=3, g=3, page=16),
+    "many rows": dict(new=[40, 130, 257], kv=[700, 130, 900], heads=2, g=2, page=32),
+    "both": dict(new=[1, 40, 3, 130, 1, 2], kv=[2700, 300, 50, 500, 64, 900], heads=2, g=4, page=16),
+    "both, some heads at a time": dict(new=[1, 40, 3, 130, 1, 2], kv=[2700, 300, 50, 500, 64, 900], heads=3, g=4, page=16, small=True),
+    "large, two rows": dict(new=[1, 1, 1], kv=[900, 64, 3000], heads=2, g=2, page=16, tiles=14000),
+    "large, six rows": dict(new=[2, 1, 1], kv=[900, 64, 3000], heads=2, g=3, page=16, tiles=14000),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", LAYERS)
+def test_layers_behind_one_another_on_one_workspace(B, dev, eo, caches, name):
+    """Nothing waits on the host between the calls, every call reads what the one before wrote, and all use one workspace: as with a
+    synchronisation behind every call."""
+    s = Layers(B, eo, caches, 6, **LAYERS[name])
+    s.reset()
+    s.step(after=torch.cuda.synchronize)
+    want = s.results()
+    assert all(np.isfinite(o.view(np.float16)).all() for o in want[:6])
+    for _ in range(5):
+        s.reset()
+        s.step()
+        for i, (w, g) in enumerate(zip(want, s.results())):
+            assert np.array_equal(w, g), i
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.step()
+    for _ in range(3):
+        s.reset()
+        graph.replay()
+        for i, (w, g) in enumerate(zip(want, s.results())):
+            assert np.array_equal(w, g), i
+    assert B.ecco_device_status() == 0
