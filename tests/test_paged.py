@@ -811,3 +811,46 @@ def test_layers_behind_one_another_on_one_workspace(B, dev, eo, caches, name):
         for i, (w, g) in enumerate(zip(want, s.results())):
             assert np.array_equal(w, g), i
     assert B.ecco_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_callers_on_several_host_threads(B, dev, eo, caches):
+    """Four threads, each with a stream, layers and a workspace of its own, at once."""
+    import threading
+
+    makers = ["few rows", "many rows", "both", "large, six rows"]
+    all_layers, want = [], []
+    for i, name in enumerate(makers):
+        s = Layers(B, eo, caches, 3, **LAYERS[name], seed=80 + 10 * i)
+        s.reset()
+        s.step(after=torch.cuda.synchronize)
+        want.append(s.results())
+        all_layers.append(s)
+    got, errors, gate = [None] * len(makers), [], threading.Barrier(len(makers))
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(10):
+                    all_layers[i].reset()
+                    stream.synchronize()
+                    gate.wait(60)
+                    for _ in range(3):                                         # the pools' new slots get the same blocks again
+                        all_layers[i].step()
+                    stream.synchronize()
+                    got[i] = all_layers[i].results()
+                    for w, g in zip(want[i], got[i]):
+                        assert np.array_equal(w, g), makers[i]
+        except BaseException as e:                                             # told by the main thread
+            errors.append(e)
+            gate.abort()
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(makers))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    assert B.ecco_device_status() == 0
