@@ -96,6 +96,82 @@ def test_argument_errors_without_a_gpu(B):
     assert need(cache(heads=1), batch(), 2) < need(cache(heads=8), batch(), 2)
 
 
+def test_every_bad_argument_is_refused_by_itself(B):
+    """All other arguments are such that the call goes on to ask for the device, of which there is none: only the one that is bad can be
+    what the call refuses."""
+    if torch.cuda.is_available():
+        pytest.skip("with a device the calls that are not refused would run on these addresses")
+    L, INV, ALIGN, GONE = B.lib(), B.ERR_INVALID_ARG, B.ERR_ALIGNMENT, B.ERR_CUDA
+
+    def check(call, names, invalid, null=()):
+        base = {n: 4096 * (i + 1) for i, n in enumerate(names)}
+        assert call(**base) == GONE
+        for name in names:
+            odd = call(**{**base, name: base[name] + 2})
+            assert odd == ALIGN, name
+            assert call(**{**base, name: None}) == (GONE if name in null else INV), name
+        for bad in invalid:
+            assert call(**{**base, **bad}) == INV, bad
+        return base
+
+    def plan(page=16, pages=8, n_req=2, n_free=4, stride=4, n_slots=9, **p):
+        return L.ecco_paged_plan(page, pages, n_req, p["ctx"], p["new"], p["free"], n_free, p["tables"], stride, p["slots"], n_slots, p["cu"], p["lens"], p["tiles"],
+                                 p["result"], None)
+
+    pages = (dict(page=0), dict(page=-16), dict(page=12), dict(page=8192), dict(pages=0), dict(pages=-1), dict(page=4096, pages=1 << 19))
+    p = check(plan, ("ctx", "new", "free", "tables", "slots", "cu", "lens", "tiles", "result"),
+              pages + (dict(n_req=-1), dict(n_req=65536), dict(n_free=-1), dict(stride=-1), dict(n_slots=-1)))
+    assert plan(**p | {"lens": p["ctx"]}) == INV and plan(**p | {"lens": p["new"]}) == INV           # the new lengths over the ones that they come from
+    for largest in (dict(page=4096, pages=(1 << 19) - 1), dict(page=1, pages=2**31 - 1), dict(n_req=65535), dict(n_free=0, free=None), dict(n_slots=0, slots=None),
+                    dict(stride=0, tables=None), dict(n_req=0, ctx=None, new=None, tables=None, lens=None)):
+        assert plan(**p | largest) == GONE, largest
+
+    def cache(k_meta, v_meta, k, v, heads=2, page=16, pages=8):
+        return ctypes.byref(B.PagedCache(k_meta, v_meta, k, v, pages, heads, page))
+
+    pools = ("k_meta", "v_meta", "k", "v")
+    caches = pages + (dict(heads=0), dict(heads=-1), dict(heads=65536, stride=1 << 30))
+
+    def append(kx, vx, slots, stride=256, n=3, **c):
+        return L.ecco_paged_append(cache(**c), kx, vx, stride, slots, n, None)
+
+    p = check(append, pools + ("kx", "vx", "slots"), caches + (dict(stride=248), dict(stride=-256), dict(n=-1)))
+    assert append(**p | {"stride": 260}) == ALIGN and append(**p | {"n": 0}) == 0
+    for largest in (dict(heads=65535, stride=65535 * 128), dict(n=2**31 - 1), dict(stride=1 << 50)):
+        assert append(**p | largest) == GONE, largest
+    for name in ("k", "v"):                                # pools: 32 bytes; metadata and rows: 16
+        assert append(**p | {name: p[name] + 16}) == ALIGN
+    for name in ("k_meta", "v_meta", "kx", "vx"):
+        assert append(**p | {name: p[name] + 8}) == ALIGN and append(**p | {name: p[name] + 16}) == GONE, name
+
+    def attn(tables, cu, lens, tiles, q, out, lse, ws, t_stride=4, n_req=2, tokens=3, new=2, kv=60, n_tiles=4, g=2, stride=512, scale=0.1, flags=1,
+             ws_bytes=1 << 30, **c):
+        b = B.PagedBatch(tables, cu, lens, tiles, t_stride, n_req, tokens, new, kv, n_tiles)
+        return L.ecco_paged_attn(cache(**c), ctypes.byref(b), g, q, stride, ctypes.c_float(scale), flags, out, lse, ws, ws_bytes, None)
+
+    # a workspace that is missing, misaligned or too small is found when the device is known
+    arrays = ("tables", "cu", "lens", "tiles", "q", "out", "lse")
+    p = check(lambda **a: attn(ws=1 << 20, **a), pools + arrays, caches + (
+        dict(g=0), dict(g=-1), dict(g=17, stride=1 << 20), dict(scale=math.nan), dict(scale=math.inf), dict(scale=-math.inf), dict(scale=3e38), dict(flags=2), dict(flags=3), dict(flags=1 << 31),
+        dict(stride=504), dict(stride=-512), dict(stride=1 << 38), dict(t_stride=-1), dict(n_req=-1), dict(n_req=65536), dict(tokens=-1), dict(new=-1), dict(kv=-1),
+        dict(n_tiles=-1), dict(n_tiles=1 << 25, heads=64, stride=1 << 20), dict(n_tiles=1 << 26, heads=1), dict(heads=4096, g=16, stride=1 << 30), dict(tokens=1 << 29),
+        dict(tokens=1 << 26, kv=1 << 26)), null=("lse",))
+    p["ws"] = 1 << 20
+    for name in ("q", "out"):
+        assert attn(**p | {name: p[name] + 8}) == ALIGN, name
+    assert attn(**p | {"stride": 516}) == ALIGN
+    for a, b in (("out", "q"), ("out", "ws"), ("q", "ws")):
+        assert attn(**p | {a: p[b]}) == INV, (a, b)
+    for fine in (dict(g=1), dict(g=16, stride=4096), dict(scale=0.0), dict(scale=-2.0), dict(scale=2e38), dict(flags=0), dict(t_stride=0, tables=None), dict(n_req=65535),
+                 dict(stride=(1 << 38) - 8), dict(new=0), dict(kv=0), dict(n_tiles=0), dict(tokens=1 << 20, kv=1 << 20), dict(n_tiles=1 << 20)):
+        assert attn(**p | fine) == GONE, fine
+    assert attn(**p | {"n_req": 0}) == 0 and attn(**p | {"tokens": 0}) == 0
+    assert L.ecco_paged_append(None, 64, 128, 256, 192, 3, None) == INV
+    assert L.ecco_paged_attn(None, ctypes.byref(B.PagedBatch(64, 128, 192, 256, 4, 2, 3, 2, 60, 4)), 2, 512, 512, ctypes.c_float(0.1), 1, 1024, None, 2048, 1 << 30, None) == INV
+    c = cache(4096, 8192, 12288, 16384)
+    assert L.ecco_paged_attn(c, None, 2, 512, 512, ctypes.c_float(0.1), 1, 1024, None, 2048, 1 << 30, None) == INV
+
+
 # ------------------------------------------------------------------ plan
 def plan_reference(page, n_pages, ctx, new, free, tables, n_slots):
     tables, slots, taken = tables.copy(), np.full(n_slots, -1, np.int32), 0
