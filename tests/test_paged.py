@@ -930,3 +930,137 @@ def test_callers_on_several_host_threads(B, dev, eo, caches):
         t.join()
     assert not errors, errors
     assert B.ecco_device_status() == 0
+
+
+# ------------------------------------------------------------------ nothing outside of the buffers
+class Guarded:
+    """A buffer between two stretches of a known pattern."""
+    EDGE = 1 << 16
+
+    def __init__(self, shape, dtype, fill=None):
+        size = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        self.all = torch.full((size + 2 * self.EDGE + 256,), 0xa5, dtype=torch.uint8, device="cuda")
+        self.at = self.EDGE + -(self.all.data_ptr() + self.EDGE) % 256
+        self.size = size
+        self.body = self.all[self.at:self.at + size].view(dtype).view(shape)
+        if fill is not None:
+            self.body.copy_(fill) if isinstance(fill, torch.Tensor) else self.body.fill_(fill)
+
+    def check(self, what):
+        assert (self.all[:self.at] == 0xa5).all() and (self.all[self.at + self.size:] == 0xa5).all(), what
+
+
+def arbitrary(rng, t, kind, largest):
+    """Any numbers, numbers in range, the extremes, or numbers in range that only rise."""
+    if kind == "any":
+        a = rng.integers(-2**31, 2**31, t.shape)
+    elif kind == "extremes":
+        a = rng.choice([-2**31, 2**31 - 1, -1, 0, 1, largest, largest + 1], t.shape)
+    else:
+        a = rng.integers(-2, largest + 2, t.shape)
+        if kind == "rising":
+            a = np.sort(a, axis=None).reshape(t.shape)
+    t.copy_(torch.from_numpy(a).int())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["few rows", "many rows", "both", "both, one head at a time", "large, one row", "large, two rows", "large, eight rows", "large, many rows"])
+def test_attention_of_arbitrary_arrays_stays_in_its_buffers(B, dev, eo, caches, form):
+    new, g, heads, tiles = {"few rows": ([1, 2, 1, 4], 3, 2, 0), "many rows": ([40, 33, 270, 60], 2, 2, 0), "both": ([1, 40, 3, 130], 4, 2, 0),
+                            "both, one head at a time": ([1, 40, 3, 130], 4, 3, 0), "large, one row": ([1] * 4, 1, 2, 14000), "large, two rows": ([1] * 4, 2, 2, 14000),
+                            "large, eight rows": ([2, 1, 1, 2], 4, 2, 14000), "large, many rows": ([70, 40, 33, 1], 2, 2, 14000)}[form]
+    p = Paged(B, eo, *caches, new, [100, 90, 700, 200], heads, g, 16, seed=53)
+    n, clean_tiles = p.tokens, p.batch.max_tiles
+    tiles = tiles or clean_tiles
+    names = ("d_tables", "d_cu", "d_lens", "d_tiles")
+    clean = {name: getattr(p, name).clone() for name in names}
+    largest = {"d_tables": p.n_pages, "d_cu": n, "d_lens": 700, "d_tiles": tiles}
+    batch = B.paged_batch(p.d_tables, p.stride, p.d_cu, p.d_lens, p.d_tiles, 4, n, max(new), 700, tiles)
+    size = p.cache
+    if "one head" in form:
+        size = B.paged_cache(p.d_meta[0], p.d_meta[1], p.d_pools[0], p.d_pools[1], p.n_pages, 1, p.page)
+    need = B.ecco_paged_attn_workspace_bytes(size, batch, g)
+    ws, out, lse = Guarded((need,), torch.uint8, 0xff), Guarded((n, heads * g, 128), torch.float16, 7.0), Guarded((n, heads * g), torch.float32, 7.0)
+    q0 = p.d_q.clone()
+    run = lambda causal: B.ecco_paged_attn(p.cache, batch, g, p.d_q, p.q_stride, 0.1, causal, out.body, lse.body, ws.body, need)  # noqa: E731
+    rng = np.random.default_rng([54, len(form)])
+    for which in [(name,) for name in names] + [names[1:], names]:
+        for kind in ("any", "extremes", "in range", "rising"):
+            for name in names:
+                getattr(p, name).copy_(clean[name])
+            for name in which:
+                arbitrary(rng, getattr(p, name), kind, largest[name])
+            given = [getattr(p, name).clone() for name in names]
+            run(int(rng.integers(2)))
+            assert B.ecco_device_status() in (0, B.ERR_INVALID_ARG)
+            for what, buffer in (("workspace", ws), ("out", out), ("lse", lse)):
+                buffer.check((what, which, kind))
+            assert torch.equal(p.d_q, q0) and all(torch.equal(getattr(p, name), was) for name, was in zip(names, given)), (which, kind)
+            assert all(np.array_equal(d.cpu().numpy(), h) for d, h in zip(p.d_pools, p.pools)), (which, kind)
+    for name in names:
+        getattr(p, name).copy_(clean[name])
+    run(1)
+    assert B.ecco_device_status() == 0
+    p.check(out.body.cpu().numpy(), lse.body.cpu().numpy(), True, scale=0.1, rows=5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_req", [1, 5, 1500])
+def test_plan_of_arbitrary_arrays_stays_in_its_buffers(B, dev, n_req):
+    rng = np.random.default_rng([55, n_req])
+    stride, n_slots, n_free, page, pages = 4, 3 * n_req + 2, n_req, 16, 2 * n_req + 1
+    served = 0
+    for kinds in [(a, b) for a in ("any", "extremes", "in range") for b in ("any", "extremes", "in range")] + [("fitting", "fitting")] * 3:
+        t = {name: Guarded(shape, torch.int32, -7) for name, shape in dict(ctx=(n_req,), new=(n_req,), free=(n_free,), tables=(n_req, stride), slots=(n_slots,), cu=(n_req + 1,),
+                                                                           lens=(n_req,), tiles=(n_req + 1,), result=(4,)).items()}
+        if kinds[0] == "fitting":                          # lengths that can be served, over tables and free pages that say anything
+            t["ctx"].body.copy_(ints(rng.integers(0, 15, n_req)))
+            t["new"].body.copy_(ints(rng.integers(0, 4, n_req) * (np.arange(n_req) < 3 * n_req // 4)))
+        else:
+            arbitrary(rng, t["ctx"].body, kinds[0], 64)
+            arbitrary(rng, t["new"].body, kinds[1], 3)
+        for name in ("free", "tables"):
+            arbitrary(rng, t[name].body, "extremes", pages)
+        before = {name: b.body.clone() for name, b in t.items()}
+        B.ecco_paged_plan(page, pages, n_req, t["ctx"].body, t["new"].body, t["free"].body, n_free, t["tables"].body, stride, t["slots"].body, n_slots, t["cu"].body,
+                          t["lens"].body, t["tiles"].body, t["result"].body)
+        for name, b in t.items():
+            b.check((name, kinds))
+        for name in ("ctx", "new", "free"):
+            assert torch.equal(t[name].body, before[name]), (name, kinds)
+        ctx, new = t["ctx"].body.cpu().numpy().astype(np.int64), t["new"].body.cpu().numpy().astype(np.int64)
+        held, total = -(-ctx // page), -(-(ctx + new) // page)
+        fine = (ctx >= 0).all() and (new >= 0).all() and (ctx + new <= page * stride).all()
+        status = t["result"].body[0].item()
+        assert status == (B.ERR_INVALID_ARG if not fine else B.ERR_WORKSPACE if new.sum() > n_slots or (total - held).sum() > n_free else 0), kinds
+        if status:
+            assert torch.equal(t["tables"].body, before["tables"]) and (t["slots"].body == -1).all() and not t["cu"].body.any() and not t["tiles"].body.any(), kinds
+        else:
+            want = plan_reference(page, pages, ctx, new, before["free"].cpu().numpy(), before["tables"].cpu().numpy(), n_slots)
+            for name, w in zip(("tables", "slots", "cu", "lens", "tiles", "result"), want):
+                assert np.array_equal(w, t[name].body.cpu().numpy()), (name, kinds)
+            served += 1
+    assert served >= 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,heads", [(7, 3), (600, 8), (2600, 8), (10500, 8)])
+def test_append_to_arbitrary_slots_stays_in_the_pools(B, dev, eo, kv_small, tokens, heads):
+    """Launches of either compressor, K and V in one and in two launches; places that no slot names stay as they are."""
+    rng = np.random.default_rng([56, tokens])
+    page, pages = 16, tokens // 8 + 2
+    d_meta = B.meta_to_device(lib_meta_from_oracle(B, kv_small["meta"]))
+    src = kv_small["k"].reshape(-1, 128)
+    x = torch.from_numpy(src[rng.integers(0, len(src), tokens * 2 * heads)].reshape(tokens, -1)).cuda()
+    for kind in ("any", "extremes", "in range"):
+        pools = [Guarded((pages, heads, page, 64), torch.uint8, 0x3c) for _ in range(2)]
+        cache = B.paged_cache(d_meta, d_meta, pools[0].body, pools[1].body, pages, heads, page)
+        slots = torch.empty(tokens, dtype=torch.int32, device="cuda")
+        arbitrary(rng, slots, kind, pages * page)
+        B.ecco_paged_append(cache, x.data_ptr(), x.data_ptr() + heads * 256, 2 * heads * 128, slots, tokens)
+        named = slots[(slots >= 0) & (slots < pages * page)].long()
+        untouched = torch.ones(pages * page, dtype=torch.bool, device="cuda")
+        untouched[named] = False
+        for pool in pools:
+            pool.check(kind)
+            assert (pool.body.permute(0, 2, 1, 3).reshape(pages * page, -1)[untouched] == 0x3c).all(), kind
