@@ -663,7 +663,7 @@ constexpr uint64_t kKvManyGroups = 16384;
 template <class Groups>
 static int launch_kv_compress(const DeviceInfo& di, const Groups& groups, uint64_t n_groups, int kinds, cudaStream_t s)
 {
-    if (n_groups * kinds >= kKvManyGroups) {
+    if (!Groups::kFewToo || n_groups * kinds >= kKvManyGroups) {
         static thread_local bool configured[64] = {};
         if (!configured[di.device]) {
             const int rc = set_smem(ecco_kv_compress_many_kernel<Groups>, sizeof(KvManySmem));
@@ -673,10 +673,12 @@ static int launch_kv_compress(const DeviceInfo& di, const Groups& groups, uint64
         return launch_overlapped(ecco_kv_compress_many_kernel<Groups>, static_cast<unsigned>(kinds * spread_ctas(static_cast<int64_t>((n_groups + 3) / 4), di.sms / kinds)),
                                  static_cast<unsigned>(kKvManyWarps * 32), sizeof(KvManySmem), s, groups, n_groups);
     }
-    const uint64_t ctas = (n_groups + kKvWarps - 1) / kKvWarps;
-    const uint64_t cap = static_cast<uint64_t>(di.sms) * 8 / kinds;
-    return launch_overlapped(ecco_kv_compress_kernel<Groups>, static_cast<unsigned>(kinds * (ctas < cap ? ctas : cap)), static_cast<unsigned>(kKvWarps * 32), 0, s, groups,
-                             n_groups);
+    if constexpr (Groups::kFewToo) {
+        const uint64_t ctas = (n_groups + kKvWarps - 1) / kKvWarps;
+        const uint64_t cap = static_cast<uint64_t>(di.sms) * 8 / kinds;
+        return launch_overlapped(ecco_kv_compress_kernel<Groups>, static_cast<unsigned>(kinds * (ctas < cap ? ctas : cap)), static_cast<unsigned>(kKvWarps * 32), 0, s, groups,
+                                 n_groups);
+    }
 }
 
 extern "C" int ecco_kv_compress(const void* d_meta, const void* d_x_fp16, uint64_t n_groups, uint8_t* d_blocks, void* stream)
@@ -742,6 +744,7 @@ extern "C" int ecco_paged_plan(int32_t page_size, int32_t n_pages, int32_t n_req
 // Groups from which on K and V are compressed one after the other, each by all CTAs: they rarely take equally long, and half of the
 // CTAs would wait for the others.
 constexpr uint64_t kAppendTwoGroups = 65536;
+static_assert(kAppendTwoGroups >= kKvManyGroups, "K or V alone is always a call of many groups");
 extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k, const void* d_v, int64_t token_stride, const int32_t* d_slots,
                                  int32_t n_tokens, void* stream)
 {

@@ -22,6 +22,7 @@ namespace {
 // Where the groups of a call lie and where their blocks go.  cta of ctas: this CTA among those that share its groups.  A place is what both
 // follow from.
 struct DenseGroups {                                       // one after the other
+    static constexpr bool kFewToo = true;                  // calls of few groups come in this form
     using Place = uint64_t;
     const uint8_t* image;
     const __half* x;
@@ -41,6 +42,7 @@ struct DenseGroups {                                       // one after the othe
 // New tokens of a paged cache: group g is head g % heads of token g / heads.  kKind 0: K, 1: V, 2: even CTAs K, odd ones V.
 template <int kKind>
 struct PagedGroups {
+    static constexpr bool kFewToo = kKind == 2;
     struct Place { uint32_t token, head; };
     const uint8_t *k_image, *v_image;
     const __half *k, *v;

@@ -298,6 +298,29 @@ def test_append_writes_the_oracles_blocks_into_the_slots(B, dev, eo, kv_small, t
     assert B.ecco_device_status() == 0
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,heads", [(1023, 8), (1024, 8), (2731, 3), (8191, 8), (8192, 8), (10239, 8), (10240, 8), (27307, 3), (1300, 64)])
+def test_append_gives_the_blocks_of_kv_compress(B, dev, eo, kv_small, tokens, heads):
+    """On both sides of the lines between the two compressors and between one launch and two, with metadata of their own for K and V."""
+    rng = np.random.default_rng([70, tokens])
+    meta_v = eo.calibrate(kv_small["cal"].reshape(-1)[:128 * 512], S=16, H=4, seed=9, select=eo.SELECT_MINMAX)
+    d_meta = [B.meta_to_device(lib_meta_from_oracle(B, m)) for m in (kv_small["meta"], meta_v)]
+    src = torch.from_numpy(kv_small["k"].reshape(-1, 128)).cuda()
+    x = src[torch.from_numpy(rng.integers(0, len(src), (tokens, 2, heads))).cuda()]
+    page = 16
+    pages = tokens // page + 2
+    slots = torch.from_numpy(rng.permutation(pages * page)[:tokens]).cuda()
+    pools = [torch.zeros((pages, heads, page, 64), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = B.paged_cache(*d_meta, *pools, pages, heads, page)
+    B.ecco_paged_append(cache, x.data_ptr(), x.data_ptr() + heads * 256, 2 * heads * 128, slots.int(), tokens)
+    for which in range(2):
+        rows = x[:, which].contiguous()
+        want = torch.empty((tokens, heads, 64), dtype=torch.uint8, device="cuda")
+        B.ecco_kv_compress(d_meta[which], rows, tokens * heads, want)
+        assert torch.equal(pools[which].permute(0, 2, 1, 3).reshape(pages * page, heads, 64)[slots], want), which
+    assert B.ecco_device_status() == 0
+
+
 # ------------------------------------------------------------------ attention
 class Paged:
     """Requests of given lengths over pools of blocks drawn from the oracle-encoded cache."""
