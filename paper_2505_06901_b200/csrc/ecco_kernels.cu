@@ -741,9 +741,10 @@ extern "C" int ecco_paged_plan(int32_t page_size, int32_t n_pages, int32_t n_req
                              static_cast<cudaStream_t>(stream), p);
 }
 
-// Groups from which on K and V are compressed one after the other, each by all CTAs: they rarely take equally long, and half of the
-// CTAs would wait for the others.
-constexpr uint64_t kAppendTwoGroups = 65536;
+// Groups (of K, and as many of V) from which on K and V are compressed one after the other, each by all CTAs: they rarely take equally long, and
+// half of the CTAs would wait for the others; below, the second launch costs more.  One launch / two, in us: 48 000 groups 61 / 64,
+// 65 536 groups 72 / 77 (74 / 77 of 32 heads), 88 000 groups 96 / 91, 96 000 groups 98 / 99, 109 000 groups 113 / 105, 131 072 groups 125 / 118.
+constexpr uint64_t kAppendTwoGroups = 81920;
 static_assert(kAppendTwoGroups >= kKvManyGroups, "K or V alone is always a call of many groups");
 extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k, const void* d_v, int64_t token_stride, const int32_t* d_slots,
                                  int32_t n_tokens, void* stream)
