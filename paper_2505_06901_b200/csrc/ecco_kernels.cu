@@ -776,11 +776,13 @@ extern "C" int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k,
 
 namespace {
 constexpr float kLog2E = 1.4426950408889634f;
-// Tiles per warp (of each kind) from which on every CTA decodes both kinds (between one and three it makes no difference), and from
+// Tiles per warp (of each kind) from which on every CTA decodes both kinds, which costs a second set of tables and saves the wait of those
+// CTAs whose kind is done first (8 requests of five rows, 8 heads, halves / both, in us: 1.0 tiles 90 / 97, 2.0 tiles 129 / 129, 3.0 tiles 167 / 170,
+// 4.0 tiles 207 / 205, 4.6 tiles 229 / 232, 5.0 tiles 248 / 244, 5.6 tiles 265 / 268, 6.0 tiles 284 / 277, 10 tiles 437 / 419), and from
 // which on one or two rows to a request take the products with K at once (8 requests of 1600 tokens, 32 heads, 2.8 tiles: 118 -> 106 us;
 // of 1024, 1.8 tiles: 80 -> 75; of 800, 1.4 tiles: 67 -> 66).  With three to eight rows that pays later: 8 requests, 8 heads, three / eight
 // rows, 2.1 tiles: 99 / 101 -> 103 / 106; 4.1 tiles: 163 / 167 -> 164 / 170; 6.1 tiles: 234 / 234 -> 225 / 234; 13.6 tiles: 530 / 531 -> 506 / 520.
-constexpr int kStageBothTiles = 3, kScoresTiles = 1, kScoresMmaTiles = 6;
+constexpr int kStageBothTiles = 5, kScoresTiles = 1, kScoresMmaTiles = 6;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
 //   tiles | schedule: few_tiles, block_tiles, blocks, n_blocks, tickets, cuts | few rows: sums, maxima | many rows: sums, maxima
 struct PagedAttnPlan {
