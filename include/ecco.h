@@ -248,8 +248,8 @@ int ecco_kv_compress(const void* d_meta, const void* d_x_fp16, uint64_t n_groups
  * of their queries.  All lengths are device arrays, and the sizes that the host passes are upper bounds, so a step
  * may be captured into a graph and replayed with other lengths.
  *
- * Pools are 32-byte aligned, arrays of int32 4-byte aligned; page_size is a power of two up to 4096, and
- * n_pages * page_size is below 2^31.  Whatever the device arrays hold, no call reads or writes outside the buffers that
+ * Pools are 32-byte aligned, arrays of int32 4-byte aligned; page_size is a power of two up to 4096,
+ * n_pages * page_size is below 2^31, n_kv_heads up to 65535.  Whatever the device arrays hold, no call reads or writes outside the buffers that
  * it was given. */
 typedef struct ecco_paged_cache {
     const void* d_k_meta;      /* device: metadata images of the K and of the V cache */
@@ -292,12 +292,14 @@ int ecco_paged_append(const ecco_paged_cache* cache, const void* d_k_fp16, const
  * cu_new[n_req] are left as they are.  q_per_kv in 1..16; q_stride a multiple of 8.
  * Scores, maxima, sums of weights and the sums over tokens are held in fp32; weights enter the tensor cores as fp16 (rounding
  * 2^-11 of each weight, or 2^-32 of the row's largest).  A decoded value beyond fp16's range enters as +-65504.  A q that is not finite
- * spoils the rows of its own token only (NaN gives NaN); scale, times log2(e), is finite.  The result does not depend on scheduling.  d_out and d_lse overlap
- * neither q nor the pools nor the workspace.
+ * spoils the rows of its own token only (NaN gives NaN), and a score beyond fp32's range its own row; scale, times log2(e), is finite.
+ * The result does not depend on scheduling.  d_out and d_lse overlap neither q nor the pools nor the workspace.
  * Upper bounds that the host knows: n_tokens of d_cu_new[n_req] (the rows of q and out), max_new and max_kv of one request's new tokens and
  * of its length, max_tiles of d_kv_tiles[n_req].  What exceeds them, prefix sums that are negative or fall, lengths that do not fit their
- * tiles, and tokens whose page is not one of the pool, give unspecified values for the request and make ecco_device_status() report
- * ECCO_ERR_INVALID_ARG.
+ * tiles, and tokens whose page is not one of the pool, give unspecified values for the requests concerned and make ecco_device_status()
+ * report ECCO_ERR_INVALID_ARG.
+ * n_req and n_kv_heads * q_per_kv go up to 65535, n_tokens * n_kv_heads * q_per_kv to 2^31 - 1025; max_tiles is below 2^26, max_tiles *
+ * n_kv_heads below 2^30, and the product of n_tokens / (2 * (128 / q_per_kv)) + n_req + 1 and max_kv / 128 + 1, integer divisions, below 2^31.
  * The blocks are decoded once per call, into 512 bytes of the workspace per token and KV head.  A workspace that is smaller than
  * ecco_paged_attn_workspace_bytes (for the same arguments), down to what that gives for n_kv_heads = 1, makes the call
  * take some heads at a time.  16-byte aligned; contents irrelevant before and undefined after; calls sharing a workspace must

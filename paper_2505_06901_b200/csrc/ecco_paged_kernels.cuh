@@ -595,8 +595,9 @@ ecco_paged_scores_mma_kernel(const __grid_constant__ PagedKv kv, const __grid_co
 //   S = Q K^T (16 rows x 32 tokens a tile, mma.sync), the softmax on the way in fp32, O += P V
 // with P taken from the scores' registers as they are.  A piece of a request that lies in one run as a whole is written out; the others
 // leave sums and maxima in the workspace and are joined by ecco_paged_join_kernel.
-// Bound by memory: 512 bytes per token and KV head (1.09 GB in 165 us, the copy rate); the products take as long at sixteen rows, mma.sync being
-// slow here, so requests of more rows are for ecco_paged_many_kernel (20 to 32 rows: 57 us here with two tiles of rows, 42 there).
+// Bound by memory: 512 bytes per token and KV head (2.1 M tokens and KV heads, 1.09 GB, twelve or sixteen rows: 189 us = 5.75 TB/s, 89 % of the copy
+// rate, some of it from L2; scores given, eight rows, 0.61 GB: 111 us = 5.5 TB/s).  The products take nearly as long at sixteen rows, mma.sync being
+// slow here, so requests of more rows are for ecco_paged_many_kernel (20 to 32 rows took 57 us here with two tiles of rows, 42 there).
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewRows = 16;
 template <bool kScores> constexpr int kFewWarps = kScores ? 8 : 6;
@@ -617,7 +618,10 @@ __device__ __forceinline__ UnitSplit few_split(int64_t units, int ctas)
     return UnitSplit(units, static_cast<int>(max(static_cast<int64_t>(1), min(static_cast<int64_t>(ctas) * kFewWarps<kScores>, runs))));
 }
 
-// Weights enter the tensor cores times 2^15: taken as they are, those below 6e-5 would lose bits and those below 3e-8 vanish.
+// Weights enter the tensor cores as one fp16 number each: half a step, 2^-11 of a weight, is 2^-11 sum p |v| of an output, beside the 2^-11 |out|
+// that the output's own rounding costs (measured against 64 bits, norms: 2.2e-4 of the output instead of 2.1e-4 with few rows, 2.8e-4 with
+// many).  Two numbers as in ecco_attn_values would leave the latter alone, for half as many products again.  Their sum is taken in fp32 before the
+// rounding.  They stand at 2^15 times what they are: taken as they are, those below 6e-5 would lose bits and those below 3e-8 vanish.
 constexpr float kWeightLog2 = 15.0f;
 __device__ __forceinline__ float exp2_fast(float x)
 {
