@@ -318,6 +318,85 @@ int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_batch* batch
                     int64_t q_stride, float scale, uint32_t flags, void* d_out_fp16, float* d_lse_or_null, void* d_workspace,
                     size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------- rotary positions
+ * The first rot_dim dims of a 128-wide head form rot_dim / 2 pairs, (i, i + rot_dim / 2) or, with ECCO_ROPE_NEIGHBOURS, (2i, 2i + 1); the others
+ * stay as they are.  Pair i of a row at position p is turned by the angle p * inv_freq[i]:
+ *   (a, b) -> gain * (a cos - b sin, b cos + a sin),  with ECCO_ROPE_INVERSE  gain * (a cos + b sin, b cos - a sin),
+ * the transposed map: what a gradient goes through and, with a gain of 1, what takes the positions out again.  Angles are
+ * kept as 64-bit fractions of a turn, of which a position is a whole multiple: whatever the position, cos and sin are those of the angle to a
+ * few 2^-24.  Products and sums in fp32, rounded once to fp16; a pair with a value that is not finite gives values that are not finite. */
+#define ECCO_ROPE_NEIGHBOURS 1u
+#define ECCO_ROPE_INVERSE 2u
+typedef struct ecco_rope {             /* made by ecco_rope_init; read before a call returns */
+    uint64_t turn[ECCO_GROUP / 2];     /* fraction of a turn per position, times 2^64 */
+    float gain;
+    int32_t rot_dim;
+    uint32_t flags;
+} ecco_rope;
+
+/* Frequencies (radians per position) of rot_dim / 2 pairs (host arrays): base^(-2i / rot_dim), for contexts longer than the trained ones
+ * slowed down by `factor`:
+ *   ECCO_ROPE_SCALE_LINEAR   all alike
+ *   ECCO_ROPE_SCALE_BASE     by a larger base, base * factor^(rot_dim / (rot_dim - 2)): the first pair not at all, the last one by factor
+ *   ECCO_ROPE_SCALE_BANDS    pairs that make `low` turns or fewer over trained_len by factor, those with `high` or more not at all, the others in
+ *                            between, in proportion to their turns
+ *   ECCO_ROPE_SCALE_RAMP     the same, in proportion to the pair's number, between the pairs (rounded outwards) that make `high` and `low` turns;
+ *                            *gain is 0.1 ln(factor) + 1 then and 1 otherwise
+ * scaling NULL: ECCO_ROPE_SCALE_NONE.  rot_dim: a multiple of 16 up to 128; base above 1; factor at least 1, and 0 < low < high and trained_len > 0
+ * where they count. */
+enum { ECCO_ROPE_SCALE_NONE = 0, ECCO_ROPE_SCALE_LINEAR = 1, ECCO_ROPE_SCALE_BASE = 2, ECCO_ROPE_SCALE_BANDS = 3, ECCO_ROPE_SCALE_RAMP = 4 };
+typedef struct ecco_rope_scaling {
+    int32_t kind;
+    double factor, low, high, trained_len;
+} ecco_rope_scaling;
+int ecco_rope_frequencies(int32_t rot_dim, double base, const ecco_rope_scaling* scaling_or_null, double* inv_freq, float* gain);
+/* *rope from rot_dim / 2 frequencies of any origin, all finite; gain finite; flags as above. */
+int ecco_rope_init(int32_t rot_dim, const double* inv_freq, float gain, uint32_t flags, ecco_rope* rope);
+
+/* n_tokens rows of n_heads heads, row i at d_x_fp16 + i * x_stride values, turned by d_positions[i] (any int32) into d_out_fp16 + i * out_stride:
+ * the queries and keys in the rows of one projection, say.  In place (the same address and stride) or without overlap.  16-byte aligned; strides
+ * multiples of 8, at least 128 * n_heads, below 2^38; n_heads in 1..65535. */
+int ecco_rope_apply(const ecco_rope* rope, const int32_t* d_positions, int32_t n_tokens, int32_t n_heads, const void* d_x_fp16, int64_t x_stride,
+                    void* d_out_fp16, int64_t out_stride, void* stream);
+
+/* ---------------------------------------------------------------- paged KV cache in 8 bits (device)
+ * A paged cache of half the size of fp16, for what the 64-byte blocks hold too coarsely.  Pages, block tables and slots are those of
+ * the paged cache above, and ecco_paged_plan serves both; the head vector of (page, head, place) is 128 E4M3 bytes at byte
+ * 128 * ((page * n_kv_heads + head) * page_size + place).  min(16, page_size) consecutive places of a page are a block and share, head by head, a
+ * power of two: byte (page * n_kv_heads + head) * max(1, page_size / 16) + place / 16 of the scales holds its exponent e plus 127
+ * (E8M0), e in -15..7 (others count as the nearest of these).  A value is its E4M3 number times 2^e: exactly an fp16 number.
+ *
+ * Pools are 16-byte aligned; page_size, n_pages and n_kv_heads as above.  Whatever the device arrays hold, no call reads or writes outside the buffers
+ * that it was given. */
+#define ECCO_PAGED8_BLOCK 16
+typedef struct ecco_paged8_cache {
+    uint8_t* d_k;              /* device: 128 * n_pages * n_kv_heads * page_size bytes each */
+    uint8_t* d_v;
+    uint8_t* d_k_scales;       /* device: n_pages * n_kv_heads * max(1, page_size / 16) bytes each */
+    uint8_t* d_v_scales;
+    int32_t n_pages, n_kv_heads, page_size;
+} ecco_paged8_cache;
+
+/* New tokens into their slots: K and V of token i, fp16 [n_kv_heads][128] at d_k_fp16 and d_v_fp16 + i * token_stride values, K turned by
+ * d_positions[i] on the way and rounded to fp16, as by ecco_rope_apply (rope NULL: taken as it is, no positions).  A block gets the smallest e with |x| <= 448 * 2^e
+ * for all the tokens that the call brings, and every value the nearest E4M3 number (ties to even) to x / 2^e; larger values than 448 * 2^7
+ * saturate, infinities too, NaN becomes zero.  A call that brings the token of a block's first place begins the block anew.  Otherwise e is no smaller than
+ * it was, and where it is larger the block's other values are rounded again.
+ * Tokens whose slot is negative or beyond the pool are left out.  The slots of a call are distinct, and the tokens of one block stand in consecutive rows
+ * in ascending order (as ecco_paged_plan has them); other orders give unspecified values in the blocks concerned.  token_stride is a multiple of 8, at least
+ * 128 * n_kv_heads; d_k_fp16 and d_v_fp16 16-byte aligned. */
+int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope_or_null, const int32_t* d_positions, const void* d_k_fp16, const void* d_v_fp16,
+                       int64_t token_stride, const int32_t* d_slots, int32_t n_tokens, void* stream);
+
+/* ecco_paged_attn over this cache: the same batch, flags, rows, bounds, in- and outputs and limits; so is what is said there of masks, of values that are
+ * not finite and of arrays that are wrong.  Bytes 0x7f and 0xff (NaN), which ecco_paged8_append never writes, spoil the rows of the request and head that they
+ * are in, where they lie within its length.  Weights enter the tensor cores as fp16 with 2^-11 of each, or 2^-30 of the largest product of a weight and
+ * its block's 2^e.  A workspace that is smaller than ecco_paged8_attn_workspace_bytes, down to what that gives for n_kv_heads = 1, makes the call take
+ * some heads at a time; 16-byte aligned; contents irrelevant before and undefined after; calls sharing a workspace must not overlap. */
+size_t ecco_paged8_attn_workspace_bytes(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv);
+int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q_fp16, int64_t q_stride, float scale,
+                     uint32_t flags, void* d_out_fp16, float* d_lse_or_null, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------- variable-length container */
 
 /* The same per-group fields as the 64-byte block (scale byte, ID_HF, ID_KP codeword, 128 codewords;

@@ -20,6 +20,10 @@ SELECT_MSE = 0
 SELECT_MINMAX = 1
 KEEP_EXPONENT = 2
 ATTN_CAUSAL = 1
+ROPE_NEIGHBOURS = 1
+ROPE_INVERSE = 2
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP = range(5)
+PAGED8_BLOCK = 16
 
 ECCO_OK = 0
 ERR_INVALID_ARG = -1
@@ -37,6 +41,7 @@ EXPORTS = [
     "ecco_gemv", "ecco_gemv_batch_workspace_bytes", "ecco_gemv_batch", "ecco_gemv_static_ws", "ecco_attn_scores", "ecco_act_compress", "ecco_act_decompress",
     "ecco_attn_values_workspace_bytes", "ecco_attn_values", "ecco_kv_compress",
     "ecco_paged_plan", "ecco_paged_append", "ecco_paged_attn_workspace_bytes", "ecco_paged_attn",
+    "ecco_rope_frequencies", "ecco_rope_init", "ecco_rope_apply", "ecco_paged8_append", "ecco_paged8_attn_workspace_bytes", "ecco_paged8_attn",
     "ecco_var_stream_bytes_bound", "ecco_var_index_bytes", "ecco_var_encode_host", "ecco_var_decompress", "ecco_error_string", "ecco_last_cuda_error", "ecco_device_status",
     "ecco_kernel_launch_count", "ecco_test_wait_timeout", "ecco_test_gemv_give_up", "ecco_test_attn_values_give_up",
 ]
@@ -64,6 +69,22 @@ class PagedBatch(C.Structure):
     _fields_ = [("d_block_tables", C.c_void_p), ("d_cu_new", C.c_void_p), ("d_kv_lens", C.c_void_p), ("d_kv_tiles", C.c_void_p),
                 ("table_stride", C.c_int32), ("n_req", C.c_int32), ("n_tokens", C.c_int32),
                 ("max_new", C.c_int32), ("max_kv", C.c_int32), ("max_tiles", C.c_int32)]
+
+
+class Paged8Cache(C.Structure):
+    """ecco_paged8_cache of include/ecco.h."""
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p),
+                ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("page_size", C.c_int32)]
+
+
+class Rope(C.Structure):
+    """ecco_rope of include/ecco.h."""
+    _fields_ = [("turn", C.c_uint64 * (GROUP // 2)), ("gain", C.c_float), ("rot_dim", C.c_int32), ("flags", C.c_uint32)]
+
+
+class RopeScaling(C.Structure):
+    """ecco_rope_scaling of include/ecco.h."""
+    _fields_ = [("kind", C.c_int32), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("trained_len", C.c_double)]
 
 
 class EccoError(RuntimeError):
@@ -130,6 +151,13 @@ def lib():
         L.ecco_paged_attn_workspace_bytes.argtypes = [C.POINTER(PagedCache), C.POINTER(PagedBatch), i32]
         L.ecco_paged_attn_workspace_bytes.restype = sz
         L.ecco_paged_attn.argtypes = [C.POINTER(PagedCache), C.POINTER(PagedBatch), i32, vp, C.c_int64, C.c_float, C.c_uint32, vp, vp, vp, sz, vp]
+        L.ecco_rope_frequencies.argtypes = [i32, C.c_double, C.POINTER(RopeScaling), vp, C.POINTER(C.c_float)]
+        L.ecco_rope_init.argtypes = [i32, vp, C.c_float, C.c_uint32, C.POINTER(Rope)]
+        L.ecco_rope_apply.argtypes = [C.POINTER(Rope), vp, i32, i32, vp, C.c_int64, vp, C.c_int64, vp]
+        L.ecco_paged8_append.argtypes = [C.POINTER(Paged8Cache), C.POINTER(Rope), vp, vp, vp, C.c_int64, vp, i32, vp]
+        L.ecco_paged8_attn_workspace_bytes.argtypes = [C.POINTER(Paged8Cache), C.POINTER(PagedBatch), i32]
+        L.ecco_paged8_attn_workspace_bytes.restype = sz
+        L.ecco_paged8_attn.argtypes = [C.POINTER(Paged8Cache), C.POINTER(PagedBatch), i32, vp, C.c_int64, C.c_float, C.c_uint32, vp, vp, vp, sz, vp]
         L.ecco_var_stream_bytes_bound.argtypes = [u64]
         L.ecco_var_stream_bytes_bound.restype = sz
         L.ecco_var_index_bytes.argtypes = [u64]
@@ -439,6 +467,57 @@ def ecco_paged_attn(cache: PagedCache, batch: PagedBatch, q_per_kv: int, d_q_fp1
     _check(lib().ecco_paged_attn(C.byref(cache), C.byref(batch), q_per_kv, _ptr(d_q_fp16), q_stride, C.c_float(scale), flags, _ptr(d_out_fp16),
                                  _ptr(d_lse) if d_lse is not None else None, _ptr(d_workspace) if d_workspace is not None else None,
                                  workspace_bytes, _stream(stream)), "ecco_paged_attn")
+
+
+def ecco_rope_frequencies(rot_dim: int, base: float, kind: int = ROPE_SCALE_NONE, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                          trained_len: float = 0.0):
+    """-> (frequencies float64 [rot_dim / 2] in radians per position, gain), as ecco_rope_init takes them (see include/ecco.h)."""
+    inv_freq, gain = np.zeros(max(rot_dim // 2, 1)), C.c_float()
+    scaling = RopeScaling(kind, factor, low, high, trained_len)
+    _check(lib().ecco_rope_frequencies(rot_dim, base, C.byref(scaling), inv_freq.ctypes.data, C.byref(gain)), "ecco_rope_frequencies")
+    return inv_freq, gain.value
+
+
+def ecco_rope_init(rot_dim: int, inv_freq, gain: float = 1.0, flags: int = 0) -> Rope:
+    """The rotation that ecco_rope_apply and ecco_paged8_append take: a host object, made once and kept."""
+    inv_freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    if inv_freq.shape != (rot_dim // 2,):
+        raise ValueError("inv_freq must hold rot_dim / 2 numbers")
+    rope = Rope()
+    _check(lib().ecco_rope_init(rot_dim, inv_freq.ctypes.data, C.c_float(gain), flags, C.byref(rope)), "ecco_rope_init")
+    return rope
+
+
+def ecco_rope_apply(rope: Rope, d_positions, n_tokens: int, n_heads: int, d_x_fp16, x_stride: int, d_out_fp16, out_stride: int, stream=None) -> None:
+    """Rows of heads turned by their positions; in place where d_out_fp16 is d_x_fp16 with the same stride."""
+    _check(lib().ecco_rope_apply(C.byref(rope), _ptr(d_positions), n_tokens, n_heads, _ptr(d_x_fp16), x_stride, _ptr(d_out_fp16), out_stride,
+                                 _stream(stream)), "ecco_rope_apply")
+
+
+def paged8_cache(d_k, d_v, d_k_scales, d_v_scales, n_pages: int, n_kv_heads: int, page_size: int) -> Paged8Cache:
+    """The pools of a paged cache in 8 bits as ecco_paged8_append and ecco_paged8_attn take them.  Built once and kept; it keeps the
+    tensors alive whose addresses it holds."""
+    cache = Paged8Cache(_ptr(d_k), _ptr(d_v), _ptr(d_k_scales), _ptr(d_v_scales), n_pages, n_kv_heads, page_size)
+    cache.keeps = (d_k, d_v, d_k_scales, d_v_scales)
+    return cache
+
+
+def ecco_paged8_append(cache: Paged8Cache, rope, d_positions, d_k_fp16, d_v_fp16, token_stride: int, d_slots, n_tokens: int, stream=None) -> None:
+    """New tokens into the slots of a paged cache in 8 bits, K turned by its positions on the way; rope None: K as it is, no positions."""
+    _check(lib().ecco_paged8_append(C.byref(cache), C.byref(rope) if rope is not None else None, _ptr(d_positions) if d_positions is not None else None,
+                                    _ptr(d_k_fp16), _ptr(d_v_fp16), token_stride, _ptr(d_slots), n_tokens, _stream(stream)), "ecco_paged8_append")
+
+
+def ecco_paged8_attn_workspace_bytes(cache: Paged8Cache, batch: PagedBatch, q_per_kv: int) -> int:
+    return int(lib().ecco_paged8_attn_workspace_bytes(C.byref(cache), C.byref(batch), q_per_kv))
+
+
+def ecco_paged8_attn(cache: Paged8Cache, batch: PagedBatch, q_per_kv: int, d_q_fp16, q_stride: int, scale: float, flags: int, d_out_fp16,
+                     d_lse, d_workspace, workspace_bytes: int, stream=None) -> None:
+    """ecco_paged_attn over a paged cache in 8 bits -> fp16 [n_tokens][n_kv_heads*q_per_kv][128]; d_lse may be None."""
+    _check(lib().ecco_paged8_attn(C.byref(cache), C.byref(batch), q_per_kv, _ptr(d_q_fp16), q_stride, C.c_float(scale), flags, _ptr(d_out_fp16),
+                                  _ptr(d_lse) if d_lse is not None else None, _ptr(d_workspace) if d_workspace is not None else None,
+                                  workspace_bytes, _stream(stream)), "ecco_paged8_attn")
 
 
 def ecco_var_decompress(d_meta, d_stream, d_index, n_groups: int, d_out_fp16, stream=None) -> None:

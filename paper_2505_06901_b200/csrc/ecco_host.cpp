@@ -1039,6 +1039,68 @@ extern "C" int ecco_meta_serialize_device(const ecco_meta* m, void* host_staging
     return ECCO_OK;
 }
 
+// ---------------------------------------------------------------------------------------------
+// rotary positions: frequencies and fractions of a turn
+// ---------------------------------------------------------------------------------------------
+namespace {
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+bool rope_dim_fine(int32_t rot_dim) { return rot_dim >= 16 && rot_dim <= kGroup && rot_dim % 16 == 0; }
+}  // namespace
+
+extern "C" int ecco_rope_frequencies(int32_t rot_dim, double base, const ecco_rope_scaling* scaling, double* inv_freq, float* gain)
+{
+    if (!rope_dim_fine(rot_dim) || !(base > 1.0) || !std::isfinite(base) || !inv_freq || !gain) return ECCO_ERR_INVALID_ARG;
+    const ecco_rope_scaling none = {};
+    const ecco_rope_scaling& sc = scaling ? *scaling : none;
+    if (sc.kind < ECCO_ROPE_SCALE_NONE || sc.kind > ECCO_ROPE_SCALE_RAMP) return ECCO_ERR_INVALID_ARG;
+    if (sc.kind != ECCO_ROPE_SCALE_NONE && (!(sc.factor >= 1.0) || !std::isfinite(sc.factor))) return ECCO_ERR_INVALID_ARG;
+    const bool bands = sc.kind == ECCO_ROPE_SCALE_BANDS || sc.kind == ECCO_ROPE_SCALE_RAMP;
+    if (bands && (!(sc.low > 0.0) || !(sc.high > sc.low) || !std::isfinite(sc.high) || !(sc.trained_len > 0.0) || !std::isfinite(sc.trained_len)))
+        return ECCO_ERR_INVALID_ARG;
+    const int pairs = rot_dim / 2;
+    double b = base;
+    if (sc.kind == ECCO_ROPE_SCALE_BASE) b = base * std::pow(sc.factor, static_cast<double>(rot_dim) / (rot_dim - 2));
+    if (!std::isfinite(b)) return ECCO_ERR_INVALID_ARG;
+    // the pair that makes n turns over the trained length, as a real number
+    auto pair_of = [&](double n) { return pairs * std::log(sc.trained_len / (n * kTwoPi)) / std::log(base); };
+    double from = 0.0, to = 0.0;
+    if (sc.kind == ECCO_ROPE_SCALE_RAMP) {
+        from = std::max(std::floor(pair_of(sc.high)), 0.0);
+        to = std::min(std::ceil(pair_of(sc.low)), static_cast<double>(rot_dim - 1));
+        if (to <= from) to = from + 0.001;
+    }
+    for (int i = 0; i < pairs; ++i) {
+        const double f = std::pow(b, -2.0 * i / rot_dim);
+        double as_it_is = 1.0;                             // share of the frequency that is not slowed down
+        if (sc.kind == ECCO_ROPE_SCALE_LINEAR) as_it_is = 0.0;
+        if (sc.kind == ECCO_ROPE_SCALE_BANDS) as_it_is = std::min(std::max((sc.trained_len * f / kTwoPi - sc.low) / (sc.high - sc.low), 0.0), 1.0);
+        if (sc.kind == ECCO_ROPE_SCALE_RAMP) as_it_is = 1.0 - std::min(std::max((i - from) / (to - from), 0.0), 1.0);
+        inv_freq[i] = as_it_is == 1.0 ? f : f * as_it_is + f / sc.factor * (1.0 - as_it_is);
+    }
+    *gain = sc.kind == ECCO_ROPE_SCALE_RAMP ? static_cast<float>(0.1 * std::log(sc.factor) + 1.0) : 1.0f;
+    return ECCO_OK;
+}
+
+extern "C" int ecco_rope_init(int32_t rot_dim, const double* inv_freq, float gain, uint32_t flags, ecco_rope* rope)
+{
+    if (!rope_dim_fine(rot_dim) || !inv_freq || !rope || !std::isfinite(gain) || (flags & ~(ECCO_ROPE_NEIGHBOURS | ECCO_ROPE_INVERSE))) return ECCO_ERR_INVALID_ARG;
+    for (int i = 0; i < rot_dim / 2; ++i)
+        if (!std::isfinite(inv_freq[i])) return ECCO_ERR_INVALID_ARG;
+    std::memset(rope, 0, sizeof *rope);
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        // turns per position, whole ones dropped, with the 64 bits of a long double's mantissa: positions are whole numbers, so only the
+        // fraction counts
+        long double turns = static_cast<long double>(inv_freq[i]) / 6.283185307179586476925286766559005768L;
+        turns -= std::floor(turns);
+        const long double scaled = std::ldexp(turns, 64);
+        rope->turn[i] = scaled >= 18446744073709551615.0L ? 0 : static_cast<uint64_t>(scaled + 0.5L);
+    }
+    rope->gain = gain;
+    rope->rot_dim = rot_dim;
+    rope->flags = flags;
+    return ECCO_OK;
+}
+
 extern "C" const char* ecco_error_string(int code)
 {
     switch (code) {

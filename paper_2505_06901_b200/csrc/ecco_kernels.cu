@@ -29,6 +29,8 @@
 //   ecco_kv_compress_kernel.cuh     online 4x compressor
 //   ecco_paged_kernels.cuh          paged KV cache: slots and block tables, pages into tiles, attention of few rows
 //   ecco_paged_many_kernel.cuh      attention of many rows over it, on tcgen05
+//   ecco_rope_kernels.cuh           rotary positions
+//   ecco_paged8_kernels.cuh         paged KV cache in 8 bits: append, pages into tiles, attention of few rows
 //   ecco_launch.cuh                 device query, overlapped launches, work plans
 //   this file                       the C ABI: argument checks and launches
 #include "ecco_device_core.cuh"
@@ -43,6 +45,8 @@
 #include "ecco_kv_compress_kernel.cuh"
 #include "ecco_paged_kernels.cuh"
 #include "ecco_paged_many_kernel.cuh"
+#include "ecco_rope_kernels.cuh"
+#include "ecco_paged8_kernels.cuh"
 
 
 // ---------------------------------------------------------------------------------------------
@@ -1004,4 +1008,221 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
         if (rc) return rc;
     }
     return ECCO_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rotary positions
+// ---------------------------------------------------------------------------------------------
+static bool rope_fine(const ecco_rope* r)
+{
+    return r && r->rot_dim >= 16 && r->rot_dim <= kGroup && r->rot_dim % 16 == 0 && std::isfinite(r->gain) && !(r->flags & ~(ECCO_ROPE_NEIGHBOURS | ECCO_ROPE_INVERSE));
+}
+
+extern "C" int ecco_rope_apply(const ecco_rope* rope, const int32_t* d_positions, int32_t n_tokens, int32_t n_heads, const void* d_x, int64_t x_stride,
+                               void* d_out, int64_t out_stride, void* stream)
+{
+    if (!rope_fine(rope) || n_tokens < 0 || n_heads < 1 || n_heads > 65535) return ECCO_ERR_INVALID_ARG;
+    if (n_tokens == 0) return ECCO_OK;
+    const int64_t row = static_cast<int64_t>(n_heads) * kGroup;
+    if (!d_positions || !d_x || !d_out || x_stride < row || out_stride < row || x_stride >= 1ll << 38 || out_stride >= 1ll << 38) return ECCO_ERR_INVALID_ARG;
+    if (!aligned16(d_x) || !aligned16(d_out) || x_stride % 8 || out_stride % 8 || !aligned_to(d_positions, 4)) return ECCO_ERR_ALIGNMENT;
+    if (d_x == d_out && x_stride != out_stride) return ECCO_ERR_INVALID_ARG;       // rows over one another's
+    DeviceInfo di;
+    const int rc = device_info(&di);
+    if (rc) return rc;
+    RopeRows p = {};
+    p.positions = d_positions;
+    p.x = static_cast<const __half*>(d_x); p.out = static_cast<__half*>(d_out);
+    p.x_stride = x_stride; p.out_stride = out_stride;
+    p.n_tokens = n_tokens; p.n_heads = n_heads;
+    // few tokens: their heads shared out, as far as every team of lanes has one
+    const int64_t windows = (static_cast<int64_t>(n_tokens) + kRopeTokens - 1) / kRopeTokens;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((2 * di.sms + windows - 1) / windows, (n_heads + kRopeTeams - 1) / kRopeTeams));
+    p.per_part = static_cast<int32_t>((n_heads + parts - 1) / parts);
+    p.parts = (n_heads + p.per_part - 1) / p.per_part;
+    return launch_overlapped(ecco_rope_kernel, static_cast<unsigned>(windows * p.parts), static_cast<unsigned>(kRopeThreads), 0, static_cast<cudaStream_t>(stream), *rope, p);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Paged KV cache in 8 bits
+// ---------------------------------------------------------------------------------------------
+static int check_paged8_cache(const ecco_paged8_cache* c)
+{
+    if (!c || !c->d_k || !c->d_v || !c->d_k_scales || !c->d_v_scales) return ECCO_ERR_INVALID_ARG;
+    if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 65535 || page_shift_of(c->page_size) < 0) return ECCO_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(c->n_pages) * c->page_size > INT32_MAX) return ECCO_ERR_INVALID_ARG;
+    if (!aligned16(c->d_k) || !aligned16(c->d_v)) return ECCO_ERR_ALIGNMENT;
+    return ECCO_OK;
+}
+
+extern "C" int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope, const int32_t* d_positions, const void* d_k, const void* d_v,
+                                  int64_t token_stride, const int32_t* d_slots, int32_t n_tokens, void* stream)
+{
+    int rc = check_paged8_cache(cache);
+    if (rc) return rc;
+    if (n_tokens < 0 || (rope && !rope_fine(rope))) return ECCO_ERR_INVALID_ARG;
+    if (n_tokens == 0) return ECCO_OK;
+    if (!d_k || !d_v || !d_slots || (rope && !d_positions) || token_stride < static_cast<int64_t>(cache->n_kv_heads) * kGroup || token_stride >= 1ll << 38) return ECCO_ERR_INVALID_ARG;
+    if (!aligned16(d_k) || !aligned16(d_v) || token_stride % 8 || !aligned_to(d_slots, 4) || (rope && !aligned_to(d_positions, 4))) return ECCO_ERR_ALIGNMENT;
+    DeviceInfo di;
+    rc = device_info(&di);
+    if (rc) return rc;
+    P8Append p = {};
+    p.positions = d_positions; p.slots = d_slots;
+    p.k = static_cast<const __half*>(d_k); p.v = static_cast<const __half*>(d_v);
+    p.k_codes = cache->d_k; p.v_codes = cache->d_v; p.k_scales = cache->d_k_scales; p.v_scales = cache->d_v_scales;
+    p.token_stride = token_stride;
+    p.n_tokens = n_tokens; p.n_slots = cache->n_pages * cache->page_size;
+    p.heads = cache->n_kv_heads; p.page_shift = page_shift_of(cache->page_size);
+    const int64_t windows = (static_cast<int64_t>(n_tokens) + kP8Rows - 1) / kP8Rows;
+    p.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>((4 * di.sms + windows - 1) / windows, 4ll * p.heads)));
+    const unsigned grid = static_cast<unsigned>(windows * p.parts);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (rope) return launch_overlapped(ecco_paged8_append_kernel<true>, grid, static_cast<unsigned>(kP8AppendThreads), 0, s, *rope, p);
+    return launch_overlapped(ecco_paged8_append_kernel<false>, grid, static_cast<unsigned>(kP8AppendThreads), 0, s, ecco_rope{}, p);
+}
+
+namespace {
+// rows of a request up to which they go to ecco_paged8_few_kernel, sixteen at a time
+constexpr int kP8FewRows = 64;
+// Workspace of a launch over some KV heads, all offsets multiples of 256:
+//   tiles (for many rows) | schedule | few rows: tickets, sums, maxima | many rows: sums, maxima
+struct P8AttnPlan {
+    bool many, line;                   // there may be requests of more rows; more requests than the kernel for few rows schedules itself
+    int few_ctas, many_ctas, max_blocks;
+    size_t few_tiles, block_tiles, blocks, n_blocks, tickets, few_tickets, few_part, few_ml, many_part, many_ml, bytes;
+};
+P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int all_heads, int q_per_kv, int ctas_max)
+{
+    P8AttnPlan p = {};
+    const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
+    p.many = rows > kP8FewRows;
+    p.line = b.n_req > kP8Reqs;
+    const int64_t groups = std::min<int64_t>((rows + kP8Rows16 - 1) / kP8Rows16, kP8FewRows / kP8Rows16);
+    p.few_ctas = std::max(1, spread_ctas((static_cast<int64_t>(b.max_tiles) * all_heads * std::max<int64_t>(groups, 1) + kP8Warps - 1) / kP8Warps, ctas_max));
+    p.many_ctas = ctas_max;
+    p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
+    size_t at = p.many ? static_cast<size_t>(std::max(b.max_tiles, 1)) * heads * 2 * kKvTileBytes : 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at = (at + bytes + 255) & ~static_cast<size_t>(255);
+        return here;
+    };
+    // room for the few rows of all heads: it does not depend on how many heads at a time the tiles are for
+    const size_t few_slots = static_cast<size_t>(ctas_max) * 2 * kP8Rows16, many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
+    p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
+    p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
+    p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
+    p.n_blocks = take(8);
+    p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
+    p.few_tickets = take(static_cast<size_t>(ctas_max) * kTicketStride * sizeof(Ticket));
+    p.few_part = take(few_slots * kGroup * sizeof(float));
+    p.few_ml = take(few_slots * sizeof(float2));
+    p.many_part = take(many_slots * kGroup * sizeof(float));
+    p.many_ml = take(many_slots * sizeof(float2));
+    p.bytes = at;
+    return p;
+}
+template <int kN>
+int launch_paged8_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const P8Few& f, int ctas, cudaStream_t s)
+{
+    static thread_local bool configured[64] = {};
+    if (!configured[di.device]) {
+        const int rc = set_smem(ecco_paged8_few_kernel<kN>, kP8SmemBytes);
+        if (rc) return rc;
+        configured[di.device] = true;
+    }
+    return launch_overlapped(ecco_paged8_few_kernel<kN>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8Warps * 32), kP8SmemBytes, s, kv, o, f);
+}
+// the part of the batch's checks that ecco_paged_attn has: the pages are the same
+bool paged8_batch_fine(const ecco_paged8_cache& c, const ecco_paged_batch& b, int q_per_kv)
+{
+    ecco_paged_cache same = {};
+    same.n_kv_heads = c.n_kv_heads;
+    return paged_batch_fine(same, b, q_per_kv);
+}
+}  // namespace
+
+extern "C" size_t ecco_paged8_attn_workspace_bytes(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv)
+{
+    if (!cache || !batch || cache->n_kv_heads < 1 || cache->n_kv_heads > 65535 || !paged8_batch_fine(*cache, *batch, q_per_kv)) return 0;
+    return paged8_attn_plan(*batch, cache->n_kv_heads, cache->n_kv_heads, q_per_kv, 256).bytes;
+}
+
+extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q, int64_t q_stride, float scale,
+                                uint32_t flags, void* d_out, float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = check_paged8_cache(cache);
+    if (rc) return rc;
+    if (!batch || !paged8_batch_fine(*cache, *batch, q_per_kv) || (flags & ~ECCO_ATTN_CAUSAL) || !std::isfinite(scale * kLog2E)) return ECCO_ERR_INVALID_ARG;
+    const ecco_paged_batch& b = *batch;
+    if (b.n_req == 0 || b.n_tokens == 0) return ECCO_OK;
+    const int q_heads = cache->n_kv_heads * q_per_kv;
+    if (!b.d_cu_new || !b.d_kv_lens || !b.d_kv_tiles || (b.table_stride && !b.d_block_tables) || !d_q || !d_out) return ECCO_ERR_INVALID_ARG;
+    if (q_stride < static_cast<int64_t>(q_heads) * kGroup || q_stride >= 1ll << 38) return ECCO_ERR_INVALID_ARG;
+    if (!aligned16(d_q) || q_stride % 8 || !aligned16(d_out) || !aligned_to(d_lse, 4)) return ECCO_ERR_ALIGNMENT;
+    for (const int32_t* p : {b.d_block_tables, b.d_cu_new, b.d_kv_lens, b.d_kv_tiles})
+        if (!aligned_to(p, 4)) return ECCO_ERR_ALIGNMENT;
+    // in place it cannot be done: a row of q is read by whoever has tokens that it sees, at any time
+    if (d_workspace && (d_out == d_q || d_out == d_workspace || d_q == d_workspace)) return ECCO_ERR_INVALID_ARG;
+    DeviceInfo di;
+    rc = device_info(&di);
+    if (rc) return rc;
+    if (!d_workspace || !aligned16(d_workspace)) return d_workspace ? ECCO_ERR_ALIGNMENT : ECCO_ERR_WORKSPACE;
+    const int ctas = di.sms < 256 ? di.sms : 256, all_heads = cache->n_kv_heads;
+    int heads = all_heads;             // as many at a time as the workspace holds
+    while (heads > 0 && paged8_attn_plan(b, heads, all_heads, q_per_kv, ctas).bytes > workspace_bytes) --heads;
+    if (heads == 0) return ECCO_ERR_WORKSPACE;
+    PagedKv kv = {};
+    kv.k_meta = cache->d_k_scales; kv.v_meta = cache->d_v_scales;
+    kv.k_blocks = cache->d_k; kv.v_blocks = cache->d_v;
+    kv.tables = b.d_block_tables; kv.cu_new = b.d_cu_new; kv.kv_lens = b.d_kv_lens; kv.kv_tiles = b.d_kv_tiles;
+    kv.n_pages = cache->n_pages; kv.page_shift = page_shift_of(cache->page_size); kv.all_heads = all_heads;
+    kv.stride = b.table_stride; kv.n_req = b.n_req; kv.n_tokens = b.n_tokens; kv.max_tiles = std::max(b.max_tiles, 1);
+    kv.max_new = b.max_new; kv.max_kv = b.max_kv;
+    kv.staged = static_cast<uint8_t*>(d_workspace);
+    PagedOut o = {};
+    o.q = static_cast<const __half*>(d_q); o.q_stride = q_stride;
+    o.scale_log2 = scale * kLog2E;
+    o.q_per_kv = q_per_kv; o.q_heads = q_heads; o.causal = flags & ECCO_ATTN_CAUSAL;
+    o.out = static_cast<__half*>(d_out); o.lse = d_lse;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    P8AttnPlan p = {};
+    for (kv.head0 = 0; kv.head0 < all_heads; kv.head0 += kv.heads) {
+        kv.heads = std::min(heads, all_heads - kv.head0);
+        p = paged8_attn_plan(b, kv.heads, all_heads, q_per_kv, ctas);
+        if (!p.many && !p.line) break;
+        PagedSchedule sc = {};
+        sc.few_tiles = reinterpret_cast<int32_t*>(kv.staged + p.few_tiles);
+        sc.block_tiles = reinterpret_cast<int32_t*>(kv.staged + p.block_tiles);
+        sc.blocks = reinterpret_cast<int2*>(kv.staged + p.blocks);
+        sc.n_blocks = reinterpret_cast<int32_t*>(kv.staged + p.n_blocks);
+        sc.n_cuts = sc.n_blocks + 1;
+        sc.max_blocks = p.max_blocks;
+        sc.few_rows = kP8FewRows;
+        sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
+        sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
+        const int64_t units = p.many ? static_cast<int64_t>(b.max_tiles) * kv.heads * 2 : 0;
+        const unsigned grid = static_cast<unsigned>(spread_ctas(units / kP8StageWarps + 1, di.sms * 4));
+        rc = launch_overlapped(ecco_paged8_stage_kernel, grid, static_cast<unsigned>(kP8StageWarps * 32), 0, s, kv, o, sc, static_cast<int32_t>(p.many), static_cast<int32_t>(p.line));
+        if (rc) return rc;
+        if (!p.many) break;
+        PagedOut many = o;
+        many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
+        many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
+        PagedAttnPlan as = {};
+        as.many_ctas = p.many_ctas;
+        rc = launch_paged_many(di, kv, many, sc, as, s);
+        if (rc) return rc;
+    }
+    kv.head0 = 0;
+    kv.heads = all_heads;
+    P8Few f = {};
+    f.line = p.line ? reinterpret_cast<const int32_t*>(kv.staged + p.few_tiles) : nullptr;
+    f.few_rows = kP8FewRows;
+    f.part = reinterpret_cast<float*>(kv.staged + p.few_part);
+    f.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
+    f.tickets = reinterpret_cast<Ticket*>(kv.staged + p.few_tickets);
+    f.tag = next_ticket_tag();
+    return static_cast<int64_t>(b.max_new) * q_per_kv <= 8 ? launch_paged8_few<1>(di, kv, o, f, p.few_ctas, s) : launch_paged8_few<2>(di, kv, o, f, p.few_ctas, s);
 }

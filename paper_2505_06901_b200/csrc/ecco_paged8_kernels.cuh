@@ -1,0 +1,783 @@
+// ecco_paged8_kernels.cuh -- K8: the paged KV cache in 8 bits: new tokens into blocks, pages into tiles, attention of few rows
+// Part of the one translation unit ecco_kernels.cu; included from there only.
+#pragma once
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// The cache: E4M3 numbers, and a power of two 2^e for each block of min(16, page size) places of a page and head.  With e in -15 .. 7 every
+// value is an fp16 number, so reading the cache rounds nothing; and a power of two that grows rounds only what becomes
+// subnormal.
+// ---------------------------------------------------------------------------------------------
+constexpr int kP8Lowest = -15, kP8Highest = 7;
+__device__ __forceinline__ int p8_exponent(uint32_t byte) { return min(max(static_cast<int>(byte) - 127, kP8Lowest), kP8Highest); }
+// two E4M3 numbers of the lower / upper half of a word -> fp16, exactly
+__device__ __forceinline__ uint32_t e4m3_low(uint32_t v)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3_high(uint32_t v)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(v));
+    return r;
+}
+// four fp16 numbers -> E4M3, to nearest even, saturating
+__device__ __forceinline__ uint32_t to_e4m3(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f16x2 l, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 h, %2;\n\tmov.b32 %0, {l, h};\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b)
+{
+    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// 2^n twice as fp16, n in -24 .. 15
+__device__ __forceinline__ uint32_t power_h2(int n)
+{
+    const uint32_t h = n >= -14 ? static_cast<uint32_t>(n + 15) << 10 : 1u << (n + 24);
+    return h | (h << 16);
+}
+
+// ---------------------------------------------------------------------------------------------
+// K8a: new tokens into the cache.  A run is what a call brings for one block: rows one after the other whose slots ascend within
+// it.  A CTA has the runs that begin in sixteen rows, and a share of their heads; a warp takes a run of one head, of K or of V, as a whole: eight
+// lanes to a token, so that its up to 2048 values stay in registers from the load over the rotation and the largest value to the E4M3 numbers.
+// Bound by memory: 768 bytes per token and KV head.
+// ---------------------------------------------------------------------------------------------
+constexpr int kP8AppendThreads = 256, kP8Rows = 16;
+struct P8Append {
+    const int32_t *positions, *slots;
+    const __half *k, *v;
+    uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+    int64_t token_stride;
+    int32_t n_tokens, n_slots, heads, page_shift, parts;
+};
+
+template <bool kTurn>
+__global__ void __launch_bounds__(kP8AppendThreads)
+ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_constant__ P8Append p)
+{
+    constexpr unsigned full = 0xffffffffu;
+    __shared__ __align__(16) float2 table[kTurn ? 32 : 1][kGroup / 2];
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5, s = lane & 7, team = lane >> 3;
+    const int32_t window = static_cast<int32_t>(blockIdx.x) / p.parts, part = static_cast<int32_t>(blockIdx.x) - window * p.parts;
+    const int block_shift = min(4, p.page_shift), places = 1 << block_shift;
+    release_dependents();
+    dependency_wait();
+    // lane l: row 16 window - 1 + l.  Runs begin in lanes 1 .. 16 and are sixteen rows at most.
+    const int64_t row = static_cast<int64_t>(window) * kP8Rows - 1 + lane;
+    int32_t slot = row >= 0 && row < p.n_tokens ? __ldcg(p.slots + row) : -1;
+    if (slot >= p.n_slots) slot = -1;
+    const int32_t before = __shfl_up_sync(full, slot, 1);
+    const bool valid = slot >= 0, begins = valid && (before < 0 || slot >> block_shift != before >> block_shift || slot <= before);
+    const unsigned stops = __ballot_sync(full, begins || !valid), starts = __ballot_sync(full, begins) & 0x1fffeu;
+    auto run_end = [&](int l) {
+        const unsigned behind = l < 31 ? stops >> (l + 1) : 0u;
+        return behind ? l + __ffs(behind) : 32;
+    };
+    const int n_runs = __popc(starts);
+    if (n_runs == 0) return;
+    if (kTurn) {
+        const int from = __ffs(starts) - 1, to = run_end(31 - __clz(starts)), pairs = rope.rot_dim / 2;
+        for (int i = tid; i < (to - from) * (kGroup / 2); i += kP8AppendThreads) {
+            const int l = from + i / (kGroup / 2), pair = i % (kGroup / 2);
+            const int64_t r = static_cast<int64_t>(window) * kP8Rows - 1 + l;
+            if (pair < pairs && r < p.n_tokens) table[l][pair] = rope_angle(rope, pair, __ldcg(p.positions + r));
+        }
+        __syncthreads();
+    }
+    const int2 turned_piece = kTurn ? rope_pieces(rope, s) : make_int2(2 * s, 2 * s + 1);
+    const bool turns = kTurn && rope_turns(rope, s), neighbours = rope.flags & ECCO_ROPE_NEIGHBOURS;
+    const int n_items = n_runs * p.heads * 2;
+    for (int item = part * (kP8AppendThreads / 32) + warp; item < n_items; item += p.parts * (kP8AppendThreads / 32)) {
+        const int run = item / (2 * p.heads), in_run = item - run * 2 * p.heads, is_v = in_run >= p.heads, head = in_run - (is_v ? p.heads : 0);
+        const int l0 = __fns(starts, 0, run + 1), n = min(run_end(l0) - l0, 16);
+        const int32_t slot0 = __shfl_sync(full, slot, l0), page = slot0 >> p.page_shift, base = slot0 & ((1 << p.page_shift) - 1) & ~(places - 1);
+        const __half* const src = (is_v ? p.v : p.k) + (static_cast<int64_t>(window) * kP8Rows - 1 + l0) * p.token_stride + static_cast<int64_t>(head) * kGroup;
+        const int64_t of_head = static_cast<int64_t>(page) * p.heads + head;
+        uint8_t* const block = (is_v ? p.v_codes : p.k_codes) + ((of_head << p.page_shift) + base) * kGroup;
+        uint8_t* const scale = (is_v ? p.v_scales : p.k_scales) + (of_head << (p.page_shift - block_shift)) + (base >> block_shift);
+        const int2 piece = is_v ? make_int2(2 * s, 2 * s + 1) : turned_piece;
+        const bool anew = (slot0 & (places - 1)) == 0;
+        int e = kP8Lowest, e_before = kP8Lowest;
+        if (!anew) e_before = p8_exponent(__ldcg(scale));
+        uint4 v[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i][0] = v[i][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (4 * i + team < n) {
+                const uint4* const from = reinterpret_cast<const uint4*>(src + (4 * i + team) * p.token_stride);
+                v[i][0] = __ldcg(from + piece.x);
+                v[i][1] = __ldcg(from + piece.y);
+            }
+        }
+        uint32_t top = 0;                                  // largest magnitudes, as bits of two fp16 numbers
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (4 * i >= n) break;
+            if (turns && !is_v && 4 * i + team < n) {
+                float2 cs[8];
+                rope_load(cs, table[l0 + 4 * i + team], s);
+                rope_turn(v[i][0], v[i][1], cs, neighbours);
+            }
+            uint32_t* const w = reinterpret_cast<uint32_t*>(v[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const __half2 h = *reinterpret_cast<const __half2*>(&w[j]);
+                w[j] &= __heq2_mask(h, h);                 // NaN becomes zero
+                top = __vmaxu2(top, w[j] & 0x7fff7fffu);
+            }
+        }
+        const uint32_t largest = __reduce_max_sync(full, max(top & 0xffffu, top >> 16));
+        // 448 is 1.75 times a power of two: a larger mantissa (above 0x300) needs the next one
+        e = min(max(static_cast<int>((largest + 0xffu) >> 10) - 23, kP8Lowest), kP8Highest);
+        e = max(e, e_before);
+        if (!anew && e > e_before) {                       // what the block has already, under the new power of two
+            unsigned mine = 0;                             // places that the call brings
+            for (int j = 0; j < n; ++j) mine |= 1u << (__shfl_sync(full, slot, l0 + j) & (places - 1));
+            const uint32_t shrink = power_h2(e_before - e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int place = 4 * i + team;
+                if (place >= places || (mine >> place & 1u)) continue;
+                uint4* const at = reinterpret_cast<uint4*>(block + place * kGroup) + s;
+                uint4 x = __ldcg(at);
+                auto again = [&](uint32_t c) { return to_e4m3(mul_h2(e4m3_low(c), shrink), mul_h2(e4m3_high(c), shrink)); };
+                *at = make_uint4(again(x.x), again(x.y), again(x.z), again(x.w));
+            }
+        }
+        if (lane == 0) *scale = static_cast<uint8_t>(e + 127);
+        const uint32_t inverse = power_h2(-e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (4 * i >= n) break;
+            const int32_t to = __shfl_sync(full, slot, min(l0 + 4 * i + team, 31)) & (places - 1);
+            if (4 * i + team >= n) continue;
+            auto codes = [&](const uint4& x) {
+                return make_uint2(to_e4m3(mul_h2(x.x, inverse), mul_h2(x.y, inverse)), to_e4m3(mul_h2(x.z, inverse), mul_h2(x.w, inverse)));
+            };
+            const uint2 a = codes(v[i][0]), b = codes(v[i][1]);
+            uint8_t* const dst = block + to * kGroup;
+            if (piece.y == piece.x + 1) {
+                reinterpret_cast<uint4*>(dst)[s] = make_uint4(a.x, a.y, b.x, b.y);
+            } else {
+                reinterpret_cast<uint2*>(dst)[piece.x] = a;
+                reinterpret_cast<uint2*>(dst)[piece.y] = b;
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// K8s: the pages of requests of many rows into fp16 tiles, which ecco_paged_many_kernel reads (see K6s for their layout); the first CTA makes the
+// schedule.  A warp has a tile of K or of V: four tokens a load, 32 bytes of a piece a lane and store.
+// ---------------------------------------------------------------------------------------------
+// rows of a request that ecco_paged8_few_kernel takes together
+constexpr int kP8Rows16 = 16;
+__device__ __forceinline__ int32_t p8_row_groups(int64_t rows) { return static_cast<int32_t>((rows + kP8Rows16 - 1) / kP8Rows16); }
+// a request's tiles in the line of ecco_paged8_few_kernel: once for each sixteen rows
+__device__ __forceinline__ int64_t p8_line_tiles(const PagedReq& q, int32_t q_per_kv, int32_t few_rows)
+{
+    const int64_t rows = static_cast<int64_t>(q.rows) * q_per_kv;
+    return rows > few_rows ? 0 : static_cast<int64_t>(p8_row_groups(rows)) * ((q.kv + 31) >> 5);
+}
+// The line never passes this, whatever the arrays hold: sums of requests that share no tile do not reach it.
+__device__ __forceinline__ int64_t p8_line_limit(int32_t T, int32_t few_rows) { return static_cast<int64_t>(T) * p8_row_groups(few_rows); }
+// by one warp: rows of requests whose lanes say so get zeros and -infinity
+__device__ __forceinline__ void p8_empty_rows(const PagedKv& kv, const PagedOut& o, const PagedReq& q, bool empty)
+{
+    constexpr unsigned full = 0xffffffffu;
+    const int lane = static_cast<int>(threadIdx.x & 31u);
+    for (unsigned left = __ballot_sync(full, empty); left; left &= left - 1u) {
+        const int src = __ffs(left) - 1;
+        const int64_t row0 = __shfl_sync(full, q.row0, src), n = static_cast<int64_t>(__shfl_sync(full, q.rows, src)) * o.q_heads;
+        for (int64_t i = 0; i < n; ++i) {
+            const int64_t at = row0 * o.q_heads + i;
+            reinterpret_cast<uint2*>(o.out + at * kGroup)[lane] = make_uint2(0u, 0u);
+            if (o.lse && lane == 0) o.lse[at] = -INFINITY;
+        }
+    }
+}
+constexpr int kP8StageWarps = 8;
+__global__ void __launch_bounds__(kP8StageWarps * 32)
+ecco_paged8_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int32_t with_tiles,
+                         int32_t with_line)
+{
+    constexpr unsigned full = 0xffffffffu;
+    __shared__ int32_t firsts[kStageTiles + 1];
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5), block_shift = min(4, kv.page_shift);
+    release_dependents();
+    dependency_wait();
+    fetch_firsts(kv, firsts);
+    const int32_t T = paged_tiles(kv);
+    if (blockIdx.x == 0 && warp == 0) {
+        if (lane == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        paged_schedule(kv, sc, o);
+        if (with_line) {                                   // more requests than ecco_paged8_few_kernel keeps in shared memory
+            int64_t line = 0;
+            const int64_t limit = p8_line_limit(T, sc.few_rows);
+            for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
+                PagedReq q = {};
+                if (r0 + lane < kv.n_req) q = paged_req(kv, r0 + lane, T);
+                int64_t upto = p8_line_tiles(q, o.q_per_kv, sc.few_rows);
+                p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows && q.kv == 0);
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int64_t x = __shfl_up_sync(full, upto, d);
+                    if (lane >= d) upto += x;
+                }
+                upto = min(line + upto, limit);
+                if (r0 + lane < kv.n_req) sc.few_tiles[r0 + lane + 1] = static_cast<int32_t>(upto);
+                line = __shfl_sync(full, upto, 31);
+            }
+        }
+        return;
+    }
+    if (!with_tiles) return;                               // there is no room for any
+    const int64_t units = static_cast<int64_t>(T) * kv.heads * 2, warps = static_cast<int64_t>(gridDim.x) * kP8StageWarps - 1;
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * kP8StageWarps + warp - 1; u < units; u += warps) {
+        const int64_t pair = u >> 1;
+        const int which = static_cast<int>(u & 1);
+        const int32_t head = static_cast<int32_t>(divide(static_cast<uint64_t>(pair), static_cast<uint64_t>(T))), tile = static_cast<int32_t>(pair - static_cast<int64_t>(head) * T);
+        int32_t first;
+        const int r = request_of(kv, firsts, tile, first);
+        const PagedReq q = paged_req(kv, r, T);
+        if (static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows) continue;
+        const uint8_t *const codes = which ? kv.v_blocks : kv.k_blocks, *const scales = which ? kv.v_meta : kv.k_meta;
+        const int64_t token0 = (static_cast<int64_t>(tile) - first) * 32;
+        // lane l: where token l is
+        const int64_t token = token0 + lane, entry = token >> kv.page_shift;
+        int32_t page = -1;
+        if (token >= 0 && token < q.kv) {
+            page = entry < kv.stride ? __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + entry) : -1;
+            if (page < 0 || page >= kv.n_pages) {
+                atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+                page = -1;
+            }
+        }
+        const int64_t of_head = static_cast<int64_t>(max(page, 0)) * kv.all_heads + kv.head0 + head;
+        const int32_t place = static_cast<int32_t>(token & ((1 << kv.page_shift) - 1));
+        const int64_t at = (of_head << kv.page_shift) + place;
+        uint32_t scale = 0;
+        if (page >= 0) scale = power_h2(p8_exponent(__ldcg(scales + (of_head << (kv.page_shift - block_shift)) + (place >> block_shift))));
+        uint4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = 4 * i + (lane >> 3);
+            const int64_t from = __shfl_sync(full, at, t);
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (__shfl_sync(full, page, t) >= 0) v[i] = __ldcg(reinterpret_cast<const uint4*>(codes + from * kGroup) + (lane & 7));
+        }
+        uint8_t* const dst = staged_tile(kv, which, head, tile) + (lane & 7) * kPieceBytes;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = 4 * i + (lane >> 3);
+            const uint32_t by = __shfl_sync(full, scale, t);
+            const uint32_t c[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            uint32_t h[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { h[2 * j] = mul_h2(e4m3_low(c[j]), by); h[2 * j + 1] = mul_h2(e4m3_high(c[j]), by); }
+            const bool swapped = (t >> 2) & 1;
+            const uint32_t out[8] = {swapped ? h[4] : h[0], swapped ? h[5] : h[1], swapped ? h[6] : h[2], swapped ? h[7] : h[3],
+                                     swapped ? h[0] : h[4], swapped ? h[1] : h[5], swapped ? h[2] : h[6], swapped ? h[3] : h[7]};
+            stg_v8(dst + t * 32, out);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// K8a: attention of requests of few rows (new tokens x query heads per KV head), straight from the pages.
+// All tiles of 32 tokens of all requests and heads, once for each sixteen rows, form one line, cut into equal parts for the CTAs and, in these, for
+// the warps.  A warp keeps a ring of tiles in shared memory, filled by bulk copies out of the pages, and does
+//   S^T = K Q^T   tokens x rows, mma.sync: a lane's four consecutive E4M3 numbers are its part of a step of sixteen dims, Q having the same order
+//   the softmax   in fp32; K's power of two is a factor of the score, V's goes into the weight: w = 2^(s + e - m), sum of 2^-e w
+//   O^T = V^T W   two tokens' bytes side by side become the fp16 pair that an operand wants, W turned by movmatrix
+// so that the conversion from E4M3 is one instruction per two values and there is no other between shared memory and the tensor cores.
+// Pieces of a request that lie in several warps of a CTA are joined in shared memory, those in several CTAs by the CTA that comes last, in their order.
+// Bound by memory: 256 bytes per token and KV head.
+// ---------------------------------------------------------------------------------------------
+constexpr int kP8Warps = 8, kP8Stages = 2, kP8Reqs = 1024;
+constexpr uint32_t kP8TileBytes = 32 * kGroup;             // of K or of V
+constexpr uint32_t kP8StageBytes = 2 * kP8TileBytes + 3 * 128;       // and K's factors, V's exponents and their powers' inverses, by blocks
+constexpr uint32_t kP8PieceBytes = kP8Rows16 * kGroup * 4; // sums of a piece
+struct alignas(16) P8Piece { int64_t begin; int32_t units, head, row0, rows, group, valid; };
+struct P8Span { int64_t begin; int32_t units, head, row0, rows, group, valid, lo, hi; };
+constexpr uint32_t kP8Pieces = 256, kP8Spans = kP8Pieces + kP8Warps * 2 * sizeof(P8Piece), kP8Ml = kP8Spans + 128, kP8Lists = kP8Ml + kP8Warps * 2 * kP8Rows16 * 8;
+static_assert(2 * sizeof(P8Span) <= 112 && kP8Lists % 16 == 0, "the misc area");
+constexpr uint32_t kP8ListBytes = 4 * (kP8Reqs + 4) * 4;   // the line, lengths, first rows and rows of the requests
+constexpr uint32_t kP8First = (kP8Lists + kP8ListBytes + 127) / 128 * 128, kP8Ring = kP8First + kP8Warps * kP8PieceBytes;
+constexpr uint32_t kP8SmemBytes = kP8Ring + kP8Warps * kP8Stages * kP8StageBytes;
+static_assert(kP8SmemBytes <= kSmemCtaBytes && kP8Stages * kP8StageBytes >= kP8PieceBytes, "fits an SM");
+
+struct P8Few {
+    const int32_t* line;       // [n_req + 1], or NULL: the kernel makes it
+    int32_t few_rows;
+    float* part;               // [CTA][first, last][kP8Rows16][128]
+    float2* part_ml;           // [CTA][first, last][kP8Rows16]
+    Ticket* tickets;           // [CTA * kTicketStride]
+    Ticket tag;
+};
+__device__ __forceinline__ uint4 lds_v4(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ float lds_f32(uint32_t at) { return __uint_as_float(lds_u32(at)); }
+__device__ __forceinline__ uint32_t turn_8x8(uint32_t v)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+// kN: eight rows each, of a piece
+template <int kN>
+__global__ void __launch_bounds__(kP8Warps * 32, 1)
+ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ P8Few f)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    constexpr unsigned full = 0xffffffffu;
+    const int tid = static_cast<int>(threadIdx.x);
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3u, base = smem_u32(smem);
+    const uint32_t bar = base + warp * kP8Stages * 8, ring = base + kP8Ring + warp * kP8Stages * kP8StageBytes;
+    int32_t* const line = reinterpret_cast<int32_t*>(smem + kP8Lists);
+    int32_t *const kvs = line + kP8Reqs + 4, *const row0s = kvs + kP8Reqs + 4, *const rows_of = row0s + kP8Reqs + 4;
+    P8Piece* const pieces = reinterpret_cast<P8Piece*>(smem + kP8Pieces);              // [warp][first, last]
+    P8Span* const spans = reinterpret_cast<P8Span*>(smem + kP8Spans);
+    volatile int* const joins = reinterpret_cast<volatile int*>(smem + kP8Spans + 112);
+    float2* const ml = reinterpret_cast<float2*>(smem + kP8Ml);                        // [warp][first, last][row]
+    int64_t* const sums = reinterpret_cast<int64_t*>(smem + kP8First);                 // before there are pieces
+    if (lane == 0)
+        for (int i = 0; i < kP8Stages; ++i) mbar_init(bar + i * 8, 1);
+    if (tid < kP8Warps * 2) pieces[tid].valid = 0;
+    __syncthreads();
+    release_dependents();
+    dependency_wait();
+    const int32_t T = paged_tiles(kv);
+    if (!f.line) {
+        // the line: prefix sums over the requests, in rounds of a request per thread
+        int64_t before = 0;
+        const int64_t limit = p8_line_limit(T, f.few_rows);
+        if (tid == 0) {
+            line[0] = 0;
+            if (blockIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        }
+        for (int r0 = 0; r0 < kv.n_req; r0 += kP8Warps * 32) {
+            const int r = r0 + tid;
+            PagedReq q = {};
+            if (r < kv.n_req) q = paged_req(kv, r, T);
+            if ((q.cut || q.rows > kv.max_new) && blockIdx.x == 0) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+            int64_t upto = p8_line_tiles(q, o.q_per_kv, f.few_rows);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int64_t x = __shfl_up_sync(full, upto, d);
+                if (static_cast<int>(lane) >= d) upto += x;
+            }
+            if (lane == 31) sums[warp] = upto;
+            __syncthreads();
+            int64_t all = 0;
+#pragma unroll
+            for (int w = 0; w < kP8Warps; ++w) {
+                if (w < static_cast<int>(warp)) upto += sums[w];
+                all += sums[w];
+            }
+            if (r < kv.n_req) {
+                line[r + 1] = static_cast<int32_t>(min(before + upto, limit));
+                kvs[r] = q.kv;
+                row0s[r] = q.row0;
+                rows_of[r] = q.rows;
+            }
+            before = min(before + all, limit);
+            // requests without a token: nobody else comes to their rows
+            if (r0 / (kP8Warps * 32) % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x))
+                p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= f.few_rows && q.kv == 0);
+            __syncthreads();
+        }
+    }
+    const int32_t L = f.line ? __ldcg(f.line + kv.n_req) : line[kv.n_req];
+    const int64_t U = static_cast<int64_t>(L) * kv.heads;
+    const UnitSplit cta_split(U, static_cast<int>(gridDim.x));
+    const int64_t c0 = cta_split.begin(static_cast<int>(blockIdx.x)), c1 = cta_split.begin(static_cast<int>(blockIdx.x) + 1);
+    const UnitSplit split(c1 - c0, kP8Warps);
+    const int64_t u0 = c0 + split.begin(static_cast<int>(warp)), u1 = c0 + split.begin(static_cast<int>(warp) + 1);
+
+    // a place in the line: unit u is tile `tile` of a piece, i.e. of sixteen rows (group) of a request for a head, which has units [begin, begin + units)
+    struct Place { int64_t u, begin, end; int32_t units, head, tile, r, kv, row0, rows, group; };
+    auto seek = [&](Place& p, int64_t stop) {
+        if (p.u >= stop) return;
+        const int32_t nth = static_cast<int32_t>(divide(static_cast<uint64_t>(p.u), static_cast<uint64_t>(L))), off = static_cast<int32_t>(p.u - static_cast<int64_t>(nth) * L);
+        int r = 0;
+        int32_t from, to;
+        if (f.line) {
+            r = warp_find(f.line, kv.n_req, off);
+            from = __ldcg(f.line + r);
+            to = __ldcg(f.line + r + 1);
+            const PagedReq q = paged_req(kv, r, T);
+            p.kv = q.kv; p.row0 = q.row0; p.rows = q.rows;
+        } else {
+            for (int n = kv.n_req; n > 1;) {               // the last request that begins at or before the place
+                const int half = n >> 1;
+                if (line[r + half] <= off) { r += half; n -= half; } else n = half;
+            }
+            from = line[r];
+            to = line[r + 1];
+            p.kv = kvs[r]; p.row0 = row0s[r]; p.rows = rows_of[r];
+        }
+        const int32_t tiles = max((p.kv + 31) >> 5, 1);
+        p.r = r;
+        p.head = nth;
+        p.group = (off - from) / tiles;
+        const int32_t at = from + p.group * tiles;
+        p.begin = static_cast<int64_t>(nth) * L + at;
+        p.units = min(tiles, to - at);
+        p.end = min(p.begin + p.units, stop);
+        p.tile = off - at;
+    };
+    const int piece_shift = min(5, kv.page_shift), block_shift = min(4, kv.page_shift);
+    const int32_t in_page = (1 << kv.page_shift) - 1;
+    // the page of the lane's part of a tile: -1: none, -2: there is nothing to look for
+    auto page_of = [&](const Place& p) {
+        const int32_t token = p.tile * 32 + static_cast<int32_t>(lane << piece_shift), e = token >> kv.page_shift;
+        if (p.u >= u1 || (lane << piece_shift) >= 32u || token >= p.kv) return -2;
+        return e < kv.stride ? max(__ldcg(kv.tables + static_cast<int64_t>(p.r) * kv.stride + e), -1) : -1;
+    };
+    // The way of a tile: its pages are looked up with the tile before it, its bytes are asked for, and its scales, with the next tile, written down.
+    Place load = {};
+    load.u = u0;
+    seek(load, u1);
+    int32_t page_next = page_of(load);
+    uint32_t asked = 0, taken = 0, k_scale = 0, v_scale = 0;
+    int scales_for = -1;
+    auto write_scales = [&]() {
+        if (scales_for < 0) return;
+        if ((lane << block_shift) < 32u) {
+            const uint32_t at = ring + scales_for * kP8StageBytes + 2 * kP8TileBytes + lane * 4;
+            const int e = p8_exponent(v_scale);
+            sts_u32(at, static_cast<uint32_t>(p8_exponent(k_scale) + 127) << 23);
+            sts_u32(at + 128, __float_as_uint(static_cast<float>(e)));
+            sts_u32(at + 256, static_cast<uint32_t>(127 - e) << 23);
+        }
+        __syncwarp();
+        scales_for = -1;
+    };
+    auto ask = [&]() {
+        write_scales();
+        if (load.u >= u1) return;
+        const uint32_t stage = asked % kP8Stages, b = bar + stage * 8, dst = ring + stage * kP8StageBytes;
+        if (page_next == -1 || page_next >= kv.n_pages) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        const bool there = page_next >= 0 && page_next < kv.n_pages;
+        const int n = __popc(__ballot_sync(full, there));
+        if (lane == 0) mbar_expect_tx(b, (n * 2) << (piece_shift + 7));
+        __syncwarp();
+        const int32_t token0 = load.tile * 32, of_page = load.head + kv.head0;
+        if (there) {
+            const int32_t place = (token0 + static_cast<int32_t>(lane << piece_shift)) & in_page;
+            const int64_t from = ((((static_cast<int64_t>(page_next) * kv.all_heads + of_page) << kv.page_shift) + place) * kGroup);
+            const uint32_t to = dst + (lane << (piece_shift + 7)), bytes = 1u << (piece_shift + 7);
+            bulk_g2s(to, kv.k_blocks + from, bytes, b);
+            bulk_g2s(to + kP8TileBytes, kv.v_blocks + from, bytes, b);
+        }
+        const int32_t page = __shfl_sync(full, page_next, ((lane << block_shift) & 31u) >> piece_shift);
+        k_scale = v_scale = 127;
+        if ((lane << block_shift) < 32u && page >= 0 && page < kv.n_pages) {
+            const int32_t place = (token0 + static_cast<int32_t>(lane << block_shift)) & in_page;
+            const int64_t at = ((static_cast<int64_t>(page) * kv.all_heads + of_page) << (kv.page_shift - block_shift)) + (place >> block_shift);
+            k_scale = __ldcg(kv.k_meta + at);
+            v_scale = __ldcg(kv.v_meta + at);
+        }
+        scales_for = static_cast<int>(stage);
+        ++asked;
+        ++load.tile;
+        if (++load.u == load.end) seek(load, u1);
+        page_next = page_of(load);
+    };
+    __syncwarp();
+    Place at = load;
+    for (int i = 0; i < kP8Stages; ++i) ask();
+    // pieces of this CTA that other CTAs have parts of: at its begin and at its end
+    if (warp == kP8Warps - 1) {
+        Place p = {};
+        P8Span sp[2] = {};
+        for (int i = 0; i < 2; ++i) {
+            p.u = i ? c1 - 1 : c0;
+            if (c0 < c1) seek(p, c1);
+            const bool out = c0 < c1 && (p.begin < c0 || p.begin + p.units > c1) && !(i && sp[0].valid && sp[0].begin == p.begin);
+            sp[i] = P8Span{p.begin, p.units, p.head, p.row0, p.rows, p.group, out, 0, 0};
+            if (out) {
+                sp[i].lo = cta_split.owner(p.begin);
+                sp[i].hi = cta_split.owner(p.begin + p.units - 1);
+                if (lane == 0) {
+                    Ticket* const word = f.tickets + static_cast<int64_t>(sp[i].lo) * kTicketStride;
+                    claim_ticket(word, look_at_ticket(word), f.tag);
+                }
+            }
+            if (lane == 0) spans[i] = sp[i];
+        }
+    }
+
+    bool ok = true;
+    while (ok && at.u < u1) {
+        const int R = min(at.rows * o.q_per_kv - at.group * kP8Rows16, kN * 8);
+        const int64_t from_u = at.u;
+        // Q: lane (row g, c) has dims 32 c .. 32 c + 31, which are its part of all steps; what belongs to no row is zero
+        uint32_t q[kN][16];
+        int32_t seen[kN][2];
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+            const int row = n * 8 + static_cast<int>(g), i = at.group * kP8Rows16 + row, token = i / o.q_per_kv, h = i - token * o.q_per_kv;
+            const uint4* const src = reinterpret_cast<const uint4*>(o.q + static_cast<int64_t>(at.row0 + token) * o.q_stride + (static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + h) * kGroup) + c * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint4 v = row < R ? __ldcg(src + j) : make_uint4(0u, 0u, 0u, 0u);
+                q[n][4 * j] = v.x; q[n][4 * j + 1] = v.y; q[n][4 * j + 2] = v.z; q[n][4 * j + 3] = v.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int mine = n * 8 + static_cast<int>(c) * 2 + e;
+                seen[n][e] = mine < R ? tokens_seen(PagedReq{0, 0, at.kv, at.row0, at.rows, false}, (at.group * kP8Rows16 + mine) / o.q_per_kv, o.causal) : 0;
+            }
+        }
+        float acc[8][kN][4], m[kN][2], l[kN][2];
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][n][e] = 0.0f;
+        }
+        for (; at.u < at.end; ++at.u, ++at.tile) {
+            const uint32_t stage = taken % kP8Stages, k_at = ring + stage * kP8StageBytes, v_at = k_at + kP8TileBytes, s_at = k_at + 2 * kP8TileBytes;
+            ok = warp_wait(bar + stage * 8, (taken / kP8Stages) & 1u);
+            if (!ok) break;
+            ++taken;
+            // scores: sixteen tokens x eight rows
+            float s[2][kN][4];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[mt][n][e] = 0.0f;
+                const uint32_t row = k_at + (mt * 16 + g) * kGroup + c * 32;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint4 x = lds_v4(row + half * 16), y = lds_v4(row + 8 * kGroup + half * 16);
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t a[4] = {e4m3_low(xs[j]), e4m3_low(ys[j]), e4m3_high(xs[j]), e4m3_high(ys[j])};
+#pragma unroll
+                        for (int n = 0; n < kN; ++n) mma_16816(s[mt][n], a, q[n][2 * (4 * half + j)], q[n][2 * (4 * half + j) + 1]);
+                    }
+                }
+            }
+            // softmax: weights of V's E4M3 numbers, relative to the largest so far
+            float inverse[2][2], top[kN][2];
+#pragma unroll
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) top[n][e] = m[n][e];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t t = mt * 16 + h * 8 + g, sc = s_at + (t >> block_shift) * 4;
+                    const float by = lds_f32(sc) * o.scale_log2, plus = lds_f32(sc + 128);
+                    inverse[mt][h] = lds_f32(sc + 256);
+                    const int32_t token = at.tile * 32 + static_cast<int32_t>(t);
+#pragma unroll
+                    for (int n = 0; n < kN; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float& x = s[mt][n][2 * h + e];
+                            x = token < seen[n][e] ? fmaf(x, by, plus) : -INFINITY;
+                            top[n][e] = fmaxf(top[n][e], x);
+                        }
+                }
+            float sub[kN][2];
+            bool grow = false;
+#pragma unroll
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float& t = top[n][e];
+                    t = fmaxf(t, __shfl_xor_sync(full, t, 4));
+                    t = fmaxf(t, __shfl_xor_sync(full, t, 8));
+                    t = fmaxf(t, __shfl_xor_sync(full, t, 16));
+                    grow = grow || t > m[n][e];
+                    sub[n][e] = t == -INFINITY ? 0.0f : t;
+                }
+            if (__any_sync(full, grow)) {
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float by = exp2_fast(m[n][e] - sub[n][e]);
+                        l[n][e] *= by;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) { acc[j][n][e] *= by; acc[j][n][2 + e] *= by; }
+                        m[n][e] = top[n][e];
+                    }
+            }
+            uint32_t w[2][kN][2];                          // of sixteen tokens and eight rows each, as the second operand
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float p[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            p[e] = exp2_fast(s[mt][n][2 * h + e] - sub[n][e] + kWeightLog2);
+                            l[n][e] = fmaf(p[e], inverse[mt][h], l[n][e]);
+                        }
+                        w[mt][n][h] = turn_8x8(pack_h2(p[0], p[1]));
+                    }
+            const int32_t left = at.kv - at.tile * 32;     // tokens that there are
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                // tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of sixteen; dims 16 g .. 16 g + 15
+                uint4 x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t t = kt * 16 + 2 * c + (i & 1) + (i >> 1) * 8;
+                    x[i] = lds_v4(v_at + t * kGroup + g * 16);
+                    if (left < 32 && static_cast<int32_t>(t) >= left) x[i] = make_uint4(0u, 0u, 0u, 0u);     // whatever is there: nobody sees it
+                }
+                const uint32_t* const x0 = reinterpret_cast<const uint32_t*>(&x[0]);
+                const uint32_t* const x1 = reinterpret_cast<const uint32_t*>(&x[1]);
+                const uint32_t* const x2 = reinterpret_cast<const uint32_t*>(&x[2]);
+                const uint32_t* const x3 = reinterpret_cast<const uint32_t*>(&x[3]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {              // output dims 16 g + 2 j, 16 g + 2 j + 1
+                    const uint32_t sel = j & 1 ? 0x7362u : 0x5140u;
+                    const uint32_t near = prmt(x0[j >> 1], x1[j >> 1], sel), far = prmt(x2[j >> 1], x3[j >> 1], sel);
+                    const uint32_t a[4] = {e4m3_low(near), e4m3_high(near), e4m3_low(far), e4m3_high(far)};
+#pragma unroll
+                    for (int n = 0; n < kN; ++n) mma_16816(acc[j][n], a, w[kt][n][0], w[kt][n][1]);
+                }
+            }
+            __syncwarp();                                  // the whole warp has read the tile
+            ask();
+        }
+        if (!ok) break;
+        // out, or to be joined
+        const bool whole = at.begin >= u0 && at.begin + at.units <= u1;
+        const int which = from_u == u0 ? 0 : 1;
+        float* const to = reinterpret_cast<float*>(which ? smem + (ring - base) : smem + kP8First + warp * kP8PieceBytes);
+        if (!whole && which) __syncwarp();
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[n][e];
+                sum += __shfl_xor_sync(full, sum, 4);
+                sum += __shfl_xor_sync(full, sum, 8);
+                sum += __shfl_xor_sync(full, sum, 16);
+                const int row = n * 8 + static_cast<int>(c) * 2 + e;
+                if (row >= R) continue;
+                if (whole) {
+                    const int i = at.group * kP8Rows16 + row, token = i / o.q_per_kv;
+                    const int64_t out_row = static_cast<int64_t>(at.row0 + token) * o.q_heads + static_cast<int64_t>(kv.head0 + at.head) * o.q_per_kv + (i - token * o.q_per_kv);
+                    const float inv = inverse_of(sum);
+                    uint4* const dst = reinterpret_cast<uint4*>(o.out + out_row * kGroup + g * 16);
+                    auto two = [&](int j) { return pack_h2(acc[j][n][e] * inv, acc[j][n][2 + e] * inv); };
+                    dst[0] = make_uint4(two(0), two(1), two(2), two(3));
+                    dst[1] = make_uint4(two(4), two(5), two(6), two(7));
+                    if (o.lse && g == 0) o.lse[out_row] = lse_of(m[n][e], sum, kWeightLog2);
+                } else {
+                    float4* const dst = reinterpret_cast<float4*>(to + row * kGroup + g * 16);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) dst[j] = make_float4(acc[2 * j][n][e], acc[2 * j][n][2 + e], acc[2 * j + 1][n][e], acc[2 * j + 1][n][2 + e]);
+                    if (g == 0) ml[(warp * 2 + which) * kP8Rows16 + row] = make_float2(m[n][e], sum);
+                }
+            }
+        if (!whole && lane == 0) pieces[warp * 2 + which] = P8Piece{at.begin, at.units, at.head, at.row0, at.rows, at.group, 1};
+        seek(at, u1);
+    }
+    if (!ok)                                               // tiles on their way land before the warp leaves
+        for (; taken < asked; ++taken) warp_wait(bar + (taken % kP8Stages) * 8, (taken / kP8Stages) & 1u);
+    __syncthreads();
+
+    auto write_row = [&](int32_t group, int32_t row0, int32_t head, int row, float m, float l, const float4& v) {
+        const int i = group * kP8Rows16 + row, token = i / o.q_per_kv;
+        const int64_t out_row = static_cast<int64_t>(row0 + token) * o.q_heads + static_cast<int64_t>(kv.head0 + head) * o.q_per_kv + (i - token * o.q_per_kv);
+        const float inv = inverse_of(l);
+        reinterpret_cast<uint2*>(o.out + out_row * kGroup)[lane] = make_uint2(pack_h2(v.x * inv, v.y * inv), pack_h2(v.z * inv, v.w * inv));
+        if (o.lse && lane == 0) o.lse[out_row] = lse_of(m, l, kWeightLog2);
+    };
+    // pieces of the CTA's warps, one behind the other in the line
+    for (int i = 0; i < kP8Warps * 2;) {
+        if (!pieces[i].valid) { ++i; continue; }
+        const P8Piece p = pieces[i];
+        int last = i;
+        for (int j = i + 1; j < kP8Warps * 2; ++j)
+            if (pieces[j].valid) {
+                if (pieces[j].begin != p.begin) break;
+                last = j;
+            }
+        const int R = min(p.rows * o.q_per_kv - p.group * kP8Rows16, kN * 8);
+        for (int row = static_cast<int>(warp); row < R; row += kP8Warps) {
+            float m = -INFINITY, l = 0.0f;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int j = i; j <= last; ++j) {
+                if (!pieces[j].valid) continue;
+                const uint8_t* const from = j & 1 ? smem + kP8Ring + (j >> 1) * kP8Stages * kP8StageBytes : smem + kP8First + (j >> 1) * kP8PieceBytes;
+                join_sums(m, l, v, ml[j * kP8Rows16 + row], reinterpret_cast<const float4*>(from)[row * 32 + lane]);
+            }
+            if (p.begin >= c0 && p.begin + p.units <= c1) {
+                write_row(p.group, p.row0, p.head, row, m, l, v);
+            } else {
+                const int64_t to = (static_cast<int64_t>(blockIdx.x) * 2 + (p.begin < c0 ? 0 : 1)) * kP8Rows16 + row;
+                reinterpret_cast<float4*>(f.part + to * kGroup)[lane] = v;
+                if (lane == 0) f.part_ml[to] = make_float2(m, l);
+            }
+        }
+        i = last + 1;
+    }
+    if (!spans[0].valid && !spans[1].valid) return;
+    __threadfence();
+    __syncthreads();
+    if (tid < 2) {
+        const P8Span sp = spans[tid];
+        joins[tid] = sp.valid && take_ticket(f.tickets + static_cast<int64_t>(sp.lo) * kTicketStride) == static_cast<unsigned>(sp.hi - sp.lo);
+    }
+    __syncthreads();
+    for (int i = 0; i < 2; ++i) {
+        if (!joins[i]) continue;
+        __threadfence();
+        const P8Span sp = spans[i];
+        const int R = min(sp.rows * o.q_per_kv - sp.group * kP8Rows16, kN * 8);
+        for (int row = static_cast<int>(warp); row < R; row += kP8Warps) {
+            float m = -INFINITY, l = 0.0f;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int b0 = sp.lo; b0 <= sp.hi; b0 += 4) {   // four pieces on their way together
+                float2 x[4];
+                float4 y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int b = min(b0 + k, sp.hi);
+                    const int64_t from = (static_cast<int64_t>(b) * 2 + (sp.begin < cta_split.begin(b) ? 0 : 1)) * kP8Rows16 + row;
+                    x[k] = __ldcg(f.part_ml + from);
+                    y[k] = __ldcg(reinterpret_cast<const float4*>(f.part + from * kGroup) + lane);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (b0 + k <= sp.hi) join_sums(m, l, v, x[k], y[k]);
+            }
+            write_row(sp.group, sp.row0, sp.head, row, m, l, v);
+        }
+        if (tid == 0) *(f.tickets + static_cast<int64_t>(sp.lo) * kTicketStride) = 0;
+    }
+}
+
+}  // namespace

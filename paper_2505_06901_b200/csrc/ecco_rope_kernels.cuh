@@ -1,0 +1,141 @@
+// ecco_rope_kernels.cuh -- rotary positions
+// Part of the one translation unit ecco_kernels.cu; included from there only.
+#pragma once
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// Eight lanes to a head, sixteen values each in two 16-byte pieces: pairs 8 s .. 8 s + 7 in lane s, whichever way pairs lie; lanes behind
+// the last pair hold what is not turned.
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ bool rope_turns(const ecco_rope& r, int s) { return s * 16 < r.rot_dim; }
+// the first and the second 16-byte piece of lane s
+__device__ __forceinline__ int2 rope_pieces(const ecco_rope& r, int s)
+{
+    return rope_turns(r, s) && !(r.flags & ECCO_ROPE_NEIGHBOURS) ? make_int2(s, s + r.rot_dim / 16) : make_int2(2 * s, 2 * s + 1);
+}
+// cos and sin of a pair at a position, times the gain.  The angle is position * turn mod 2^64, in 2^-64 turns, and exact; what is left of it
+// beside the nearest quarter turn goes to fp32 (|angle| up to pi / 4: 2^-25 of it).
+__device__ __forceinline__ float2 rope_angle(const ecco_rope& r, int pair, int32_t position)
+{
+    const uint64_t phase = static_cast<uint64_t>(static_cast<int64_t>(position)) * r.turn[pair];
+    const uint32_t quarters = static_cast<uint32_t>(((phase >> 61) + 1) >> 1);                      // to the nearest, mod 4
+    const int64_t rest = static_cast<int64_t>(phase - (static_cast<uint64_t>(quarters) << 62));
+    float s, c;
+    sincospif(static_cast<float>(rest) * 1.0842021724855044e-19f, &s, &c);                          // 2^-63: in half turns
+    const float a = quarters & 1u ? -s : c, b = quarters & 1u ? c : s;
+    const float g = quarters & 2u ? -r.gain : r.gain;
+    return make_float2(a * g, r.flags & ECCO_ROPE_INVERSE ? -b * g : b * g);
+}
+// a lane's sixteen values by its pairs' cos and sin
+__device__ __forceinline__ void rope_turn(uint4& first, uint4& second, const float2 (&cs)[8], bool neighbours)
+{
+    uint32_t v[8] = {first.x, first.y, first.z, first.w, second.x, second.y, second.z, second.w};
+    auto turned = [](float a, float b, float2 k, float& x, float& y) {
+        x = __fmaf_rn(a, k.x, -__fmul_rn(b, k.y));
+        y = __fmaf_rn(b, k.x, __fmul_rn(a, k.y));
+    };
+    auto pack = [](float a, float b) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    };
+    if (neighbours) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+            float a, b;
+            turned(x.x, x.y, cs[i], a, b);
+            v[i] = pack(a, b);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&v[i])), y = __half22float2(*reinterpret_cast<const __half2*>(&v[i + 4]));
+            float2 a, b;
+            turned(x.x, y.x, cs[2 * i], a.x, b.x);
+            turned(x.y, y.y, cs[2 * i + 1], a.y, b.y);
+            v[i] = pack(a.x, a.y);
+            v[i + 4] = pack(b.x, b.y);
+        }
+    }
+    first = make_uint4(v[0], v[1], v[2], v[3]);
+    second = make_uint4(v[4], v[5], v[6], v[7]);
+}
+// cos and sin of lane s from a row of a table in shared memory
+__device__ __forceinline__ void rope_load(float2 (&cs)[8], const float2* row, int s)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 v = reinterpret_cast<const float4*>(row + 8 * s)[i];
+        cs[2 * i] = make_float2(v.x, v.y);
+        cs[2 * i + 1] = make_float2(v.z, v.w);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// K7: rows of heads turned by their positions.  A CTA has eight tokens and a share of their heads: cos and sin are made once and stand in shared
+// memory, the first heads on their way meanwhile.  Bound by memory: 512 bytes per token and head.
+// ---------------------------------------------------------------------------------------------
+constexpr int kRopeThreads = 256, kRopeTokens = 8, kRopeInFlight = 4;
+constexpr int kRopeTeams = kRopeThreads / 8 / kRopeTokens;             // of eight lanes, to a token
+
+struct RopeRows {
+    const int32_t* positions;
+    const __half* x;
+    __half* out;
+    int64_t x_stride, out_stride;
+    int32_t n_tokens, n_heads, parts, per_part;            // CTAs to eight tokens, heads to a CTA
+};
+
+__global__ void __launch_bounds__(kRopeThreads)
+ecco_rope_kernel(const __grid_constant__ ecco_rope rope, const __grid_constant__ RopeRows p)
+{
+    __shared__ __align__(16) float2 table[kRopeTokens][kGroup / 2];
+    const int tid = static_cast<int>(threadIdx.x), s = tid & 7, team = (tid >> 3) % kRopeTeams, local = (tid >> 3) / kRopeTeams;
+    const int32_t window = static_cast<int32_t>(blockIdx.x) / p.parts, part = static_cast<int32_t>(blockIdx.x) - window * p.parts;
+    const int64_t token0 = static_cast<int64_t>(window) * kRopeTokens, token = token0 + local;
+    const int32_t head_end = min(p.n_heads, (part + 1) * p.per_part);
+    const int2 piece = rope_pieces(rope, s);
+    const bool there = token < p.n_tokens;
+    release_dependents();
+    dependency_wait();
+    uint4 v[kRopeInFlight][2];
+    auto load = [&](int32_t head0) {
+#pragma unroll
+        for (int i = 0; i < kRopeInFlight; ++i) {
+            const int32_t head = head0 + i * kRopeTeams;
+            if (there && head < head_end) {
+                const uint4* const src = reinterpret_cast<const uint4*>(p.x + token * p.x_stride + static_cast<int64_t>(head) * kGroup);
+                v[i][0] = __ldcg(src + piece.x);
+                v[i][1] = __ldcg(src + piece.y);
+            }
+        }
+    };
+    int32_t head0 = part * p.per_part + team;
+    load(head0);
+    const int pairs = rope.rot_dim / 2;
+    for (int i = tid; i < kRopeTokens * (kGroup / 2); i += kRopeThreads) {
+        const int t = i / (kGroup / 2), pair = i % (kGroup / 2);
+        if (pair < pairs && token0 + t < p.n_tokens) table[t][pair] = rope_angle(rope, pair, __ldcg(p.positions + token0 + t));
+    }
+    __syncthreads();
+    if (!there) return;
+    const bool turns = rope_turns(rope, s), neighbours = rope.flags & ECCO_ROPE_NEIGHBOURS;
+    float2 cs[8];
+    if (turns) rope_load(cs, table[local], s);
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < kRopeInFlight; ++i) {
+            const int32_t head = head0 + i * kRopeTeams;
+            if (head >= head_end) return;
+            if (turns) rope_turn(v[i][0], v[i][1], cs, neighbours);
+            uint4* const dst = reinterpret_cast<uint4*>(p.out + token * p.out_stride + static_cast<int64_t>(head) * kGroup);
+            dst[piece.x] = v[i][0];
+            dst[piece.y] = v[i][1];
+        }
+        head0 += kRopeInFlight * kRopeTeams;
+        load(head0);
+    }
+}
+
+}  // namespace
