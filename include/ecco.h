@@ -366,7 +366,7 @@ int ecco_rope_apply(const ecco_rope* rope, const int32_t* d_positions, int32_t n
  * power of two: byte (page * n_kv_heads + head) * max(1, page_size / 16) + place / 16 of the scales holds its exponent e plus 127
  * (E8M0), e in -15..7 (others count as the nearest of these).  A value is its E4M3 number times 2^e: exactly an fp16 number.
  *
- * Pools are 16-byte aligned; page_size, n_pages and n_kv_heads as above.  Whatever the device arrays hold, no call reads or writes outside the buffers
+ * Pools are 16-byte aligned, scales 4-byte aligned; page_size, n_pages and n_kv_heads as above.  Whatever the device arrays hold, no call reads or writes outside the buffers
  * that it was given. */
 #define ECCO_PAGED8_BLOCK 16
 typedef struct ecco_paged8_cache {

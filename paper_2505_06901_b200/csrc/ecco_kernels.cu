@@ -1051,7 +1051,7 @@ static int check_paged8_cache(const ecco_paged8_cache* c)
     if (!c || !c->d_k || !c->d_v || !c->d_k_scales || !c->d_v_scales) return ECCO_ERR_INVALID_ARG;
     if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 65535 || page_shift_of(c->page_size) < 0) return ECCO_ERR_INVALID_ARG;
     if (static_cast<int64_t>(c->n_pages) * c->page_size > INT32_MAX) return ECCO_ERR_INVALID_ARG;
-    if (!aligned16(c->d_k) || !aligned16(c->d_v)) return ECCO_ERR_ALIGNMENT;
+    if (!aligned16(c->d_k) || !aligned16(c->d_v) || !aligned_to(c->d_k_scales, 4) || !aligned_to(c->d_v_scales, 4)) return ECCO_ERR_ALIGNMENT;
     return ECCO_OK;
 }
 
@@ -1085,10 +1085,11 @@ extern "C" int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rop
 namespace {
 // rows of a request up to which they go to ecco_paged8_few_kernel, sixteen at a time
 constexpr int kP8FewRows = 64;
+constexpr int kP8ByRequest = 2048;
 // Workspace of a launch over some KV heads, all offsets multiples of 256:
 //   tiles (for many rows) | schedule | few rows: tickets, sums, maxima | many rows: sums, maxima
 struct P8AttnPlan {
-    bool many, line;                   // there may be requests of more rows; more requests than the kernel for few rows schedules itself
+    bool many, line, by_request;       // there may be requests of more rows; more requests than the kernel for few rows schedules itself
     int few_ctas, many_ctas, max_blocks;
     size_t few_tiles, block_tiles, blocks, n_blocks, tickets, few_tickets, few_part, few_ml, many_part, many_ml, bytes;
 };
@@ -1099,7 +1100,8 @@ P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int all_heads,
     p.many = rows > kP8FewRows;
     p.line = b.n_req > kP8Reqs;
     const int64_t groups = std::min<int64_t>((rows + kP8Rows16 - 1) / kP8Rows16, kP8FewRows / kP8Rows16);
-    p.few_ctas = std::max(1, spread_ctas((static_cast<int64_t>(b.max_tiles) * all_heads * std::max<int64_t>(groups, 1) + kP8Warps - 1) / kP8Warps, ctas_max));
+    p.by_request = static_cast<int64_t>(b.n_req) * all_heads <= ctas_max && b.max_kv <= kP8ByRequest;
+    p.few_ctas = p.by_request ? std::max(b.n_req, 1) * all_heads : std::max(1, spread_ctas((static_cast<int64_t>(b.max_tiles) * all_heads * std::max<int64_t>(groups, 1) + 7) / 8, ctas_max));
     p.many_ctas = ctas_max;
     p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
     size_t at = p.many ? static_cast<size_t>(std::max(b.max_tiles, 1)) * heads * 2 * kKvTileBytes : 0;
@@ -1123,16 +1125,31 @@ P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int all_heads,
     p.bytes = at;
     return p;
 }
+// a pool as [page][head][place][128 bytes]: a box is a page's part of a tile of 32 tokens
+bool make_p8_map(CUtensorMap* map, const PagedKv& kv, const uint8_t* pool)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t page = 1ull << kv.page_shift;
+    const cuuint64_t dims[4] = {kGroup, page, static_cast<cuuint64_t>(kv.all_heads), static_cast<cuuint64_t>(kv.n_pages)};
+    const cuuint64_t strides[3] = {kGroup, kGroup * page, kGroup * page * kv.all_heads};
+    const cuuint32_t box[4] = {kGroup, static_cast<cuuint32_t>(std::min<cuuint64_t>(page, 32)), 1, 1};
+    const cuuint32_t unit[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(pool), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 template <int kN>
 int launch_paged8_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const P8Few& f, int ctas, cudaStream_t s)
 {
+    CUtensorMap k_map = {}, v_map = {};
+    if (kv.page_shift >= kP8SwizzledShift && (!make_p8_map(&k_map, kv, kv.k_blocks) || !make_p8_map(&v_map, kv, kv.v_blocks))) return ECCO_ERR_CUDA;
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {
-        const int rc = set_smem(ecco_paged8_few_kernel<kN>, kP8SmemBytes);
+        const int rc = set_smem(ecco_paged8_few_kernel<kN>, P8Smem<kN>::kBytes);
         if (rc) return rc;
         configured[di.device] = true;
     }
-    return launch_overlapped(ecco_paged8_few_kernel<kN>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8Warps * 32), kP8SmemBytes, s, kv, o, f);
+    return launch_overlapped(ecco_paged8_few_kernel<kN>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8Warps * 32), P8Smem<kN>::kBytes, s, kv, o, f, k_map, v_map);
 }
 // the part of the batch's checks that ecco_paged_attn has: the pages are the same
 bool paged8_batch_fine(const ecco_paged8_cache& c, const ecco_paged_batch& b, int q_per_kv)
@@ -1220,6 +1237,7 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
     P8Few f = {};
     f.line = p.line ? reinterpret_cast<const int32_t*>(kv.staged + p.few_tiles) : nullptr;
     f.few_rows = kP8FewRows;
+    f.by_request = p.by_request;
     f.part = reinterpret_cast<float*>(kv.staged + p.few_part);
     f.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
     f.tickets = reinterpret_cast<Ticket*>(kv.staged + p.few_tickets);

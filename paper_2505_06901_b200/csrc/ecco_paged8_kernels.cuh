@@ -301,22 +301,28 @@ ecco_paged8_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 // Pieces of a request that lie in several warps of a CTA are joined in shared memory, those in several CTAs by the CTA that comes last, in their order.
 // Bound by memory: 256 bytes per token and KV head.
 // ---------------------------------------------------------------------------------------------
-constexpr int kP8Warps = 8, kP8Stages = 2, kP8Reqs = 1024;
+constexpr int kP8Warps = 8, kP8Stages = 2, kP8Reqs = 512;
+// Pages of eight tokens and more come through tensor maps that swap the 16-byte pieces of a row by its number mod 8, so that neither operand's loads meet in a
+// bank; smaller ones as they are.
+constexpr int kP8SwizzledShift = 3;
 constexpr uint32_t kP8TileBytes = 32 * kGroup;             // of K or of V
-constexpr uint32_t kP8StageBytes = 2 * kP8TileBytes + 3 * 128;       // and K's factors, V's exponents and their powers' inverses, by blocks
-constexpr uint32_t kP8PieceBytes = kP8Rows16 * kGroup * 4; // sums of a piece
+constexpr uint32_t kP8StageBytes = 2 * kP8TileBytes, kP8ScaleBytes = 32 * 16;          // beside it words that the blocks' powers of two are in, and where in these
 struct alignas(16) P8Piece { int64_t begin; int32_t units, head, row0, rows, group, valid; };
 struct P8Span { int64_t begin; int32_t units, head, row0, rows, group, valid, lo, hi; };
-constexpr uint32_t kP8Pieces = 256, kP8Spans = kP8Pieces + kP8Warps * 2 * sizeof(P8Piece), kP8Ml = kP8Spans + 128, kP8Lists = kP8Ml + kP8Warps * 2 * kP8Rows16 * 8;
-static_assert(2 * sizeof(P8Span) <= 112 && kP8Lists % 16 == 0, "the misc area");
-constexpr uint32_t kP8ListBytes = 4 * (kP8Reqs + 4) * 4;   // the line, lengths, first rows and rows of the requests
-constexpr uint32_t kP8First = (kP8Lists + kP8ListBytes + 127) / 128 * 128, kP8Ring = kP8First + kP8Warps * kP8PieceBytes;
-constexpr uint32_t kP8SmemBytes = kP8Ring + kP8Warps * kP8Stages * kP8StageBytes;
-static_assert(kP8SmemBytes <= kSmemCtaBytes && kP8Stages * kP8StageBytes >= kP8PieceBytes, "fits an SM");
+// Shared memory of a kernel for kN times eight rows.
+template <int kN> struct P8Smem {
+    static constexpr int kWarps = kP8Warps;
+    static constexpr uint32_t kPieceBytes = kN * 8 * kGroup * 4;                  // sums of a piece
+    static constexpr uint32_t kPieces = kWarps * kP8Stages * 8, kSpans = kPieces + kWarps * 2 * sizeof(P8Piece), kMl = kSpans + 128;
+    static constexpr uint32_t kLists = kMl + kWarps * 2 * kN * 8 * 8, kListBytes = 4 * (kP8Reqs + 4) * 4;          // the line, lengths, first rows and rows of the requests
+    static constexpr uint32_t kScales = (kLists + kListBytes + 15) / 16 * 16, kFirst = kScales + kWarps * kP8Stages * kP8ScaleBytes;
+    static constexpr uint32_t kRing = (kFirst + kWarps * kPieceBytes + 1023) / 1024 * 1024, kBytes = kRing + kWarps * kP8Stages * kP8StageBytes;
+    static_assert(2 * sizeof(P8Span) <= 112 && kPieces % 16 == 0 && kLists % 16 == 0 && kBytes <= kSmemCtaBytes && kP8Stages * kP8StageBytes >= kPieceBytes, "fits an SM");
+};
 
 struct P8Few {
     const int32_t* line;       // [n_req + 1], or NULL: the kernel makes it
-    int32_t few_rows;
+    int32_t few_rows, by_request;
     float* part;               // [CTA][first, last][kP8Rows16][128]
     float2* part_ml;           // [CTA][first, last][kP8Rows16]
     Ticket* tickets;           // [CTA * kTicketStride]
@@ -328,7 +334,40 @@ __device__ __forceinline__ uint4 lds_v4(uint32_t at)
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
     return v;
 }
-__device__ __forceinline__ float lds_f32(uint32_t at) { return __uint_as_float(lds_u32(at)); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// more bytes to come before the barrier's phase is over, without an arrival
+__device__ __forceinline__ void mbar_expect_more(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// a look that does not wait
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// The first n (1 .. 4) bytes of a word global -> shared, the others zero; the barrier counts an arrival of this thread's when all such copies that it has
+// begun have come.
+__device__ __forceinline__ void copy_word(uint32_t dst, const uint8_t* src, int n)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void arrive_with_words(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
+// a 4-D tiled bulk load global -> shared through a tensor map (TMA)
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z),
+                 "r"(w), "r"(bar)
+                 : "memory");
+}
+// as mma_16816, for the compiler to place
+__device__ __forceinline__ void mma_h2(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ uint32_t turn_8x8(uint32_t v)
 {
     uint32_t r;
@@ -339,169 +378,181 @@ __device__ __forceinline__ uint32_t turn_8x8(uint32_t v)
 // kN: eight rows each, of a piece
 template <int kN>
 __global__ void __launch_bounds__(kP8Warps * 32, 1)
-ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ P8Few f)
+ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ P8Few f, const __grid_constant__ CUtensorMap k_map,
+                       const __grid_constant__ CUtensorMap v_map)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
+    using Smem = P8Smem<kN>;
+    constexpr int kP8Threads = kP8Warps * 32, kRows = kN * 8;
     constexpr unsigned full = 0xffffffffu;
     const int tid = static_cast<int>(threadIdx.x);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3u, base = smem_u32(smem);
-    const uint32_t bar = base + warp * kP8Stages * 8, ring = base + kP8Ring + warp * kP8Stages * kP8StageBytes;
-    int32_t* const line = reinterpret_cast<int32_t*>(smem + kP8Lists);
+    int32_t* const line = reinterpret_cast<int32_t*>(smem + Smem::kLists);
     int32_t *const kvs = line + kP8Reqs + 4, *const row0s = kvs + kP8Reqs + 4, *const rows_of = row0s + kP8Reqs + 4;
-    P8Piece* const pieces = reinterpret_cast<P8Piece*>(smem + kP8Pieces);              // [warp][first, last]
-    P8Span* const spans = reinterpret_cast<P8Span*>(smem + kP8Spans);
-    volatile int* const joins = reinterpret_cast<volatile int*>(smem + kP8Spans + 112);
-    float2* const ml = reinterpret_cast<float2*>(smem + kP8Ml);                        // [warp][first, last][row]
-    int64_t* const sums = reinterpret_cast<int64_t*>(smem + kP8First);                 // before there are pieces
-    if (lane == 0)
-        for (int i = 0; i < kP8Stages; ++i) mbar_init(bar + i * 8, 1);
+    P8Piece* const pieces = reinterpret_cast<P8Piece*>(smem + Smem::kPieces);              // [warp][first, last]
+    P8Span* const spans = reinterpret_cast<P8Span*>(smem + Smem::kSpans);
+    volatile int* const joins = reinterpret_cast<volatile int*>(smem + Smem::kSpans + 112);
+    float2* const ml = reinterpret_cast<float2*>(smem + Smem::kMl);                        // [warp][first, last][row]
+    int64_t* const sums = reinterpret_cast<int64_t*>(smem + Smem::kFirst);                 // before there are pieces
+    const int piece_shift = min(5, kv.page_shift), block_shift = min(4, kv.page_shift), n_blocks = 32 >> block_shift;      // of a tile
+    if (tid < kP8Warps * kP8Stages) {
+        mbar_init(base + tid * 8, n_blocks);
+    }
     if (tid < kP8Warps * 2) pieces[tid].valid = 0;
     __syncthreads();
     release_dependents();
     dependency_wait();
     const int32_t T = paged_tiles(kv);
     if (!f.line) {
-        // the line: prefix sums over the requests, in rounds of a request per thread
-        int64_t before = 0;
-        const int64_t limit = p8_line_limit(T, f.few_rows);
+        // the line: prefix sums over the requests, in rounds of a request per thread.  Mostly it is kv_tiles as it stands: no request that would
+        // be in the line twice, or not at all, or whose lengths say something else.
         if (tid == 0) {
             line[0] = 0;
             if (blockIdx.x == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
         }
-        for (int r0 = 0; r0 < kv.n_req; r0 += kP8Warps * 32) {
-            const int r = r0 + tid;
-            PagedReq q = {};
-            if (r < kv.n_req) q = paged_req(kv, r, T);
-            if ((q.cut || q.rows > kv.max_new) && blockIdx.x == 0) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-            int64_t upto = p8_line_tiles(q, o.q_per_kv, f.few_rows);
+        auto keep = [&](int r, const PagedReq& q, int32_t upto) {
+            line[r + 1] = upto;
+            kvs[r] = q.kv;
+            row0s[r] = q.row0;
+            rows_of[r] = q.rows;
+        };
+        PagedReq q = {};
+        bool plain = kv.n_req <= kP8Threads;
+        if (plain && tid < kv.n_req) {
+            q = paged_req(kv, tid, T);
+            plain = !q.cut && q.rows > 0 && q.rows <= kv.max_new && q.rows * o.q_per_kv <= kP8Rows16 && q.kv > 0 && q.tiles == (q.kv + 31) >> 5 && (tid > 0 || q.first == 0);
+            keep(tid, q, q.first + q.tiles);
+        }
+        if (!__syncthreads_and(plain)) {
+            int64_t before = 0;
+            const int64_t limit = p8_line_limit(T, f.few_rows);
+            for (int r0 = 0; r0 < kv.n_req; r0 += kP8Threads) {
+                const int r = r0 + tid;
+                q = {};
+                if (r < kv.n_req) q = paged_req(kv, r, T);
+                if ((q.cut || q.rows > kv.max_new) && blockIdx.x == 0) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+                int64_t upto = p8_line_tiles(q, o.q_per_kv, f.few_rows);
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int64_t x = __shfl_up_sync(full, upto, d);
-                if (static_cast<int>(lane) >= d) upto += x;
-            }
-            if (lane == 31) sums[warp] = upto;
-            __syncthreads();
-            int64_t all = 0;
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int64_t x = __shfl_up_sync(full, upto, d);
+                    if (static_cast<int>(lane) >= d) upto += x;
+                }
+                if (lane == 31) sums[warp] = upto;
+                __syncthreads();
+                int64_t all = 0;
 #pragma unroll
-            for (int w = 0; w < kP8Warps; ++w) {
-                if (w < static_cast<int>(warp)) upto += sums[w];
-                all += sums[w];
+                for (int w = 0; w < kP8Threads / 32; ++w) {
+                    if (w < static_cast<int>(warp)) upto += sums[w];
+                    all += sums[w];
+                }
+                if (r < kv.n_req) keep(r, q, static_cast<int32_t>(min(before + upto, limit)));
+                before = min(before + all, limit);
+                // requests without a token: nobody else comes to their rows
+                if (r0 / kP8Threads % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x))
+                    p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= f.few_rows && q.kv == 0);
+                __syncthreads();
             }
-            if (r < kv.n_req) {
-                line[r + 1] = static_cast<int32_t>(min(before + upto, limit));
-                kvs[r] = q.kv;
-                row0s[r] = q.row0;
-                rows_of[r] = q.rows;
-            }
-            before = min(before + all, limit);
-            // requests without a token: nobody else comes to their rows
-            if (r0 / (kP8Warps * 32) % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x))
-                p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= f.few_rows && q.kv == 0);
-            __syncthreads();
         }
     }
-    const int32_t L = f.line ? __ldcg(f.line + kv.n_req) : line[kv.n_req];
+    auto line_at = [&](int r) { return f.line ? __ldcg(f.line + r) : line[r]; };
+    const int32_t L = line_at(kv.n_req);
     const int64_t U = static_cast<int64_t>(L) * kv.heads;
     const UnitSplit cta_split(U, static_cast<int>(gridDim.x));
-    const int64_t c0 = cta_split.begin(static_cast<int>(blockIdx.x)), c1 = cta_split.begin(static_cast<int>(blockIdx.x) + 1);
+    int64_t c0 = cta_split.begin(static_cast<int>(blockIdx.x)), c1 = cta_split.begin(static_cast<int>(blockIdx.x) + 1);
+    if (f.by_request) {                                    // a CTA to a request and head
+        const int32_t head = static_cast<int32_t>(blockIdx.x) / kv.n_req, r = static_cast<int32_t>(blockIdx.x) - head * kv.n_req;
+        c0 = static_cast<int64_t>(head) * L + line_at(r);
+        c1 = static_cast<int64_t>(head) * L + line_at(r + 1);
+    }
     const UnitSplit split(c1 - c0, kP8Warps);
-    const int64_t u0 = c0 + split.begin(static_cast<int>(warp)), u1 = c0 + split.begin(static_cast<int>(warp) + 1);
 
     // a place in the line: unit u is tile `tile` of a piece, i.e. of sixteen rows (group) of a request for a head, which has units [begin, begin + units)
     struct Place { int64_t u, begin, end; int32_t units, head, tile, r, kv, row0, rows, group; };
+    // the piece that unit p.u is of, of request p.r or one behind it (r = 0: any); end: at most `stop`.  Every lane for itself.
     auto seek = [&](Place& p, int64_t stop) {
         if (p.u >= stop) return;
         const int32_t nth = static_cast<int32_t>(divide(static_cast<uint64_t>(p.u), static_cast<uint64_t>(L))), off = static_cast<int32_t>(p.u - static_cast<int64_t>(nth) * L);
-        int r = 0;
-        int32_t from, to;
+        int r = nth == p.head ? p.r : 0;
+        int32_t to = line_at(r + 1);
+        for (int i = 0; i < 2 && to <= off; ++i) to = line_at(++r + 1);
+        if (to <= off) {
+            for (int n = kv.n_req - r; n > 1;) {           // the last request that begins at or before the place
+                const int half = n >> 1;
+                if (line_at(r + half) <= off) { r += half; n -= half; } else n = half;
+            }
+            to = line_at(r + 1);
+        }
+        const int32_t from = line_at(r);
         if (f.line) {
-            r = warp_find(f.line, kv.n_req, off);
-            from = __ldcg(f.line + r);
-            to = __ldcg(f.line + r + 1);
             const PagedReq q = paged_req(kv, r, T);
             p.kv = q.kv; p.row0 = q.row0; p.rows = q.rows;
         } else {
-            for (int n = kv.n_req; n > 1;) {               // the last request that begins at or before the place
-                const int half = n >> 1;
-                if (line[r + half] <= off) { r += half; n -= half; } else n = half;
-            }
-            from = line[r];
-            to = line[r + 1];
             p.kv = kvs[r]; p.row0 = row0s[r]; p.rows = rows_of[r];
         }
         const int32_t tiles = max((p.kv + 31) >> 5, 1);
         p.r = r;
         p.head = nth;
-        p.group = (off - from) / tiles;
+        p.group = off - from < tiles ? 0 : (off - from) / tiles;
         const int32_t at = from + p.group * tiles;
         p.begin = static_cast<int64_t>(nth) * L + at;
         p.units = min(tiles, to - at);
         p.end = min(p.begin + p.units, stop);
         p.tile = off - at;
     };
-    const int piece_shift = min(5, kv.page_shift), block_shift = min(4, kv.page_shift);
-    const int32_t in_page = (1 << kv.page_shift) - 1;
-    // the page of the lane's part of a tile: -1: none, -2: there is nothing to look for
-    auto page_of = [&](const Place& p) {
-        const int32_t token = p.tile * 32 + static_cast<int32_t>(lane << piece_shift), e = token >> kv.page_shift;
-        if (p.u >= u1 || (lane << piece_shift) >= 32u || token >= p.kv) return -2;
-        return e < kv.stride ? max(__ldcg(kv.tables + static_cast<int64_t>(p.r) * kv.stride + e), -1) : -1;
-    };
-    // The way of a tile: its pages are looked up with the tile before it, its bytes are asked for, and its scales, with the next tile, written down.
+    const uint32_t bar = base + warp * kP8Stages * 8, ring = base + Smem::kRing + warp * kP8Stages * kP8StageBytes;
+    const uint32_t scales = base + Smem::kScales + warp * kP8Stages * kP8ScaleBytes, swizzle = kv.page_shift >= kP8SwizzledShift ? 7u : 0u;
+    const int64_t u0 = c0 + split.begin(static_cast<int>(warp)), u1 = c0 + split.begin(static_cast<int>(warp) + 1);
+    const int64_t n_scales = static_cast<int64_t>(kv.n_pages) * kv.all_heads << (kv.page_shift - block_shift);
+    const int32_t in_page = (1 << kv.page_shift) - 1, my_token = static_cast<int32_t>(lane << block_shift);
     Place load = {};
     load.u = u0;
     seek(load, u1);
-    int32_t page_next = page_of(load);
-    uint32_t asked = 0, taken = 0, k_scale = 0, v_scale = 0;
-    int scales_for = -1;
-    auto write_scales = [&]() {
-        if (scales_for < 0) return;
-        if ((lane << block_shift) < 32u) {
-            const uint32_t at = ring + scales_for * kP8StageBytes + 2 * kP8TileBytes + lane * 4;
-            const int e = p8_exponent(v_scale);
-            sts_u32(at, static_cast<uint32_t>(p8_exponent(k_scale) + 127) << 23);
-            sts_u32(at + 128, __float_as_uint(static_cast<float>(e)));
-            sts_u32(at + 256, static_cast<uint32_t>(127 - e) << 23);
-        }
-        __syncwarp();
-        scales_for = -1;
+    Place at = load;
+    // Loads: a lane to a block.  A tile's pages are looked up with the tile before it; nothing else from memory passes through registers on its way.
+    auto page_of = [&]() {                                 // -1: none, -2: there is nothing to look for
+        const int32_t token = load.tile * 32 + my_token, e = token >> kv.page_shift;
+        if (load.u >= u1 || my_token >= 32 || token >= load.kv) return -2;
+        return e < kv.stride ? max(__ldcg(kv.tables + static_cast<int64_t>(load.r) * kv.stride + e), -1) : -1;
     };
-    auto ask = [&]() {
-        write_scales();
+    int32_t page = page_of();
+    auto ask = [&](uint32_t stage) {
         if (load.u >= u1) return;
-        const uint32_t stage = asked % kP8Stages, b = bar + stage * 8, dst = ring + stage * kP8StageBytes;
-        if (page_next == -1 || page_next >= kv.n_pages) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-        const bool there = page_next >= 0 && page_next < kv.n_pages;
-        const int n = __popc(__ballot_sync(full, there));
-        if (lane == 0) mbar_expect_tx(b, (n * 2) << (piece_shift + 7));
-        __syncwarp();
-        const int32_t token0 = load.tile * 32, of_page = load.head + kv.head0;
-        if (there) {
-            const int32_t place = (token0 + static_cast<int32_t>(lane << piece_shift)) & in_page;
-            const int64_t from = ((((static_cast<int64_t>(page_next) * kv.all_heads + of_page) << kv.page_shift) + place) * kGroup);
-            const uint32_t to = dst + (lane << (piece_shift + 7)), bytes = 1u << (piece_shift + 7);
-            bulk_g2s(to, kv.k_blocks + from, bytes, b);
-            bulk_g2s(to + kP8TileBytes, kv.v_blocks + from, bytes, b);
+        if (my_token < 32) {
+            const uint32_t b = bar + stage * 8, words = scales + stage * kP8ScaleBytes + lane * 16;
+            if (page == -1 || page >= kv.n_pages) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+            if (page < 0 || page >= kv.n_pages) {          // nobody sees the block, or what is seen is unspecified
+                sts_v4(words, 127u, 127u, 0u, 0u);
+            } else {
+                const int32_t head = kv.head0 + load.head, place = (load.tile * 32 + my_token) & in_page;
+                const int64_t of_head = static_cast<int64_t>(page) * kv.all_heads + head;
+                if ((my_token & ((1 << piece_shift) - 1)) == 0) {
+                    const uint32_t to = ring + stage * kP8StageBytes + (lane << (block_shift + 7)), bytes = 1u << (piece_shift + 7);
+                    mbar_expect_more(b, 2 * bytes);
+                    if (kv.page_shift >= kP8SwizzledShift) {
+                        tma_load_4d(to, &k_map, 0, place, head, page, b);
+                        tma_load_4d(to + kP8TileBytes, &v_map, 0, place, head, page, b);
+                    } else {
+                        const int64_t from = ((of_head << kv.page_shift) + place) * kGroup;
+                        bulk_g2s(to, kv.k_blocks + from, bytes, b);
+                        bulk_g2s(to + kP8TileBytes, kv.v_blocks + from, bytes, b);
+                    }
+                }
+                const int64_t scale = (of_head << (kv.page_shift - block_shift)) + (place >> block_shift), word = scale & ~3ll;
+                const int there = static_cast<int>(min(n_scales - word, static_cast<int64_t>(4)));
+                copy_word(words, kv.k_meta + word, there);
+                copy_word(words + 4, kv.v_meta + word, there);
+                sts_u32(words + 8, static_cast<uint32_t>(scale & 3) * 8);
+            }
+            arrive_with_words(b);
         }
-        const int32_t page = __shfl_sync(full, page_next, ((lane << block_shift) & 31u) >> piece_shift);
-        k_scale = v_scale = 127;
-        if ((lane << block_shift) < 32u && page >= 0 && page < kv.n_pages) {
-            const int32_t place = (token0 + static_cast<int32_t>(lane << block_shift)) & in_page;
-            const int64_t at = ((static_cast<int64_t>(page) * kv.all_heads + of_page) << (kv.page_shift - block_shift)) + (place >> block_shift);
-            k_scale = __ldcg(kv.k_meta + at);
-            v_scale = __ldcg(kv.v_meta + at);
-        }
-        scales_for = static_cast<int>(stage);
-        ++asked;
         ++load.tile;
         if (++load.u == load.end) seek(load, u1);
-        page_next = page_of(load);
+        page = page_of();
     };
-    __syncwarp();
-    Place at = load;
-    for (int i = 0; i < kP8Stages; ++i) ask();
+    for (uint32_t i = 0; i < kP8Stages; ++i) ask(i);
+    uint32_t taken = 0;
     // pieces of this CTA that other CTAs have parts of: at its begin and at its end
-    if (warp == kP8Warps - 1) {
+    if (!f.by_request && warp == kP8Warps - 1) {
         Place p = {};
         P8Span sp[2] = {};
         for (int i = 0; i < 2; ++i) {
@@ -540,9 +591,13 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int mine = n * 8 + static_cast<int>(c) * 2 + e;
-                seen[n][e] = mine < R ? tokens_seen(PagedReq{0, 0, at.kv, at.row0, at.rows, false}, (at.group * kP8Rows16 + mine) / o.q_per_kv, o.causal) : 0;
+                seen[n][e] = mine < R ? tokens_seen(PagedReq{0, 0, at.kv, at.row0, at.rows, false}, (at.group * kP8Rows16 + mine) / o.q_per_kv, o.causal) : at.kv;
             }
         }
+        int32_t least = at.kv;                             // that a row sees (rows that there are not, with zeros for q, see all)
+#pragma unroll
+        for (int n = 0; n < kN; ++n) least = min(least, min(seen[n][0], seen[n][1]));
+        const int32_t tile_of_masks = __reduce_min_sync(full, least) >> 5;
         float acc[8][kN][4], m[kN][2], l[kN][2];
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
@@ -554,79 +609,129 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 for (int e = 0; e < 4; ++e) acc[j][n][e] = 0.0f;
         }
         for (; at.u < at.end; ++at.u, ++at.tile) {
-            const uint32_t stage = taken % kP8Stages, k_at = ring + stage * kP8StageBytes, v_at = k_at + kP8TileBytes, s_at = k_at + 2 * kP8TileBytes;
+            const uint32_t stage = taken % kP8Stages, k_at = ring + stage * kP8StageBytes, v_at = k_at + kP8TileBytes, s_at = scales + stage * kP8ScaleBytes;
             ok = warp_wait(bar + stage * 8, (taken / kP8Stages) & 1u);
             if (!ok) break;
             ++taken;
-            // scores: sixteen tokens x eight rows
-            float s[2][kN][4];
+            // The tile goes into registers, K as the scores need it: token mt * 16 + g and the eighth behind it, dims 32 c .. 32 c + 31; V as the second
+            // products need it: tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of sixteen, dims 16 g .. 16 g + 15.  With eight rows both find room at once, and the
+            // place in the ring is free again before there is any product.
+            uint4 kx[2][2][2], vx[2][4];
+            auto load_v = [&]() {
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
+                for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int n = 0; n < kN; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[mt][n][e] = 0.0f;
-                const uint32_t row = k_at + (mt * 16 + g) * kGroup + c * 32;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint4 x = lds_v4(row + half * 16), y = lds_v4(row + 8 * kGroup + half * 16);
-                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t a[4] = {e4m3_low(xs[j]), e4m3_low(ys[j]), e4m3_high(xs[j]), e4m3_high(ys[j])};
-#pragma unroll
-                        for (int n = 0; n < kN; ++n) mma_16816(s[mt][n], a, q[n][2 * (4 * half + j)], q[n][2 * (4 * half + j) + 1]);
-                    }
-                }
-            }
-            // softmax: weights of V's E4M3 numbers, relative to the largest so far
-            float inverse[2][2], top[kN][2];
-#pragma unroll
-            for (int n = 0; n < kN; ++n)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) top[n][e] = m[n][e];
+                    for (int i = 0; i < 4; ++i) vx[kt][i] = lds_v4(v_at + (kt * 16 + 2 * c + (i & 1) + (i >> 1) * 8) * kGroup + (g ^ ((2 * c + (i & 1)) & swizzle)) * 16);
+            };
+            uint4 words[2][2];
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t t = mt * 16 + h * 8 + g, sc = s_at + (t >> block_shift) * 4;
-                    const float by = lds_f32(sc) * o.scale_log2, plus = lds_f32(sc + 128);
-                    inverse[mt][h] = lds_f32(sc + 256);
-                    const int32_t token = at.tile * 32 + static_cast<int32_t>(t);
+                    words[mt][h] = h == 0 || block_shift < 4 ? lds_v4(s_at + ((mt * 16 + h * 8 + g) >> block_shift) * 16) : words[mt][0];
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) kx[mt][h][half] = lds_v4(k_at + (mt * 16 + h * 8 + g) * kGroup + ((2 * c + half) ^ (g & swizzle)) * 16);
+                }
+            if (kN == 1) {
+                load_v();
+                __syncwarp();                              // the whole warp has read the tile
+                ask(stage);
+            }
+            float4 by[2][2];                               // K's factor, V's exponent, the inverse of V's power of two
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h && block_shift == 4) {
+                        by[mt][h] = by[mt][0];
+                        continue;
+                    }
+                    const uint4 x = words[mt][h];
+                    const int k = p8_exponent((x.x >> x.z) & 0xffu), v = p8_exponent((x.y >> x.z) & 0xffu);
+                    by[mt][h] = make_float4(__uint_as_float(static_cast<uint32_t>(k + 127) << 23) * o.scale_log2, static_cast<float>(v), __uint_as_float(static_cast<uint32_t>(127 - v) << 23), 0.0f);
+                }
+            // scores: sixteen tokens x eight rows; with eight rows in two sums each, for four products to be under way
+            constexpr int kSums = kN == 1 ? 2 : 1;
+            float s[2][kN][4], part[2][kN][4];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[mt][n][e] = part[mt][n][e] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt) {
+                        const uint32_t x = reinterpret_cast<const uint32_t*>(&kx[mt][0][half])[j], y = reinterpret_cast<const uint32_t*>(&kx[mt][1][half])[j];
+                        const uint32_t a[4] = {e4m3_low(x), e4m3_low(y), e4m3_high(x), e4m3_high(y)};
+#pragma unroll
+                        for (int n = 0; n < kN; ++n) mma_h2(half < kSums - 1 ? part[mt][n] : s[mt][n], a, q[n][2 * (4 * half + j)], q[n][2 * (4 * half + j) + 1]);
+                    }
+            if (kSums > 1) {
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int n = 0; n < kN; ++n)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float& x = s[mt][n][2 * h + e];
-                            x = token < seen[n][e] ? fmaf(x, by, plus) : -INFINITY;
-                            top[n][e] = fmaxf(top[n][e], x);
-                        }
-                }
-            float sub[kN][2];
+                        for (int e = 0; e < 4; ++e) s[mt][n][e] += part[mt][n][e];
+            }
+            if (kN > 1) {
+                load_v();
+                __syncwarp();
+                ask(stage);
+            }
+            // softmax: weights of V's E4M3 numbers, relative to the largest so far
+            float top[kN][2];
+            const int32_t left = at.kv - at.tile * 32;     // tokens that there are
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[mt][n][e] = fmaf(s[mt][n][e], by[mt][e >> 1].x, by[mt][e >> 1].y);
+            if (at.tile >= tile_of_masks) {                // some row does not see all of the tile
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int n = 0; n < kN; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (at.tile * 32 + mt * 16 + (e >> 1) * 8 + static_cast<int32_t>(g) >= seen[n][e & 1]) s[mt][n][e] = -INFINITY;
+            }
+            // The reference m is a row's largest when it was last taken; another one is taken only when a lane has one that is more than 2^8 larger
+            // (the weights stand at 2^7 times what they are, at most 2^15), so mostly one vote is all that the lanes need of one another.
             bool grow = false;
 #pragma unroll
             for (int n = 0; n < kN; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float& t = top[n][e];
-                    t = fmaxf(t, __shfl_xor_sync(full, t, 4));
-                    t = fmaxf(t, __shfl_xor_sync(full, t, 8));
-                    t = fmaxf(t, __shfl_xor_sync(full, t, 16));
-                    grow = grow || t > m[n][e];
-                    sub[n][e] = t == -INFINITY ? 0.0f : t;
+                    top[n][e] = fmaxf(max3(s[0][n][e], s[0][n][2 + e], s[1][n][e]), s[1][n][2 + e]);
+                    grow = grow || top[n][e] > m[n][e] + kLazyLog2;            // -inf + 8 is -inf
                 }
             if (__any_sync(full, grow)) {
 #pragma unroll
                 for (int n = 0; n < kN; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float by = exp2_fast(m[n][e] - sub[n][e]);
+                        float t = top[n][e];
+                        t = fmaxf(t, __shfl_xor_sync(full, t, 4));
+                        t = fmaxf(t, __shfl_xor_sync(full, t, 8));
+                        t = max3(t, __shfl_xor_sync(full, t, 16), m[n][e]);
+                        const float by = exp2_fast(m[n][e] - (t == -INFINITY ? 0.0f : t));
                         l[n][e] *= by;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) { acc[j][n][e] *= by; acc[j][n][2 + e] *= by; }
-                        m[n][e] = top[n][e];
+                        m[n][e] = t;
                     }
             }
+            float plus[kN][2];
+#pragma unroll
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) plus[n][e] = m[n][e] == -INFINITY ? 0.0f : kManyWeightLog2 - m[n][e];
             uint32_t w[2][kN][2];                          // of sixteen tokens and eight rows each, as the second operand
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
@@ -637,21 +742,18 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                         float p[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            p[e] = exp2_fast(s[mt][n][2 * h + e] - sub[n][e] + kWeightLog2);
-                            l[n][e] = fmaf(p[e], inverse[mt][h], l[n][e]);
+                            p[e] = exp2_fast(s[mt][n][2 * h + e] + plus[n][e]);
+                            l[n][e] = fmaf(p[e], by[mt][h].z, l[n][e]);
                         }
                         w[mt][n][h] = turn_8x8(pack_h2(p[0], p[1]));
                     }
-            const int32_t left = at.kv - at.tile * 32;     // tokens that there are
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
-                // tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of sixteen; dims 16 g .. 16 g + 15
-                uint4 x[4];
+                uint4(&x)[4] = vx[kt];
+                if (left < 32) {                           // places behind the last token: whatever is there, nobody sees it
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t t = kt * 16 + 2 * c + (i & 1) + (i >> 1) * 8;
-                    x[i] = lds_v4(v_at + t * kGroup + g * 16);
-                    if (left < 32 && static_cast<int32_t>(t) >= left) x[i] = make_uint4(0u, 0u, 0u, 0u);     // whatever is there: nobody sees it
+                    for (int i = 0; i < 4; ++i)
+                        if (static_cast<int32_t>(kt * 16 + 2 * c + (i & 1) + (i >> 1) * 8) >= left) x[i] = make_uint4(0u, 0u, 0u, 0u);
                 }
                 const uint32_t* const x0 = reinterpret_cast<const uint32_t*>(&x[0]);
                 const uint32_t* const x1 = reinterpret_cast<const uint32_t*>(&x[1]);
@@ -663,18 +765,15 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                     const uint32_t near = prmt(x0[j >> 1], x1[j >> 1], sel), far = prmt(x2[j >> 1], x3[j >> 1], sel);
                     const uint32_t a[4] = {e4m3_low(near), e4m3_high(near), e4m3_low(far), e4m3_high(far)};
 #pragma unroll
-                    for (int n = 0; n < kN; ++n) mma_16816(acc[j][n], a, w[kt][n][0], w[kt][n][1]);
+                    for (int n = 0; n < kN; ++n) mma_h2(acc[j][n], a, w[kt][n][0], w[kt][n][1]);
                 }
             }
-            __syncwarp();                                  // the whole warp has read the tile
-            ask();
         }
         if (!ok) break;
         // out, or to be joined
         const bool whole = at.begin >= u0 && at.begin + at.units <= u1;
         const int which = from_u == u0 ? 0 : 1;
-        float* const to = reinterpret_cast<float*>(which ? smem + (ring - base) : smem + kP8First + warp * kP8PieceBytes);
-        if (!whole && which) __syncwarp();
+        float* const to = reinterpret_cast<float*>(which ? smem + (ring - base) : smem + Smem::kFirst + warp * Smem::kPieceBytes);
 #pragma unroll
         for (int n = 0; n < kN; ++n)
 #pragma unroll
@@ -693,19 +792,19 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                     auto two = [&](int j) { return pack_h2(acc[j][n][e] * inv, acc[j][n][2 + e] * inv); };
                     dst[0] = make_uint4(two(0), two(1), two(2), two(3));
                     dst[1] = make_uint4(two(4), two(5), two(6), two(7));
-                    if (o.lse && g == 0) o.lse[out_row] = lse_of(m[n][e], sum, kWeightLog2);
+                    if (o.lse && g == 0) o.lse[out_row] = lse_of(m[n][e], sum, kManyWeightLog2);
                 } else {
                     float4* const dst = reinterpret_cast<float4*>(to + row * kGroup + g * 16);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) dst[j] = make_float4(acc[2 * j][n][e], acc[2 * j][n][2 + e], acc[2 * j + 1][n][e], acc[2 * j + 1][n][2 + e]);
-                    if (g == 0) ml[(warp * 2 + which) * kP8Rows16 + row] = make_float2(m[n][e], sum);
+                    if (g == 0) ml[(warp * 2 + which) * kRows + row] = make_float2(m[n][e], sum);
                 }
             }
         if (!whole && lane == 0) pieces[warp * 2 + which] = P8Piece{at.begin, at.units, at.head, at.row0, at.rows, at.group, 1};
         seek(at, u1);
     }
     if (!ok)                                               // tiles on their way land before the warp leaves
-        for (; taken < asked; ++taken) warp_wait(bar + (taken % kP8Stages) * 8, (taken / kP8Stages) & 1u);
+        for (uint32_t i = taken; i < taken + kP8Stages && static_cast<int64_t>(i) < u1 - u0; ++i) warp_wait(bar + (i % kP8Stages) * 8, (i / kP8Stages) & 1u);
     __syncthreads();
 
     auto write_row = [&](int32_t group, int32_t row0, int32_t head, int row, float m, float l, const float4& v) {
@@ -713,26 +812,28 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         const int64_t out_row = static_cast<int64_t>(row0 + token) * o.q_heads + static_cast<int64_t>(kv.head0 + head) * o.q_per_kv + (i - token * o.q_per_kv);
         const float inv = inverse_of(l);
         reinterpret_cast<uint2*>(o.out + out_row * kGroup)[lane] = make_uint2(pack_h2(v.x * inv, v.y * inv), pack_h2(v.z * inv, v.w * inv));
-        if (o.lse && lane == 0) o.lse[out_row] = lse_of(m, l, kWeightLog2);
+        if (o.lse && lane == 0) o.lse[out_row] = lse_of(m, l, kManyWeightLog2);
     };
-    // pieces of the CTA's warps, one behind the other in the line
-    for (int i = 0; i < kP8Warps * 2;) {
-        if (!pieces[i].valid) { ++i; continue; }
+    // pieces of the CTA's warps, one behind the other in the line: lane i looks at the i-th of them
+    const uint32_t nth = min(lane, 2u * kP8Warps - 1u);
+    const int64_t of_lane = pieces[nth].begin;
+    const unsigned valid = __ballot_sync(full, lane < 2 * kP8Warps && pieces[nth].valid);
+    const unsigned ahead = valid & ((1u << lane) - 1u);
+    const int64_t of_ahead = __shfl_sync(full, of_lane, ahead ? 31 - __clz(ahead) : 0);
+    unsigned firsts = __ballot_sync(full, (valid >> lane & 1u) && (!ahead || of_ahead != of_lane));
+    while (firsts) {
+        const int i = __ffs(firsts) - 1;
+        firsts &= firsts - 1u;
+        const unsigned members = valid & ~((1u << i) - 1u) & (firsts ? (1u << (__ffs(firsts) - 1)) - 1u : full);
         const P8Piece p = pieces[i];
-        int last = i;
-        for (int j = i + 1; j < kP8Warps * 2; ++j)
-            if (pieces[j].valid) {
-                if (pieces[j].begin != p.begin) break;
-                last = j;
-            }
         const int R = min(p.rows * o.q_per_kv - p.group * kP8Rows16, kN * 8);
         for (int row = static_cast<int>(warp); row < R; row += kP8Warps) {
             float m = -INFINITY, l = 0.0f;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int j = i; j <= last; ++j) {
-                if (!pieces[j].valid) continue;
-                const uint8_t* const from = j & 1 ? smem + kP8Ring + (j >> 1) * kP8Stages * kP8StageBytes : smem + kP8First + (j >> 1) * kP8PieceBytes;
-                join_sums(m, l, v, ml[j * kP8Rows16 + row], reinterpret_cast<const float4*>(from)[row * 32 + lane]);
+            for (unsigned left = members; left; left &= left - 1u) {
+                const int j = __ffs(left) - 1;
+                const uint8_t* const from = j & 1 ? smem + Smem::kRing + (j >> 1) * kP8Stages * kP8StageBytes : smem + Smem::kFirst + (j >> 1) * Smem::kPieceBytes;
+                join_sums(m, l, v, ml[j * kRows + row], reinterpret_cast<const float4*>(from)[row * 32 + lane]);
             }
             if (p.begin >= c0 && p.begin + p.units <= c1) {
                 write_row(p.group, p.row0, p.head, row, m, l, v);
@@ -742,8 +843,8 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 if (lane == 0) f.part_ml[to] = make_float2(m, l);
             }
         }
-        i = last + 1;
     }
+    if (f.by_request) return;
     if (!spans[0].valid && !spans[1].valid) return;
     __threadfence();
     __syncthreads();
