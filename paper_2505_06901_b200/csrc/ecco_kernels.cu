@@ -1055,6 +1055,17 @@ static int check_paged8_cache(const ecco_paged8_cache* c)
     return ECCO_OK;
 }
 
+template <bool kTurn>
+static int launch_paged8_append(const DeviceInfo& di, const ecco_rope& rope, const P8Append& p, int64_t ctas, cudaStream_t s)
+{
+    static thread_local bool configured[64] = {};
+    if (!configured[di.device]) {
+        const int rc = set_smem(ecco_paged8_append_kernel<kTurn>, kP8AppendSmemBytes);
+        if (rc) return rc;
+        configured[di.device] = true;
+    }
+    return launch_overlapped(ecco_paged8_append_kernel<kTurn>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8AppendThreads), kP8AppendSmemBytes, s, rope, p);
+}
 extern "C" int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope, const int32_t* d_positions, const void* d_k, const void* d_v,
                                   int64_t token_stride, const int32_t* d_slots, int32_t n_tokens, void* stream)
 {
@@ -1075,11 +1086,11 @@ extern "C" int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rop
     p.n_tokens = n_tokens; p.n_slots = cache->n_pages * cache->page_size;
     p.heads = cache->n_kv_heads; p.page_shift = page_shift_of(cache->page_size);
     const int64_t windows = (static_cast<int64_t>(n_tokens) + kP8Rows - 1) / kP8Rows;
-    p.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>((4 * di.sms + windows - 1) / windows, 4ll * p.heads)));
-    const unsigned grid = static_cast<unsigned>(windows * p.parts);
+    const int64_t slots = 3 * di.sms / windows;
+    p.kinds = slots >= 2 ? 2 : 1;
+    p.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(slots / p.kinds, 2ll * p.heads)));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (rope) return launch_overlapped(ecco_paged8_append_kernel<true>, grid, static_cast<unsigned>(kP8AppendThreads), 0, s, *rope, p);
-    return launch_overlapped(ecco_paged8_append_kernel<false>, grid, static_cast<unsigned>(kP8AppendThreads), 0, s, ecco_rope{}, p);
+    return rope ? launch_paged8_append<true>(di, *rope, p, windows * p.parts * p.kinds, s) : launch_paged8_append<false>(di, ecco_rope{}, p, windows * p.parts * p.kinds, s);
 }
 
 namespace {

@@ -43,30 +43,44 @@ __device__ __forceinline__ uint32_t power_h2(int n)
     return h | (h << 16);
 }
 
+__device__ __forceinline__ uint4 lds_v4(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+
 // ---------------------------------------------------------------------------------------------
 // K8a: new tokens into the cache.  A run is what a call brings for one block: rows one after the other whose slots ascend within
 // it.  A CTA has the runs that begin in sixteen rows, and a share of their heads; a warp takes a run of one head, of K or of V, as a whole: eight
 // lanes to a token, so that its up to 2048 values stay in registers from the load over the rotation and the largest value to the E4M3 numbers.
 // Bound by memory: 768 bytes per token and KV head.
 // ---------------------------------------------------------------------------------------------
-constexpr int kP8AppendThreads = 256, kP8Rows = 16;
+constexpr int kP8AppendThreads = 256, kP8AppendWarps = kP8AppendThreads / 32, kP8Rows = 16;
+constexpr uint32_t kP8RunBytes = kP8Rows * kGroup * 2;     // a run's rows in shared memory: the next one's are on their way while one is dealt with
+constexpr uint32_t kP8AppendTable = 128, kP8AppendRuns = kP8AppendTable + 32 * sizeof(RopeRow), kP8AppendSmemBytes = kP8AppendRuns + kP8AppendWarps * 2 * kP8RunBytes;
 struct P8Append {
     const int32_t *positions, *slots;
     const __half *k, *v;
     uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
     int64_t token_stride;
-    int32_t n_tokens, n_slots, heads, page_shift, parts;
+    int32_t n_tokens, n_slots, heads, page_shift;
+    int32_t kinds, parts;      // CTAs to a window: one of each kind (K, V) or for both, and as many for a share of the heads
 };
 
 template <bool kTurn>
-__global__ void __launch_bounds__(kP8AppendThreads)
+__global__ void __launch_bounds__(kP8AppendThreads, 2)
 ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_constant__ P8Append p)
 {
+    extern __shared__ __align__(1024) uint8_t smem[];
     constexpr unsigned full = 0xffffffffu;
-    __shared__ __align__(16) float2 table[kTurn ? 32 : 1][kGroup / 2];
+    RopeRow* const table = reinterpret_cast<RopeRow*>(smem + kP8AppendTable);
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5, s = lane & 7, team = lane >> 3;
-    const int32_t window = static_cast<int32_t>(blockIdx.x) / p.parts, part = static_cast<int32_t>(blockIdx.x) - window * p.parts;
+    const int32_t cta = static_cast<int32_t>(blockIdx.x) / p.kinds, kind = static_cast<int32_t>(blockIdx.x) - cta * p.kinds, window = cta / p.parts, part = cta - window * p.parts;
     const int block_shift = min(4, p.page_shift), places = 1 << block_shift;
+    const uint32_t bar = smem_u32(smem) + warp * 16, rows_at = smem_u32(smem) + kP8AppendRuns + warp * 2 * kP8RunBytes;
+    if (lane < 2) mbar_init(bar + lane * 8, 1);
+    __syncwarp();
     release_dependents();
     dependency_wait();
     // lane l: row 16 window - 1 + l.  Runs begin in lanes 1 .. 16 and are sixteen rows at most.
@@ -82,23 +96,47 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
     };
     const int n_runs = __popc(starts);
     if (n_runs == 0) return;
-    if (kTurn) {
+    // the warp's work: run by run, of each K and V of all heads; a place in it
+    struct Item { unsigned left; int of_run, l0, n; };     // runs from this one on, as bits; the item of the run; its first lane and its rows
+    const int per_run = p.kinds == 2 ? p.heads : 2 * p.heads, first_v = p.kinds == 2 ? (kind ? 0 : p.heads) : p.heads, step = p.parts * kP8AppendWarps;
+    auto open = [&](Item& it) {
+        while (it.left && it.of_run >= per_run) { it.of_run -= per_run; it.left &= it.left - 1u; }
+        if (!it.left) return;
+        it.l0 = __ffs(it.left) - 1;
+        it.n = min(run_end(it.l0) - it.l0, kP8Rows);
+    };
+    auto source = [&](const Item& it) {
+        const int head = it.of_run < first_v ? it.of_run : it.of_run - first_v;
+        return (it.of_run < first_v ? p.k : p.v) + (static_cast<int64_t>(window) * kP8Rows - 1 + it.l0) * p.token_stride + static_cast<int64_t>(head) * kGroup;
+    };
+    auto fetch = [&](const Item& it, uint32_t stage) {
+        if (!it.left) return;
+        if (lane == 0) mbar_expect_tx(bar + stage * 8, it.n * kGroup * 2);
+        __syncwarp();
+        if (lane < it.n) bulk_g2s(rows_at + stage * kP8RunBytes + lane * kGroup * 2, source(it) + lane * p.token_stride, kGroup * 2, bar + stage * 8);
+    };
+    Item now = {starts, part * kP8AppendWarps + warp, 0, 0};
+    open(now);
+    fetch(now, 0);
+    if (kTurn && first_v > 0) {
         const int from = __ffs(starts) - 1, to = run_end(31 - __clz(starts)), pairs = rope.rot_dim / 2;
         for (int i = tid; i < (to - from) * (kGroup / 2); i += kP8AppendThreads) {
             const int l = from + i / (kGroup / 2), pair = i % (kGroup / 2);
             const int64_t r = static_cast<int64_t>(window) * kP8Rows - 1 + l;
-            if (pair < pairs && r < p.n_tokens) table[l][pair] = rope_angle(rope, pair, __ldcg(p.positions + r));
+            if (pair < pairs && r < p.n_tokens) rope_store(table[l], pair, rope_angle(rope, pair, __ldcg(p.positions + r)));
         }
         __syncthreads();
     }
     const int2 turned_piece = kTurn ? rope_pieces(rope, s) : make_int2(2 * s, 2 * s + 1);
     const bool turns = kTurn && rope_turns(rope, s), neighbours = rope.flags & ECCO_ROPE_NEIGHBOURS;
-    const int n_items = n_runs * p.heads * 2;
-    for (int item = part * (kP8AppendThreads / 32) + warp; item < n_items; item += p.parts * (kP8AppendThreads / 32)) {
-        const int run = item / (2 * p.heads), in_run = item - run * 2 * p.heads, is_v = in_run >= p.heads, head = in_run - (is_v ? p.heads : 0);
-        const int l0 = __fns(starts, 0, run + 1), n = min(run_end(l0) - l0, 16);
+    for (uint32_t nth = 0; now.left; ++nth) {
+        Item next = now;
+        next.of_run += step;
+        open(next);
+        fetch(next, (nth + 1) & 1u);
+        const int l0 = now.l0, n = now.n, is_v = now.of_run >= first_v, head = now.of_run - (is_v ? first_v : 0);
+        now = next;
         const int32_t slot0 = __shfl_sync(full, slot, l0), page = slot0 >> p.page_shift, base = slot0 & ((1 << p.page_shift) - 1) & ~(places - 1);
-        const __half* const src = (is_v ? p.v : p.k) + (static_cast<int64_t>(window) * kP8Rows - 1 + l0) * p.token_stride + static_cast<int64_t>(head) * kGroup;
         const int64_t of_head = static_cast<int64_t>(page) * p.heads + head;
         uint8_t* const block = (is_v ? p.v_codes : p.k_codes) + ((of_head << p.page_shift) + base) * kGroup;
         uint8_t* const scale = (is_v ? p.v_scales : p.k_scales) + (of_head << (p.page_shift - block_shift)) + (base >> block_shift);
@@ -106,14 +144,19 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
         const bool anew = (slot0 & (places - 1)) == 0;
         int e = kP8Lowest, e_before = kP8Lowest;
         if (!anew) e_before = p8_exponent(__ldcg(scale));
+        const uint32_t stage = nth & 1u;
+        if (!warp_wait(bar + stage * 8, (nth >> 1) & 1u)) {                        // what is on its way lands before the CTA leaves
+            if (now.left) warp_wait(bar + (stage ^ 1u) * 8, ((nth + 1) >> 1) & 1u);
+            return;
+        }
         uint4 v[4][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[i][0] = v[i][1] = make_uint4(0u, 0u, 0u, 0u);
             if (4 * i + team < n) {
-                const uint4* const from = reinterpret_cast<const uint4*>(src + (4 * i + team) * p.token_stride);
-                v[i][0] = __ldcg(from + piece.x);
-                v[i][1] = __ldcg(from + piece.y);
+                const uint32_t from = rows_at + stage * kP8RunBytes + (4 * i + team) * kGroup * 2;
+                v[i][0] = lds_v4(from + piece.x * 16);
+                v[i][1] = lds_v4(from + piece.y * 16);
             }
         }
         uint32_t top = 0;                                  // largest magnitudes, as bits of two fp16 numbers
@@ -121,19 +164,29 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
         for (int i = 0; i < 4; ++i) {
             if (4 * i >= n) break;
             if (turns && !is_v && 4 * i + team < n) {
-                float2 cs[8];
+                RopePairs cs[4];
                 rope_load(cs, table[l0 + 4 * i + team], s);
                 rope_turn(v[i][0], v[i][1], cs, neighbours);
             }
-            uint32_t* const w = reinterpret_cast<uint32_t*>(v[i]);
+            const uint32_t* const w = reinterpret_cast<const uint32_t*>(v[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const __half2 h = *reinterpret_cast<const __half2*>(&w[j]);
-                w[j] &= __heq2_mask(h, h);                 // NaN becomes zero
-                top = __vmaxu2(top, w[j] & 0x7fff7fffu);
-            }
+            for (int j = 0; j < 8; ++j) top = __vmaxu2(top, w[j] & 0x7fff7fffu);
         }
-        const uint32_t largest = __reduce_max_sync(full, max(top & 0xffffu, top >> 16));
+        uint32_t largest = __reduce_max_sync(full, max(top & 0xffffu, top >> 16));
+        if (largest > 0x7c00u) {                           // NaN becomes zero
+            top = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t* const w = reinterpret_cast<uint32_t*>(v[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const __half2 h = *reinterpret_cast<const __half2*>(&w[j]);
+                    w[j] &= __heq2_mask(h, h);
+                    top = __vmaxu2(top, w[j] & 0x7fff7fffu);
+                }
+            }
+            largest = __reduce_max_sync(full, max(top & 0xffffu, top >> 16));
+        }
         // 448 is 1.75 times a power of two: a larger mantissa (above 0x300) needs the next one
         e = min(max(static_cast<int>((largest + 0xffu) >> 10) - 23, kP8Lowest), kP8Highest);
         e = max(e, e_before);
@@ -328,12 +381,6 @@ struct P8Few {
     Ticket* tickets;           // [CTA * kTicketStride]
     Ticket tag;
 };
-__device__ __forceinline__ uint4 lds_v4(uint32_t at)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
-}
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // more bytes to come before the barrier's phase is over, without an arrival
 __device__ __forceinline__ void mbar_expect_more(uint32_t bar, uint32_t bytes)
