@@ -1230,8 +1230,8 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
         sc.few_rows = kP8FewRows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
         sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
-        const int64_t units = p.many ? static_cast<int64_t>(b.max_tiles) * kv.heads * 2 : 0;
-        const unsigned grid = static_cast<unsigned>(spread_ctas(units / kP8StageWarps + 1, di.sms * 4));
+        const int64_t units = p.many ? static_cast<int64_t>(b.max_tiles) * kv.heads : 0;
+        const unsigned grid = static_cast<unsigned>(spread_ctas(units / kP8StageWarps + 1, di.sms * 2));
         rc = launch_overlapped(ecco_paged8_stage_kernel, grid, static_cast<unsigned>(kP8StageWarps * 32), 0, s, kv, o, sc, static_cast<int32_t>(p.many), static_cast<int32_t>(p.line));
         if (rc) return rc;
         if (!p.many) break;

@@ -347,22 +347,25 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             tmem_fence_after();
             const bool whole = pc.whole;
             const float inv = inverse_of(l);
-            float* const part = o.part + (static_cast<int64_t>(pc.slot) * kManyRows + x * 128 + t) * kGroup;
+            // a piece's sums: 16 bytes of all rows of a tile side by side, so that the threads' stores, and the loads that join them, are whole lines
+            auto sums_of = [&](int64_t slot) { return reinterpret_cast<float4*>(o.part + (slot * kManyRows + x * 128) * kGroup) + t; };
+            {
+                uint32_t v[128];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                tmem_ld32(v, o_at + 32 * c);
+                for (int c = 0; c < 4; ++c) tmem_ld32(v + 32 * c, o_at + 32 * c);
                 tmem_wait_ld();
-                tie32(v);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tie32(v + 32 * c);
                 if (exists && whole) {
-                    uint4* const dst = reinterpret_cast<uint4*>(o.out + out_row * kGroup) + 4 * c;
+                    uint4* const dst = reinterpret_cast<uint4*>(o.out + out_row * kGroup);
                     // a row that has seen nothing: O may not have been written at all
                     auto two = [&](int i) { return l != 0.0f ? pack_h2(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv) : 0u; };
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dst[i] = make_uint4(two(8 * i), two(8 * i + 2), two(8 * i + 4), two(8 * i + 6));
+                    for (int i = 0; i < 16; ++i) dst[i] = make_uint4(two(8 * i), two(8 * i + 2), two(8 * i + 4), two(8 * i + 6));
                 } else if (exists) {
+                    uint4* const dst = reinterpret_cast<uint4*>(sums_of(pc.slot));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(part)[8 * c + i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    for (int i = 0; i < 32; ++i) dst[i * 128] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                 }
                 __syncwarp();
             }
@@ -372,7 +375,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             }
             tmem_fence_before();                           // O has been read before the next block's P arrives
             if (!whole) {
-                // The tile's four warps count themselves in; the last run's read all pieces, a warp to eight rows.  (They meet at barriers whose
+                // The tile's four warps count themselves in; the last run's read all pieces.  (They meet at barriers whose
                 // waits are bounded: a warp that has given up does not come.)
                 __threadfence();
                 warp_arrive(in_bar + 8 * x);
@@ -384,38 +387,45 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 if (!ok) break;
                 if (last_in[x]) {
                     __threadfence();
-                    // eight rows at a time, so that their loads are on their way together
-                    const int n_rows = min(tile_rows_tokens(o.q_per_kv), pc.r_rows - pc.token) * o.q_per_kv;
+                    // a thread to a row, 32 columns at a time: two pieces' loads are on their way together
 #pragma unroll 1
-                    for (int i0 = static_cast<int>(warp & 3u) * 8; i0 < n_rows; i0 += 32) {
-                        float jm[8], jl[8];
+                    for (int c = 0; c < 4 && exists; ++c) {
+                        float jm = -INFINITY, jl = 0.0f;
                         float4 acc[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) { jm[k] = -INFINITY; jl[k] = 0.0f; acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+                        for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
-                        for (int w = pc.run_lo; w <= pc.run_hi; ++w) {
-                            const int64_t at = (2 * static_cast<int64_t>(w) + (w == pc.run_lo ? pc.second : 0)) * kManyRows + x * 128 + i0;
-                            float2 ml[8];
-                            float4 v[8];
+                        for (int w0 = pc.run_lo; w0 <= pc.run_hi; w0 += 2) {
+                            float2 ml[2];
+                            float4 v[2][8];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const int64_t r = at + min(k, n_rows - 1 - i0);
-                                ml[k] = __ldcg(o.part_ml + r);
-                                v[k] = __ldcg(reinterpret_cast<const float4*>(o.part + r * kGroup) + lane);
+                            for (int k = 0; k < 2; ++k) {
+                                const int w = min(w0 + k, pc.run_hi);
+                                const int64_t slot = 2 * static_cast<int64_t>(w) + (w == pc.run_lo ? pc.second : 0);
+                                ml[k] = __ldcg(o.part_ml + slot * kManyRows + x * 128 + t);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[k][i] = __ldcg(sums_of(slot) + (8 * c + i) * 128);
                             }
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) join_sums(jm[k], jl[k], acc[k], ml[k], v[k]);
-                        }
+                            for (int k = 0; k < 2; ++k) {
+                                if (w0 + k > pc.run_hi) break;
+                                const float m0 = jm, l0 = jl;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            if (i0 + k >= n_rows) break;
-                            const int tile_token = (i0 + k) / o.q_per_kv, i_g = i0 + k - tile_token * o.q_per_kv;
-                            const int64_t to = static_cast<int64_t>(pc.r_row0 + pc.token + tile_token) * o.q_heads + (kv.head0 + pc.head) * o.q_per_kv + i_g;
-                            const float j_inv = inverse_of(jl[k]);
-                            reinterpret_cast<uint2*>(o.out + to * kGroup)[lane] =
-                                make_uint2(pack_h2(acc[k].x * j_inv, acc[k].y * j_inv), pack_h2(acc[k].z * j_inv, acc[k].w * j_inv));
-                            if (o.lse && lane == 0) o.lse[to] = lse_of(jm[k], jl[k], kManyWeightLog2);
+                                for (int i = 0; i < 8; ++i) {
+                                    jm = m0;
+                                    jl = l0;
+                                    join_sums(jm, jl, acc[i], ml[k], v[k][i]);
+                                }
+                            }
                         }
+                        const float j_inv = inverse_of(jl);
+                        uint4* const dst = reinterpret_cast<uint4*>(o.out + out_row * kGroup) + 4 * c;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 a = acc[2 * i], b = acc[2 * i + 1];
+                            dst[i] = make_uint4(pack_h2(a.x * j_inv, a.y * j_inv), pack_h2(a.z * j_inv, a.w * j_inv), pack_h2(b.x * j_inv, b.y * j_inv), pack_h2(b.z * j_inv, b.w * j_inv));
+                        }
+                        if (o.lse && c == 0) o.lse[out_row] = lse_of(jm, jl, kManyWeightLog2);
                     }
                 }
             }
