@@ -391,8 +391,9 @@ int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope_or_
 /* ecco_paged_attn over this cache: the same batch, flags, rows, bounds, in- and outputs and limits; so is what is said there of masks, of values that are
  * not finite and of arrays that are wrong.  Bytes 0x7f and 0xff (NaN), which ecco_paged8_append never writes, spoil the rows of the request and head that they
  * are in, where they lie within its length.  Weights enter the tensor cores as fp16 with 2^-11 of each, or 2^-30 of the largest product of a weight and
- * its block's 2^e.  A workspace that is smaller than ecco_paged8_attn_workspace_bytes, down to what that gives for n_kv_heads = 1, makes the call take
- * some heads at a time; 16-byte aligned; contents irrelevant before and undefined after; calls sharing a workspace must not overlap. */
+ * its block's 2^e.
+ * d_workspace: at least ecco_paged8_attn_workspace_bytes(...) bytes for the same arguments, whatever the lengths a few MB; 16-byte aligned, contents irrelevant
+ * before and undefined after; calls sharing a workspace must not overlap. */
 size_t ecco_paged8_attn_workspace_bytes(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv);
 int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q_fp16, int64_t q_stride, float scale,
                      uint32_t flags, void* d_out_fp16, float* d_lse_or_null, void* d_workspace, size_t workspace_bytes, void* stream);

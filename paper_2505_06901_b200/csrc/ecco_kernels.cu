@@ -30,7 +30,8 @@
 //   ecco_paged_kernels.cuh          paged KV cache: slots and block tables, pages into tiles, attention of few rows
 //   ecco_paged_many_kernel.cuh      attention of many rows over it, on tcgen05
 //   ecco_rope_kernels.cuh           rotary positions
-//   ecco_paged8_kernels.cuh         paged KV cache in 8 bits: append, pages into tiles, attention of few rows
+//   ecco_paged8_core.cuh            the format of a paged KV cache in 8 bits
+//   ecco_paged8_kernels.cuh         append to it, attention of few rows over it
 //   ecco_launch.cuh                 device query, overlapped launches, work plans
 //   this file                       the C ABI: argument checks and launches
 #include "ecco_device_core.cuh"
@@ -44,6 +45,7 @@
 #include "ecco_act2x_kernels.cuh"
 #include "ecco_kv_compress_kernel.cuh"
 #include "ecco_paged_kernels.cuh"
+#include "ecco_paged8_core.cuh"
 #include "ecco_paged_many_kernel.cuh"
 #include "ecco_rope_kernels.cuh"
 #include "ecco_paged8_kernels.cuh"
@@ -859,17 +861,19 @@ bool make_q_map(CUtensorMap* map, const PagedKv& kv, const PagedOut& o)
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<__half*>(o.q), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-int launch_paged_many(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
+// k_map, v_map: as the kernel has them
+template <bool k8>
+int launch_paged_many(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, int ctas, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t s)
 {
-    CUtensorMap map, q_map;
-    if (!make_tile_map(&map, kv) || !make_q_map(&q_map, kv, o)) return ECCO_ERR_CUDA;
+    CUtensorMap q_map;
+    if (!make_q_map(&q_map, kv, o)) return ECCO_ERR_CUDA;
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {
-        const int rc = set_smem(ecco_paged_many_kernel, kManySmemBytes);
+        const int rc = set_smem(ecco_paged_many_kernel<k8>, ManyShape<k8>::kBytes);
         if (rc) return rc;
         configured[di.device] = true;
     }
-    return launch_overlapped(ecco_paged_many_kernel, static_cast<unsigned>(p.many_ctas), static_cast<unsigned>(kManyThreads), kManySmemBytes, s, kv, o, sc, map, q_map);
+    return launch_overlapped(ecco_paged_many_kernel<k8>, static_cast<unsigned>(ctas), static_cast<unsigned>(ManyShape<k8>::kThreads), ManyShape<k8>::kBytes, s, kv, o, sc, k_map, v_map, q_map);
 }
 template <bool kScores>
 int launch_paged_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const PagedSchedule& sc, const PagedAttnPlan& p, cudaStream_t s)
@@ -1000,7 +1004,9 @@ extern "C" int ecco_paged_attn(const ecco_paged_cache* cache, const ecco_paged_b
             PagedOut many = o;
             many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
             many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
-            rc = launch_paged_many(di, kv, many, sc, p, s);
+            CUtensorMap map;
+            if (!make_tile_map(&map, kv)) return ECCO_ERR_CUDA;
+            rc = launch_paged_many<false>(di, kv, many, sc, p.many_ctas, map, map, s);
             if (rc) return rc;
             o.early = 1;
         }
@@ -1097,38 +1103,37 @@ namespace {
 // rows of a request up to which they go to ecco_paged8_few_kernel, sixteen at a time
 constexpr int kP8FewRows = 64;
 constexpr int kP8ByRequest = 2048;
-// Workspace of a launch over some KV heads, all offsets multiples of 256:
-//   tiles (for many rows) | schedule | few rows: tickets, sums, maxima | many rows: sums, maxima
+// Workspace, all offsets multiples of 256:
+//   schedule | few rows: tickets, sums, maxima | many rows: sums, maxima
 struct P8AttnPlan {
     bool many, line, by_request;       // there may be requests of more rows; more requests than the kernel for few rows schedules itself
     int few_ctas, many_ctas, max_blocks;
     size_t few_tiles, block_tiles, blocks, n_blocks, tickets, few_tickets, few_part, few_ml, many_part, many_ml, bytes;
 };
-P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int all_heads, int q_per_kv, int ctas_max)
+P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, int ctas_max)
 {
     P8AttnPlan p = {};
     const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
     p.many = rows > kP8FewRows;
     p.line = b.n_req > kP8Reqs;
     const int64_t groups = std::min<int64_t>((rows + kP8Rows16 - 1) / kP8Rows16, kP8FewRows / kP8Rows16);
-    p.by_request = static_cast<int64_t>(b.n_req) * all_heads <= ctas_max && b.max_kv <= kP8ByRequest;
-    p.few_ctas = p.by_request ? std::max(b.n_req, 1) * all_heads : std::max(1, spread_ctas((static_cast<int64_t>(b.max_tiles) * all_heads * std::max<int64_t>(groups, 1) + 7) / 8, ctas_max));
+    p.by_request = static_cast<int64_t>(b.n_req) * heads <= ctas_max && b.max_kv <= kP8ByRequest;
+    p.few_ctas = p.by_request ? std::max(b.n_req, 1) * heads : std::max(1, spread_ctas((static_cast<int64_t>(b.max_tiles) * heads * std::max<int64_t>(groups, 1) + 7) / 8, ctas_max));
     p.many_ctas = ctas_max;
     p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
-    size_t at = p.many ? static_cast<size_t>(std::max(b.max_tiles, 1)) * heads * 2 * kKvTileBytes : 0;
+    size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
         at = (at + bytes + 255) & ~static_cast<size_t>(255);
         return here;
     };
-    // room for the few rows of all heads: it does not depend on how many heads at a time the tiles are for
-    const size_t few_slots = static_cast<size_t>(ctas_max) * 2 * kP8Rows16, many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
+    const size_t few_slots = static_cast<size_t>(p.few_ctas) * 2 * kP8Rows16, many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
     p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
     p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
     p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
     p.n_blocks = take(8);
     p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
-    p.few_tickets = take(static_cast<size_t>(ctas_max) * kTicketStride * sizeof(Ticket));
+    p.few_tickets = take(static_cast<size_t>(p.few_ctas) * kTicketStride * sizeof(Ticket));
     p.few_part = take(few_slots * kGroup * sizeof(float));
     p.few_ml = take(few_slots * sizeof(float2));
     p.many_part = take(many_slots * kGroup * sizeof(float));
@@ -1136,24 +1141,27 @@ P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int all_heads,
     p.bytes = at;
     return p;
 }
-// a pool as [page][head][place][128 bytes]: a box is a page's part of a tile of 32 tokens
-bool make_p8_map(CUtensorMap* map, const PagedKv& kv, const uint8_t* pool)
+// a pool as [page][head][place][128 bytes]: a box is a page's part of a tile of some tokens
+bool make_p8_map(CUtensorMap* map, const PagedKv& kv, const uint8_t* pool, int tokens)
 {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
     const cuuint64_t page = 1ull << kv.page_shift;
     const cuuint64_t dims[4] = {kGroup, page, static_cast<cuuint64_t>(kv.all_heads), static_cast<cuuint64_t>(kv.n_pages)};
     const cuuint64_t strides[3] = {kGroup, kGroup * page, kGroup * page * kv.all_heads};
-    const cuuint32_t box[4] = {kGroup, static_cast<cuuint32_t>(std::min<cuuint64_t>(page, 32)), 1, 1};
+    const cuuint32_t box[4] = {kGroup, static_cast<cuuint32_t>(std::min<cuuint64_t>(page, static_cast<cuuint64_t>(tokens))), 1, 1};
     const cuuint32_t unit[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(pool), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-template <int kN>
-int launch_paged8_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const P8Few& f, int ctas, cudaStream_t s)
+// of K and of V, where the kernels use them
+bool make_p8_maps(CUtensorMap* k_map, CUtensorMap* v_map, const PagedKv& kv, int tokens)
 {
-    CUtensorMap k_map = {}, v_map = {};
-    if (kv.page_shift >= kP8SwizzledShift && (!make_p8_map(&k_map, kv, kv.k_blocks) || !make_p8_map(&v_map, kv, kv.v_blocks))) return ECCO_ERR_CUDA;
+    return kv.page_shift < kP8SwizzledShift || (make_p8_map(k_map, kv, kv.k_blocks, tokens) && make_p8_map(v_map, kv, kv.v_blocks, tokens));
+}
+template <int kN>
+int launch_paged8_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o, const P8Few& f, int ctas, const CUtensorMap& k_map, const CUtensorMap& v_map, cudaStream_t s)
+{
     static thread_local bool configured[64] = {};
     if (!configured[di.device]) {
         const int rc = set_smem(ecco_paged8_few_kernel<kN>, P8Smem<kN>::kBytes);
@@ -1174,7 +1182,7 @@ bool paged8_batch_fine(const ecco_paged8_cache& c, const ecco_paged_batch& b, in
 extern "C" size_t ecco_paged8_attn_workspace_bytes(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv)
 {
     if (!cache || !batch || cache->n_kv_heads < 1 || cache->n_kv_heads > 65535 || !paged8_batch_fine(*cache, *batch, q_per_kv)) return 0;
-    return paged8_attn_plan(*batch, cache->n_kv_heads, cache->n_kv_heads, q_per_kv, 256).bytes;
+    return paged8_attn_plan(*batch, cache->n_kv_heads, q_per_kv, 256).bytes;
 }
 
 extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q, int64_t q_stride, float scale,
@@ -1197,15 +1205,13 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
     rc = device_info(&di);
     if (rc) return rc;
     if (!d_workspace || !aligned16(d_workspace)) return d_workspace ? ECCO_ERR_ALIGNMENT : ECCO_ERR_WORKSPACE;
-    const int ctas = di.sms < 256 ? di.sms : 256, all_heads = cache->n_kv_heads;
-    int heads = all_heads;             // as many at a time as the workspace holds
-    while (heads > 0 && paged8_attn_plan(b, heads, all_heads, q_per_kv, ctas).bytes > workspace_bytes) --heads;
-    if (heads == 0) return ECCO_ERR_WORKSPACE;
+    const P8AttnPlan p = paged8_attn_plan(b, cache->n_kv_heads, q_per_kv, di.sms < 256 ? di.sms : 256);
+    if (workspace_bytes < p.bytes) return ECCO_ERR_WORKSPACE;
     PagedKv kv = {};
     kv.k_meta = cache->d_k_scales; kv.v_meta = cache->d_v_scales;
     kv.k_blocks = cache->d_k; kv.v_blocks = cache->d_v;
     kv.tables = b.d_block_tables; kv.cu_new = b.d_cu_new; kv.kv_lens = b.d_kv_lens; kv.kv_tiles = b.d_kv_tiles;
-    kv.n_pages = cache->n_pages; kv.page_shift = page_shift_of(cache->page_size); kv.all_heads = all_heads;
+    kv.n_pages = cache->n_pages; kv.page_shift = page_shift_of(cache->page_size); kv.all_heads = kv.heads = cache->n_kv_heads;
     kv.stride = b.table_stride; kv.n_req = b.n_req; kv.n_tokens = b.n_tokens; kv.max_tiles = std::max(b.max_tiles, 1);
     kv.max_new = b.max_new; kv.max_kv = b.max_kv;
     kv.staged = static_cast<uint8_t*>(d_workspace);
@@ -1215,11 +1221,8 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
     o.q_per_kv = q_per_kv; o.q_heads = q_heads; o.causal = flags & ECCO_ATTN_CAUSAL;
     o.out = static_cast<__half*>(d_out); o.lse = d_lse;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    P8AttnPlan p = {};
-    for (kv.head0 = 0; kv.head0 < all_heads; kv.head0 += kv.heads) {
-        kv.heads = std::min(heads, all_heads - kv.head0);
-        p = paged8_attn_plan(b, kv.heads, all_heads, q_per_kv, ctas);
-        if (!p.many && !p.line) break;
+    CUtensorMap k_map = {}, v_map = {};
+    if (p.many || p.line) {
         PagedSchedule sc = {};
         sc.few_tiles = reinterpret_cast<int32_t*>(kv.staged + p.few_tiles);
         sc.block_tiles = reinterpret_cast<int32_t*>(kv.staged + p.block_tiles);
@@ -1230,21 +1233,19 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
         sc.few_rows = kP8FewRows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
         sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
-        const int64_t units = p.many ? static_cast<int64_t>(b.max_tiles) * kv.heads : 0;
-        const unsigned grid = static_cast<unsigned>(spread_ctas(units / kP8StageWarps + 1, di.sms * 2));
-        rc = launch_overlapped(ecco_paged8_stage_kernel, grid, static_cast<unsigned>(kP8StageWarps * 32), 0, s, kv, o, sc, static_cast<int32_t>(p.many), static_cast<int32_t>(p.line));
+        rc = launch_overlapped(ecco_paged8_schedule_kernel, 1u, 32u, 0, s, kv, o, sc, static_cast<int32_t>(p.line));
         if (rc) return rc;
-        if (!p.many) break;
-        PagedOut many = o;
-        many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
-        many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
-        PagedAttnPlan as = {};
-        as.many_ctas = p.many_ctas;
-        rc = launch_paged_many(di, kv, many, sc, as, s);
-        if (rc) return rc;
+        if (p.many) {
+            PagedOut many = o;
+            many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
+            many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
+            if (!make_p8_maps(&k_map, &v_map, kv, kManyTokens)) return ECCO_ERR_CUDA;
+            rc = launch_paged_many<true>(di, kv, many, sc, p.many_ctas, k_map, v_map, s);
+            if (rc) return rc;
+            o.early = 1;
+        }
     }
-    kv.head0 = 0;
-    kv.heads = all_heads;
+    if (!make_p8_maps(&k_map, &v_map, kv, 32)) return ECCO_ERR_CUDA;
     P8Few f = {};
     f.line = p.line ? reinterpret_cast<const int32_t*>(kv.staged + p.few_tiles) : nullptr;
     f.few_rows = kP8FewRows;
@@ -1253,5 +1254,5 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
     f.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
     f.tickets = reinterpret_cast<Ticket*>(kv.staged + p.few_tickets);
     f.tag = next_ticket_tag();
-    return static_cast<int64_t>(b.max_new) * q_per_kv <= 8 ? launch_paged8_few<1>(di, kv, o, f, p.few_ctas, s) : launch_paged8_few<2>(di, kv, o, f, p.few_ctas, s);
+    return static_cast<int64_t>(b.max_new) * q_per_kv <= 8 ? launch_paged8_few<1>(di, kv, o, f, p.few_ctas, k_map, v_map, s) : launch_paged8_few<2>(di, kv, o, f, p.few_ctas, k_map, v_map, s);
 }

@@ -1,54 +1,8 @@
-// ecco_paged8_kernels.cuh -- K8: the paged KV cache in 8 bits: new tokens into blocks, pages into tiles, attention of few rows
+// ecco_paged8_kernels.cuh -- K8: the paged KV cache in 8 bits: new tokens into blocks, attention of few rows
 // Part of the one translation unit ecco_kernels.cu; included from there only.
 #pragma once
 
 namespace {
-
-// ---------------------------------------------------------------------------------------------
-// The cache: E4M3 numbers, and a power of two 2^e for each block of min(16, page size) places of a page and head.  With e in -15 .. 7 every
-// value is an fp16 number, so reading the cache rounds nothing; and a power of two that grows rounds only what becomes
-// subnormal.
-// ---------------------------------------------------------------------------------------------
-constexpr int kP8Lowest = -15, kP8Highest = 7;
-__device__ __forceinline__ int p8_exponent(uint32_t byte) { return min(max(static_cast<int>(byte) - 127, kP8Lowest), kP8Highest); }
-// two E4M3 numbers of the lower / upper half of a word -> fp16, exactly
-__device__ __forceinline__ uint32_t e4m3_low(uint32_t v)
-{
-    uint32_t r;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(v));
-    return r;
-}
-__device__ __forceinline__ uint32_t e4m3_high(uint32_t v)
-{
-    uint32_t r;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(v));
-    return r;
-}
-// four fp16 numbers -> E4M3, to nearest even, saturating
-__device__ __forceinline__ uint32_t to_e4m3(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f16x2 l, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 h, %2;\n\tmov.b32 %0, {l, h};\n\t}" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b)
-{
-    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-// 2^n twice as fp16, n in -24 .. 15
-__device__ __forceinline__ uint32_t power_h2(int n)
-{
-    const uint32_t h = n >= -14 ? static_cast<uint32_t>(n + 15) << 10 : 1u << (n + 24);
-    return h | (h << 16);
-}
-
-__device__ __forceinline__ uint4 lds_v4(uint32_t at)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
-}
 
 // ---------------------------------------------------------------------------------------------
 // K8a: new tokens into the cache.  A run is what a call brings for one block: rows one after the other whose slots ascend within
@@ -226,10 +180,6 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
     }
 }
 
-// ---------------------------------------------------------------------------------------------
-// K8s: the pages of requests of many rows into fp16 tiles, which ecco_paged_many_kernel reads (see K6s for their layout); the first CTA makes the
-// schedule.  A warp has a tile of K and of V: four tokens a load, 32 bytes of a piece a lane and store.
-// ---------------------------------------------------------------------------------------------
 // rows of a request that ecco_paged8_few_kernel takes together
 constexpr int kP8Rows16 = 16;
 __device__ __forceinline__ int32_t p8_row_groups(int64_t rows) { return static_cast<int32_t>((rows + kP8Rows16 - 1) / kP8Rows16); }
@@ -256,94 +206,34 @@ __device__ __forceinline__ void p8_empty_rows(const PagedKv& kv, const PagedOut&
         }
     }
 }
-constexpr int kP8StageWarps = 8;
-__global__ void __launch_bounds__(kP8StageWarps * 32, 2)
-ecco_paged8_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int32_t with_tiles,
-                         int32_t with_line)
+// K8s: by one warp, what the attention kernels need to know of a batch: the blocks of requests of many rows (paged_schedule) and, of more requests than
+// ecco_paged8_few_kernel keeps in shared memory, its line.
+__global__ void __launch_bounds__(32)
+ecco_paged8_schedule_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int32_t with_line)
 {
     constexpr unsigned full = 0xffffffffu;
-    __shared__ int32_t firsts[kStageTiles + 1];
-    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5), block_shift = min(4, kv.page_shift);
+    const int lane = static_cast<int>(threadIdx.x);
     release_dependents();
     dependency_wait();
-    fetch_firsts(kv, firsts);
     const int32_t T = paged_tiles(kv);
-    if (blockIdx.x == 0 && warp == 0) {
-        if (lane == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-        paged_schedule(kv, sc, o);
-        if (with_line) {                                   // more requests than ecco_paged8_few_kernel keeps in shared memory
-            int64_t line = 0;
-            const int64_t limit = p8_line_limit(T, sc.few_rows);
-            for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
-                PagedReq q = {};
-                if (r0 + lane < kv.n_req) q = paged_req(kv, r0 + lane, T);
-                int64_t upto = p8_line_tiles(q, o.q_per_kv, sc.few_rows);
-                p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows && q.kv == 0);
+    if (lane == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+    paged_schedule(kv, sc, o);
+    if (!with_line) return;
+    int64_t line = 0;
+    const int64_t limit = p8_line_limit(T, sc.few_rows);
+    for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
+        PagedReq q = {};
+        if (r0 + lane < kv.n_req) q = paged_req(kv, r0 + lane, T);
+        int64_t upto = p8_line_tiles(q, o.q_per_kv, sc.few_rows);
+        p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows && q.kv == 0);
 #pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int64_t x = __shfl_up_sync(full, upto, d);
-                    if (lane >= d) upto += x;
-                }
-                upto = min(line + upto, limit);
-                if (r0 + lane < kv.n_req) sc.few_tiles[r0 + lane + 1] = static_cast<int32_t>(upto);
-                line = __shfl_sync(full, upto, 31);
-            }
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t x = __shfl_up_sync(full, upto, d);
+            if (lane >= d) upto += x;
         }
-        return;
-    }
-    if (!with_tiles) return;                               // there is no room for any
-    const int64_t units = static_cast<int64_t>(T) * kv.heads, warps = static_cast<int64_t>(gridDim.x) * kP8StageWarps - 1;
-    for (int64_t u = static_cast<int64_t>(blockIdx.x) * kP8StageWarps + warp - 1; u < units; u += warps) {
-        const int32_t head = static_cast<int32_t>(divide(static_cast<uint64_t>(u), static_cast<uint64_t>(T))), tile = static_cast<int32_t>(u - static_cast<int64_t>(head) * T);
-        int32_t first;
-        const int r = request_of(kv, firsts, tile, first);
-        const PagedReq q = paged_req(kv, r, T);
-        // lane l: where token l is
-        const int64_t token = (static_cast<int64_t>(tile) - first) * 32 + lane, entry = token >> kv.page_shift;
-        int32_t page = -2;
-        if (token >= 0 && entry < kv.stride) page = __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + entry);     // whether or not it is needed
-        if (static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows) continue;
-        if (token < 0 || token >= q.kv) {
-            page = -1;
-        } else if (page < 0 || page >= kv.n_pages) {
-            atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-            page = -1;
-        }
-        const int64_t of_head = static_cast<int64_t>(max(page, 0)) * kv.all_heads + kv.head0 + head;
-        const int32_t place = static_cast<int32_t>(token & ((1 << kv.page_shift) - 1));
-        const int64_t at = (of_head << kv.page_shift) + place, of_scale = (of_head << (kv.page_shift - block_shift)) + (place >> block_shift);
-        uint32_t scale[2] = {127, 127};
-        if (page >= 0) { scale[0] = __ldcg(kv.k_meta + of_scale); scale[1] = __ldcg(kv.v_meta + of_scale); }
-        uint4 v[2][8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = 4 * i + (lane >> 3);
-            const int64_t from = __shfl_sync(full, at, t) * kGroup;
-            const bool there = __shfl_sync(full, page, t) >= 0;
-            v[0][i] = v[1][i] = make_uint4(0u, 0u, 0u, 0u);
-            if (there) {
-                v[0][i] = __ldcg(reinterpret_cast<const uint4*>(kv.k_blocks + from) + (lane & 7));
-                v[1][i] = __ldcg(reinterpret_cast<const uint4*>(kv.v_blocks + from) + (lane & 7));
-            }
-        }
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const uint32_t by_lane = power_h2(p8_exponent(scale[which]));
-            uint8_t* const dst = staged_tile(kv, which, head, tile) + (lane & 7) * kPieceBytes;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = 4 * i + (lane >> 3);
-                const uint32_t by = __shfl_sync(full, by_lane, t);
-                const uint32_t c[4] = {v[which][i].x, v[which][i].y, v[which][i].z, v[which][i].w};
-                uint32_t h[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { h[2 * j] = mul_h2(e4m3_low(c[j]), by); h[2 * j + 1] = mul_h2(e4m3_high(c[j]), by); }
-                const bool swapped = (t >> 2) & 1;
-                const uint32_t out[8] = {swapped ? h[4] : h[0], swapped ? h[5] : h[1], swapped ? h[6] : h[2], swapped ? h[7] : h[3],
-                                         swapped ? h[0] : h[4], swapped ? h[1] : h[5], swapped ? h[2] : h[6], swapped ? h[3] : h[7]};
-                stg_v8(dst + t * 32, out);
-            }
-        }
+        upto = min(line + upto, limit);
+        if (r0 + lane < kv.n_req) sc.few_tiles[r0 + lane + 1] = static_cast<int32_t>(upto);
+        line = __shfl_sync(full, upto, 31);
     }
 }
 
@@ -359,9 +249,6 @@ ecco_paged8_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 // Bound by memory: 256 bytes per token and KV head.
 // ---------------------------------------------------------------------------------------------
 constexpr int kP8Warps = 8, kP8Stages = 2, kP8Reqs = 512;
-// Pages of eight tokens and more come through tensor maps that swap the 16-byte pieces of a row by its number mod 8, so that neither operand's loads meet in a
-// bank; smaller ones as they are.
-constexpr int kP8SwizzledShift = 3;
 constexpr uint32_t kP8TileBytes = 32 * kGroup;             // of K or of V
 constexpr uint32_t kP8StageBytes = 2 * kP8TileBytes, kP8ScaleBytes = 32 * 16;          // beside it words that the blocks' powers of two are in, and where in these
 struct alignas(16) P8Piece { int64_t begin; int32_t units, head, row0, rows, group, valid; };
@@ -385,33 +272,6 @@ struct P8Few {
     Ticket* tickets;           // [CTA * kTicketStride]
     Ticket tag;
 };
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// more bytes to come before the barrier's phase is over, without an arrival
-__device__ __forceinline__ void mbar_expect_more(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-// a look that does not wait
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-// The first n (1 .. 4) bytes of a word global -> shared, the others zero; the barrier counts an arrival of this thread's when all such copies that it has
-// begun have come.
-__device__ __forceinline__ void copy_word(uint32_t dst, const uint8_t* src, int n)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void arrive_with_words(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
-// a 4-D tiled bulk load global -> shared through a tensor map (TMA)
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z),
-                 "r"(w), "r"(bar)
-                 : "memory");
-}
 // as mma_16816, for the compiler to place
 __device__ __forceinline__ void mma_h2(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -451,8 +311,10 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     }
     if (tid < kP8Warps * 2) pieces[tid].valid = 0;
     __syncthreads();
+    // Behind ecco_paged_many_kernel the wait comes at the end, on the conditions that stand at ecco_paged_few_kernel: what is read here was there before
+    // that kernel began, it is read through L2 alone, and neither writes what the other reads or writes.
+    if (!o.early) dependency_wait();
     release_dependents();
-    dependency_wait();
     const int32_t T = paged_tiles(kv);
     if (!f.line) {
         // the line: prefix sums over the requests, in rounds of a request per thread.  Mostly it is kv_tiles as it stands: no request that would
@@ -895,6 +757,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             }
         }
     }
+    if (o.early) dependency_wait();
     if (f.by_request) return;
     if (!spans[0].valid && !spans[1].valid) return;
     __threadfence();

@@ -26,11 +26,19 @@ namespace {
 // All blocks' tiles of all heads form one line, which is cut into equal runs, one per CTA (see paged_schedule).  A block that is cut leaves
 // its sums in the workspace, and whoever comes last joins them, in the order of the runs.
 // ---------------------------------------------------------------------------------------------
-constexpr int kManyThreads = 384;
 constexpr uint32_t kOperandBytes = 8 * 4096;               // eight pieces of [128][16] fp16, 32-byte swizzle
-constexpr int kManyStages = 5;                             // tiles of K and V in flight
-constexpr uint32_t kManySmemBytes = 1024 + (2 + kManyStages) * kOperandBytes;
-static_assert(kManySmemBytes <= kSmemCtaBytes, "fits an SM");
+// k8: K and V come as E4M3 numbers from the pages of a cache in 8 bits (ecco_paged8_kernels.cuh), and four more warps make the tiles of them, a thread to a token: 16
+// bytes of shared memory become 32, exactly, with the token's power of two multiplied in.  That costs no time beside the softmax (the tiles
+// made beforehand, in memory: 2 x 2048 tokens x 32 heads over 8000 tokens 23 us, a sixth of what 24 mixed requests took).
+constexpr uint32_t kCodeBytes = 128 * kGroup;              // an operand as E4M3 numbers
+constexpr int kCodeStages = 2;
+template <bool k8> struct ManyShape {
+    static constexpr int kThreads = k8 ? 512 : 384;
+    static constexpr int kStages = k8 ? 4 : 5;             // tiles of K and V in flight
+    static constexpr uint32_t kCodes = 1024 + (2 + kStages) * kOperandBytes, kWords = kCodes + kCodeStages * kCodeBytes;
+    static constexpr uint32_t kBytes = k8 ? kWords + kCodeStages * 128 * 8 : kCodes;
+    static_assert(kBytes <= kSmemCtaBytes, "fits an SM");
+};
 constexpr float kManyWeightLog2 = 7.0f, kLazyLog2 = 8.0f;
 
 // 3-D tiled bulk load global -> shared through a tensor map (TMA); what lies outside of the tensor reads as zero
@@ -190,13 +198,17 @@ struct ManyTask {
     int32_t run_lo, run_hi, second;    // the runs that have pieces of the block; the first of them has it in its second slot
 };
 
-__global__ void __launch_bounds__(kManyThreads, 1)
+// k_map: the tiles; k8: the pool of K
+template <bool k8>
+__global__ void __launch_bounds__(ManyShape<k8>::kThreads, 1)
 ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc,
-                       const __grid_constant__ CUtensorMap tile_map, const __grid_constant__ CUtensorMap q_map)
+                       const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap q_map)
 {
+    constexpr int kManyStages = ManyShape<k8>::kStages;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, base = smem_u32(smem);
     // barriers: tiles have come / are free again, Q there, S there, P there, O there
+    const uint32_t code_at = base + 80, code_free = code_at + 8 * kCodeStages;         // k8: numbers have come / have been read
     const uint32_t full_at = base, free_at = base + 8 * kManyStages, q_bar = base + 128, s_bar = base + 144, p_bar = base + 160 /* halves, tiles of rows */, o_bar = base + 192, q_free = base + 208, end_bar = base + 224, in_bar = base + 272, told_bar = base + 288;
     const uint32_t q_smem = base + 1024, ring = q_smem + 2 * kOperandBytes;
     uint32_t* const tmem_word = reinterpret_cast<uint32_t*>(smem + 256);
@@ -205,7 +217,9 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     static_assert(320 + 4 * sizeof(ManyTask) <= 1008, "tasks fit");
     volatile int* const last_in = reinterpret_cast<volatile int*>(smem + 1008);          // [tile of rows]
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kManyStages; ++i) { mbar_init(full_at + 8 * i, 1); mbar_init(free_at + 8 * i, 1); }
+        for (int i = 0; i < kManyStages; ++i) { mbar_init(full_at + 8 * i, k8 ? 4 : 1); mbar_init(free_at + 8 * i, 1); }
+        if (k8)
+            for (int i = 0; i < kCodeStages; ++i) { mbar_init(code_at + 8 * i, 33); mbar_init(code_free + 8 * i, 4); }
         for (int x = 0; x < 2; ++x) { mbar_init(q_bar + 8 * x, 1); mbar_init(q_free + 8 * x, 5); mbar_init(s_bar + 8 * x, 1); mbar_init(p_bar + 8 * x, 4); mbar_init(p_bar + 16 + 8 * x, 4); mbar_init(o_bar + 8 * x, 1); }
         for (int x = 0; x < 2; ++x) { mbar_init(in_bar + 8 * x, 4); mbar_init(told_bar + 8 * x, 1); }
         mbar_init(end_bar, 1);
@@ -240,9 +254,14 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         return false;
     };
 
-    // 384 threads x 168 registers = 128 x 40 + 256 x 232
-    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    // 384 threads x 168 registers = 128 x 40 + 256 x 232; 512 x 128 = 256 x 48 + 256 x 208
+    if (k8) {
+        if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    } else {
+        if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    }
     if (warp < 8) {
         // softmax: thread t of tile x holds row 128 x + t
         const uint32_t x = warp >> 2, t = threadIdx.x & 127u, s_at = tmem + ((warp & 3u) << 21) + x * 128, o_at = s_at + 256;
@@ -430,7 +449,102 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 }
             }
         }
-    } else if (warp == 8) {
+    } else if (k8 && warp == 8) {
+        // loads of E4M3 numbers, K and V by turns in the order in which they are used; a lane to a block of tokens that share a power of two.  The pages
+        // of a tile are looked up with the tile before it.
+        const int piece_shift = min(7, kv.page_shift), block_shift = min(4, kv.page_shift), n_scaled = 128 >> block_shift;
+        const int32_t in_page = (1 << kv.page_shift) - 1;
+        const int64_t n_scales = static_cast<int64_t>(kv.n_pages) * kv.all_heads << (kv.page_shift - block_shift);
+        int32_t* const lefts = reinterpret_cast<int32_t*>(smem + 112);
+        uint32_t n = 0;
+        bool ok = true;
+        for (int64_t u = u0; u < u1 && ok;) {
+            const ManyPiece pc = many_piece(sc, kv.heads, n_blocks, total, u, u1);
+            const PagedReq q = paged_req(kv, pc.r, T);
+            u = pc.next;
+            const int32_t head = kv.head0 + pc.head;
+            auto page_of = [&](int32_t j, int i) {         // -1: none, -2: there is nothing to look for
+                const int64_t token = static_cast<int64_t>(j) * kManyTokens + (i << block_shift), e = token >> kv.page_shift;
+                if (j >= pc.to || i >= n_scaled || token >= q.kv) return -2;
+                return e < kv.stride ? max(__ldcg(kv.tables + static_cast<int64_t>(pc.r) * kv.stride + e), -1) : -1;
+            };
+            int32_t page_next = page_of(pc.from, static_cast<int>(lane));
+            for (int32_t j = pc.from; j < pc.to && ok; ++j) {
+                const int32_t page_now = page_next;
+                page_next = page_of(j + 1, static_cast<int>(lane));
+                for (int which = 0; which < 2; ++which) {
+                    const uint32_t st = n % kCodeStages, bar = code_at + 8 * st;
+                    if (n >= kCodeStages) ok = wait(code_free + 8 * st, (n / kCodeStages - 1) & 1u);
+                    if (!ok) break;
+                    ++n;
+                    for (int i = static_cast<int>(lane); i < n_scaled; i += 32) {
+                        const int32_t page = i < 32 ? page_now : page_of(j, i), place = static_cast<int32_t>((static_cast<int64_t>(j) * kManyTokens + (i << block_shift)) & in_page);
+                        const uint32_t words = base + ManyShape<k8>::kWords + st * 128 * 8 + i * 8;
+                        if (page == -1 || page >= kv.n_pages) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+                        if (page < 0 || page >= kv.n_pages) {
+                            sts_v2(words, 127u, 0u);
+                            continue;
+                        }
+                        const int64_t of_head = static_cast<int64_t>(page) * kv.all_heads + head;
+                        if (((i << block_shift) & ((1 << piece_shift) - 1)) == 0) {
+                            const uint32_t to = base + ManyShape<k8>::kCodes + st * kCodeBytes + (i << (block_shift + 7)), bytes = 1u << (piece_shift + 7);
+                            mbar_expect_more(bar, bytes);
+                            if (kv.page_shift >= kP8SwizzledShift) tma_load_4d(to, which ? &v_map : &k_map, 0, place, head, page, bar);
+                            else bulk_g2s(to, (which ? kv.v_blocks : kv.k_blocks) + ((of_head << kv.page_shift) + place) * kGroup, bytes, bar);
+                        }
+                        const int64_t scale = (of_head << (kv.page_shift - block_shift)) + (place >> block_shift), word = scale & ~3ll;
+                        copy_word(words, (which ? kv.v_meta : kv.k_meta) + word, static_cast<int>(min(n_scales - word, static_cast<int64_t>(4))));
+                        sts_u32(words + 4, static_cast<uint32_t>(scale & 3) * 8);
+                    }
+                    arrive_with_words(bar);
+                    __syncwarp();
+                    if (lane == 0) {                       // and what has been written here
+                        lefts[st] = q.kv - j * kManyTokens;
+                        mbar_arrive(bar);
+                    }
+                }
+            }
+        }
+        if (!ok)                                           // what is on its way lands before the CTA leaves
+            for (uint32_t i = n < kCodeStages ? 0 : n - kCodeStages; i < n; ++i)
+                for (int k = 0; k < kWaitLimit && !mbar_try_wait(code_at + 8 * (i % kCodeStages), (i / kCodeStages) & 1u); ++k) {}
+    } else if (k8 && warp >= 12) {
+        // E4M3 numbers into operands: thread t has row t
+        const uint32_t t = threadIdx.x - 384u, block_shift = static_cast<uint32_t>(min(4, kv.page_shift)), swizzle = kv.page_shift >= kP8SwizzledShift ? t & 7u : 0u;
+        const uint32_t second = ((t >> 2) & 1u) << 4;      // the halves of a row's 32 bytes
+        const volatile int32_t* const lefts = reinterpret_cast<const volatile int32_t*>(smem + 112);
+        const int64_t n_all = 2 * (u1 - u0);
+        for (int64_t i = 0; i < n_all; ++i) {
+            const uint32_t n = static_cast<uint32_t>(i), cs = n % kCodeStages, st = n % kManyStages;
+            if (!wait(code_at + 8 * cs, (n / kCodeStages) & 1u)) break;
+            const uint32_t codes = base + ManyShape<k8>::kCodes + cs * kCodeBytes + t * kGroup, words = base + ManyShape<k8>::kWords + cs * 128 * 8 + (t >> block_shift) * 8;
+            const uint32_t to = ring + st * kOperandBytes + t * 32;
+            const bool there = static_cast<int32_t>(t) < lefts[cs];                 // else whatever is there: zeros, which any weight may meet
+            const uint32_t by = power_h2(p8_exponent((lds_u32(words) >> lds_u32(words + 4)) & 0xffu));
+            bool ok = true;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint4 x[4];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    x[d] = lds_v4(codes + (((half * 4 + d) ^ swizzle) << 4));
+                    if (!there) x[d] = make_uint4(0u, 0u, 0u, 0u);
+                }
+                if (half) warp_arrive(code_free + 8 * cs);                          // the numbers have been read
+                else if (n >= kManyStages) ok = wait(free_at + 8 * st, (n / kManyStages - 1) & 1u);
+                if (!ok) break;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const uint32_t row = to + (half * 4 + d) * 4096;
+                    sts_v4(row + second, mul_h2(e4m3_low(x[d].x), by), mul_h2(e4m3_high(x[d].x), by), mul_h2(e4m3_low(x[d].y), by), mul_h2(e4m3_high(x[d].y), by));
+                    sts_v4(row + (second ^ 16u), mul_h2(e4m3_low(x[d].z), by), mul_h2(e4m3_high(x[d].z), by), mul_h2(e4m3_low(x[d].w), by), mul_h2(e4m3_high(x[d].w), by));
+                }
+            }
+            if (!ok) break;
+            fence_async_smem();                            // for the tensor cores to see
+            warp_arrive(full_at + 8 * st);
+        }
+    } else if (!k8 && warp == 8) {
         // loads: K and V tiles in the order in which they are used
         uint32_t n = 0;
         bool ok = true;
@@ -447,7 +561,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                     if (lane == 0) {
                         mbar_expect_tx(bar, kOperandBytes);
                         // four tiles of 32 tokens, their pieces side by side; tiles that are not the request's are not used
-                        tma_load_3d(ring + st * kOperandBytes, &tile_map, 0, (which * kv.heads + pc.head) * kv.max_tiles + q.first + 4 * j, 0, bar);
+                        tma_load_3d(ring + st * kOperandBytes, &k_map, 0, (which * kv.heads + pc.head) * kv.max_tiles + q.first + 4 * j, 0, bar);
                     }
                     __syncwarp();
                 }
@@ -471,7 +585,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             const ManyTask* const pc = tasks + (n_q & 1) * 2;
             ++n_q;
             const bool two = same_in_warp(pc[1].used) != 0;
-            const int n_tiles = same_in_warp(pc->to - pc->from), steps_left = same_in_warp(max(pc->tiles - 4 * pc->from, 0) * 2);
+            const int n_tiles = same_in_warp(pc->to - pc->from), steps_left = k8 ? INT_MAX : same_in_warp(max(pc->tiles - 4 * pc->from, 0) * 2);       // k8: no rows but the request's, or zeros
             u += n_tiles;
             tmem_fence_after();
 #pragma unroll
@@ -484,7 +598,7 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             mma_commit(free_at + 8 * st);
             advance();
             for (int j = 0; j < n_tiles && ok; ++j) {
-                const int v_st = st, steps = min(steps_left - 8 * j, 8);        // sixteen tokens at a time, as far as there are tiles
+                const int v_st = st, steps = k8 ? 8 : min(steps_left - 8 * j, 8);        // sixteen tokens at a time, as far as there are tiles
                 const bool more = j + 1 < n_tiles;
                 ok = wait(full_at + 8 * st, turn & 1);
                 advance();

@@ -106,7 +106,7 @@ def test_every_bad_argument_is_refused_by_itself(B):
     assert L.ecco_paged8_attn(None, ctypes.byref(batch), 2, 512, 512, ctypes.c_float(0.1), 1, 1024, None, 2048, 1 << 30, None) == INV
     assert L.ecco_paged8_attn(c, None, 2, 512, 512, ctypes.c_float(0.1), 1, 1024, None, 2048, 1 << 30, None) == INV
     need = lambda heads, new, g: int(L.ecco_paged8_attn_workspace_bytes(cache(64, 64, 64, 64, heads), ctypes.byref(B.PagedBatch(64, 64, 64, 64, 4, 2, 99, new, 6000, 400)), g))  # noqa: E731
-    assert need(2, 1, 0) == 0 and 0 < need(2, 1, 1) < need(2, 90, 16) < need(8, 90, 16) and need(2, 90, 16) >= 400 * 2 * 2 * 8192
+    assert need(2, 1, 0) == 0 and 0 < need(2, 1, 1) < need(2, 90, 16) < 1 << 27
     assert need(0, 1, 1) == 0 and L.ecco_paged8_attn_workspace_bytes(None, ctypes.byref(batch), 2) == 0 and L.ecco_paged8_attn_workspace_bytes(c, None, 2) == 0
 
 
@@ -488,7 +488,7 @@ def test_q_that_is_not_finite_spoils_its_own_rows(B, dev, new):
 
 
 @pytest.mark.gpu
-def test_strided_q_and_a_small_workspace(B, dev):
+def test_strided_q_and_no_workspace(B, dev):
     for new, kv in (([1, 3], [300, 70]), ([50, 1, 70], [400, 300, 70])):
         c = Case(B, np.random.default_rng(new), new, kv, 4, 4, 16)
         out, lse = c.run()
@@ -497,15 +497,9 @@ def test_strided_q_and_a_small_workspace(B, dev):
         wide[:, :c.heads * c.g * 128] = c.q.reshape(c.tokens, -1)
         again, _ = c.run(q=wide, q_stride=wide.shape[1])
         assert torch.equal(out.view(torch.int16), again.view(torch.int16))
-        one = int(B.lib().ecco_paged8_attn_workspace_bytes(ctypes.byref(B.Paged8Cache(64, 64, 64, 64, 8, 1, 16)), ctypes.byref(c.batch), c.g))
-        few = [one, one + (c.need() - one) // 2, c.need()]
-        for n in few:                                      # some heads at a time
-            some, some_lse = c.run(ws_bytes=n)
-            c.check(some, some_lse)
-        if max(new) * c.g > 64:
-            with pytest.raises(B.EccoError) as e:
-                c.run(ws_bytes=256)
-            assert e.value.code == B.ERR_WORKSPACE
+        with pytest.raises(B.EccoError) as e:
+            c.run(ws_bytes=256)
+        assert e.value.code == B.ERR_WORKSPACE
         with pytest.raises(B.EccoError) as e:
             B.ecco_paged8_attn(c.cache, c.batch, c.g, c.q, c.heads * c.g * 128, 0.1, 0, torch.empty_like(c.q), None, None, 1 << 30)
         assert e.value.code == B.ERR_WORKSPACE
