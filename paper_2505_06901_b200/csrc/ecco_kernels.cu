@@ -1103,12 +1103,17 @@ namespace {
 // rows of a request up to which they go to ecco_paged8_few_kernel, sixteen at a time
 constexpr int kP8FewRows = 64;
 constexpr int kP8ByRequest = 2048;
+// Rows of a request from which on tiles of its pages in fp16 are made beforehand, if the workspace has room for them: every block of 256 rows reads
+// them again.
+constexpr int64_t kP8StagedRows = 2304;
+constexpr size_t kP8StagedMost = static_cast<size_t>(2) << 30;                   // more is not asked for
 // Workspace, all offsets multiples of 256:
-//   schedule | few rows: tickets, sums, maxima | many rows: sums, maxima
+//   schedule | few rows: tickets, sums, maxima | many rows: sums, maxima | tiles, if any
 struct P8AttnPlan {
     bool many, line, by_request;       // there may be requests of more rows; more requests than the kernel for few rows schedules itself
     int few_ctas, many_ctas, max_blocks;
     size_t few_tiles, block_tiles, blocks, n_blocks, tickets, few_tickets, few_part, few_ml, many_part, many_ml, bytes;
+    size_t tiles, bytes_with_tiles;    // the same as bytes where there are none
 };
 P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, int ctas_max)
 {
@@ -1127,18 +1132,20 @@ P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, 
         at = (at + bytes + 255) & ~static_cast<size_t>(255);
         return here;
     };
-    const size_t few_slots = static_cast<size_t>(p.few_ctas) * 2 * kP8Rows16, many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
+    const size_t few_slots = static_cast<size_t>(ctas_max) * 2 * kP8Rows16, many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
     p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
     p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
     p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
     p.n_blocks = take(8);
     p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
-    p.few_tickets = take(static_cast<size_t>(p.few_ctas) * kTicketStride * sizeof(Ticket));
+    p.few_tickets = take(static_cast<size_t>(ctas_max) * kTicketStride * sizeof(Ticket));
     p.few_part = take(few_slots * kGroup * sizeof(float));
     p.few_ml = take(few_slots * sizeof(float2));
     p.many_part = take(many_slots * kGroup * sizeof(float));
     p.many_ml = take(many_slots * sizeof(float2));
-    p.bytes = at;
+    p.tiles = p.bytes = p.bytes_with_tiles = at;
+    const size_t tiles = static_cast<size_t>(b.max_tiles) * heads * 2 * kKvTileBytes;
+    if (rows > kP8StagedRows && tiles <= kP8StagedMost) p.bytes_with_tiles = at + tiles;
     return p;
 }
 // a pool as [page][head][place][128 bytes]: a box is a page's part of a tile of some tokens
@@ -1182,7 +1189,7 @@ bool paged8_batch_fine(const ecco_paged8_cache& c, const ecco_paged_batch& b, in
 extern "C" size_t ecco_paged8_attn_workspace_bytes(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv)
 {
     if (!cache || !batch || cache->n_kv_heads < 1 || cache->n_kv_heads > 65535 || !paged8_batch_fine(*cache, *batch, q_per_kv)) return 0;
-    return paged8_attn_plan(*batch, cache->n_kv_heads, q_per_kv, 256).bytes;
+    return paged8_attn_plan(*batch, cache->n_kv_heads, q_per_kv, 256).bytes_with_tiles;
 }
 
 extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q, int64_t q_stride, float scale,
@@ -1233,14 +1240,25 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
         sc.few_rows = kP8FewRows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
         sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
-        rc = launch_overlapped(ecco_paged8_schedule_kernel, 1u, 32u, 0, s, kv, o, sc, static_cast<int32_t>(p.line));
+        const bool tiles = p.bytes_with_tiles > p.bytes && p.bytes_with_tiles <= workspace_bytes;
+        PagedKv staged = kv;
+        staged.staged = kv.staged + p.tiles;
+        const unsigned grid = tiles ? static_cast<unsigned>(spread_ctas(static_cast<int64_t>(b.max_tiles) * kv.heads / kP8StageWarps + 1, di.sms * 2)) : 1u;
+        rc = launch_overlapped(ecco_paged8_stage_kernel, grid, tiles ? static_cast<unsigned>(kP8StageWarps * 32) : 32u, 0, s, staged, o, sc, static_cast<int32_t>(tiles),
+                               static_cast<int32_t>(p.line));
         if (rc) return rc;
         if (p.many) {
             PagedOut many = o;
             many.part = reinterpret_cast<float*>(kv.staged + p.many_part);
             many.part_ml = reinterpret_cast<float2*>(kv.staged + p.many_ml);
-            if (!make_p8_maps(&k_map, &v_map, kv, kManyTokens)) return ECCO_ERR_CUDA;
-            rc = launch_paged_many<true>(di, kv, many, sc, p.many_ctas, k_map, v_map, s);
+            if (tiles) {
+                CUtensorMap map;
+                if (!make_tile_map(&map, staged)) return ECCO_ERR_CUDA;
+                rc = launch_paged_many<false>(di, staged, many, sc, p.many_ctas, map, map, s);
+            } else {
+                if (!make_p8_maps(&k_map, &v_map, kv, kManyTokens)) return ECCO_ERR_CUDA;
+                rc = launch_paged_many<true>(di, kv, many, sc, p.many_ctas, k_map, v_map, s);
+            }
             if (rc) return rc;
             o.early = 1;
         }

@@ -206,34 +206,98 @@ __device__ __forceinline__ void p8_empty_rows(const PagedKv& kv, const PagedOut&
         }
     }
 }
-// K8s: by one warp, what the attention kernels need to know of a batch: the blocks of requests of many rows (paged_schedule) and, of more requests than
+// K8s: by the first warp, what the attention kernels need to know of a batch: the blocks of requests of many rows (paged_schedule) and, of more requests than
 // ecco_paged8_few_kernel keeps in shared memory, its line.
-__global__ void __launch_bounds__(32)
-ecco_paged8_schedule_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int32_t with_line)
+// with_tiles: the others bring the pages of the requests of many rows into fp16 tiles, which ecco_paged_many_kernel reads as it does those of K6s.  A warp has
+// a tile of K and of V: four tokens a load, 32 bytes of a piece a lane and store.
+constexpr int kP8StageWarps = 8;
+__global__ void __launch_bounds__(kP8StageWarps * 32, 2)
+ecco_paged8_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ PagedSchedule sc, int32_t with_tiles,
+                         int32_t with_line)
 {
     constexpr unsigned full = 0xffffffffu;
-    const int lane = static_cast<int>(threadIdx.x);
+    __shared__ int32_t firsts[kStageTiles + 1];
+    const int lane = static_cast<int>(threadIdx.x & 31u), warp = static_cast<int>(threadIdx.x >> 5), block_shift = min(4, kv.page_shift);
     release_dependents();
     dependency_wait();
+    fetch_firsts(kv, firsts);
     const int32_t T = paged_tiles(kv);
-    if (lane == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-    paged_schedule(kv, sc, o);
-    if (!with_line) return;
-    int64_t line = 0;
-    const int64_t limit = p8_line_limit(T, sc.few_rows);
-    for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
-        PagedReq q = {};
-        if (r0 + lane < kv.n_req) q = paged_req(kv, r0 + lane, T);
-        int64_t upto = p8_line_tiles(q, o.q_per_kv, sc.few_rows);
-        p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows && q.kv == 0);
+    if (blockIdx.x == 0 && warp == 0) {
+        if (lane == 0 && __ldcg(kv.kv_tiles + kv.n_req) > kv.max_tiles) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+        paged_schedule(kv, sc, o);
+        if (with_line) {                                   // more requests than ecco_paged8_few_kernel keeps in shared memory
+            int64_t line = 0;
+            const int64_t limit = p8_line_limit(T, sc.few_rows);
+            for (int r0 = 0; r0 < kv.n_req; r0 += 32) {
+                PagedReq q = {};
+                if (r0 + lane < kv.n_req) q = paged_req(kv, r0 + lane, T);
+                int64_t upto = p8_line_tiles(q, o.q_per_kv, sc.few_rows);
+                p8_empty_rows(kv, o, q, q.rows > 0 && static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows && q.kv == 0);
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t x = __shfl_up_sync(full, upto, d);
-            if (lane >= d) upto += x;
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int64_t x = __shfl_up_sync(full, upto, d);
+                    if (lane >= d) upto += x;
+                }
+                upto = min(line + upto, limit);
+                if (r0 + lane < kv.n_req) sc.few_tiles[r0 + lane + 1] = static_cast<int32_t>(upto);
+                line = __shfl_sync(full, upto, 31);
+            }
         }
-        upto = min(line + upto, limit);
-        if (r0 + lane < kv.n_req) sc.few_tiles[r0 + lane + 1] = static_cast<int32_t>(upto);
-        line = __shfl_sync(full, upto, 31);
+        return;
+    }
+    if (!with_tiles) return;                               // there is no room for any
+    const int64_t units = static_cast<int64_t>(T) * kv.heads, warps = static_cast<int64_t>(gridDim.x) * kP8StageWarps - 1;
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * kP8StageWarps + warp - 1; u < units; u += warps) {
+        const int32_t head = static_cast<int32_t>(divide(static_cast<uint64_t>(u), static_cast<uint64_t>(T))), tile = static_cast<int32_t>(u - static_cast<int64_t>(head) * T);
+        int32_t first;
+        const int r = request_of(kv, firsts, tile, first);
+        const PagedReq q = paged_req(kv, r, T);
+        // lane l: where token l is
+        const int64_t token = (static_cast<int64_t>(tile) - first) * 32 + lane, entry = token >> kv.page_shift;
+        int32_t page = -2;
+        if (token >= 0 && entry < kv.stride) page = __ldcg(kv.tables + static_cast<int64_t>(r) * kv.stride + entry);     // whether or not it is needed
+        if (static_cast<int64_t>(q.rows) * o.q_per_kv <= sc.few_rows) continue;
+        if (token < 0 || token >= q.kv) {
+            page = -1;
+        } else if (page < 0 || page >= kv.n_pages) {
+            atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+            page = -1;
+        }
+        const int64_t of_head = static_cast<int64_t>(max(page, 0)) * kv.all_heads + kv.head0 + head;
+        const int32_t place = static_cast<int32_t>(token & ((1 << kv.page_shift) - 1));
+        const int64_t at = (of_head << kv.page_shift) + place, of_scale = (of_head << (kv.page_shift - block_shift)) + (place >> block_shift);
+        uint32_t scale[2] = {127, 127};
+        if (page >= 0) { scale[0] = __ldcg(kv.k_meta + of_scale); scale[1] = __ldcg(kv.v_meta + of_scale); }
+        uint4 v[2][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int t = 4 * i + (lane >> 3);
+            const int64_t from = __shfl_sync(full, at, t) * kGroup;
+            const bool there = __shfl_sync(full, page, t) >= 0;
+            v[0][i] = v[1][i] = make_uint4(0u, 0u, 0u, 0u);
+            if (there) {
+                v[0][i] = __ldcg(reinterpret_cast<const uint4*>(kv.k_blocks + from) + (lane & 7));
+                v[1][i] = __ldcg(reinterpret_cast<const uint4*>(kv.v_blocks + from) + (lane & 7));
+            }
+        }
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const uint32_t by_lane = power_h2(p8_exponent(scale[which]));
+            uint8_t* const dst = staged_tile(kv, which, head, tile) + (lane & 7) * kPieceBytes;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = 4 * i + (lane >> 3);
+                const uint32_t by = __shfl_sync(full, by_lane, t);
+                const uint32_t c[4] = {v[which][i].x, v[which][i].y, v[which][i].z, v[which][i].w};
+                uint32_t h[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { h[2 * j] = mul_h2(e4m3_low(c[j]), by); h[2 * j + 1] = mul_h2(e4m3_high(c[j]), by); }
+                const bool swapped = (t >> 2) & 1;
+                const uint32_t out[8] = {swapped ? h[4] : h[0], swapped ? h[5] : h[1], swapped ? h[6] : h[2], swapped ? h[7] : h[3],
+                                         swapped ? h[0] : h[4], swapped ? h[1] : h[5], swapped ? h[2] : h[6], swapped ? h[3] : h[7]};
+                stg_v8(dst + t * 32, out);
+            }
+        }
     }
 }
 

@@ -28,8 +28,8 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 constexpr uint32_t kOperandBytes = 8 * 4096;               // eight pieces of [128][16] fp16, 32-byte swizzle
 // k8: K and V come as E4M3 numbers from the pages of a cache in 8 bits (ecco_paged8_kernels.cuh), and four more warps make the tiles of them, a thread to a token: 16
-// bytes of shared memory become 32, exactly, with the token's power of two multiplied in.  That costs no time beside the softmax (the tiles
-// made beforehand, in memory: 2 x 2048 tokens x 32 heads over 8000 tokens 23 us, a sixth of what 24 mixed requests took).
+// bytes of shared memory become 32, exactly, with the token's power of two multiplied in.  With 64 KB more through shared memory, whose pipe is busy for two
+// thirds of the time as it is, a tile of tokens takes a sixth longer; tiles made beforehand (K8s) cost as much as nine blocks lose by that.
 constexpr uint32_t kCodeBytes = 128 * kGroup;              // an operand as E4M3 numbers
 constexpr int kCodeStages = 2;
 template <bool k8> struct ManyShape {
@@ -519,17 +519,17 @@ ecco_paged_many_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             if (!wait(code_at + 8 * cs, (n / kCodeStages) & 1u)) break;
             const uint32_t codes = base + ManyShape<k8>::kCodes + cs * kCodeBytes + t * kGroup, words = base + ManyShape<k8>::kWords + cs * 128 * 8 + (t >> block_shift) * 8;
             const uint32_t to = ring + st * kOperandBytes + t * 32;
-            const bool there = static_cast<int32_t>(t) < lefts[cs];                 // else whatever is there: zeros, which any weight may meet
+            const int32_t left = lefts[cs];                // tokens that there are; behind them zeros, which any weight may meet
             const uint32_t by = power_h2(p8_exponent((lds_u32(words) >> lds_u32(words + 4)) & 0xffu));
             bool ok = true;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint4 x[4];
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    x[d] = lds_v4(codes + (((half * 4 + d) ^ swizzle) << 4));
-                    if (!there) x[d] = make_uint4(0u, 0u, 0u, 0u);
-                }
+                for (int d = 0; d < 4; ++d) x[d] = lds_v4(codes + (((half * 4 + d) ^ swizzle) << 4));
+                if (left < 128 && static_cast<int32_t>(t) >= left)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) x[d] = make_uint4(0u, 0u, 0u, 0u);
                 if (half) warp_arrive(code_free + 8 * cs);                          // the numbers have been read
                 else if (n >= kManyStages) ok = wait(free_at + 8 * st, (n / kManyStages - 1) & 1u);
                 if (!ok) break;

@@ -106,7 +106,7 @@ def test_every_bad_argument_is_refused_by_itself(B):
     assert L.ecco_paged8_attn(None, ctypes.byref(batch), 2, 512, 512, ctypes.c_float(0.1), 1, 1024, None, 2048, 1 << 30, None) == INV
     assert L.ecco_paged8_attn(c, None, 2, 512, 512, ctypes.c_float(0.1), 1, 1024, None, 2048, 1 << 30, None) == INV
     need = lambda heads, new, g: int(L.ecco_paged8_attn_workspace_bytes(cache(64, 64, 64, 64, heads), ctypes.byref(B.PagedBatch(64, 64, 64, 64, 4, 2, 99, new, 6000, 400)), g))  # noqa: E731
-    assert need(2, 1, 0) == 0 and 0 < need(2, 1, 1) < need(2, 90, 16) < 1 << 27
+    assert need(2, 1, 0) == 0 and 0 < need(2, 1, 1) < need(2, 90, 16) < 1 << 27 and need(2, 145, 16) >= need(2, 90, 16) + 400 * 2 * 2 * 8192
     assert need(0, 1, 1) == 0 and L.ecco_paged8_attn_workspace_bytes(None, ctypes.byref(batch), 2) == 0 and L.ecco_paged8_attn_workspace_bytes(c, None, 2) == 0
 
 
@@ -503,6 +503,22 @@ def test_strided_q_and_no_workspace(B, dev):
         with pytest.raises(B.EccoError) as e:
             B.ecco_paged8_attn(c.cache, c.batch, c.g, c.q, c.heads * c.g * 128, 0.1, 0, torch.empty_like(c.q), None, None, 1 << 30)
         assert e.value.code == B.ERR_WORKSPACE
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("page", [1, 4, 16, 64, 256])
+def test_a_long_prompt_with_and_without_room_for_its_tiles(B, dev, page, causal):
+    """2304 rows of a request are the last for which no tiles are made beforehand, where there is room for them."""
+    c = Case(B, np.random.default_rng([page, causal]), [288, 289, 1, 577], [1000, 289, 130, 700], 2, 8, page)
+    least = int(B.lib().ecco_paged8_attn_workspace_bytes(ctypes.byref(c.cache), ctypes.byref(c.make_batch(*c.arrays, max_tiles=0)), c.g))
+    assert least < c.need() == int(B.lib().ecco_paged8_attn_workspace_bytes(ctypes.byref(c.cache), ctypes.byref(c.batch), c.g))
+    for n in (c.need(), c.need() - 1, least):
+        out, lse = c.run(causal, ws_bytes=n)
+        c.check(out, lse, causal)
+    with pytest.raises(B.EccoError) as e:
+        c.run(causal, ws_bytes=least // 4)             # the sizes are for up to 256 SMs
+    assert e.value.code == B.ERR_WORKSPACE
 
 
 @pytest.mark.gpu
