@@ -729,3 +729,106 @@ def test_steps_of_a_server(B, dev, page, rot, flags):
                     tol = np.expm1(2 * d_s)[:, None] * (p @ np.abs(v)) * (1 + 2.0**-4) + p @ (np.abs(v) * 2.0**-4 + 2.0**-15) + 2e-3
                     assert np.all(np.abs(got - p @ v) <= tol)
             first += k
+
+
+# ------------------------------------------------------------------ the far ends
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(B, dev):
+    """Pools of 6.4 GB each: the last pages and the first."""
+    rng = np.random.default_rng(41)
+    page, heads, g, pages = 32, 2, 4, 780_000
+    codes = [torch.empty((pages, heads, page, 128), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.empty((pages, heads, 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = B.paged8_cache(codes[0], codes[1], scales[0], scales[1], pages, heads, page)
+    kv, new = [100, 70, 33], [1, 70, 5]
+    tables = np.array([[pages - 1, 0, pages - 2, 524_288], [pages - 3, 1, 655_360, -1], [2, pages - 4, -1, -1]], np.int32)
+    rows = sum(kv)
+    k, v = (rng.standard_normal((rows, heads, 128)).astype(np.float16) for _ in range(2))
+    slots = [int(tables[r, t // page]) * page + t % page for r, n in enumerate(kv) for t in range(n)]
+    d = torch.from_numpy(np.stack([k, v])).cuda()
+    B.ecco_paged8_append(cache, None, None, d[0], d[1], heads * 128, ints(slots), rows)
+    small = [[np.zeros((8, heads, page, 128), np.uint8), np.zeros((8, heads, 2), np.uint8)] for _ in range(2)]
+    names = sorted({int(p) for r, n in enumerate(kv) for p in tables[r, :-(-n // page)]})
+    local = [names.index(s // page) * page + s % page for s in slots]
+    for i, x in enumerate((k, v)):
+        small[i][0] = np.zeros((len(names), heads, page, 128), np.uint8)
+        small[i][1] = np.zeros((len(names), heads, 2), np.uint8)
+        append_reference(*small[i], x, local, page)
+        here = codes[i][torch.tensor(names, device="cuda")].cpu().numpy()
+        taken = np.zeros((len(names), page), bool)
+        for s in local:
+            taken[s // page, s % page] = True
+        assert np.array_equal(here.transpose(0, 2, 1, 3)[taken], small[i][0].transpose(0, 2, 1, 3)[taken])
+    cu, tiles = np.concatenate([[0], np.cumsum(new)]), np.concatenate([[0], np.cumsum([-(-n // 32) for n in kv])])
+    batch = B.paged_batch(ints(tables), 4, ints(cu), ints(kv), ints(tiles), 3, sum(new), max(new), max(kv), int(tiles[-1]))
+    q = torch.from_numpy(rng.standard_normal((sum(new), heads * g, 128)).astype(np.float16)).cuda()
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    ws = torch.empty(B.ecco_paged8_attn_workspace_bytes(cache, batch, g), dtype=torch.uint8, device="cuda")
+    B.ecco_paged8_attn(cache, batch, g, q, heads * g * 128, 128**-0.5, B.ATTN_CAUSAL, out, lse, ws, len(ws))
+    c = Case.__new__(Case)
+    c.B, c.new, c.kv, c.heads, c.g, c.page, c.tables, c.cu, c.q = B, new, kv, heads, g, page, tables, cu, q
+    c.pools = [codes[0], scales[0], codes[1], scales[1]]
+    c.check(out, lse)
+
+
+@pytest.mark.gpu
+def test_a_replay_after_one_with_wrong_arrays(B, dev):
+    """What a call with arrays that cannot be leaves in the workspace does not change what the same graph computes afterwards."""
+    for new in (1, 40):
+        c = Case(B, np.random.default_rng([new, 51]), [new] * 5, [700, 650, 900, 40, 800], 4, 4, 16, padding=0)
+        out, lse = torch.zeros_like(c.q), torch.zeros(c.q.shape[:2], device="cuda")
+        ws = torch.empty(c.need(), dtype=torch.uint8, device="cuda")
+        call = lambda: B.ecco_paged8_attn(c.cache, c.batch, c.g, c.q, c.heads * c.g * 128, 128**-0.5, B.ATTN_CAUSAL, out, lse, ws, len(ws))  # noqa: E731
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        good = [a.clone() for a in c.arrays]
+        for which, at, value in ((3, 2, 0), (2, 1, 10_000), (1, 3, -5), (3, 5, 1 << 20), (0, 0, 1 << 30)):
+            c.arrays[which].view(-1)[at] = value
+            graph.replay()
+            assert B.ecco_device_status() == B.ERR_INVALID_ARG, (which, at)
+            c.arrays[which].copy_(good[which])
+            out.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            c.check(out, lse)
+
+
+@pytest.mark.gpu
+def test_calls_behind_one_another(B, dev):
+    """Turned, appended and attended to many times without a pause: each kernel begins while the one in front ends."""
+    rng = np.random.default_rng(61)
+    heads, g, page, n, steps = 2, 4, 16, 7, 40
+    rope = B.ecco_rope_init(128, 10000.0 ** (-np.arange(64) / 64))
+    stride, pages = 8, n * 8
+    tables = np.arange(pages).reshape(n, stride)[:, ::-1].astype(np.int32).copy()
+    qkv = rng.standard_normal((steps, n, heads * (g + 2), 128)).astype(np.float16)
+    row = heads * (g + 2) * 128
+
+    def serve(wait):
+        codes = [torch.full((pages, heads, page, 128), 127, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        scales = [torch.zeros((pages, heads, 1), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        cache = B.paged8_cache(codes[0], codes[1], scales[0], scales[1], pages, heads, page)
+        d, outs = torch.from_numpy(qkv).cuda(), []
+        arrays = [[ints(tables), ints(np.arange(n + 1)), ints([s + 1] * n), ints(np.arange(n + 1) * (s // 32 + 1))] for s in range(steps)]
+        slots = [ints([int(tables[r, s // page]) * page + s % page for r in range(n)]) for s in range(steps)]
+        positions = [ints([s] * n) for s in range(steps)]
+        batches = [B.paged_batch(a[0], stride, a[1], a[2], a[3], n, n, 1, steps, n * 2) for a in arrays]
+        ws = torch.empty(B.ecco_paged8_attn_workspace_bytes(cache, batches[0], g), dtype=torch.uint8, device="cuda")
+        outs = [torch.zeros((n, heads * g, 128), dtype=torch.float16, device="cuda") for _ in range(steps)]
+        torch.cuda.synchronize()
+        for s in range(steps):
+            at = d[s].data_ptr()
+            for call in (lambda: B.ecco_rope_apply(rope, positions[s], n, heads * g, d[s], row, d[s], row),
+                         lambda: B.ecco_paged8_append(cache, rope, positions[s], at + heads * g * 256, at + heads * (g + 1) * 256, row, slots[s], n),
+                         lambda: B.ecco_paged8_attn(cache, batches[s], g, d[s], row, 128**-0.5, B.ATTN_CAUSAL, outs[s], None, ws, len(ws))):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return [*codes, *scales, *outs]
+
+    for a, b in zip(serve(False), serve(True)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
