@@ -798,13 +798,13 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     const unsigned ahead = valid & ((1u << lane) - 1u);
     const int64_t of_ahead = __shfl_sync(full, of_lane, ahead ? 31 - __clz(ahead) : 0);
     unsigned firsts = __ballot_sync(full, (valid >> lane & 1u) && (!ahead || of_ahead != of_lane));
-    while (firsts) {
+    for (uint32_t first_row = warp; firsts; first_row ^= kP8Warps / 2) {               // pieces of few rows one after the other go to other warps
         const int i = __ffs(firsts) - 1;
         firsts &= firsts - 1u;
         const unsigned members = valid & ~((1u << i) - 1u) & (firsts ? (1u << (__ffs(firsts) - 1)) - 1u : full);
         const P8Piece p = pieces[i];
         const int R = min(p.rows * o.q_per_kv - p.group * kP8Rows16, kN * 8);
-        for (int row = static_cast<int>(warp); row < R; row += kP8Warps) {
+        for (int row = static_cast<int>(first_row); row < R; row += kP8Warps) {
             float m = -INFINITY, l = 0.0f;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             for (unsigned left = members; left; left &= left - 1u) {
@@ -824,19 +824,19 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     if (o.early) dependency_wait();
     if (f.by_request) return;
     if (!spans[0].valid && !spans[1].valid) return;
-    __threadfence();
     __syncthreads();
     if (tid < 2) {
         const P8Span sp = spans[tid];
+        __threadfence();                                   // what all threads have written before the barrier
         joins[tid] = sp.valid && take_ticket(f.tickets + static_cast<int64_t>(sp.lo) * kTicketStride) == static_cast<unsigned>(sp.hi - sp.lo);
+        __threadfence();
     }
     __syncthreads();
     for (int i = 0; i < 2; ++i) {
         if (!joins[i]) continue;
-        __threadfence();
         const P8Span sp = spans[i];
         const int R = min(sp.rows * o.q_per_kv - sp.group * kP8Rows16, kN * 8);
-        for (int row = static_cast<int>(warp); row < R; row += kP8Warps) {
+        for (int row = static_cast<int>(warp ^ (i ? kP8Warps / 2 : 0)); row < R; row += kP8Warps) {
             float m = -INFINITY, l = 0.0f;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             for (int b0 = sp.lo; b0 <= sp.hi; b0 += 4) {   // four pieces on their way together
