@@ -1102,9 +1102,14 @@ extern "C" int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rop
 namespace {
 // rows of a request up to which they go to ecco_paged8_few_kernel, sixteen at a time
 constexpr int kP8FewRows = 64;
-constexpr int kP8ByRequest = 2048;
+// CTAs for few rows.  One to a request and head, so that no sums pass through memory, where there are at most as many and they have few tiles (2
+// requests of 300 / 780 / 2000 tokens, 8 heads: 7.6 / 9.8 / 15.7 us, with equal parts of the line of four tiles or more 8.2 / 8.7 / 10.1), or where they fill the machine
+// anyway (16 of 1500 to 2000 tokens, 8 heads 20.5 / 22.2).  Else equal parts, of four tiles at least (2 requests of 780, of two, four, eight: 9.8 / 8.7 / 11.0), and
+// not so small that one request's sums come from more than 32 CTAs (one head of 16000 tokens, from 32, 64: 14.2 / 17.3).
+constexpr int kP8OneCtaTiles = 16, kP8CtaTiles = 4, kP8JoinCtas = 32;
 // Rows of a request from which on tiles of its pages in fp16 are made beforehand, if the workspace has room for them: every block of 256 rows reads
-// them again.
+// them again.  Beforehand / in the kernel: 4 requests, 8 heads over 4096 tokens, 512 rows each 86 / 65 us, 1200 rows 137 / 141, 2308 rows 200 / 218; 2 of 8192
+// rows 310 / 346; 8 of 4800 rows over 3000 tokens 511 / 639.
 constexpr int64_t kP8StagedRows = 2304;
 constexpr size_t kP8StagedMost = static_cast<size_t>(2) << 30;                   // more is not asked for
 // Workspace, all offsets multiples of 256:
@@ -1122,8 +1127,10 @@ P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, 
     p.many = rows > kP8FewRows;
     p.line = b.n_req > kP8Reqs;
     const int64_t groups = std::min<int64_t>((rows + kP8Rows16 - 1) / kP8Rows16, kP8FewRows / kP8Rows16);
-    p.by_request = static_cast<int64_t>(b.n_req) * heads <= ctas_max && b.max_kv <= kP8ByRequest;
-    p.few_ctas = p.by_request ? std::max(b.n_req, 1) * heads : std::max(1, spread_ctas((static_cast<int64_t>(b.max_tiles) * heads * std::max<int64_t>(groups, 1) + 7) / 8, ctas_max));
+    const int64_t tiles_of_one = (static_cast<int64_t>(b.max_kv) + 31) / 32 * std::max<int64_t>(groups, 1), units = static_cast<int64_t>(b.max_tiles) * heads * std::max<int64_t>(groups, 1);
+    p.by_request = static_cast<int64_t>(b.n_req) * heads <= ctas_max && (tiles_of_one <= kP8OneCtaTiles || tiles_of_one * ctas_max * 3 <= units * 4);
+    const int64_t per_cta = std::max<int64_t>(kP8CtaTiles, tiles_of_one / kP8JoinCtas);
+    p.few_ctas = p.by_request ? std::max(b.n_req, 1) * heads : std::max(1, spread_ctas((units + per_cta - 1) / per_cta, ctas_max));
     p.many_ctas = ctas_max;
     p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
     size_t at = 0;

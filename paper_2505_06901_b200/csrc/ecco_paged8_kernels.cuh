@@ -839,18 +839,18 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         for (int row = static_cast<int>(warp ^ (i ? kP8Warps / 2 : 0)); row < R; row += kP8Warps) {
             float m = -INFINITY, l = 0.0f;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int b0 = sp.lo; b0 <= sp.hi; b0 += 4) {   // four pieces on their way together
-                float2 x[4];
-                float4 y[4];
+            for (int b0 = sp.lo; b0 <= sp.hi; b0 += 8) {   // eight pieces on their way together
+                float2 x[8];
+                float4 y[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 8; ++k) {
                     const int b = min(b0 + k, sp.hi);
                     const int64_t from = (static_cast<int64_t>(b) * 2 + (sp.begin < cta_split.begin(b) ? 0 : 1)) * kP8Rows16 + row;
                     x[k] = __ldcg(f.part_ml + from);
                     y[k] = __ldcg(reinterpret_cast<const float4*>(f.part + from * kGroup) + lane);
                 }
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < 8; ++k)
                     if (b0 + k <= sp.hi) join_sums(m, l, v, x[k], y[k]);
             }
             write_row(sp.group, sp.row0, sp.head, row, m, l, v);
