@@ -1061,6 +1061,18 @@ static int check_paged8_cache(const ecco_paged8_cache* c)
     return ECCO_OK;
 }
 
+// rows of new tokens as [token][head][128]: a box is a run's
+static bool make_rows_map(CUtensorMap* map, const P8Append& p, const __half* rows)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {kGroup, static_cast<cuuint64_t>(p.heads), static_cast<cuuint64_t>(p.n_tokens)};
+    const cuuint64_t strides[2] = {kGroup * 2, static_cast<cuuint64_t>(p.token_stride) * 2};
+    const cuuint32_t box[3] = {kGroup, 1, kP8Rows};
+    const cuuint32_t unit[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<__half*>(rows), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 template <bool kTurn>
 static int launch_paged8_append(const DeviceInfo& di, const ecco_rope& rope, const P8Append& p, int64_t ctas, cudaStream_t s)
 {
@@ -1070,7 +1082,9 @@ static int launch_paged8_append(const DeviceInfo& di, const ecco_rope& rope, con
         if (rc) return rc;
         configured[di.device] = true;
     }
-    return launch_overlapped(ecco_paged8_append_kernel<kTurn>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8AppendThreads), kP8AppendSmemBytes, s, rope, p);
+    CUtensorMap k_map, v_map;
+    if (!make_rows_map(&k_map, p, p.k) || !make_rows_map(&v_map, p, p.v)) return ECCO_ERR_CUDA;
+    return launch_overlapped(ecco_paged8_append_kernel<kTurn>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8AppendThreads), kP8AppendSmemBytes, s, rope, p, k_map, v_map);
 }
 extern "C" int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope, const int32_t* d_positions, const void* d_k, const void* d_v,
                                   int64_t token_stride, const int32_t* d_slots, int32_t n_tokens, void* stream)

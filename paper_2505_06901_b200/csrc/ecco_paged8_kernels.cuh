@@ -24,7 +24,7 @@ struct P8Append {
 
 template <bool kTurn>
 __global__ void __launch_bounds__(kP8AppendThreads, 2)
-ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_constant__ P8Append p)
+ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_constant__ P8Append p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     constexpr unsigned full = 0xffffffffu;
@@ -59,15 +59,20 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
         it.l0 = __ffs(it.left) - 1;
         it.n = min(run_end(it.l0) - it.l0, kP8Rows);
     };
-    auto source = [&](const Item& it) {
-        const int head = it.of_run < first_v ? it.of_run : it.of_run - first_v;
-        return (it.of_run < first_v ? p.k : p.v) + (static_cast<int64_t>(window) * kP8Rows - 1 + it.l0) * p.token_stride + static_cast<int64_t>(head) * kGroup;
-    };
+    // A whole run comes by one copy of sixteen rows, a shorter one row by row: a copy takes ten instructions to issue, whatever its size.
+    const int32_t row0 = window * kP8Rows - 1;
     auto fetch = [&](const Item& it, uint32_t stage) {
         if (!it.left) return;
-        if (lane == 0) mbar_expect_tx(bar + stage * 8, it.n * kGroup * 2);
+        const bool is_v = it.of_run >= first_v;
+        const int head = it.of_run - (is_v ? first_v : 0);
+        const uint32_t to = rows_at + stage * kP8RunBytes, b = bar + stage * 8;
+        if (lane == 0) mbar_expect_tx(b, it.n * kGroup * 2);
         __syncwarp();
-        if (lane < it.n) bulk_g2s(rows_at + stage * kP8RunBytes + lane * kGroup * 2, source(it) + lane * p.token_stride, kGroup * 2, bar + stage * 8);
+        if (it.n == kP8Rows) {
+            if (lane == 0) tma_load_3d(to, is_v ? &v_map : &k_map, 0, head, row0 + it.l0, b);
+        } else if (lane < it.n) {
+            bulk_g2s(to + lane * kGroup * 2, (is_v ? p.v : p.k) + (static_cast<int64_t>(row0) + it.l0 + lane) * p.token_stride + static_cast<int64_t>(head) * kGroup, kGroup * 2, b);
+        }
     };
     Item now = {starts, part * kP8AppendWarps + warp, 0, 0};
     open(now);
@@ -113,7 +118,7 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
                 v[i][1] = lds_v4(from + piece.y * 16);
             }
         }
-        uint32_t top = 0;                                  // largest magnitudes, as bits of two fp16 numbers
+        __half2 top = __floats2half2_rn(0.0f, 0.0f);       // largest magnitudes; NaN if there is one
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (4 * i >= n) break;
@@ -124,11 +129,15 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
             }
             const uint32_t* const w = reinterpret_cast<const uint32_t*>(v[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = __vmaxu2(top, w[j] & 0x7fff7fffu);
+            for (int j = 0; j < 8; ++j) top = __hmax2_nan(top, __habs2(*reinterpret_cast<const __half2*>(&w[j])));
         }
-        uint32_t largest = __reduce_max_sync(full, max(top & 0xffffu, top >> 16));
+        auto bits_of = [](__half2 v) {
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(&v);
+            return max(u & 0xffffu, u >> 16);
+        };
+        uint32_t largest = __reduce_max_sync(full, bits_of(top));
         if (largest > 0x7c00u) {                           // NaN becomes zero
-            top = 0;
+            top = __floats2half2_rn(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t* const w = reinterpret_cast<uint32_t*>(v[i]);
@@ -136,10 +145,10 @@ ecco_paged8_append_kernel(const __grid_constant__ ecco_rope rope, const __grid_c
                 for (int j = 0; j < 8; ++j) {
                     const __half2 h = *reinterpret_cast<const __half2*>(&w[j]);
                     w[j] &= __heq2_mask(h, h);
-                    top = __vmaxu2(top, w[j] & 0x7fff7fffu);
+                    top = __hmax2(top, __habs2(*reinterpret_cast<const __half2*>(&w[j])));
                 }
             }
-            largest = __reduce_max_sync(full, max(top & 0xffffu, top >> 16));
+            largest = __reduce_max_sync(full, bits_of(top));
         }
         // 448 is 1.75 times a power of two: a larger mantissa (above 0x300) needs the next one
         e = min(max(static_cast<int>((largest + 0xffu) >> 10) - 23, kP8Lowest), kP8Highest);

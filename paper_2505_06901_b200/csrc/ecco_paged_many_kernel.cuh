@@ -41,13 +41,6 @@ template <bool k8> struct ManyShape {
 };
 constexpr float kManyWeightLog2 = 7.0f, kLazyLog2 = 8.0f;
 
-// 3-D tiled bulk load global -> shared through a tensor map (TMA); what lies outside of the tensor reads as zero
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x),
-                 "r"(y), "r"(z), "r"(bar)
-                 : "memory");
-}
 __device__ __forceinline__ void tmem_ld32(uint32_t* r, uint32_t at)
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
