@@ -414,8 +414,10 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             const int64_t limit = p8_line_limit(T, f.few_rows);
             for (int r0 = 0; r0 < kv.n_req; r0 += kP8Threads) {
                 const int r = r0 + tid;
-                q = {};
-                if (r < kv.n_req) q = paged_req(kv, r, T);
+                if (kv.n_req > kP8Threads) {               // else it is at hand
+                    q = {};
+                    if (r < kv.n_req) q = paged_req(kv, r, T);
+                }
                 if ((q.cut || q.rows > kv.max_new) && blockIdx.x == 0) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
                 int64_t upto = p8_line_tiles(q, o.q_per_kv, f.few_rows);
 #pragma unroll
