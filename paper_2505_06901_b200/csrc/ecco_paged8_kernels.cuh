@@ -815,20 +815,30 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         const unsigned members = valid & ~((1u << i) - 1u) & (firsts ? (1u << (__ffs(firsts) - 1)) - 1u : full);
         const P8Piece p = pieces[i];
         const int R = min(p.rows * o.q_per_kv - p.group * kP8Rows16, kN * 8);
-        for (int row = static_cast<int>(first_row); row < R; row += kP8Warps) {
-            float m = -INFINITY, l = 0.0f;
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (unsigned left = members; left; left &= left - 1u) {
-                const int j = __ffs(left) - 1;
-                const uint8_t* const from = j & 1 ? smem + Smem::kRing + (j >> 1) * kP8Stages * kP8StageBytes : smem + Smem::kFirst + (j >> 1) * Smem::kPieceBytes;
-                join_sums(m, l, v, ml[j * kRows + row], reinterpret_cast<const float4*>(from)[row * 32 + lane]);
+        // a warp's rows, of which there are one or two, side by side
+        float m[kN], l[kN];
+        float4 v[kN];
+#pragma unroll
+        for (int n = 0; n < kN; ++n) { m[n] = -INFINITY; l[n] = 0.0f; v[n] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+        for (unsigned left = static_cast<int>(first_row) < R ? members : 0u; left; left &= left - 1u) {
+            const int j = __ffs(left) - 1;
+            const uint8_t* const from = j & 1 ? smem + Smem::kRing + (j >> 1) * kP8Stages * kP8StageBytes : smem + Smem::kFirst + (j >> 1) * Smem::kPieceBytes;
+#pragma unroll
+            for (int n = 0; n < kN; ++n) {
+                const int row = min(static_cast<int>(first_row) + n * kP8Warps, R - 1);
+                join_sums(m[n], l[n], v[n], ml[j * kRows + row], reinterpret_cast<const float4*>(from)[row * 32 + lane]);
             }
+        }
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+            const int row = static_cast<int>(first_row) + n * kP8Warps;
+            if (row >= R) break;
             if (p.begin >= c0 && p.begin + p.units <= c1) {
-                write_row(p.group, p.row0, p.head, row, m, l, v);
+                write_row(p.group, p.row0, p.head, row, m[n], l[n], v[n]);
             } else {
                 const int64_t to = (static_cast<int64_t>(blockIdx.x) * 2 + (p.begin < c0 ? 0 : 1)) * kP8Rows16 + row;
-                reinterpret_cast<float4*>(f.part + to * kGroup)[lane] = v;
-                if (lane == 0) f.part_ml[to] = make_float2(m, l);
+                reinterpret_cast<float4*>(f.part + to * kGroup)[lane] = v[n];
+                if (lane == 0) f.part_ml[to] = make_float2(m[n], l[n]);
             }
         }
     }
@@ -847,25 +857,33 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         if (!joins[i]) continue;
         const P8Span sp = spans[i];
         const int R = min(sp.rows * o.q_per_kv - sp.group * kP8Rows16, kN * 8);
-        for (int row = static_cast<int>(warp ^ (i ? kP8Warps / 2 : 0)); row < R; row += kP8Warps) {
-            float m = -INFINITY, l = 0.0f;
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int b0 = sp.lo; b0 <= sp.hi; b0 += 8) {   // eight pieces on their way together
-                float2 x[8];
-                float4 y[8];
+        const int first_row = static_cast<int>(warp ^ (i ? kP8Warps / 2 : 0));
+        float m[kN], l[kN];
+        float4 v[kN];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int b = min(b0 + k, sp.hi);
-                    const int64_t from = (static_cast<int64_t>(b) * 2 + (sp.begin < cta_split.begin(b) ? 0 : 1)) * kP8Rows16 + row;
-                    x[k] = __ldcg(f.part_ml + from);
-                    y[k] = __ldcg(reinterpret_cast<const float4*>(f.part + from * kGroup) + lane);
+        for (int n = 0; n < kN; ++n) { m[n] = -INFINITY; l[n] = 0.0f; v[n] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+        for (int b0 = sp.lo; b0 <= sp.hi && first_row < R; b0 += 8) {                  // eight pieces on their way together
+            float2 x[8][kN];
+            float4 y[8][kN];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int b = min(b0 + k, sp.hi);
+#pragma unroll
+                for (int n = 0; n < kN; ++n) {
+                    const int64_t from = (static_cast<int64_t>(b) * 2 + (sp.begin < cta_split.begin(b) ? 0 : 1)) * kP8Rows16 + min(first_row + n * kP8Warps, R - 1);
+                    x[k][n] = __ldcg(f.part_ml + from);
+                    y[k][n] = __ldcg(reinterpret_cast<const float4*>(f.part + from * kGroup) + lane);
                 }
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (b0 + k <= sp.hi) join_sums(m, l, v, x[k], y[k]);
             }
-            write_row(sp.group, sp.row0, sp.head, row, m, l, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (b0 + k <= sp.hi)
+#pragma unroll
+                    for (int n = 0; n < kN; ++n) join_sums(m[n], l[n], v[n], x[k][n], y[k][n]);
         }
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+            if (first_row + n * kP8Warps < R) write_row(sp.group, sp.row0, sp.head, first_row + n * kP8Warps, m[n], l[n], v[n]);
         if (tid == 0) *(f.tickets + static_cast<int64_t>(sp.lo) * kTicketStride) = 0;
     }
 }
