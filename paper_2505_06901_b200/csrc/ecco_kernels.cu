@@ -1196,7 +1196,7 @@ int launch_paged8_few(const DeviceInfo& di, const PagedKv& kv, const PagedOut& o
         if (rc) return rc;
         configured[di.device] = true;
     }
-    return launch_overlapped(ecco_paged8_few_kernel<kN>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8Warps * 32), P8Smem<kN>::kBytes, s, kv, o, f, k_map, v_map);
+    return launch_overlapped(ecco_paged8_few_kernel<kN>, static_cast<unsigned>(ctas), static_cast<unsigned>(kP8Threads), P8Smem<kN>::kBytes, s, kv, o, f, k_map, v_map);
 }
 // the part of the batch's checks that ecco_paged_attn has: the pages are the same
 bool paged8_batch_fine(const ecco_paged8_cache& c, const ecco_paged_batch& b, int q_per_kv)

@@ -321,7 +321,7 @@ ecco_paged8_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 // Pieces of a request that lie in several warps of a CTA are joined in shared memory, those in several CTAs by the CTA that comes last, in their order.
 // Bound by memory: 256 bytes per token and KV head.
 // ---------------------------------------------------------------------------------------------
-constexpr int kP8Warps = 8, kP8Stages = 2, kP8Reqs = 512;
+constexpr int kP8Warps = 8, kP8Loaders = 4, kP8Threads = (kP8Warps + kP8Loaders) * 32, kP8Stages = 2, kP8Reqs = 512;
 constexpr uint32_t kP8TileBytes = 32 * kGroup;             // of K or of V
 constexpr uint32_t kP8StageBytes = 2 * kP8TileBytes, kP8ScaleBytes = 32 * 16;          // beside it words that the blocks' powers of two are in, and where in these
 struct alignas(16) P8Piece { int64_t begin; int32_t units, head, row0, rows, group, valid; };
@@ -330,7 +330,8 @@ struct P8Span { int64_t begin; int32_t units, head, row0, rows, group, valid, lo
 template <int kN> struct P8Smem {
     static constexpr int kWarps = kP8Warps;
     static constexpr uint32_t kPieceBytes = kN * 8 * kGroup * 4;                  // sums of a piece
-    static constexpr uint32_t kPieces = kWarps * kP8Stages * 8, kSpans = kPieces + kWarps * 2 * sizeof(P8Piece), kMl = kSpans + 128;
+    // barriers: a warp's tiles have come, are free again
+    static constexpr uint32_t kFree = kWarps * kP8Stages * 8, kPieces = 2 * kFree, kSpans = kPieces + kWarps * 2 * sizeof(P8Piece), kMl = kSpans + 128;
     static constexpr uint32_t kLists = kMl + kWarps * 2 * kN * 8 * 8, kListBytes = 4 * (kP8Reqs + 4) * 4;          // the line, lengths, first rows and rows of the requests
     static constexpr uint32_t kScales = (kLists + kListBytes + 15) / 16 * 16, kFirst = kScales + kWarps * kP8Stages * kP8ScaleBytes;
     static constexpr uint32_t kRing = (kFirst + kWarps * kPieceBytes + 1023) / 1024 * 1024, kBytes = kRing + kWarps * kP8Stages * kP8StageBytes;
@@ -361,13 +362,13 @@ __device__ __forceinline__ uint32_t turn_8x8(uint32_t v)
 
 // kN: eight rows each, of a piece
 template <int kN>
-__global__ void __launch_bounds__(kP8Warps * 32, 1)
+__global__ void __launch_bounds__(kP8Threads, 1)
 ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant__ PagedOut o, const __grid_constant__ P8Few f, const __grid_constant__ CUtensorMap k_map,
                        const __grid_constant__ CUtensorMap v_map)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     using Smem = P8Smem<kN>;
-    constexpr int kP8Threads = kP8Warps * 32, kRows = kN * 8;
+    constexpr int kRows = kN * 8;
     constexpr unsigned full = 0xffffffffu;
     const int tid = static_cast<int>(threadIdx.x);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3u, base = smem_u32(smem);
@@ -380,7 +381,8 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     int64_t* const sums = reinterpret_cast<int64_t*>(smem + Smem::kFirst);                 // before there are pieces
     const int piece_shift = min(5, kv.page_shift), block_shift = min(4, kv.page_shift), n_blocks = 32 >> block_shift;      // of a tile
     if (tid < kP8Warps * kP8Stages) {
-        mbar_init(base + tid * 8, n_blocks);
+        mbar_init(base + tid * 8, 2 * min(n_blocks, 16));
+        mbar_init(base + Smem::kFree + tid * 8, 1);
     }
     if (tid < kP8Warps * 2) pieces[tid].valid = 0;
     __syncthreads();
@@ -487,57 +489,88 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         p.end = min(p.begin + p.units, stop);
         p.tile = off - at;
     };
+    const int32_t in_page = (1 << kv.page_shift) - 1;
+    if (warp >= kP8Warps) {
+        // Loads: half a warp to a warp's ring, a lane to a block or two of a tile.  A tile's pages are looked up with the tile before it; nothing else from memory
+        // passes through registers on its way.  384 threads x 168 registers = 128 x 72 + 256 x 216.  (Each warp with its own loads, half of a tile's 2400 clocks
+        // went into these; one warp with all of them came too late: 8 requests of 4050 tokens, 32 heads 59 and 62 us.)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        const int w = static_cast<int>(warp - kP8Warps) * 2 + static_cast<int>(lane >> 4), j = static_cast<int>(lane & 15u);
+        const uint32_t full_at = base + w * kP8Stages * 8, free_at = full_at + Smem::kFree, ring = base + Smem::kRing + w * kP8Stages * kP8StageBytes;
+        const uint32_t scales = base + Smem::kScales + w * kP8Stages * kP8ScaleBytes;
+        const int64_t n_scales = static_cast<int64_t>(kv.n_pages) * kv.all_heads << (kv.page_shift - block_shift);
+        const int64_t stop = j < n_blocks ? c0 + split.begin(w + 1) : 0;
+        Place p = {};
+        p.u = j < n_blocks ? c0 + split.begin(w) : 0;
+        seek(p, stop);
+        // the page of a block of the tile that p is at: -1: none, -2: there is nothing to look for
+        auto page_of = [&](int i) {
+            const int32_t token = p.tile * 32 + (i << block_shift), e = token >> kv.page_shift;
+            if (p.u >= stop || token >= p.kv) return -2;
+            return e < kv.stride ? max(__ldcg(kv.tables + static_cast<int64_t>(p.r) * kv.stride + e), -1) : -1;
+        };
+        int32_t page_next = page_of(j);
+        uint32_t n = 0;
+        int idle = 0;
+        while (__any_sync(full, p.u < stop)) {
+            const uint32_t stage = n % kP8Stages;
+            const bool go = p.u < stop && (n < kP8Stages || mbar_test(free_at + stage * 8, (n / kP8Stages - 1) & 1u));
+            if (go) {
+                const uint32_t b = full_at + stage * 8;
+                auto ask = [&](int i, int32_t page) {
+                    const uint32_t words = scales + stage * kP8ScaleBytes + i * 16;
+                    if (page == -1 || page >= kv.n_pages) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
+                    if (page < 0 || page >= kv.n_pages) {  // nobody sees the block, or what is seen is unspecified
+                        sts_v4(words, 127u, 127u, 0u, 0u);
+                        return;
+                    }
+                    const int32_t head = kv.head0 + p.head, place = (p.tile * 32 + (i << block_shift)) & in_page;
+                    const int64_t of_head = static_cast<int64_t>(page) * kv.all_heads + head;
+                    if (((i << block_shift) & ((1 << piece_shift) - 1)) == 0) {
+                        const uint32_t to = ring + stage * kP8StageBytes + (i << (block_shift + 7)), bytes = 1u << (piece_shift + 7);
+                        mbar_expect_more(b, 2 * bytes);
+                        if (kv.page_shift >= kP8SwizzledShift) {
+                            tma_load_4d(to, &k_map, 0, place, head, page, b);
+                            tma_load_4d(to + kP8TileBytes, &v_map, 0, place, head, page, b);
+                        } else {
+                            const int64_t from = ((of_head << kv.page_shift) + place) * kGroup;
+                            bulk_g2s(to, kv.k_blocks + from, bytes, b);
+                            bulk_g2s(to + kP8TileBytes, kv.v_blocks + from, bytes, b);
+                        }
+                    }
+                    const int64_t scale = (of_head << (kv.page_shift - block_shift)) + (place >> block_shift), word = scale & ~3ll;
+                    const int there = static_cast<int>(min(n_scales - word, static_cast<int64_t>(4)));
+                    copy_word(words, kv.k_meta + word, there);
+                    copy_word(words + 4, kv.v_meta + word, there);
+                    sts_u32(words + 8, static_cast<uint32_t>(scale & 3) * 8);
+                };
+                ask(j, page_next);
+                if (j + 16 < n_blocks) ask(j + 16, page_of(j + 16));   // pages of one token
+                arrive_with_words(b);
+                mbar_arrive(b);                            // and with what has been written here
+                ++n;
+                ++p.tile;
+                if (++p.u == p.end) seek(p, stop);
+                page_next = page_of(j);
+            }
+            idle = __any_sync(full, go) ? 0 : idle + 1;
+            if (idle > kWaitLimit) {                       // a warp has given up: what is on its way lands before the CTA leaves
+                if (lane == 0) atomicExch(&g_device_status, ECCO_ERR_DEVICE_TIMEOUT);
+                for (uint32_t i = n < kP8Stages ? 0 : n - kP8Stages; i < n; ++i)
+                    for (int k = 0; k < kWaitLimit && !mbar_test(full_at + (i % kP8Stages) * 8, (i / kP8Stages) & 1u); ++k) {}
+                break;
+            }
+        }
+        return;
+    }
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kP8Warps * 32) : "memory"); };          // the warps with tiles, without those that load them
     const uint32_t bar = base + warp * kP8Stages * 8, ring = base + Smem::kRing + warp * kP8Stages * kP8StageBytes;
     const uint32_t scales = base + Smem::kScales + warp * kP8Stages * kP8ScaleBytes, swizzle = kv.page_shift >= kP8SwizzledShift ? 7u : 0u;
     const int64_t u0 = c0 + split.begin(static_cast<int>(warp)), u1 = c0 + split.begin(static_cast<int>(warp) + 1);
-    const int64_t n_scales = static_cast<int64_t>(kv.n_pages) * kv.all_heads << (kv.page_shift - block_shift);
-    const int32_t in_page = (1 << kv.page_shift) - 1, my_token = static_cast<int32_t>(lane << block_shift);
-    Place load = {};
-    load.u = u0;
-    seek(load, u1);
-    Place at = load;
-    // Loads: a lane to a block.  A tile's pages are looked up with the tile before it; nothing else from memory passes through registers on its way.
-    auto page_of = [&]() {                                 // -1: none, -2: there is nothing to look for
-        const int32_t token = load.tile * 32 + my_token, e = token >> kv.page_shift;
-        if (load.u >= u1 || my_token >= 32 || token >= load.kv) return -2;
-        return e < kv.stride ? max(__ldcg(kv.tables + static_cast<int64_t>(load.r) * kv.stride + e), -1) : -1;
-    };
-    int32_t page = page_of();
-    auto ask = [&](uint32_t stage) {
-        if (load.u >= u1) return;
-        if (my_token < 32) {
-            const uint32_t b = bar + stage * 8, words = scales + stage * kP8ScaleBytes + lane * 16;
-            if (page == -1 || page >= kv.n_pages) atomicExch(&g_device_status, ECCO_ERR_INVALID_ARG);
-            if (page < 0 || page >= kv.n_pages) {          // nobody sees the block, or what is seen is unspecified
-                sts_v4(words, 127u, 127u, 0u, 0u);
-            } else {
-                const int32_t head = kv.head0 + load.head, place = (load.tile * 32 + my_token) & in_page;
-                const int64_t of_head = static_cast<int64_t>(page) * kv.all_heads + head;
-                if ((my_token & ((1 << piece_shift) - 1)) == 0) {
-                    const uint32_t to = ring + stage * kP8StageBytes + (lane << (block_shift + 7)), bytes = 1u << (piece_shift + 7);
-                    mbar_expect_more(b, 2 * bytes);
-                    if (kv.page_shift >= kP8SwizzledShift) {
-                        tma_load_4d(to, &k_map, 0, place, head, page, b);
-                        tma_load_4d(to + kP8TileBytes, &v_map, 0, place, head, page, b);
-                    } else {
-                        const int64_t from = ((of_head << kv.page_shift) + place) * kGroup;
-                        bulk_g2s(to, kv.k_blocks + from, bytes, b);
-                        bulk_g2s(to + kP8TileBytes, kv.v_blocks + from, bytes, b);
-                    }
-                }
-                const int64_t scale = (of_head << (kv.page_shift - block_shift)) + (place >> block_shift), word = scale & ~3ll;
-                const int there = static_cast<int>(min(n_scales - word, static_cast<int64_t>(4)));
-                copy_word(words, kv.k_meta + word, there);
-                copy_word(words + 4, kv.v_meta + word, there);
-                sts_u32(words + 8, static_cast<uint32_t>(scale & 3) * 8);
-            }
-            arrive_with_words(b);
-        }
-        ++load.tile;
-        if (++load.u == load.end) seek(load, u1);
-        page = page_of();
-    };
-    for (uint32_t i = 0; i < kP8Stages; ++i) ask(i);
+    Place at = {};
+    at.u = u0;
+    seek(at, u1);
     uint32_t taken = 0;
     // pieces of this CTA that other CTAs have parts of: at its begin and at its end
     if (!f.by_request && warp == kP8Warps - 1) {
@@ -622,8 +655,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 }
             if (kN == 1) {
                 load_v();
-                __syncwarp();                              // the whole warp has read the tile
-                ask(stage);
+                warp_arrive(bar + Smem::kFree + stage * 8);            // the whole warp has read the tile
             }
             float4 by[2][2];                               // K's factor, V's exponent, the inverse of V's power of two
 #pragma unroll
@@ -668,8 +700,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
             }
             if (kN > 1) {
                 load_v();
-                __syncwarp();
-                ask(stage);
+                warp_arrive(bar + Smem::kFree + stage * 8);
             }
             // softmax: weights of V's E4M3 numbers, relative to the largest so far
             float top[kN][2];
@@ -791,9 +822,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
         if (!whole && lane == 0) pieces[warp * 2 + which] = P8Piece{at.begin, at.units, at.head, at.row0, at.rows, at.group, 1};
         seek(at, u1);
     }
-    if (!ok)                                               // tiles on their way land before the warp leaves
-        for (uint32_t i = taken; i < taken + kP8Stages && static_cast<int64_t>(i) < u1 - u0; ++i) warp_wait(bar + (i % kP8Stages) * 8, (i / kP8Stages) & 1u);
-    __syncthreads();
+    meet();
 
     auto write_row = [&](int32_t group, int32_t row0, int32_t head, int row, float m, float l, const float4& v) {
         const int i = group * kP8Rows16 + row, token = i / o.q_per_kv;
@@ -845,14 +874,14 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     if (o.early) dependency_wait();
     if (f.by_request) return;
     if (!spans[0].valid && !spans[1].valid) return;
-    __syncthreads();
+    meet();
     if (tid < 2) {
         const P8Span sp = spans[tid];
         __threadfence();                                   // what all threads have written before the barrier
         joins[tid] = sp.valid && take_ticket(f.tickets + static_cast<int64_t>(sp.lo) * kTicketStride) == static_cast<unsigned>(sp.hi - sp.lo);
         __threadfence();
     }
-    __syncthreads();
+    meet();
     for (int i = 0; i < 2; ++i) {
         if (!joins[i]) continue;
         const P8Span sp = spans[i];
