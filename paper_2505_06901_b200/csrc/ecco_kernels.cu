@@ -1114,8 +1114,13 @@ extern "C" int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rop
 }
 
 namespace {
-// rows of a request up to which they go to ecco_paged8_few_kernel, sixteen at a time
+// Rows of a request up to which they go to ecco_paged8_few_kernel, sixteen at a time; all rows do, where the tiles of the call, each once for sixteen rows, are few
 constexpr int kP8FewRows = 64;
+// (a request of 80 rows over 4000 tokens, 8 heads 59 -> 23 us, of 800 over 700 34.6 -> 29.2, over 200 24.5 -> 22.4; 16 000 tiles are as fast the other way).
+constexpr int64_t kP8FewPasses = 10000;
+// CTAs that a block's sums come from: a head of 800 rows over 16000 tokens from 126 / 32 / 16 CTAs 92 / 83 / 66 us, 8 heads of 320 rows over 4000 tokens from 9 / 8
+// / 4 50 / 40 / 42
+constexpr int kP8ManyJoins = 8;
 // CTAs for few rows.  One to a request and head, so that no sums pass through memory, where there are at most as many and they have few tiles (2
 // requests of 300 / 780 / 2000 tokens, 8 heads: 7.6 / 9.8 / 15.7 us, with equal parts of the line of four tiles or more 8.2 / 8.7 / 10.1), or where they fill the machine
 // anyway (16 of 1500 to 2000 tokens, 8 heads 20.5 / 22.2).  Else equal parts, of four tiles at least (2 requests of 780, of two, four, eight: 9.8 / 8.7 / 11.0), and
@@ -1130,7 +1135,7 @@ constexpr size_t kP8StagedMost = static_cast<size_t>(2) << 30;                  
 //   schedule | few rows: tickets, sums, maxima | many rows: sums, maxima | tiles, if any
 struct P8AttnPlan {
     bool many, line, by_request;       // there may be requests of more rows; more requests than the kernel for few rows schedules itself
-    int few_ctas, many_ctas, max_blocks;
+    int few_rows, few_ctas, many_ctas, max_blocks;
     size_t few_tiles, block_tiles, blocks, n_blocks, tickets, few_tickets, few_part, few_ml, many_part, many_ml, bytes;
     size_t tiles, bytes_with_tiles;    // the same as bytes where there are none
 };
@@ -1138,35 +1143,40 @@ P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, 
 {
     P8AttnPlan p = {};
     const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
-    p.many = rows > kP8FewRows;
+    const int64_t all_groups = (rows + kP8Rows16 - 1) / kP8Rows16, tiles = static_cast<int64_t>(b.max_tiles) * heads;
+    p.few_rows = static_cast<int>(all_groups * tiles <= kP8FewPasses ? std::max<int64_t>(rows, kP8FewRows) : kP8FewRows);
+    p.many = rows > p.few_rows;
+    const bool room_for_many = rows > kP8FewRows;          // whatever max_tiles says
     p.line = b.n_req > kP8Reqs;
-    const int64_t groups = std::min<int64_t>((rows + kP8Rows16 - 1) / kP8Rows16, kP8FewRows / kP8Rows16);
-    const int64_t tiles_of_one = (static_cast<int64_t>(b.max_kv) + 31) / 32 * std::max<int64_t>(groups, 1), units = static_cast<int64_t>(b.max_tiles) * heads * std::max<int64_t>(groups, 1);
+    const int64_t groups = std::min<int64_t>(all_groups, (p.few_rows + kP8Rows16 - 1) / kP8Rows16);
+    const int64_t tiles_of_one = (static_cast<int64_t>(b.max_kv) + 31) / 32 * std::max<int64_t>(groups, 1), units = tiles * std::max<int64_t>(groups, 1);
     p.by_request = static_cast<int64_t>(b.n_req) * heads <= ctas_max && (tiles_of_one <= kP8OneCtaTiles || tiles_of_one * ctas_max * 3 <= units * 4);
     const int64_t per_cta = std::max<int64_t>(kP8CtaTiles, tiles_of_one / kP8JoinCtas);
     p.few_ctas = p.by_request ? std::max(b.n_req, 1) * heads : std::max(1, spread_ctas((units + per_cta - 1) / per_cta, ctas_max));
-    p.many_ctas = ctas_max;
-    p.max_blocks = p.many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
+    // blocks' tiles of 128 tokens, at most; a block's sums come from some eight CTAs at most
+    const int64_t many_units = (rows + kManyRows - 1) / kManyRows * ((tiles + 3) / 4), per_many = std::max<int64_t>(1, b.max_kv / (kManyTokens * kP8ManyJoins));
+    p.many_ctas = static_cast<int>(std::min<int64_t>(ctas_max, std::max<int64_t>(1, many_units / per_many)));
+    p.max_blocks = room_for_many ? b.n_tokens / (2 * tile_rows_tokens(q_per_kv)) + std::min(b.n_req, b.n_tokens) + 1 : 0;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
         at = (at + bytes + 255) & ~static_cast<size_t>(255);
         return here;
     };
-    const size_t few_slots = static_cast<size_t>(ctas_max) * 2 * kP8Rows16, many_slots = p.many ? static_cast<size_t>(p.many_ctas) * 2 * kManyRows : 0;
+    const size_t few_slots = static_cast<size_t>(ctas_max) * 2 * kP8Rows16, many_slots = room_for_many ? static_cast<size_t>(ctas_max) * 2 * kManyRows : 0;
     p.few_tiles = take((static_cast<size_t>(b.n_req) + 1) * 4);
     p.block_tiles = take((static_cast<size_t>(p.max_blocks) + 1) * 4);
     p.blocks = take(static_cast<size_t>(p.max_blocks) * 8);
     p.n_blocks = take(8);
-    p.tickets = take(static_cast<size_t>(2) * p.many_ctas * 4);
+    p.tickets = take(static_cast<size_t>(2) * ctas_max * 4);
     p.few_tickets = take(static_cast<size_t>(ctas_max) * kTicketStride * sizeof(Ticket));
     p.few_part = take(few_slots * kGroup * sizeof(float));
     p.few_ml = take(few_slots * sizeof(float2));
     p.many_part = take(many_slots * kGroup * sizeof(float));
     p.many_ml = take(many_slots * sizeof(float2));
     p.tiles = p.bytes = p.bytes_with_tiles = at;
-    const size_t tiles = static_cast<size_t>(b.max_tiles) * heads * 2 * kKvTileBytes;
-    if (rows > kP8StagedRows && tiles <= kP8StagedMost) p.bytes_with_tiles = at + tiles;
+    const size_t tile_bytes = static_cast<size_t>(tiles) * 2 * kKvTileBytes;
+    if (p.many && rows > kP8StagedRows && tile_bytes <= kP8StagedMost) p.bytes_with_tiles = at + tile_bytes;
     return p;
 }
 // a pool as [page][head][place][128 bytes]: a box is a page's part of a tile of some tokens
@@ -1258,7 +1268,7 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
         sc.n_blocks = reinterpret_cast<int32_t*>(kv.staged + p.n_blocks);
         sc.n_cuts = sc.n_blocks + 1;
         sc.max_blocks = p.max_blocks;
-        sc.few_rows = kP8FewRows;
+        sc.few_rows = p.few_rows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
         sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
         const bool tiles = p.bytes_with_tiles > p.bytes && p.bytes_with_tiles <= workspace_bytes;
@@ -1287,7 +1297,7 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
     if (!make_p8_maps(&k_map, &v_map, kv, 32)) return ECCO_ERR_CUDA;
     P8Few f = {};
     f.line = p.line ? reinterpret_cast<const int32_t*>(kv.staged + p.few_tiles) : nullptr;
-    f.few_rows = kP8FewRows;
+    f.few_rows = p.few_rows;
     f.by_request = p.by_request;
     f.part = reinterpret_cast<float*>(kv.staged + p.few_part);
     f.part_ml = reinterpret_cast<float2*>(kv.staged + p.few_ml);
