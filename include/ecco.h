@@ -390,8 +390,8 @@ int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope_or_
 
 /* ecco_paged_attn over this cache: the same batch, flags, rows, bounds, in- and outputs and limits; so is what is said there of masks, of values that are
  * not finite and of arrays that are wrong.  Bytes 0x7f and 0xff (NaN), which ecco_paged8_append never writes, spoil the rows of the request and head that they
- * are in, where they lie within its length.  Weights enter the tensor cores as fp16 with 2^-11 of each, or 2^-30 of the largest product of a weight and
- * its block's 2^e.
+ * are in, where they lie within its length.  Weights enter the tensor cores as fp16 (rounding 2^-11 of each, or 2^-32 of a row's largest; of requests of few
+ * rows 2^-32 of the largest product of a weight and its block's 2^e, times the E4M3 numbers).
  * d_workspace: ecco_paged8_attn_workspace_bytes(...) bytes for the same arguments; 16-byte aligned, contents irrelevant before and undefined after; calls sharing a
  * workspace must not overlap.  Where max_new * q_per_kv is large that has room for the pages' values in fp16, 512 bytes per token and KV head; what the function
  * gives with max_tiles = 0, a few MB, is enough, too, and takes up to a sixth longer. */

@@ -418,6 +418,9 @@ SHAPES = [
     ([4, 3, 8], [600, 3, 2500], 2, 4, 16), ([16, 15], [100, 500], 1, 4, 64), ([13, 1], [700, 700], 2, 5, 16), ([17, 1, 40], [64, 300, 41], 2, 4, 16),
     ([100, 1, 1], [1500, 900, 2], 2, 2, 8), ([300, 5, 0, 64], [300, 800, 10, 130], 1, 8, 4096), ([65], [65], 3, 1, 1), ([129, 2, 70], [200, 2000, 700], 2, 16, 32),
     ([1] * 300, [37] * 300, 1, 2, 16), ([1] * 40, list(range(0, 400, 10)), 4, 4, 16),
+    # enough tiles for the kernel of many rows
+    ([300, 5, 0, 64], [3000, 800, 10, 130], 2, 8, 16), ([130, 1, 1], [1500, 900, 2], 8, 3, 8), ([400, 33], [400, 2000], 2, 16, 128), ([70, 70, 1], [4000, 69, 31], 3, 16, 4),
+    ([1000], [1000], 4, 2, 32), ([257, 1, 300], [5000, 0, 257], 1, 13, 1), ([515, 20], [20, 515], 6, 4, 64),
 ]
 
 
@@ -437,18 +440,18 @@ def test_attention(B, dev, shape, causal):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("scale", [0.0, -0.1, 1e-4, 3.0])
-@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("new", [1, 40, 300])
 def test_scales(B, dev, scale, new):
-    c = Case(B, np.random.default_rng([new]), [new, 2], [400, 90], 2, 4, 16)
+    c = Case(B, np.random.default_rng([new]), [new, 2], [400, 90], 2 if new < 300 else 16, 4, 16)
     out, lse = c.run(scale=scale)
     c.check(out, lse, scale=scale)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("new", [1, 5, 60])
+@pytest.mark.parametrize("new", [1, 5, 60, 300])
 def test_powers_of_two_of_all_sizes(B, dev, new):
     """Blocks of 2^-15 beside blocks of 2^7: the weights of the first are not lost beside the second's."""
-    c = Case(B, np.random.default_rng([new, 7]), [new, new], [700, 130], 2, 3, 16, qscale=2.0**-7, exps=(-15, 7))
+    c = Case(B, np.random.default_rng([new, 7]), [new, new], [700, 130], 2 if new < 300 else 8, 3, 16, qscale=2.0**-7, exps=(-15, 7))
     out, lse = c.run()
     c.check(out, lse)
     # V of the smallest power of two where K draws the weight, of the largest where it does not
@@ -464,19 +467,22 @@ def test_powers_of_two_of_all_sizes(B, dev, new):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("new", [[3, 1], [70, 1], [9, 4]])
+@pytest.mark.parametrize("new", [[3, 1], [70, 1], [9, 4], [900, 900]])
 def test_more_new_tokens_than_the_request_holds(B, dev, new):
     """The first rows of such a request see nothing: zeros, and minus infinity."""
-    c = Case(B, np.random.default_rng(new), new, [2, 0], 2, 2, 16)
+    kv, heads = [2, 0], 2
+    if new[0] == 900:                                      # the tiles of another request make it a call for the kernel of many rows
+        new, kv, heads = new + [1], kv + [900], 8
+    c = Case(B, np.random.default_rng(new), new, kv, heads, 2, 16)
     out, lse = c.run()
     c.check(out, lse)
     assert not out[:new[0] - 2].any() and bool((lse[:new[0] - 2] == -math.inf).all())
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("new", [1, 30])
+@pytest.mark.parametrize("new", [1, 30, 300])
 def test_q_that_is_not_finite_spoils_its_own_rows(B, dev, new):
-    c = Case(B, np.random.default_rng([new, 5]), [new, new], [200, 64], 2, 4, 16)
+    c = Case(B, np.random.default_rng([new, 5]), [new, new], [max(200, new), max(64, new)], 2 if new < 300 else 16, 4, 16)
     clean, clean_lse = c.run()
     q = c.q.clone()
     q[0, 1, 5], q[new, 6, 0] = math.nan, math.inf
@@ -489,7 +495,7 @@ def test_q_that_is_not_finite_spoils_its_own_rows(B, dev, new):
 
 @pytest.mark.gpu
 def test_strided_q_and_no_workspace(B, dev):
-    for new, kv in (([1, 3], [300, 70]), ([50, 1, 70], [400, 300, 70])):
+    for new, kv in (([1, 3], [300, 70]), ([50, 1, 70], [400, 300, 70]), ([500, 1], [3000, 70])):
         c = Case(B, np.random.default_rng(new), new, kv, 4, 4, 16)
         out, lse = c.run()
         c.check(out, lse)
@@ -522,7 +528,7 @@ def test_a_long_prompt_with_and_without_room_for_its_tiles(B, dev, page, causal)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("new", [1, 70, 300])
 def test_more_requests_than_fit_shared_memory(B, dev, new):
     rng = np.random.default_rng([new, 11])
     n = 1500
@@ -550,7 +556,7 @@ def test_a_long_request_alone(B, dev):
 def test_captured_and_replayed_with_other_lengths(B, dev):
     """The sizes that the host passes are upper bounds; two graphs share a workspace."""
     rng = np.random.default_rng(21)
-    for max_new, g in ((1, 4), (40, 4)):
+    for max_new, g in ((1, 4), (40, 4), (200, 8)):
         cases = [Case(B, np.random.default_rng([s, max_new]), rng.integers(0, max_new + 1, 6), rng.integers(0, 900, 6), 2, g, 16, padding=0) for s in range(3)]
         bound = dict(tokens=6 * max_new, max_new=max_new, max_kv=1000, max_tiles=6 * 32)
         c = cases[0]
@@ -594,7 +600,7 @@ def test_captured_and_replayed_with_other_lengths(B, dev):
 
 @pytest.mark.gpu
 def test_two_streams_at_once(B, dev):
-    cases = [Case(B, np.random.default_rng([s, 3]), new, kv, 4, 4, 16) for s, (new, kv) in enumerate((([1] * 6, [900] * 6), ([40, 1, 1], [800, 700, 600])))]
+    cases = [Case(B, np.random.default_rng([s, 3]), new, kv, 4, 4, 16) for s, (new, kv) in enumerate((([1] * 6, [900] * 6), ([40, 1, 1], [800, 700, 600]), ([300, 80], [900, 700])))]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in cases]
     results = []
@@ -613,10 +619,10 @@ def test_two_streams_at_once(B, dev):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("what", ["page", "no page", "falling", "negative", "too long", "too many", "more rows", "lengths", "beyond"])
-@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("new", [1, 40, 600, 1200])
 def test_wrong_arrays_are_reported(B, dev, what, new):
     """Arrays that say what cannot be: reported, nothing beside the buffers is touched, and the next call is what it always is."""
-    c = Case(B, np.random.default_rng([new, 8]), [new, 1, 2], [150, 90, 33], 2, 4, 16)
+    c = Case(B, np.random.default_rng([new, 8]), [new, 1, 2], [150, 90, 33], 2 if new < 600 else 16, 4, 16)
     tables, cu, kv, tiles = c.tables.copy(), c.cu.copy(), np.array(c.kv), c.tiles.copy()
     bounds = {}
     if what == "page":
@@ -651,10 +657,10 @@ def test_wrong_arrays_are_reported(B, dev, what, new):
 @pytest.mark.gpu
 def test_random_batches(B, dev):
     rng = np.random.default_rng(31)
-    for _ in range(40):
+    for _ in range(60):
         heads, g, page = int(rng.choice([1, 2, 3, 8])), int(rng.choice([1, 2, 3, 4, 5, 7, 8, 16])), int(rng.choice([1, 2, 4, 8, 16, 32, 64, 256]))
         n = int(rng.integers(1, 30))
-        most = int(rng.choice([1, 1, 2, 5, 20, 150]))
+        most = int(rng.choice([1, 1, 2, 5, 20, 150, 400]))
         new = rng.integers(0, most + 1, n)
         new[0] = max(new[0], 1)
         kv = (new * rng.integers(0, 2, n) + rng.integers(0, int(10 ** rng.uniform(0.5, 3.3)), n)).astype(int)
@@ -747,18 +753,16 @@ def test_offsets_beyond_32_bits(B, dev):
     slots = [int(tables[r, t // page]) * page + t % page for r, n in enumerate(kv) for t in range(n)]
     d = torch.from_numpy(np.stack([k, v])).cuda()
     B.ecco_paged8_append(cache, None, None, d[0], d[1], heads * 128, ints(slots), rows)
-    small = [[np.zeros((8, heads, page, 128), np.uint8), np.zeros((8, heads, 2), np.uint8)] for _ in range(2)]
     names = sorted({int(p) for r, n in enumerate(kv) for p in tables[r, :-(-n // page)]})
     local = [names.index(s // page) * page + s % page for s in slots]
     for i, x in enumerate((k, v)):
-        small[i][0] = np.zeros((len(names), heads, page, 128), np.uint8)
-        small[i][1] = np.zeros((len(names), heads, 2), np.uint8)
-        append_reference(*small[i], x, local, page)
+        want = np.zeros((len(names), heads, page, 128), np.uint8)
+        append_reference(want, np.zeros((len(names), heads, 2), np.uint8), x, local, page)
         here = codes[i][torch.tensor(names, device="cuda")].cpu().numpy()
         taken = np.zeros((len(names), page), bool)
         for s in local:
             taken[s // page, s % page] = True
-        assert np.array_equal(here.transpose(0, 2, 1, 3)[taken], small[i][0].transpose(0, 2, 1, 3)[taken])
+        assert np.array_equal(here.transpose(0, 2, 1, 3)[taken], want.transpose(0, 2, 1, 3)[taken])
     cu, tiles = np.concatenate([[0], np.cumsum(new)]), np.concatenate([[0], np.cumsum([-(-n // 32) for n in kv])])
     batch = B.paged_batch(ints(tables), 4, ints(cu), ints(kv), ints(tiles), 3, sum(new), max(new), max(kv), int(tiles[-1]))
     q = torch.from_numpy(rng.standard_normal((sum(new), heads * g, 128)).astype(np.float16)).cuda()
@@ -774,8 +778,8 @@ def test_offsets_beyond_32_bits(B, dev):
 @pytest.mark.gpu
 def test_a_replay_after_one_with_wrong_arrays(B, dev):
     """What a call with arrays that cannot be leaves in the workspace does not change what the same graph computes afterwards."""
-    for new in (1, 40):
-        c = Case(B, np.random.default_rng([new, 51]), [new] * 5, [700, 650, 900, 40, 800], 4, 4, 16, padding=0)
+    for new in (1, 40, 150):
+        c = Case(B, np.random.default_rng([new, 51]), [new] * 5, [700, 650, 900, 40, 800], 4 if new < 150 else 8, 4, 16, padding=0)
         out, lse = torch.zeros_like(c.q), torch.zeros(c.q.shape[:2], device="cuda")
         ws = torch.empty(c.need(), dtype=torch.uint8, device="cuda")
         call = lambda: B.ecco_paged8_attn(c.cache, c.batch, c.g, c.q, c.heads * c.g * 128, 128**-0.5, B.ATTN_CAUSAL, out, lse, ws, len(ws))  # noqa: E731
