@@ -394,7 +394,7 @@ int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope_or_
  * rows 2^-32 of the largest product of a weight and its block's 2^e, times the E4M3 numbers).
  * d_workspace: ecco_paged8_attn_workspace_bytes(...) bytes for the same arguments; 16-byte aligned, contents irrelevant before and undefined after; calls sharing a
  * workspace must not overlap.  Where max_new * q_per_kv is large that has room for the pages' values in fp16, 512 bytes per token and KV head; what the function
- * gives with max_tiles = 0, a few MB, is enough, too, and takes up to a sixth longer. */
+ * gives with max_tiles = 0, some MB, is enough, too, and takes up to a sixth longer, as does a workspace that is not 32-byte aligned. */
 size_t ecco_paged8_attn_workspace_bytes(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv);
 int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q_fp16, int64_t q_stride, float scale,
                      uint32_t flags, void* d_out_fp16, float* d_lse_or_null, void* d_workspace, size_t workspace_bytes, void* stream);

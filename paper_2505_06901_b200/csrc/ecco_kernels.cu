@@ -1142,7 +1142,7 @@ struct P8AttnPlan {
 P8AttnPlan paged8_attn_plan(const ecco_paged_batch& b, int heads, int q_per_kv, int ctas_max)
 {
     P8AttnPlan p = {};
-    const int64_t rows = static_cast<int64_t>(b.max_new) * q_per_kv;
+    const int64_t rows = std::min<int64_t>(static_cast<int64_t>(b.max_new) * q_per_kv, INT32_MAX);      // a batch has no more, see paged_batch_fine
     const int64_t all_groups = (rows + kP8Rows16 - 1) / kP8Rows16, tiles = static_cast<int64_t>(b.max_tiles) * heads;
     p.few_rows = static_cast<int>(all_groups * tiles <= kP8FewPasses ? std::max<int64_t>(rows, kP8FewRows) : kP8FewRows);
     p.many = rows > p.few_rows;
@@ -1271,7 +1271,8 @@ extern "C" int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged
         sc.few_rows = p.few_rows;
         sc.tickets = reinterpret_cast<int32_t*>(kv.staged + p.tickets);
         sc.n_tickets = p.many ? 2 * p.many_ctas : 0;
-        const bool tiles = p.bytes_with_tiles > p.bytes && p.bytes_with_tiles <= workspace_bytes;
+        // they are written 32 bytes at a time
+        const bool tiles = p.bytes_with_tiles > p.bytes && p.bytes_with_tiles <= workspace_bytes && aligned_to(d_workspace, 32);
         PagedKv staged = kv;
         staged.staged = kv.staged + p.tiles;
         const unsigned grid = tiles ? static_cast<unsigned>(spread_ctas(static_cast<int64_t>(b.max_tiles) * kv.heads / kP8StageWarps + 1, di.sms * 2)) : 1u;

@@ -836,3 +836,51 @@ def test_calls_behind_one_another(B, dev):
 
     for a, b in zip(serve(False), serve(True)):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("page", [4, 16])
+def test_the_least_alignment(B, dev, page):
+    """Pools, q, rows, out and workspace at odd multiples of 16 bytes, scales, lse and arrays at odd multiples of 4."""
+    def at(t, off):
+        d = torch.zeros(t.numel() * t.element_size() + 64, dtype=torch.uint8, device="cuda")
+        assert d.data_ptr() % 64 == 0
+        d[off:off + t.numel() * t.element_size()] = t.contiguous().view(-1).view(torch.uint8)
+        return d, d.data_ptr() + off
+
+    for new, kv, heads, g in (([1, 1], [300, 40], 2, 4), ([300, 30], [2000, 700], 4, 4), ([600, 30], [2000, 700], 2, 8)):
+        c = Case(B, np.random.default_rng([page] + new), new, kv, heads, g, page)
+        out, lse = c.run()
+        keep = [at(t, off) for t, off in zip(c.pools, (16, 4, 48, 12))] + [at(t, 4) for t in c.arrays]
+        q, o, l = at(c.q, 16), at(torch.full_like(out, 7.0), 48), at(torch.full_like(lse, 7.0), 4)
+        ws = torch.zeros(c.need() + 64, dtype=torch.uint8, device="cuda")
+        cache = B.paged8_cache(keep[0][1], keep[2][1], keep[1][1], keep[3][1], c.pages, heads, page)
+        batch = B.paged_batch(keep[4][1], c.stride, keep[5][1], keep[6][1], keep[7][1], len(new), c.tokens, max(new), max(kv), int(c.tiles[-1]))
+        B.ecco_paged8_attn(cache, batch, g, q[1], heads * g * 128, 128**-0.5, B.ATTN_CAUSAL, o[1], l[1], ws.data_ptr() + 16, c.need())
+        torch.cuda.synchronize()
+        c.check(o[0][48:48 + out.numel() * 2].view(torch.float16).view(out.shape), l[0][4:4 + lse.numel() * 4].view(torch.float32).view(lse.shape))
+    rng = np.random.default_rng([page, 5])
+    slots, pages = request_slots(rng, [3, 0, 20], [30, 70, 1], page)
+    k, v = (random_rows(rng, (len(slots), 3, 128)) for _ in range(2))
+    pools = [old_pool(rng, pages, 3, page) for _ in range(2)]
+    want = [[a.copy() for a in kind] for kind in pools]
+    for w, x in zip(want, (k, v)):
+        append_reference(*w, x, slots, page)
+    held = [at(torch.from_numpy(a), off) for a, off in zip([a for kind in pools for a in kind], (16, 4, 48, 12))]
+    rows = [at(torch.from_numpy(x), 16) for x in (k, v)]
+    index = at(ints(slots), 4)
+    B.ecco_paged8_append(B.paged8_cache(held[0][1], held[2][1], held[1][1], held[3][1], pages, 3, page), None, None, rows[0][1], rows[1][1], 3 * 128, index[1], len(slots))
+    torch.cuda.synchronize()
+    for (d, _), off, w in zip(held, (16, 4, 48, 12), [a for kind in want for a in kind]):
+        assert np.array_equal(d[off:off + w.size].cpu().numpy(), w.reshape(-1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new,kv", [([3, 1], [0, 0]), ([1, 2, 40], [0, 300, 90]), ([2, 700, 1], [2100, 700, 0])])
+def test_the_largest_bounds(B, dev, new, kv):
+    """Bounds far above what the arrays say, and of tiles none where there are none."""
+    c = Case(B, np.random.default_rng(new), new, kv, 2, 16, 16)
+    tiles = int(c.tiles[-1])
+    for most in (dict(max_new=2**31 - 1, max_tiles=tiles), dict(max_new=2**31 - 1, max_tiles=tiles, max_kv=2**31 - 1 if c.tokens < 600 else 1 << 24), dict(max_new=2**31 - 1, max_tiles=tiles + 5000)):
+        out, lse = c.run(batch=c.make_batch(*c.arrays, **most))
+        c.check(out, lse)
