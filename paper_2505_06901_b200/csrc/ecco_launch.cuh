@@ -32,7 +32,7 @@ int device_info(DeviceInfo* out)
 
 int check_launch();
 // Launch with the programmatic stream-serialisation attribute (see dependency_wait in the kernels):
-// the kernel must call dependency_wait() before its first access to global memory (the one exception and its conditions stand there).
+// the kernel must call dependency_wait() before its first access to global memory (the exceptions and their conditions stand there).
 template <class... Params, class... Args>
 int launch_overlapped(void (*kernel)(Params...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, Args... args)
 {

@@ -64,7 +64,7 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 // The first n (1 .. 4) bytes of a word global -> shared, the others zero; the barrier counts an arrival of this thread's when all such copies that it has
-// begun have come.
+// begun have come.  They go through L1 (copies past it have sixteen bytes, at addresses that scales need not have): only behind dependency_wait().
 __device__ __forceinline__ void copy_word(uint32_t dst, const uint8_t* src, int n)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");

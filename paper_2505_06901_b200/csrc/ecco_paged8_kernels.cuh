@@ -391,7 +391,8 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     if (tid < kP8Warps * 2) pieces[tid].valid = 0;
     __syncthreads();
     // Behind ecco_paged_many_kernel the wait comes at the end, on the conditions that stand at ecco_paged_few_kernel: what is read here was there before
-    // that kernel began, it is read through L2 alone, and neither writes what the other reads or writes.
+    // that kernel began, it is read through L2 alone (the tensor maps' and bulk copies, __ldcg; the powers of two by __ldcg, too, and not by copy_word), and
+    // neither writes what the other reads or writes.
     if (!o.early) dependency_wait();
     release_dependents();
     const int32_t T = paged_tiles(kv);
@@ -496,7 +497,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
     const int32_t in_page = (1 << kv.page_shift) - 1;
     if (warp >= kP8Warps) {
         // Loads: half a warp to a warp's ring, a lane to a block or two of a tile.  A tile's pages are looked up with the tile before it; nothing else from memory
-        // passes through registers on its way.  384 threads x 168 registers = 128 x 72 + 256 x 216.  (Each warp with its own loads, half of a tile's 2400 clocks
+        // passes through registers on its way, but for the powers of two behind ecco_paged_many_kernel.  384 threads x 168 registers = 128 x 72 + 256 x 216.  (Each warp with its own loads, half of a tile's 2400 clocks
         // went into these; one warp with all of them came too late: 8 requests of 4050 tokens, 32 heads 59 and 62 us.)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         const int w = static_cast<int>(warp - kP8Warps) * 2 + static_cast<int>(lane >> 4), j = static_cast<int>(lane & 15u);
@@ -543,6 +544,10 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                         }
                     }
                     const int64_t scale = (of_head << (kv.page_shift - block_shift)) + (place >> block_shift), word = scale & ~3ll;
+                    if (o.early) {                         // through L2: copy_word goes through L1, where older bytes may be before the wait
+                        sts_v4(words, __ldcg(kv.k_meta + scale), __ldcg(kv.v_meta + scale), 0u, 0u);
+                        return;
+                    }
                     const int there = static_cast<int>(min(n_scales - word, static_cast<int64_t>(4)));
                     copy_word(words, kv.k_meta + word, there);
                     copy_word(words + 4, kv.v_meta + word, there);

@@ -884,3 +884,65 @@ def test_the_largest_bounds(B, dev, new, kv):
     for most in (dict(max_new=2**31 - 1, max_tiles=tiles), dict(max_new=2**31 - 1, max_tiles=tiles, max_kv=2**31 - 1 if c.tokens < 600 else 1 << 24), dict(max_new=2**31 - 1, max_tiles=tiles + 5000)):
         out, lse = c.run(batch=c.make_batch(*c.arrays, **most))
         c.check(out, lse)
+
+
+@pytest.mark.gpu
+def test_mixed_calls_behind_one_another(B, dev):
+    """As above with a piece of a prompt beside single tokens in every step, so that the kernel for few rows begins while the one for many ends, right
+    behind an append that has given the blocks in question other powers of two."""
+    rng = np.random.default_rng(62)
+    heads, g, page, n, piece, steps = 8, 4, 16, 24, 100, 24
+    rope = B.ecco_rope_init(128, 10000.0 ** (-np.arange(64) / 64))
+    ctx = np.r_[rng.integers(1, 400, n - 1), 1500]
+    new = np.r_[np.ones(n - 1, int), piece]
+    held = -(-(ctx + steps * new) // page)
+    stride, pages, rows = int(held.max()), int(held.sum()), int(new.sum())
+    order, tables = rng.permutation(pages), np.full((n, stride), -1, np.int32)
+    for r, at in enumerate(np.cumsum(held) - held):
+        tables[r, :held[r]] = order[at:at + held[r]]
+    row = heads * (g + 2) * 128
+    place = lambda r, t: [int(tables[r, i // page]) * page + i % page for i in t]  # noqa: E731
+    start = torch.from_numpy(rng.standard_normal((int(ctx.sum()), heads * 2, 128)).astype(np.float16)).cuda()
+    start_slots = ints([s for r in range(n) for s in place(r, range(ctx[r]))])
+    # a step's K and V are up to twice as large as the step's before, sixteen steps long, then small again
+    gen = torch.Generator(device="cuda").manual_seed(63)
+    qkv = torch.randn((steps, rows, heads * (g + 2), 128), generator=gen, device="cuda")
+    qkv[:, :, heads * g:] *= 2.0 ** (torch.arange(steps, device="cuda") % 16 - 8)[:, None, None, None]
+    qkv = qkv.half()
+    lens = [ctx + (s + 1) * new for s in range(steps)]
+    tiles = [np.r_[0, np.cumsum(-(-x // 32))] for x in lens]
+    tokens = [np.concatenate([np.arange(c, c + k) for c, k in zip(ctx + s * new, new)]) for s in range(steps)]
+    slots = [ints([x for r in range(n) for x in place(r, range(ctx[r] + s * new[r], lens[s][r]))]) for s in range(steps)]
+    positions, cu, d_tables = [ints(t) for t in tokens], ints(np.r_[0, np.cumsum(new)]), ints(tables)
+    arrays = [(ints(x), ints(t)) for x, t in zip(lens, tiles)]
+    batches = [B.paged_batch(d_tables, stride, cu, a, t, n, rows, piece, int(lens[-1].max()), int(tiles[-1][-1])) for a, t in arrays]
+
+    def serve(wait):
+        codes = [torch.full((pages, heads, page, 128), 127, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        scales = [torch.zeros((pages, heads, 1), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        cache = B.paged8_cache(codes[0], codes[1], scales[0], scales[1], pages, heads, page)
+        B.ecco_paged8_append(cache, None, None, start, start.data_ptr() + heads * 256, heads * 256, start_slots, len(start))
+        need = B.ecco_paged8_attn_workspace_bytes(cache, batches[0], g)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        d = qkv.clone()
+        outs = [torch.zeros((rows, heads * g, 128), dtype=torch.float16, device="cuda") for _ in range(steps)]
+        torch.cuda.synchronize()
+        before = B.ecco_kernel_launch_count()
+        for s in range(steps):
+            at = d[s].data_ptr()
+            for call in (lambda: B.ecco_rope_apply(rope, positions[s], rows, heads * g, d[s], row, d[s], row),
+                         lambda: B.ecco_paged8_append(cache, rope, positions[s], at + heads * g * 256, at + heads * (g + 1) * 256, row, slots[s], rows),
+                         lambda: B.ecco_paged8_attn(cache, batches[s], g, d[s], row, 128**-0.5, B.ATTN_CAUSAL, outs[s], None, ws, need)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert B.ecco_kernel_launch_count() == before + 5 * steps              # of the attention's three: the schedule, many rows, few rows
+        assert B.ecco_device_status() == 0
+        return [*codes, *scales, *outs]
+
+    one_at_a_time = serve(True)
+    assert bool((one_at_a_time[2].int() - one_at_a_time[2].int().amin() > 8).any()) and all(bool(o.isfinite().all()) for o in one_at_a_time[4:])
+    for _ in range(5):
+        for a, b in zip(serve(False), one_at_a_time):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
