@@ -1089,8 +1089,10 @@ extern "C" int ecco_rope_init(int32_t rot_dim, const double* inv_freq, float gai
     std::memset(rope, 0, sizeof *rope);
     for (int i = 0; i < rot_dim / 2; ++i) {
         // turns per position, whole ones dropped, with the 64 bits of a long double's mantissa: positions are whole numbers, so only the
-        // fraction counts
-        long double turns = static_cast<long double>(inv_freq[i]) / 6.283185307179586476925286766559005768L;
+        // fraction counts.  Where there are whole ones, which would take of these bits, by the angle that sine and cosine are of.
+        constexpr long double two_pi = 6.283185307179586476925286766559005768L;
+        const long double f = inv_freq[i];
+        long double turns = (std::fabs(f) < two_pi ? f : std::atan2(std::sin(f), std::cos(f))) / two_pi;
         turns -= std::floor(turns);
         const long double scaled = std::ldexp(turns, 64);
         rope->turn[i] = scaled >= 18446744073709551615.0L ? 0 : static_cast<uint64_t>(scaled + 0.5L);

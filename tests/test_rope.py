@@ -256,3 +256,44 @@ def test_captured_and_on_another_stream(B, dev):
         pos.copy_(torch.arange(first, first + 33, dtype=torch.int32))
         graph.replay()
         check(out.cpu().numpy(), x.cpu().numpy(), np.arange(first, first + 33), f, 1.0, 0, 128)
+
+
+def long_pi(digits):
+    """pi as a fraction, by 16 atan(1/5) - 4 atan(1/239) in whole numbers."""
+    one = 10 ** (digits + 10)
+
+    def atan_of_inverse(n):
+        total, term, k = 0, one // n, 1
+        while term:
+            total += term // k if k % 4 == 1 else -(term // k)
+            term //= n * n
+            k += 2
+        return total
+
+    return Fraction(16 * atan_of_inverse(5) - 4 * atan_of_inverse(239), one)
+
+
+def test_fractions_of_frequencies_of_any_size(B):
+    """Frequencies of many turns a position: what is left of a turn is as exact as of others.  (The whole turns of 1e308 have 308 digits.)"""
+    pi = long_pi(400)
+    assert abs(pi - PI) < Fraction(1, 10**63)
+    rng = np.random.default_rng(4)
+    f = np.concatenate([10.0 ** rng.uniform(0.8, 308, 50) * rng.choice([-1, 1], 50), [1e4, -1e4, 1e9, 2.0**53 + 2, 2.0**64, 2.0**66, 1e100, 1.7e308, -1.7e308, 6.2831853071795862,
+                                                                                     6.2831853071795871, 12.566370614359172, -6.283185307179587, 1e22]])
+    for x, turn in zip(f, B.ecco_rope_init(128, f).turn):
+        off = abs(Fraction(float(x)) / (2 * pi) % 1 * 2**64 - turn)
+        # the angle's sine, cosine and arc, its quotient by 2 pi: within a unit each of at most half a turn's last place, and the rounding to 64 bits
+        assert min(off, 2**64 - off) <= 4, x
+
+
+@pytest.mark.gpu
+def test_far_positions_of_many_turns_each(B, dev):
+    """Frequencies of up to 10^9 turns a position, at the furthest positions: within the same tolerance."""
+    rng = np.random.default_rng(10)
+    f = 10.0 ** rng.uniform(1, 10, 64) * rng.choice([-1, 1], 64)
+    x = rng.standard_normal((4, 4, 128)).astype(np.float16)
+    positions = [2**31 - 1, -(2**31), 2**30 + 1, 1]
+    out = torch.empty((4, 4, 128), dtype=torch.float16, device="cuda")
+    B.ecco_rope_apply(B.ecco_rope_init(128, f), torch.tensor(positions, dtype=torch.int32, device="cuda"), 4, 4, torch.from_numpy(x).cuda(), 512, out, 512)
+    # a turn's fraction is within 4 * 2^-64: 2^-31 of a turn at the furthest position
+    check(out.cpu().numpy(), x, positions, f, 1.0, 0, 128)
