@@ -1061,8 +1061,8 @@ extern "C" int ecco_rope_frequencies(int32_t rot_dim, double base, const ecco_ro
     double b = base;
     if (sc.kind == ECCO_ROPE_SCALE_BASE) b = base * std::pow(sc.factor, static_cast<double>(rot_dim) / (rot_dim - 2));
     if (!std::isfinite(b)) return ECCO_ERR_INVALID_ARG;
-    // the pair that makes n turns over the trained length, as a real number
-    auto pair_of = [&](double n) { return pairs * std::log(sc.trained_len / (n * kTwoPi)) / std::log(base); };
+    // the pair that makes n turns over the trained length, as a real number; by logarithms, since quotients may leave the range
+    auto pair_of = [&](double n) { return pairs * (std::log(sc.trained_len) - std::log(n) - std::log(kTwoPi)) / std::log(base); };
     double from = 0.0, to = 0.0;
     if (sc.kind == ECCO_ROPE_SCALE_RAMP) {
         from = std::max(std::floor(pair_of(sc.high)), 0.0);

@@ -297,3 +297,21 @@ def test_far_positions_of_many_turns_each(B, dev):
     B.ecco_rope_apply(B.ecco_rope_init(128, f), torch.tensor(positions, dtype=torch.int32, device="cuda"), 4, 4, torch.from_numpy(x).cuda(), 512, out, 512)
     # a turn's fraction is within 4 * 2^-64: 2^-31 of a turn at the furthest position
     check(out.cpu().numpy(), x, positions, f, 1.0, 0, 128)
+
+
+@pytest.mark.parametrize("base", [1.0 + 2.0**-52, 2.0, 10000.0, 1e300])
+@pytest.mark.parametrize("low,high,trained", [(1e-310, 1e-309, 1e300), (1e307, 1e308, 1e-300), (1e-320, 1e308, 1.0), (1.0, 1e308, 1e308), (5e-324, 1e-323, 1.7e308), (1e300, 1e301, 5e-324)])
+def test_frequencies_at_the_ends_of_the_range(B, base, low, high, trained):
+    """Arguments that are allowed give numbers: between the frequency as it is and the slowed one."""
+    for rot in (16, 128):
+        f = base ** (-2.0 * np.arange(rot // 2) / rot)
+        for kind in (B.ROPE_SCALE_BANDS, B.ROPE_SCALE_RAMP):
+            got, gain = B.ecco_rope_frequencies(rot, base, kind, 8.0, low, high, trained)
+            assert np.all(got <= f * (1 + 1e-13)) and np.all(got >= f / 8 * (1 - 1e-13)) and math.isfinite(gain), (rot, kind)
+            # bands: a pair's turns over the trained length; all of these are far from both borders or between them
+            if kind == B.ROPE_SCALE_BANDS and not (low < trained / (2 * math.pi) * f.min() < high):
+                slow, fast = trained / (2 * math.pi) * f <= low, trained / (2 * math.pi) * f >= high
+                assert np.allclose(got[slow], f[slow] / 8, rtol=1e-13, atol=0) and np.allclose(got[fast], f[fast], rtol=1e-13, atol=0)
+            # ramp: every pair makes more turns than `high`, or fewer than `low`
+            if kind == B.ROPE_SCALE_RAMP and trained / (2 * math.pi) * f.min() > high and base > 1.5:
+                assert np.allclose(got, f, rtol=1e-13, atol=0)
