@@ -946,3 +946,65 @@ def test_mixed_calls_behind_one_another(B, dev):
     for _ in range(5):
         for a, b in zip(serve(False), one_at_a_time):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.gpu
+def test_callers_on_several_host_threads(B, dev):
+    """Four threads, each with a stream, a cache and a workspace of its own, at once: turned, appended and attended to, few rows, many, both, and many by way
+    of tiles; against the same calls alone."""
+    import threading
+
+    rng = np.random.default_rng(71)
+    batches = [([1] * 5, [300, 40, 700, 90, 1200], 8, 4), ([300, 200], [1500, 900], 4, 8), ([1, 2, 300, 1], [500, 800, 3000, 60], 8, 4), ([600, 3], [2000, 700], 2, 8)]
+    work = []
+    for i, (new, kv, heads, g) in enumerate(batches):
+        c = Case(B, rng, new, kv, heads, g, (16, 64, 8, 32)[i], padding=0)
+        slots = [int(c.tables[r, t // c.page]) * c.page + t % c.page for r, (a, n) in enumerate(zip(new, kv)) for t in range(n - a, n)]
+        tokens = np.concatenate([np.arange(n - a, n) for a, n in zip(new, kv)])
+        gen = torch.Generator(device="cuda").manual_seed(72 + i)
+        rows = [torch.randn((c.tokens, heads, 128), generator=gen, device="cuda").half() for _ in range(2)]
+        rope = B.ecco_rope_init((128, 64, 96, 16)[i], 10000.0 ** (-np.arange((64, 32, 48, 8)[i]) / 64), flags=i & 1)
+        work.append(dict(c=c, slots=ints(slots), positions=ints(tokens), rows=rows, rope=rope, ws=torch.empty(c.need(), dtype=torch.uint8, device="cuda"),
+                         pools=[p.clone() for p in c.pools], q=torch.empty_like(c.q), out=torch.empty_like(c.q), lse=torch.empty(c.q.shape[:2], device="cuda")))
+
+    def step(w):
+        c = w["c"]
+        row = c.heads * c.g * 128
+        for p, was in zip(c.pools, w["pools"]):
+            p.copy_(was)
+        w["out"].fill_(7.0)
+        B.ecco_rope_apply(w["rope"], w["positions"], c.tokens, c.heads * c.g, c.q, row, w["q"], row)
+        B.ecco_paged8_append(c.cache, w["rope"], w["positions"], w["rows"][0], w["rows"][1], c.heads * 128, w["slots"], c.tokens)
+        B.ecco_paged8_attn(c.cache, c.batch, c.g, w["q"], row, 128**-0.5, B.ATTN_CAUSAL, w["out"], w["lse"], w["ws"], len(w["ws"]))
+        return [t.clone().view(torch.uint8) for t in (*c.pools, w["out"], w["lse"])]
+
+    want = []
+    for w in work:
+        want.append(step(w))
+        torch.cuda.synchronize()
+        w["c"].check(w["out"], w["lse"], q=w["q"])
+    errors, gate = [], threading.Barrier(len(work))
+
+    def caller(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(10):
+                    gate.wait(60)
+                    got = [step(work[i]) for _ in range(3)]
+                    stream.synchronize()
+                    for g in got:
+                        for a, b in zip(g, want[i]):
+                            assert torch.equal(a, b), batches[i]
+        except BaseException as e:                         # told by the main thread
+            errors.append(e)
+            gate.abort()
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=caller, args=(i,)) for i in range(len(work))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    assert B.ecco_device_status() == 0
