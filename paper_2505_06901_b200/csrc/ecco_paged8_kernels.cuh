@@ -666,7 +666,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                 load_v();
                 warp_arrive(bar + Smem::kFree + stage * 8);            // the whole warp has read the tile
             }
-            float4 by[2][2];                               // K's factor, V's exponent, the inverse of V's power of two
+            float4 by[2][2];                               // K's power of two, V's exponent, the inverse of V's power of two
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -677,7 +677,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
                     }
                     const uint4 x = words[mt][h];
                     const int k = p8_exponent((x.x >> x.z) & 0xffu), v = p8_exponent((x.y >> x.z) & 0xffu);
-                    by[mt][h] = make_float4(__uint_as_float(static_cast<uint32_t>(k + 127) << 23) * o.scale_log2, static_cast<float>(v), __uint_as_float(static_cast<uint32_t>(127 - v) << 23), 0.0f);
+                    by[mt][h] = make_float4(__uint_as_float(static_cast<uint32_t>(k + 127) << 23), static_cast<float>(v), __uint_as_float(static_cast<uint32_t>(127 - v) << 23), 0.0f);
                 }
             // scores: sixteen tokens x eight rows; with eight rows in two sums each, for four products to be under way
             constexpr int kSums = kN == 1 ? 2 : 1;
@@ -719,7 +719,7 @@ ecco_paged8_few_kernel(const __grid_constant__ PagedKv kv, const __grid_constant
 #pragma unroll
                 for (int n = 0; n < kN; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[mt][n][e] = fmaf(s[mt][n][e], by[mt][e >> 1].x, by[mt][e >> 1].y);
+                    for (int e = 0; e < 4; ++e) s[mt][n][e] = fmaf(s[mt][n][e] * by[mt][e >> 1].x, o.scale_log2, by[mt][e >> 1].y);        // (2^k * scale may leave fp32, and 0 be NaN)
             if (at.tile >= tile_of_masks) {                // some row does not see all of the tile
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)

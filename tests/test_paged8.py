@@ -1008,3 +1008,13 @@ def test_callers_on_several_host_threads(B, dev):
         t.join()
     assert not errors, errors
     assert B.ecco_device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new,kv", [([1, 2], [100, 33]), ([4, 1, 3], [700, 40, 5]), ([600], [1500])])
+@pytest.mark.parametrize("scale", [2e38, -2e38])
+def test_scores_of_zero_under_the_largest_scale(B, dev, new, kv, scale):
+    """A row of q of zeros has scores of zero whatever the scale and the blocks' powers of two, of which the products leave fp32: all tokens alike."""
+    c = Case(B, np.random.default_rng(new), new, kv, 8, 4, 16, qscale=0.0, exps=(5, 7))
+    out, lse = c.run(scale=scale)
+    c.check(out, lse, scale=scale)
