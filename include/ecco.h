@@ -380,7 +380,7 @@ typedef struct ecco_paged8_cache {
 /* New tokens into their slots: K and V of token i, fp16 [n_kv_heads][128] at d_k_fp16 and d_v_fp16 + i * token_stride values, K turned by
  * d_positions[i] on the way and rounded to fp16, as by ecco_rope_apply (rope NULL: taken as it is, no positions).  A block gets the smallest e with |x| <= 448 * 2^e
  * for all the tokens that the call brings, and every value the nearest E4M3 number (ties to even) to x / 2^e; larger values than 448 * 2^7
- * saturate, infinities too, NaN becomes zero.  A call that brings the token of a block's first place begins the block anew.  Otherwise e is no smaller than
+ * saturate, infinities too, NaN becomes zero, and nothing reports either.  A call that brings the token of a block's first place begins the block anew.  Otherwise e is no smaller than
  * it was, and where it is larger the block's other values are rounded again.
  * Tokens whose slot is negative or beyond the pool are left out.  The slots of a call are distinct, and the tokens of one block stand in consecutive rows
  * in ascending order (as ecco_paged_plan has them); other orders give unspecified values in the blocks concerned.  token_stride is a multiple of 8, at least
@@ -394,7 +394,7 @@ int ecco_paged8_append(const ecco_paged8_cache* cache, const ecco_rope* rope_or_
  * rows 2^-32 of the largest product of a weight and its block's 2^e, times the E4M3 numbers).
  * d_workspace: ecco_paged8_attn_workspace_bytes(...) bytes for the same arguments; 16-byte aligned, contents irrelevant before and undefined after; calls sharing a
  * workspace must not overlap.  Where max_new * q_per_kv is large that has room for the pages' values in fp16, 512 bytes per token and KV head; what the function
- * gives with max_tiles = 0, some MB, is enough, too, and takes up to a sixth longer, as does a workspace that is not 32-byte aligned. */
+ * gives with max_tiles = 0, some MB, is enough, too, and takes up to a quarter longer, as does a workspace that is not 32-byte aligned. */
 size_t ecco_paged8_attn_workspace_bytes(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv);
 int ecco_paged8_attn(const ecco_paged8_cache* cache, const ecco_paged_batch* batch, int32_t q_per_kv, const void* d_q_fp16, int64_t q_stride, float scale,
                      uint32_t flags, void* d_out_fp16, float* d_lse_or_null, void* d_workspace, size_t workspace_bytes, void* stream);

@@ -9,7 +9,7 @@ namespace {
 // it.  A CTA has the runs that begin in sixteen rows, and a share of their heads; a warp takes a run of one head, of K or of V, as a whole: eight
 // lanes to a token, so that its up to 2048 values stay in registers from the load over the rotation and the largest value to the E4M3 numbers.
 // Bound by memory, 768 bytes per token and KV head, and not far behind by the issue slots, half busy: 566 instructions to a run (4096 tokens x 32 heads, 101 MB:
-// 19.6 us = 5.1 TB/s, 79 % of the copy rate).  256 windows on 148 SMs leave 40 of these with one CTA of two.
+// 19.6 to 20.1 us = 5.0 to 5.1 TB/s, 77 to 79 % of the copy rate).  256 windows on 148 SMs leave 40 of these with one CTA of two.
 // ---------------------------------------------------------------------------------------------
 constexpr int kP8AppendThreads = 256, kP8AppendWarps = kP8AppendThreads / 32, kP8Rows = 16;
 constexpr uint32_t kP8RunBytes = kP8Rows * kGroup * 2;     // a run's rows in shared memory: the next one's are on their way while one is dealt with
@@ -321,8 +321,8 @@ ecco_paged8_stage_kernel(const __grid_constant__ PagedKv kv, const __grid_consta
 // so that the conversion from E4M3 is all that lies between shared memory and the tensor cores.
 // Pieces of a request that lie in several warps of a CTA are joined in shared memory, those in several CTAs by the CTA that comes last, in their order: the
 // result does not depend on who that is.
-// Bound by memory, 256 bytes per token and KV head, where there is much of it: 32 requests of up to 16384 tokens, 8 heads of 8 rows, 589 MB: 104.5 us = 5.6 TB/s,
-// 86 % of the copy rate; 95 us of them at 6.2.  A tile takes a warp some 1250 clocks without its loads, 340 of an SM's are what memory allows.  Else by the way
+// Bound by memory, 256 bytes per token and KV head, where there is much of it: 32 requests of up to 16384 tokens, 8 heads of 8 rows, 589 MB: 104 to 109 us = 5.4 to 5.7 TB/s,
+// 82 to 86 % of the copy rate; all but some 10 us of them at 6.2.  A tile takes a warp some 1250 clocks without its loads, 340 of an SM's are what memory allows.  Else by the way
 // through one tile: launch, lengths, pages, a tile from memory, its products, and the join, some 9 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kP8Warps = 8, kP8Loaders = 4, kP8Threads = (kP8Warps + kP8Loaders) * 32, kP8Stages = 2, kP8Reqs = 512;

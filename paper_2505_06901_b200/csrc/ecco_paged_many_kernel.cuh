@@ -16,8 +16,8 @@ namespace {
 // What carries it: operands that lie in uniform registers, waits that one vote decides (see below), weights sent in two halves, the
 // next block's Q and first scores under way while this one's sums are written out.  A tile of tokens takes two tiles of rows some 3100 clocks,
 // 2048 of them products: a thread's softmax (1.7 thousand clocks, 128 exponentials in it) and the products behind its last weights follow
-// one another.  2 x 2048 tokens x 32 heads over 8000 tokens, 468 GFLOP: some 390 us = 1.2 PFLOP/s in a burst of calls (a
-// call of 412 us less the 23 that make the tiles); a second of them takes an eighth longer, the power limit holding the SMs at 1.65 of 1.965 GHz.
+// one another.  2 x 2048 tokens x 32 heads over 8000 tokens, 468 GFLOP: some 385 us = 1.2 PFLOP/s in a burst of calls (a
+// call over E4M3 numbers, 406 us, less the 22 that make the tiles); a second of them takes an eighth longer, the power limit holding the SMs at 1.65 of 1.965 GHz.
 // (Measured equal or slower: the maximum searched for beside the first weights, an eighth or a quarter of the exponentials as polynomials, a warp
 // of products for each tile of rows, the tokens of a block of one tile of rows shared out between both tiles' warps.)
 // m is the row's maximum when it was last taken; a larger one is taken only when it is more than 2^8 larger (the weights are fp16

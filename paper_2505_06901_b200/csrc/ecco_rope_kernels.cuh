@@ -89,8 +89,8 @@ __device__ __forceinline__ void rope_load(RopePairs (&cs)[4], const RopeRow& row
 
 // ---------------------------------------------------------------------------------------------
 // K7: rows of heads turned by their positions.  A CTA has eight tokens and a share of their heads: cos and sin are made once and stand in shared
-// memory, the first heads on their way meanwhile.  Bound by memory: 512 bytes per token and head (8192 tokens x 40 heads, 168 MB: 28.1 us = 6.0 TB/s, 91 % of the
-// copy rate).
+// memory, the first heads on their way meanwhile.  Bound by memory: 512 bytes per token and head (8192 tokens x 40 heads, 168 MB: 28.1 to 28.8 us = 5.8 to 6.0 TB/s, 89 to 91 % of
+// the copy rate).
 // ---------------------------------------------------------------------------------------------
 constexpr int kRopeThreads = 256, kRopeTokens = 8, kRopeInFlight = 4;
 constexpr int kRopeTeams = kRopeThreads / 8 / kRopeTokens;             // of eight lanes, to a token
